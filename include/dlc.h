@@ -55,7 +55,7 @@ extern "C" {
 
 typedef struct dlc_ctx dlc_ctx;
 
-enum { DLC_F32 = 0, DLC_F16 = 1 };
+enum { DLC_F32 = 0, DLC_F16 = 1, DLC_BF16 = 2 /* dense operators only */ };
 
 typedef enum {
     DLC_OK = 0,
@@ -328,6 +328,95 @@ int dlc_set_row_hash_multipliers(dlc_ctx* ctx, const uint32_t* h_mult, void* str
  */
 int dlc_profile_enable(dlc_ctx* ctx, int level);
 int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* total_ms, int32_t* launches);
+
+/*
+ * Dense operators: what stands behind the decompressed lookups on the same GPU, and what makes the gradient payload that
+ * dlc_compress takes next -- linear layers with bias, activation, dropout and residual in the product's epilogue, gated
+ * blocks, and dropout by itself, each with its backward pass.
+ *
+ * They take no context and keep no state.  Buffers, the workspace among them, are the caller's; a call only enqueues
+ * kernels on `stream` and may be recorded into a HIP graph.  Results do not depend on the run: sums that are cut are put
+ * together in a fixed order, there are no floating-point atomics.
+ *
+ *   types      DLC_F32, DLC_F16, DLC_BF16: every matrix, bias and gradient of a call has the one type.  Sums and the
+ *              epilogue are fp32; a result is rounded once, when it is stored.  The backward pass rounds dz (below) to the
+ *              type as well, since it is an operand of two products; the bias gradient sums it unrounded.
+ *   matrices   row-major, columns one element apart, rows a leading dimension (in elements) apart; a leading dimension of
+ *              0 means the row's length.  Pointers lie on an element's boundary.  Rows on 16-byte boundaries (pointer
+ *              and leading dimension, and for the products the row's length too) are what the fast kernels want; others
+ *              are slower, never refused.
+ *   sizes      rows 0 .. 2^30, features 1 .. 2^20, leading dimensions up to 2^20.  With no rows a forward call does
+ *              nothing and a backward call writes zero weight and bias gradients.
+ *   drop(v)    of the element in row r and column c: 0 if its 16 random bits are below t = round(65536 p), else
+ *              v * 65536 / (65536 - t).  The bits are half words, low half first, of Philox4x32-10 (Salmon et al., SC 2011)
+ *              with key `seed` and counter (c / 8, r, offset low, offset high): half word c % 8.  No mask is stored; a
+ *              backward call with the same seed and offset drops the same elements.  A dropped element is 0 whatever
+ *              its value.  d_offset, if not NULL, is a DEVICE word that the kernels read and add to `offset`: a graph that
+ *              is replayed takes other bits by counting it up.
+ *   overlap    d_residual may be d_y; d_x may be d_y in dlc_dropout (with equal leading dimensions).  No other output
+ *              may overlap an input, another output or the workspace.
+ *   d_work     16-byte aligned, work_bytes at least dlc_*_workspace_bytes of the configuration and direction (else
+ *              DLC_ECAPACITY); may be NULL where that is 0.  Not initialised, not kept: calls in order on a stream share it.
+ * Return values: DLC_OK, DLC_EINVAL (geometry, null or misaligned pointer, p outside [0, 1]), DLC_ECAPACITY, DLC_EHIP.
+ */
+enum { DLC_ACT_NONE = 0, DLC_ACT_RELU = 1, DLC_ACT_SIGMOID = 2, DLC_ACT_SILU = 3 /* z sigmoid(z) */,
+       DLC_ACT_GELU = 4 /* z/2 (1 + erf(z / sqrt 2)) */ };
+
+typedef struct {
+    int32_t dtype;             /* DLC_F32, DLC_F16 or DLC_BF16 */
+    int32_t act;               /* DLC_ACT_* */
+    int64_t rows;              /* M: samples */
+    int64_t in_features;       /* K */
+    int64_t out_features;      /* N */
+    int64_t ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw; /* leading dimensions, 0: the row's length */
+    double dropout_p;          /* 0: no dropout */
+    uint64_t seed, offset;
+    const uint64_t* d_offset;  /* DEVICE or NULL */
+} dlc_dense_config;
+
+typedef struct {
+    int32_t dtype;
+    int32_t reserved;          /* 0 */
+    int64_t rows, cols;        /* rows 0 .. 2^30, cols 1 .. 2^31 - 8 */
+    int64_t ld_x, ld_res, ld_y; /* any that hold the row; 0: the row's length */
+    double dropout_p;
+    uint64_t seed, offset;
+    const uint64_t* d_offset;  /* DEVICE or NULL */
+} dlc_dropout_config;
+
+/*
+ * Linear layer:   z = x w' + bias;   y = drop(act(z)) + residual
+ *   d_x [M][K]   d_w [N][K]   d_bias [N] or NULL   d_residual [M][N] or NULL   d_y [M][N]
+ *   d_pre [M][N] or NULL: z, for the backward pass (which needs it unless act is DLC_ACT_NONE)
+ */
+int dlc_linear_forward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_bias,
+                       const void* d_residual, void* d_y, void* d_pre, void* d_work, size_t work_bytes, void* stream);
+/*
+ * Its backward pass:   dz = drop(dy) act'(z);   dx = dz w;   dw = dz' x;   dbias = column sums of dz
+ *   d_pre as the forward call stored it (not read, may be NULL, if act is DLC_ACT_NONE)   d_dy [M][N]
+ *   d_dx [M][K]   d_dw [N][K]   d_dbias [N]: each may be NULL and is then not computed.  The residual's gradient is dy.
+ *   relu's slope at 0 is 0, and what is not finite in dy does not pass where the slope is 0.
+ */
+int dlc_linear_backward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_pre,
+                        const void* d_dy, void* d_dx, void* d_dw, void* d_dbias, void* d_work, size_t work_bytes, void* stream);
+/*
+ * Gated block:   [g | u] = x w' + bias;   y = drop(act(g) * u)
+ *   d_w [2N][K]: the gate's N rows, then the other N   d_bias [2N] or NULL   d_y [M][N]   d_pre [M][2N] or NULL: [g | u]
+ * Backward:   dh = drop(dy);   dz = [dh u act'(g) | dh act(g)];   dx = dz w;   dw = dz' x;   dbias = column sums of dz
+ *   d_pre is required; d_dw [2N][K], d_dbias [2N]; outputs may be NULL as above
+ */
+int dlc_gated_forward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_bias, void* d_y,
+                      void* d_pre, void* d_work, size_t work_bytes, void* stream);
+int dlc_gated_backward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_pre,
+                       const void* d_dy, void* d_dx, void* d_dw, void* d_dbias, void* d_work, size_t work_bytes, void* stream);
+/* Workspace of a forward (backward = 0) or backward call with any alignment; 0 also if cfg is invalid. */
+size_t dlc_linear_workspace_bytes(const dlc_dense_config* cfg /*HOST*/, int backward);
+size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg /*HOST*/, int backward);
+/*
+ * Dropout:   y = drop(x) + residual   (d_residual [rows][cols] or NULL).  The backward pass is the same call on the gradient
+ * of y, without a residual; the residual's gradient is that gradient itself.
+ */
+int dlc_dropout(const dlc_dropout_config* cfg /*HOST*/, const void* d_x, const void* d_residual, void* d_y, void* stream);
 
 const char* dlc_strerror(int status);
 

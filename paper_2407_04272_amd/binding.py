@@ -13,7 +13,8 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdlc.so")
 
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2  # BF16: dense operators only
+ACT_NONE, ACT_RELU, ACT_SIGMOID, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
 OK, EINVAL, ENOMEM, ECAPACITY, ECORRUPT, EHIP, ESTATE, ELIMIT = 0, -1, -2, -3, -4, -5, -6, -7
 STATIC_MAX_TABLES = 4096
 CLASS_SMALL, CLASS_MEDIUM, CLASS_LARGE = 0, 1, 2
@@ -39,10 +40,26 @@ class ControllerParams(C.Structure):
                 ("eb_max", C.c_double), ("rel_floor", C.c_double)]
 
 
+class DenseConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int64),
+                ("out_features", C.c_int64), ("ld_x", C.c_int64), ("ld_w", C.c_int64), ("ld_y", C.c_int64),
+                ("ld_pre", C.c_int64), ("ld_res", C.c_int64), ("ld_dy", C.c_int64), ("ld_dx", C.c_int64),
+                ("ld_dw", C.c_int64), ("dropout_p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64),
+                ("d_offset", C.c_void_p)]
+
+
+class DropoutConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld_x", C.c_int64), ("ld_res", C.c_int64), ("ld_y", C.c_int64), ("dropout_p", C.c_double),
+                ("seed", C.c_uint64), ("offset", C.c_uint64), ("d_offset", C.c_void_p)]
+
+
 EXPORTS = ["dlc_create", "dlc_destroy", "dlc_compress_bound", "dlc_workspace_bytes", "dlc_stats",
            "dlc_set_error_bounds", "dlc_compress", "dlc_decompress", "dlc_sync_status", "dlc_quantize",
            "dlc_read_histogram", "dlc_read_codebook", "dlc_read_row_refs", "dlc_set_row_match", "dlc_speedup_estimate",
            "dlc_select_compressors", "dlc_set_row_hash_multipliers", "dlc_decompress_static",
+           "dlc_linear_forward", "dlc_linear_backward", "dlc_gated_forward", "dlc_gated_backward",
+           "dlc_linear_workspace_bytes", "dlc_gated_workspace_bytes", "dlc_dropout",
            "dlc_profile_enable", "dlc_profile_read", "dlc_strerror"]
 
 _lib = None
@@ -86,6 +103,15 @@ def lib():
         L.dlc_select_compressors.argtypes = [vp, vp, vp, C.c_size_t, vp, vp, C.c_size_t, C.c_double, vp, vp, vp, vp, vp]
         L.dlc_profile_enable.argtypes = [vp, i32]
         L.dlc_profile_read.argtypes = [vp, i32, vp, vp, vp]
+        dense = C.POINTER(DenseConfig)
+        L.dlc_linear_forward.argtypes = [dense] + [vp] * 7 + [sz, vp]
+        L.dlc_gated_forward.argtypes = [dense] + [vp] * 6 + [sz, vp]
+        for f in (L.dlc_linear_backward, L.dlc_gated_backward):
+            f.argtypes = [dense] + [vp] * 8 + [sz, vp]
+        for f in (L.dlc_linear_workspace_bytes, L.dlc_gated_workspace_bytes):
+            f.argtypes = [dense, i32]
+            f.restype = sz
+        L.dlc_dropout.argtypes = [C.POINTER(DropoutConfig)] + [vp] * 4
         L.dlc_strerror.argtypes = [i32]
         L.dlc_strerror.restype = C.c_char_p
         _lib = L
@@ -147,6 +173,116 @@ def _stream_ptr(stream):
 
 def _np_ptr(a):
     return a.ctypes.data_as(C.c_void_p) if a is not None else None
+
+
+# ---- dense operators: linear layers, gated blocks, dropout (no context; see include/dlc.h) ----
+def make_dense_config(dtype, rows, in_features, out_features, act=ACT_NONE, dropout_p=0.0, seed=0, offset=0, d_offset=None,
+                      ld_x=0, ld_w=0, ld_y=0, ld_pre=0, ld_res=0, ld_dy=0, ld_dx=0, ld_dw=0) -> DenseConfig:
+    """ld_*: elements from row to row, 0 for dense rows.  d_offset: an int64 tensor of one element on the GPU that the
+    kernels add to `offset` (a replayed graph counts it up), which has to live as long as the configuration."""
+    return DenseConfig(dtype, act, rows, in_features, out_features, ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw,
+                       dropout_p, seed, offset, _ptr(d_offset))
+
+
+def make_dropout_config(dtype, rows, cols, p, seed=0, offset=0, d_offset=None, ld_x=0, ld_res=0, ld_y=0) -> DropoutConfig:
+    return DropoutConfig(dtype, 0, rows, cols, ld_x, ld_res, ld_y, p, seed, offset, _ptr(d_offset))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def dlc_linear_workspace_bytes(cfg: DenseConfig, backward: bool = False) -> int:
+    return int(lib().dlc_linear_workspace_bytes(C.byref(cfg), int(bool(backward))))
+
+
+def dlc_gated_workspace_bytes(cfg: DenseConfig, backward: bool = False) -> int:
+    return int(lib().dlc_gated_workspace_bytes(C.byref(cfg), int(bool(backward))))
+
+
+_TORCH_NAMES = ("torch.float32", "torch.float16", "torch.bfloat16")
+
+
+def _matrix(name, t, cfg, rows, cols, ld):
+    """The tensor's address; None stays None.  What the configuration says of it has to be true of it."""
+    if t is None:
+        return None
+    if str(t.dtype) != _TORCH_NAMES[cfg.dtype] or t.device.type != "cuda":
+        raise DlcError(EINVAL, f"{name}: {t.dtype} on {t.device}")
+    want = (cols,) if rows is None else (rows, cols)
+    if tuple(t.shape) != want:
+        raise DlcError(EINVAL, f"{name}: shape {tuple(t.shape)}, not {want}")
+    if cols > 1 and t.stride(-1) != 1:
+        raise DlcError(EINVAL, f"{name}: columns {t.stride(-1)} elements apart")
+    if rows is not None and rows > 1 and t.stride(0) != (ld or cols):
+        raise DlcError(EINVAL, f"{name}: rows {t.stride(0)} elements apart, not {ld or cols}")
+    return t.data_ptr()
+
+
+def _work(t):
+    if t is None:
+        return None, 0
+    if t.device.type != "cuda" or not t.is_contiguous():
+        raise DlcError(EINVAL, "workspace: not a contiguous tensor on the GPU")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _dense_dtype(cfg):
+    if not 0 <= cfg.dtype < len(_TORCH_NAMES):
+        raise DlcError(EINVAL, f"dtype {cfg.dtype}")
+
+
+def dlc_linear_forward(cfg: DenseConfig, x, w, bias, residual, y, pre=None, work=None, stream=None):
+    """y = drop(act(x w' + bias)) + residual; pre, if given, gets x w' + bias.  Raises DlcError."""
+    _dense_dtype(cfg)
+    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
+    wk, nb = _work(work)
+    _check(lib().dlc_linear_forward(
+        C.byref(cfg), _matrix("x", x, cfg, M, K, cfg.ld_x), _matrix("w", w, cfg, N, K, cfg.ld_w),
+        _matrix("bias", bias, cfg, None, N, 0), _matrix("residual", residual, cfg, M, N, cfg.ld_res),
+        _matrix("y", y, cfg, M, N, cfg.ld_y), _matrix("pre", pre, cfg, M, N, cfg.ld_pre), wk, nb, _stream_ptr(stream)),
+        "dlc_linear_forward")
+
+
+def dlc_gated_forward(cfg: DenseConfig, x, w, bias, y, pre=None, work=None, stream=None):
+    """[g | u] = x w' + bias; y = drop(act(g) u); pre, if given, gets [g | u].  Raises DlcError."""
+    _dense_dtype(cfg)
+    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
+    wk, nb = _work(work)
+    _check(lib().dlc_gated_forward(
+        C.byref(cfg), _matrix("x", x, cfg, M, K, cfg.ld_x), _matrix("w", w, cfg, 2 * N, K, cfg.ld_w),
+        _matrix("bias", bias, cfg, None, 2 * N, 0), _matrix("y", y, cfg, M, N, cfg.ld_y),
+        _matrix("pre", pre, cfg, M, 2 * N, cfg.ld_pre), wk, nb, _stream_ptr(stream)), "dlc_gated_forward")
+
+
+def _dense_backward(name, cfg, wide, x, w, pre, dy, dx, dw, dbias, work, stream):
+    _dense_dtype(cfg)
+    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
+    wk, nb = _work(work)
+    _check(getattr(lib(), name)(
+        C.byref(cfg), _matrix("x", x, cfg, M, K, cfg.ld_x), _matrix("w", w, cfg, wide, K, cfg.ld_w),
+        _matrix("pre", pre, cfg, M, wide, cfg.ld_pre), _matrix("dy", dy, cfg, M, N, cfg.ld_dy),
+        _matrix("dx", dx, cfg, M, K, cfg.ld_dx), _matrix("dw", dw, cfg, wide, K, cfg.ld_dw),
+        _matrix("dbias", dbias, cfg, None, wide, 0), wk, nb, _stream_ptr(stream)), name)
+
+
+def dlc_linear_backward(cfg: DenseConfig, x, w, pre, dy, dx, dw, dbias, work=None, stream=None):
+    """dz = drop(dy) act'(pre); dx = dz w; dw = dz' x; dbias = column sums of dz; a None is not computed.  Raises DlcError."""
+    _dense_backward("dlc_linear_backward", cfg, cfg.out_features, x, w, pre, dy, dx, dw, dbias, work, stream)
+
+
+def dlc_gated_backward(cfg: DenseConfig, x, w, pre, dy, dx, dw, dbias, work=None, stream=None):
+    """The gradients of dlc_gated_forward from pre = [g | u] and dy; a None is not computed.  Raises DlcError."""
+    _dense_backward("dlc_gated_backward", cfg, 2 * cfg.out_features, x, w, pre, dy, dx, dw, dbias, work, stream)
+
+
+def dlc_dropout(cfg: DropoutConfig, x, residual, y, stream=None):
+    """y = drop(x) + residual (None: without); the gradient is the same call on the gradient of y.  Raises DlcError."""
+    _dense_dtype(cfg)
+    M, N = cfg.rows, cfg.cols
+    _check(lib().dlc_dropout(C.byref(cfg), _matrix("x", x, cfg, M, N, cfg.ld_x),
+                             _matrix("residual", residual, cfg, M, N, cfg.ld_res), _matrix("y", y, cfg, M, N, cfg.ld_y),
+                             _stream_ptr(stream)), "dlc_dropout")
 
 
 class Context:

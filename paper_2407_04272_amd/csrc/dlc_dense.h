@@ -1,0 +1,299 @@
+// Internal declarations of the dense operators (linear layers, gated blocks, dropout): arguments of the kernels, the
+// device functions that every epilogue shares, and the launches of each element type's source file.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "dlc.h"
+
+namespace dlc {
+
+// What happens to a sum before it is stored: y = drop(act(sum + bias)) + residual, or, gated, y = drop(act(g) * u).  A
+// null pointer leaves its part out.  Leading dimensions count elements.
+struct Epi {
+    void* y;
+    void* pre;        // the sum with its bias, before the activation (training: the backward pass reads it)
+    const void* res;
+    const void* bias;
+    int64_t ld_y, ld_pre, ld_res;
+    uint64_t seed, offset;
+    const uint64_t* d_offset;  // added to offset, read by the kernel
+    uint32_t thr;     // an element is dropped if its 16 random bits are below (0: none is, 65536: all are)
+    float scale;      // 65536 / (65536 - thr)
+    int32_t act;
+    int32_t n;        // columns of y (gated: the gate's half of the sums' columns)
+    uint32_t vec;     // bit 0: y, 1: pre, 2: residual, 3: bias are read and written 16 bytes at a time
+};
+enum { VEC_Y = 1, VEC_PRE = 2, VEC_RES = 4, VEC_BIAS = 8 };
+
+// One product: C[m][n] = sum over k of A(m, k) B(n, k).
+struct GemmArgs {
+    const void* a;
+    const void* b;
+    int64_t lda, ldb;
+    int32_t M, N, K;      // gated: N counts the columns of y, B has 2 N rows
+    int32_t kper, split;  // the sum is cut into `split` ranges of `kper` (a multiple of the k tile)
+    int32_t tiles_m, tiles_n;
+    float* part;          // split > 1: [split][M][part_ld] partial sums, put together by join
+    int64_t part_ld;
+    Epi e;
+};
+
+// Adds up the partial sums of a product and does its epilogue
+struct JoinArgs {
+    const float* part;
+    int64_t part_ld;
+    int32_t M, split, gated;
+    Epi e;
+};
+
+// dz = drop(dy) * act'(pre) (gated: both halves) and the partial column sums for the bias gradient
+struct DzArgs {
+    const void* dy;
+    const void* pre;
+    void* dz;             // null: only the sums
+    float* sums;          // [row_blocks][sums_ld], null: no bias
+    int64_t ld_dy, ld_pre, ld_dz, sums_ld;
+    int64_t M;
+    int32_t n, gated, act;
+    int32_t row_blocks, rows_per_block;
+    uint32_t thr;
+    float scale;
+    uint64_t seed, offset;
+    const uint64_t* d_offset;
+    uint32_t vec;         // bit 0: dy, 1: pre, 2: dz
+};
+
+struct SumArgs {
+    const float* sums;
+    int64_t sums_ld;
+    int32_t row_blocks, n;
+    void* out;
+};
+
+struct DropArgs {
+    const void* x;
+    const void* res;
+    void* y;
+    int64_t rows, ld_x, ld_res, ld_y;
+    int32_t cols;
+    uint32_t thr;
+    float scale;
+    uint64_t seed, offset;
+    const uint64_t* d_offset;
+    uint32_t vec;
+};
+
+// operand layouts of a product: both with k along a row (x w'), a with k along a row and b with k down a column (dz w),
+// both with k down a column (dz' x)
+enum Layout { L_KK = 0, L_KT = 1, L_TT = 2 };
+
+template <typename T>
+struct DenseOps {
+    static hipError_t gemm(const GemmArgs& g, Layout lay, bool gated, int tile, bool aligned, hipStream_t s);
+    static hipError_t skinny(const GemmArgs& g, bool gated, bool aligned, hipStream_t s);
+    static hipError_t join(const JoinArgs& j, hipStream_t s);
+    static hipError_t dz(const DzArgs& d, hipStream_t s);
+    static hipError_t sum(const SumArgs& a, hipStream_t s);
+    static hipError_t drop(const DropArgs& d, hipStream_t s);
+};
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+inline __host__ __device__ int64_t round8(int64_t v) { return (v + 7) & ~int64_t(7); }
+
+// tile sizes (rows, columns, k bytes are 128)
+constexpr int kTileM[] = {256, 128, 64};
+constexpr int kTileN[] = {256, 128, 128};
+constexpr int kTileBytes = 128;  // of a k tile's row: 64 half precision or 32 fp32 elements
+constexpr int kSkinnyRows = 16;
+
+#if defined(__HIPCC__)
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// ---- random bits: Philox4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3; SC 2011) ----
+// The ten rounds give 128 bits for eight elements: columns col8*8 .. col8*8+7 of a row.  keep() holds bit v where element
+// v stays.  Sixteen bits an element: p is taken to the nearest 1/65536, and a memory-bound pass stays one (32 bits an
+// element would double the 64-bit products, which run at a quarter of the add's rate).
+__device__ __forceinline__ uint32_t keep_mask(uint32_t col8, uint32_t row, uint64_t seed, uint64_t offset, uint32_t thr) {
+    uint32_t c0 = col8, c1 = row, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c1 = (uint32_t)b;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    const uint32_t w[4] = {c0, c1, c2, c3};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        m |= ((w[i] & 0xFFFFu) >= thr ? 1u : 0u) << (2 * i);
+        m |= ((w[i] >> 16) >= thr ? 1u : 0u) << (2 * i + 1);
+    }
+    return m;
+}
+
+// ---- activations, in fp32 ----
+// The exponentials overflow to infinity for very negative arguments, and 1 / infinity is the limit 0 that is wanted;
+// silu's product with it, (-large) * 0, is too.
+__device__ __forceinline__ float sigmoidf(float z) { return 1.0f / (1.0f + expf(-z)); }
+
+__device__ __forceinline__ void act_values(int act, float z[8]) {
+    switch (act) {
+        case DLC_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];  // (NaN stays NaN)
+            break;
+        case DLC_ACT_SIGMOID:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = sigmoidf(z[i]);
+            break;
+        case DLC_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] *= sigmoidf(z[i]);
+            break;
+        case DLC_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] *= 0.5f * erfcf(z[i] * -0.70710678118654752f);
+            break;
+        default: break;
+    }
+}
+
+// values (into z) and slopes at z
+__device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
+    switch (act) {
+        case DLC_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                d[i] = z[i] <= 0.0f ? 0.0f : 1.0f;
+                z[i] = z[i] < 0.0f ? 0.0f : z[i];
+            }
+            break;
+        case DLC_ACT_SIGMOID:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = sigmoidf(z[i]);
+                z[i] = q;
+                d[i] = q * (1.0f - q);
+            }
+            break;
+        case DLC_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = sigmoidf(z[i]);
+                d[i] = q * (1.0f + z[i] * (1.0f - q));
+                z[i] *= q;
+            }
+            break;
+        case DLC_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float c = 0.5f * erfcf(z[i] * -0.70710678118654752f);
+                d[i] = c + z[i] * (expf(-0.5f * z[i] * z[i]) * 0.39894228040143268f);
+                z[i] *= c;
+            }
+            break;
+        default:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = 1.0f;
+    }
+}
+
+// ---- eight consecutive elements of a row ----
+template <typename T>
+struct alignas(16) Vec16 { T v[16 / sizeof(T)]; };
+
+// reads elements [0, cnt) of p as fp32; vec: p is on a 16-byte boundary
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int cnt, bool vec, float f[8]) {
+    if (vec && cnt >= 8) {
+        constexpr int V = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 8 / V; ++i) {
+            const Vec16<T> q = *reinterpret_cast<const Vec16<T>*>(p + i * V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[i * V + j] = (float)q.v[j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < cnt ? (float)p[i] : 0.0f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int cnt, bool vec, const float f[8]) {
+    if (vec && cnt >= 8) {
+        constexpr int V = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 8 / V; ++i) {
+            Vec16<T> q;
+#pragma unroll
+            for (int j = 0; j < V; ++j) q.v[j] = (T)f[i * V + j];
+            *reinterpret_cast<Vec16<T>*>(p + i * V) = q;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < cnt) p[i] = (T)f[i];
+    }
+}
+
+__device__ __forceinline__ uint64_t full_offset(uint64_t offset, const uint64_t* d_offset) {
+    return d_offset ? offset + *d_offset : offset;
+}
+
+// Epilogue of eight columns col .. col+7 (col a multiple of 8) of row m: s the sums; gated: s the gate's, u the other's.
+// Everything is fp32 up to the one rounding at the store.
+template <typename T, bool GATED>
+__device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t m, int col, float s[8], float u[8]) {
+    const int cnt = e.n - col;
+    if (cnt <= 0) return;
+    if (e.bias) {
+        const T* bias = static_cast<const T*>(e.bias);
+        float b[8];
+        load8(bias + col, cnt, e.vec & VEC_BIAS, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += b[i];
+        if constexpr (GATED) {
+            load8(bias + e.n + col, cnt, (e.vec & VEC_BIAS) && e.n % 8 == 0, b);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] += b[i];
+        }
+    }
+    if (e.pre) {
+        T* p = static_cast<T*>(e.pre) + m * e.ld_pre;
+        store8(p + col, cnt, e.vec & VEC_PRE, s);
+        if constexpr (GATED) store8(p + e.n + col, cnt, (e.vec & VEC_PRE) && e.n % 8 == 0, u);
+    }
+    act_values(e.act, s);
+    if constexpr (GATED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] *= u[i];
+    }
+    if (e.thr) {
+        const uint32_t keep = keep_mask((uint32_t)col >> 3, (uint32_t)m, e.seed, offset, e.thr);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = (keep >> i) & 1u ? s[i] * e.scale : 0.0f;
+    }
+    if (e.res) {
+        float r[8];
+        load8(static_cast<const T*>(e.res) + m * e.ld_res + col, cnt, e.vec & VEC_RES, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += r[i];
+    }
+    store8(static_cast<T*>(e.y) + m * e.ld_y + col, cnt, e.vec & VEC_Y, s);
+}
+
+#endif  // __HIPCC__
+}  // namespace dlc

@@ -1,0 +1,330 @@
+// Host side of the dense operators: argument checks, the choice of kernels, workspace, C ABI.
+#include "dlc_dense.h"
+
+using namespace dlc;
+
+namespace {
+
+struct Shape {
+    int64_t M, K, N;  // gated: N columns of y, 2 N rows of w
+    int64_t ldx, ldw, ldy, ldpre, ldres, lddy, lddx, lddw;
+    bool gated;
+    int es;
+    uint32_t thr;
+    float scale;
+};
+
+constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 20;
+
+bool good_ld(int64_t& ld, int64_t row) {
+    if (ld == 0) ld = row;
+    return ld >= row && ld <= (row > kMaxDim ? row : kMaxDim);
+}
+
+bool dropout_params(double p, uint32_t* thr, float* scale) {
+    if (!(p >= 0.0 && p <= 1.0)) return false;
+    *thr = (uint32_t)(p * 65536.0 + 0.5);
+    *scale = *thr < 65536u ? 65536.0f / (float)(65536u - *thr) : 0.0f;
+    return true;
+}
+
+bool make_shape(const dlc_dense_config* c, bool gated, Shape* s) {
+    if (!c) return false;
+    if (c->dtype != DLC_F32 && c->dtype != DLC_F16 && c->dtype != DLC_BF16) return false;
+    if (c->act < DLC_ACT_NONE || c->act > DLC_ACT_GELU) return false;
+    if (c->rows < 0 || c->rows > kMaxRows) return false;
+    if (c->in_features < 1 || c->in_features > kMaxDim || c->out_features < 1 || c->out_features > kMaxDim) return false;
+    const int64_t wide = gated ? 2 * c->out_features : c->out_features;
+    s->M = c->rows; s->K = c->in_features; s->N = c->out_features;
+    s->ldx = c->ld_x; s->ldw = c->ld_w; s->ldy = c->ld_y; s->ldpre = c->ld_pre;
+    s->ldres = c->ld_res; s->lddy = c->ld_dy; s->lddx = c->ld_dx; s->lddw = c->ld_dw;
+    if (!good_ld(s->ldx, s->K) || !good_ld(s->ldw, s->K) || !good_ld(s->lddx, s->K) || !good_ld(s->lddw, s->K)) return false;
+    if (!good_ld(s->ldy, s->N) || !good_ld(s->ldpre, wide) || !good_ld(s->ldres, s->N) || !good_ld(s->lddy, s->N)) return false;
+    s->gated = gated;
+    s->es = c->dtype == DLC_F32 ? 4 : 2;
+    // a launch's work-groups are counted in 31 bits, 64 x 128 elements of the result each at least
+    const int64_t wmax = wide > s->K ? wide : s->K;
+    if ((s->M / 64 + 1) * (wmax / 128 + 1) >= (int64_t(1) << 28)) return false;
+    return dropout_params(c->dropout_p, &s->thr, &s->scale);
+}
+
+bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+bool rows16(const void* p, int64_t ld, int es) { return on(p, 16) && (ld * es) % 16 == 0; }
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t a256(size_t v) { return (v + 255) & ~size_t(255); }
+
+// ---- choice of tile and cut ---------------------------------------------------------------------
+struct Plan {
+    int tile;
+    int split, kper;
+    int tiles_m, tiles_n;
+    int64_t part_ld;
+    size_t part_bytes() const { return split > 1 ? bytes : 0; }
+    size_t bytes;
+};
+
+// M x N of the result (gated: N columns of y), K the sum's length.
+Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, int es, bool aligned) {
+    const int64_t bk = kTileBytes / es, wide = gated ? 2 * N : N;
+    // estimated time of each tile and cut: rounds of work-groups over the compute units times a work-group's k tiles, plus
+    // the partial sums' way through memory
+    static const double kStep[3] = {0.90, 0.30, 0.20};   // us of a k tile, half precision, as many work-groups as fit
+    static const int kFit[3] = {256, 512, 768};
+    Plan best{};
+    double best_t = 1e300;
+    for (int tile = aligned ? 0 : 1; tile < 3; ++tile) {
+        const int64_t tm = div_up(M, kTileM[tile]), tn = div_up(wide, kTileN[tile]);
+        const int64_t tiles = tm * tn, steps = div_up(K, bk);
+        if (tiles >= (int64_t(1) << 30)) continue;
+        for (int64_t split = 1; split <= 64; ++split) {
+            if (split > 1 && (steps / split < 4 || tiles * split > 2048)) break;
+            const int64_t per = div_up(steps, split);
+            if (div_up(steps, per) != split) continue;
+            const double rounds = (double)div_up(tiles * split, kFit[tile]);
+            const double fill = (double)(tiles * split) / kFit[tile];
+            const double step = kStep[tile] * (es == 4 ? 8.0 : 1.0);
+            double t = (rounds > 1.0 ? 0.5 * (rounds + fill) : rounds) * ((double)per * step + 2.0);
+            if (split > 1) t += 3.0 + (double)split * (double)M * (double)wide * 8.0 / 4.0e6;
+            if (t < best_t) {
+                best_t = t;
+                best.tile = tile;
+                best.split = (int)split;
+                best.kper = (int)(per * bk);
+                best.tiles_m = (int)tm;
+                best.tiles_n = (int)tn;
+            }
+        }
+    }
+    best.part_ld = gated ? 2 * round8(N) : round8(N);
+    best.bytes = best.split > 1 ? (size_t)best.split * (size_t)M * (size_t)best.part_ld * 4 : 0;
+    return best;
+}
+
+size_t plan_bytes(int64_t M, int64_t N, int64_t K, bool gated, int es) {
+    const size_t a = plan_gemm(M, N, K, gated, es, true).bytes, b = plan_gemm(M, N, K, gated, es, false).bytes;
+    return a > b ? a : b;
+}
+
+// few rows: the forward product is a pass over the weights
+bool few_rows(const Shape& s) { return s.M <= kSkinnyRows; }
+
+// workspace of a backward call: dz, the bias gradient's partial sums, one product's partial sums at a time
+struct BackPlan {
+    int64_t ld_dz;
+    int row_blocks, rows_per_block;
+    int64_t sums_ld;
+    size_t off_sums, off_part, total;
+};
+
+BackPlan plan_back(const Shape& s) {
+    BackPlan b;
+    const int64_t wide = s.gated ? 2 * s.N : s.N;
+    b.ld_dz = round8(wide);
+    b.sums_ld = b.ld_dz;
+    const int64_t cols = div_up(s.N, 256);
+    int64_t blocks = div_up(2048, cols);
+    if (blocks > div_up(s.M, 8)) blocks = div_up(s.M, 8);
+    if (blocks > 512) blocks = 512;
+    if (blocks < 1) blocks = 1;
+    b.rows_per_block = (int)(div_up(div_up(s.M, blocks), 8) * 8);
+    b.row_blocks = b.rows_per_block ? (int)div_up(s.M, b.rows_per_block) : 0;
+    b.off_sums = a256((size_t)s.M * (size_t)b.ld_dz * (size_t)s.es);
+    b.off_part = b.off_sums + a256((size_t)b.row_blocks * (size_t)b.sums_ld * 4);
+    const size_t px = s.M ? plan_bytes(s.M, s.K, wide, false, s.es) : 0;
+    const size_t pw = s.M ? plan_bytes(wide, s.K, s.M, false, s.es) : 0;
+    b.total = b.off_part + a256(px > pw ? px : pw);
+    return b;
+}
+
+size_t work_bytes_of(const dlc_dense_config* c, bool gated, bool backward) {
+    Shape s;
+    if (!make_shape(c, gated, &s) || s.M == 0) return 0;
+    if (backward) return plan_back(s).total;
+    return few_rows(s) ? 0 : plan_bytes(s.M, s.N, s.K, gated, s.es);
+}
+
+template <typename T>
+int run_gemm(GemmArgs g, Layout lay, bool gated, bool aligned, int es, void* work, hipStream_t st) {
+    const Plan p = plan_gemm(g.M, g.N, g.K, gated, es, aligned);
+    g.kper = p.kper; g.split = p.split; g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_n;
+    g.part = static_cast<float*>(work);
+    g.part_ld = p.part_ld;
+    if (DenseOps<T>::gemm(g, lay, gated, p.tile, aligned, st) != hipSuccess) return DLC_EHIP;
+    if (p.split > 1) {
+        const JoinArgs j{g.part, g.part_ld, g.M, p.split, gated ? 1 : 0, g.e};
+        if (DenseOps<T>::join(j, st) != hipSuccess) return DLC_EHIP;
+    }
+    return DLC_OK;
+}
+
+template <typename T>
+int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* bias, const void* res, void* y,
+            void* pre, void* work, hipStream_t st) {
+    GemmArgs g{};
+    g.a = x; g.b = w; g.lda = s.ldx; g.ldb = s.ldw;
+    g.M = (int)s.M; g.N = (int)s.N; g.K = (int)s.K;
+    g.split = 1; g.kper = g.K;
+    Epi& e = g.e;
+    e.y = y; e.pre = pre; e.res = res; e.bias = bias;
+    e.ld_y = s.ldy; e.ld_pre = s.ldpre; e.ld_res = s.ldres;
+    e.seed = c->seed; e.offset = c->offset; e.d_offset = c->d_offset;
+    e.thr = s.thr; e.scale = s.scale; e.act = c->act; e.n = (int)s.N;
+    e.vec = (rows16(y, s.ldy, s.es) ? VEC_Y : 0) | (rows16(pre, s.ldpre, s.es) ? VEC_PRE : 0) |
+            (rows16(res, s.ldres, s.es) ? VEC_RES : 0) | (on(bias, 16) ? VEC_BIAS : 0);
+    const bool aligned = rows16(x, s.ldx, s.es) && rows16(w, s.ldw, s.es) && (s.K * s.es) % 16 == 0;
+    if (few_rows(s)) return DenseOps<T>::skinny(g, s.gated, aligned, st) == hipSuccess ? DLC_OK : DLC_EHIP;
+    return run_gemm<T>(g, L_KK, s.gated, aligned, s.es, work, st);
+}
+
+template <typename T>
+int backward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+             void* dw, void* dbias, void* work, hipStream_t st) {
+    const BackPlan b = plan_back(s);
+    char* const wk = static_cast<char*>(work);
+    const int64_t wide = s.gated ? 2 * s.N : s.N;
+    const bool same = !s.gated && c->act == DLC_ACT_NONE && s.thr == 0;  // dz is dy
+    const bool direct = same && rows16(dy, s.lddy, s.es) && (s.N * s.es) % 16 == 0;
+    const bool products = (dx || dw) && s.M > 0;
+    float* const sums = reinterpret_cast<float*>(wk + b.off_sums);
+    if (s.M > 0 && (dbias || (products && !direct))) {
+        DzArgs d{};
+        d.dy = dy; d.pre = same ? nullptr : pre;
+        if (!s.gated && c->act == DLC_ACT_NONE) d.pre = nullptr;
+        d.dz = products && !direct ? work : nullptr;
+        d.sums = dbias ? sums : nullptr;
+        d.ld_dy = s.lddy; d.ld_pre = s.ldpre; d.ld_dz = b.ld_dz; d.sums_ld = b.sums_ld;
+        d.M = s.M; d.n = (int)s.N; d.gated = s.gated; d.act = c->act;
+        d.row_blocks = b.row_blocks; d.rows_per_block = b.rows_per_block;
+        d.thr = s.thr; d.scale = s.scale; d.seed = c->seed; d.offset = c->offset; d.d_offset = c->d_offset;
+        d.vec = (rows16(dy, s.lddy, s.es) ? 1u : 0u) | (rows16(pre, s.ldpre, s.es) ? 2u : 0u);
+        if (DenseOps<T>::dz(d, st) != hipSuccess) return DLC_EHIP;
+    }
+    if (dbias) {
+        const SumArgs a{sums, b.sums_ld, s.M > 0 ? b.row_blocks : 0, (int)wide, dbias};
+        if (DenseOps<T>::sum(a, st) != hipSuccess) return DLC_EHIP;
+    }
+    const void* const dz = direct ? dy : work;
+    const int64_t lddz = direct ? s.lddy : b.ld_dz;
+    const bool w16 = rows16(w, s.ldw, s.es) && (s.K * s.es) % 16 == 0;
+    const bool x16 = rows16(x, s.ldx, s.es) && (s.K * s.es) % 16 == 0;
+    if (dx && s.M > 0) {
+        GemmArgs g{};
+        g.a = dz; g.b = w; g.lda = lddz; g.ldb = s.ldw;
+        g.M = (int)s.M; g.N = (int)s.K; g.K = (int)wide;
+        g.e.y = dx; g.e.ld_y = s.lddx; g.e.n = (int)s.K; g.e.vec = rows16(dx, s.lddx, s.es) ? VEC_Y : 0;
+        if (const int rc = run_gemm<T>(g, L_KT, false, w16, s.es, wk + b.off_part, st); rc != DLC_OK) return rc;
+    }
+    if (dw) {
+        GemmArgs g{};
+        g.a = dz; g.b = x; g.lda = lddz; g.ldb = s.ldx;
+        g.M = (int)wide; g.N = (int)s.K; g.K = (int)s.M;
+        g.e.y = dw; g.e.ld_y = s.lddw; g.e.n = (int)s.K; g.e.vec = rows16(dw, s.lddw, s.es) ? VEC_Y : 0;
+        if (s.M == 0) {  // the empty sum
+            const JoinArgs j{nullptr, 0, g.M, 0, 0, g.e};
+            if (DenseOps<T>::join(j, st) != hipSuccess) return DLC_EHIP;
+        } else if (const int rc = run_gemm<T>(g, L_TT, false, x16, s.es, wk + b.off_part, st); rc != DLC_OK) {
+            return rc;
+        }
+    }
+    return DLC_OK;
+}
+
+// d is there if `need`, and lies on an element's boundary
+bool good_ptr(const void* d, int es, bool need) { return d ? on(d, es) : !need; }
+
+int check_work(const dlc_dense_config* c, bool gated, bool backward, const void* work, size_t bytes) {
+    const size_t need = work_bytes_of(c, gated, backward);
+    if (need == 0) return DLC_OK;
+    if (!work || !on(work, 16)) return DLC_EINVAL;
+    return bytes >= need ? DLC_OK : DLC_ECAPACITY;
+}
+
+int forward_any(const dlc_dense_config* c, bool gated, const void* x, const void* w, const void* bias, const void* res, void* y,
+                void* pre, void* work, size_t bytes, void* stream) {
+    Shape s;
+    if (!make_shape(c, gated, &s)) return DLC_EINVAL;
+    const bool need = s.M > 0;
+    if (!good_ptr(x, s.es, need) || !good_ptr(w, s.es, need) || !good_ptr(bias, s.es, false) || !good_ptr(res, s.es, false) ||
+        !good_ptr(y, s.es, need) || !good_ptr(pre, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
+    if (!need) return DLC_OK;
+    if (const int rc = check_work(c, gated, false, work, bytes); rc != DLC_OK) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    switch (c->dtype) {
+        case DLC_F32: return forward<float>(c, s, x, w, bias, res, y, pre, work, st);
+        case DLC_F16: return forward<f16_t>(c, s, x, w, bias, res, y, pre, work, st);
+        default: return forward<bf16_t>(c, s, x, w, bias, res, y, pre, work, st);
+    }
+}
+
+int backward_any(const dlc_dense_config* c, bool gated, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                 void* dw, void* dbias, void* work, size_t bytes, void* stream) {
+    Shape s;
+    if (!make_shape(c, gated, &s)) return DLC_EINVAL;
+    const bool some = s.M > 0;
+    if (!good_ptr(x, s.es, some && dw) || !good_ptr(w, s.es, some && dx) || !good_ptr(dy, s.es, some) ||
+        !good_ptr(pre, s.es, some && (gated || c->act != DLC_ACT_NONE)) || !good_ptr(dx, s.es, false) || !good_ptr(dw, s.es, false) ||
+        !good_ptr(dbias, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
+    if (const int rc = check_work(c, gated, true, work, bytes); rc != DLC_OK) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    switch (c->dtype) {
+        case DLC_F32: return backward<float>(c, s, x, w, pre, dy, dx, dw, dbias, work, st);
+        case DLC_F16: return backward<f16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, st);
+        default: return backward<bf16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, st);
+    }
+}
+
+}  // namespace
+
+extern "C" size_t dlc_linear_workspace_bytes(const dlc_dense_config* cfg, int backward) { return work_bytes_of(cfg, false, backward != 0); }
+extern "C" size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg, int backward) { return work_bytes_of(cfg, true, backward != 0); }
+
+extern "C" int dlc_linear_forward(const dlc_dense_config* cfg, const void* x, const void* w, const void* bias, const void* res, void* y,
+                                  void* pre, void* work, size_t bytes, void* stream) {
+    return forward_any(cfg, false, x, w, bias, res, y, pre, work, bytes, stream);
+}
+
+extern "C" int dlc_linear_backward(const dlc_dense_config* cfg, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                                   void* dw, void* dbias, void* work, size_t bytes, void* stream) {
+    return backward_any(cfg, false, x, w, pre, dy, dx, dw, dbias, work, bytes, stream);
+}
+
+extern "C" int dlc_gated_forward(const dlc_dense_config* cfg, const void* x, const void* w, const void* bias, void* y, void* pre,
+                                 void* work, size_t bytes, void* stream) {
+    return forward_any(cfg, true, x, w, bias, nullptr, y, pre, work, bytes, stream);
+}
+
+extern "C" int dlc_gated_backward(const dlc_dense_config* cfg, const void* x, const void* w, const void* pre, const void* dy, void* dx,
+                                  void* dw, void* dbias, void* work, size_t bytes, void* stream) {
+    return backward_any(cfg, true, x, w, pre, dy, dx, dw, dbias, work, bytes, stream);
+}
+
+extern "C" int dlc_dropout(const dlc_dropout_config* c, const void* x, const void* res, void* y, void* stream) {
+    if (!c || (c->dtype != DLC_F32 && c->dtype != DLC_F16 && c->dtype != DLC_BF16) || c->reserved != 0) return DLC_EINVAL;
+    if (c->rows < 0 || c->rows > kMaxRows || c->cols < 1 || c->cols > 0x7FFFFFF8ll) return DLC_EINVAL;
+    DropArgs d{};
+    d.rows = c->rows; d.cols = (int)c->cols;
+    d.ld_x = c->ld_x ? c->ld_x : c->cols;
+    d.ld_res = c->ld_res ? c->ld_res : c->cols;
+    d.ld_y = c->ld_y ? c->ld_y : c->cols;
+    if (d.ld_x < c->cols || d.ld_res < c->cols || d.ld_y < c->cols) return DLC_EINVAL;
+    if (!dropout_params(c->dropout_p, &d.thr, &d.scale)) return DLC_EINVAL;
+    const int es = c->dtype == DLC_F32 ? 4 : 2;
+    const int64_t lim = int64_t(1) << 60;  // (a buffer's last byte has a 64-bit address)
+    const int64_t ldm = d.ld_x > d.ld_y ? (d.ld_x > d.ld_res ? d.ld_x : d.ld_res) : (d.ld_y > d.ld_res ? d.ld_y : d.ld_res);
+    if (c->rows > 0 && ldm > lim / c->rows) return DLC_EINVAL;
+    const bool need = c->rows > 0;
+    if (!good_ptr(x, es, need) || !good_ptr(res, es, false) || !good_ptr(y, es, need) || !on(c->d_offset, 8)) return DLC_EINVAL;
+    if (!need) return DLC_OK;
+    d.x = x; d.res = res; d.y = y;
+    d.seed = c->seed; d.offset = c->offset; d.d_offset = c->d_offset;
+    d.vec = (rows16(x, d.ld_x, es) ? 1u : 0u) | (rows16(y, d.ld_y, es) ? 2u : 0u) | (rows16(res, d.ld_res, es) ? 4u : 0u);
+    hipStream_t st = (hipStream_t)stream;
+    hipError_t rc;
+    switch (c->dtype) {
+        case DLC_F32: rc = DenseOps<float>::drop(d, st); break;
+        case DLC_F16: rc = DenseOps<f16_t>::drop(d, st); break;
+        default: rc = DenseOps<bf16_t>::drop(d, st); break;
+    }
+    return rc == hipSuccess ? DLC_OK : DLC_EHIP;
+}
