@@ -200,70 +200,85 @@ def dlc_gated_workspace_bytes(cfg: DenseConfig, backward: bool = False) -> int:
     return int(lib().dlc_gated_workspace_bytes(C.byref(cfg), int(bool(backward))))
 
 
-_TORCH_NAMES = ("torch.float32", "torch.float16", "torch.bfloat16")
+_torch_types = ()
 
 
-def _matrix(name, t, cfg, rows, cols, ld):
+def _dense_type(cfg):
+    """The torch type of the configuration's matrices."""
+    global _torch_types
+    if not _torch_types:
+        import torch
+        _torch_types = (torch.float32, torch.float16, torch.bfloat16)
+    if not 0 <= cfg.dtype < len(_torch_types):
+        raise DlcError(EINVAL, f"dtype {cfg.dtype}")
+    return _torch_types[cfg.dtype]
+
+
+def _matrix(name, t, dtype, rows, cols, ld):
     """The tensor's address; None stays None.  What the configuration says of it has to be true of it."""
     if t is None:
         return None
-    if str(t.dtype) != _TORCH_NAMES[cfg.dtype] or t.device.type != "cuda":
+    if t.dtype is not dtype or not t.is_cuda:
         raise DlcError(EINVAL, f"{name}: {t.dtype} on {t.device}")
-    want = (cols,) if rows is None else (rows, cols)
-    if tuple(t.shape) != want:
-        raise DlcError(EINVAL, f"{name}: shape {tuple(t.shape)}, not {want}")
-    if cols > 1 and t.stride(-1) != 1:
-        raise DlcError(EINVAL, f"{name}: columns {t.stride(-1)} elements apart")
-    if rows is not None and rows > 1 and t.stride(0) != (ld or cols):
+    if t.shape != (rows, cols):
+        raise DlcError(EINVAL, f"{name}: shape {tuple(t.shape)}, not {(rows, cols)}")
+    if ld in (0, cols) and t.is_contiguous():
+        return t.data_ptr()
+    if cols > 1 and t.stride(1) != 1:
+        raise DlcError(EINVAL, f"{name}: columns {t.stride(1)} elements apart")
+    if rows > 1 and t.stride(0) != (ld or cols):
         raise DlcError(EINVAL, f"{name}: rows {t.stride(0)} elements apart, not {ld or cols}")
+    return t.data_ptr()
+
+
+def _vector(name, t, dtype, n):
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
+        raise DlcError(EINVAL, f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _work(t):
     if t is None:
         return None, 0
-    if t.device.type != "cuda" or not t.is_contiguous():
+    if not t.is_cuda or not t.is_contiguous():
         raise DlcError(EINVAL, "workspace: not a contiguous tensor on the GPU")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _dense_dtype(cfg):
-    if not 0 <= cfg.dtype < len(_TORCH_NAMES):
-        raise DlcError(EINVAL, f"dtype {cfg.dtype}")
-
-
 def dlc_linear_forward(cfg: DenseConfig, x, w, bias, residual, y, pre=None, work=None, stream=None):
     """y = drop(act(x w' + bias)) + residual; pre, if given, gets x w' + bias.  Raises DlcError."""
-    _dense_dtype(cfg)
+    ty = _dense_type(cfg)
     M, K, N = cfg.rows, cfg.in_features, cfg.out_features
     wk, nb = _work(work)
     _check(lib().dlc_linear_forward(
-        C.byref(cfg), _matrix("x", x, cfg, M, K, cfg.ld_x), _matrix("w", w, cfg, N, K, cfg.ld_w),
-        _matrix("bias", bias, cfg, None, N, 0), _matrix("residual", residual, cfg, M, N, cfg.ld_res),
-        _matrix("y", y, cfg, M, N, cfg.ld_y), _matrix("pre", pre, cfg, M, N, cfg.ld_pre), wk, nb, _stream_ptr(stream)),
+        C.byref(cfg), _matrix("x", x, ty, M, K, cfg.ld_x), _matrix("w", w, ty, N, K, cfg.ld_w),
+        _vector("bias", bias, ty, N), _matrix("residual", residual, ty, M, N, cfg.ld_res),
+        _matrix("y", y, ty, M, N, cfg.ld_y), _matrix("pre", pre, ty, M, N, cfg.ld_pre), wk, nb, _stream_ptr(stream)),
         "dlc_linear_forward")
 
 
 def dlc_gated_forward(cfg: DenseConfig, x, w, bias, y, pre=None, work=None, stream=None):
     """[g | u] = x w' + bias; y = drop(act(g) u); pre, if given, gets [g | u].  Raises DlcError."""
-    _dense_dtype(cfg)
+    ty = _dense_type(cfg)
     M, K, N = cfg.rows, cfg.in_features, cfg.out_features
     wk, nb = _work(work)
     _check(lib().dlc_gated_forward(
-        C.byref(cfg), _matrix("x", x, cfg, M, K, cfg.ld_x), _matrix("w", w, cfg, 2 * N, K, cfg.ld_w),
-        _matrix("bias", bias, cfg, None, 2 * N, 0), _matrix("y", y, cfg, M, N, cfg.ld_y),
-        _matrix("pre", pre, cfg, M, 2 * N, cfg.ld_pre), wk, nb, _stream_ptr(stream)), "dlc_gated_forward")
+        C.byref(cfg), _matrix("x", x, ty, M, K, cfg.ld_x), _matrix("w", w, ty, 2 * N, K, cfg.ld_w),
+        _vector("bias", bias, ty, 2 * N), _matrix("y", y, ty, M, N, cfg.ld_y),
+        _matrix("pre", pre, ty, M, 2 * N, cfg.ld_pre), wk, nb, _stream_ptr(stream)), "dlc_gated_forward")
 
 
 def _dense_backward(name, cfg, wide, x, w, pre, dy, dx, dw, dbias, work, stream):
-    _dense_dtype(cfg)
+    ty = _dense_type(cfg)
     M, K, N = cfg.rows, cfg.in_features, cfg.out_features
     wk, nb = _work(work)
     _check(getattr(lib(), name)(
-        C.byref(cfg), _matrix("x", x, cfg, M, K, cfg.ld_x), _matrix("w", w, cfg, wide, K, cfg.ld_w),
-        _matrix("pre", pre, cfg, M, wide, cfg.ld_pre), _matrix("dy", dy, cfg, M, N, cfg.ld_dy),
-        _matrix("dx", dx, cfg, M, K, cfg.ld_dx), _matrix("dw", dw, cfg, wide, K, cfg.ld_dw),
-        _matrix("dbias", dbias, cfg, None, wide, 0), wk, nb, _stream_ptr(stream)), name)
+        C.byref(cfg), _matrix("x", x, ty, M, K, cfg.ld_x), _matrix("w", w, ty, wide, K, cfg.ld_w),
+        _matrix("pre", pre, ty, M, wide, cfg.ld_pre), _matrix("dy", dy, ty, M, N, cfg.ld_dy),
+        _matrix("dx", dx, ty, M, K, cfg.ld_dx), _matrix("dw", dw, ty, wide, K, cfg.ld_dw),
+        _vector("dbias", dbias, ty, wide), wk, nb, _stream_ptr(stream)), name)
 
 
 def dlc_linear_backward(cfg: DenseConfig, x, w, pre, dy, dx, dw, dbias, work=None, stream=None):
@@ -278,10 +293,10 @@ def dlc_gated_backward(cfg: DenseConfig, x, w, pre, dy, dx, dw, dbias, work=None
 
 def dlc_dropout(cfg: DropoutConfig, x, residual, y, stream=None):
     """y = drop(x) + residual (None: without); the gradient is the same call on the gradient of y.  Raises DlcError."""
-    _dense_dtype(cfg)
+    ty = _dense_type(cfg)
     M, N = cfg.rows, cfg.cols
-    _check(lib().dlc_dropout(C.byref(cfg), _matrix("x", x, cfg, M, N, cfg.ld_x),
-                             _matrix("residual", residual, cfg, M, N, cfg.ld_res), _matrix("y", y, cfg, M, N, cfg.ld_y),
+    _check(lib().dlc_dropout(C.byref(cfg), _matrix("x", x, ty, M, N, cfg.ld_x),
+                             _matrix("residual", residual, ty, M, N, cfg.ld_res), _matrix("y", y, ty, M, N, cfg.ld_y),
                              _stream_ptr(stream)), "dlc_dropout")
 
 

@@ -108,7 +108,7 @@ inline __host__ __device__ int64_t round8(int64_t v) { return (v + 7) & ~int64_t
 // tile sizes (rows, columns, k bytes are 128)
 constexpr int kTileM[] = {256, 128, 64};
 constexpr int kTileN[] = {256, 128, 128};
-constexpr int kTileBytes = 128;  // of a k tile's row: 64 half precision or 32 fp32 elements
+constexpr int kTileBytes = 128;  // a cut of k is a multiple of this many bytes of it (a k tile, or two)
 constexpr int kSkinnyRows = 16;
 
 #if defined(__HIPCC__)

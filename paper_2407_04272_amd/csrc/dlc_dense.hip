@@ -60,32 +60,41 @@ struct Plan {
     int split, kper;
     int tiles_m, tiles_n;
     int64_t part_ld;
-    size_t part_bytes() const { return split > 1 ? bytes : 0; }
-    size_t bytes;
+    size_t bytes;  // of the partial sums
 };
 
-// M x N of the result (gated: N columns of y), K the sum's length.
-Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, int es, bool aligned) {
+// What a k tile (128 bytes of k) costs with 1, 2 and 3 work-groups on a compute unit, in us, and what a work-group costs
+// besides, measured with all three layouts on full and half full cards (0: no third work-group fits).  256 x 256 is the
+// fastest per product in half precision (1560 TFLOP/s against 1280 and 850 of the other two, all compute units busy) and has
+// the longest start and end; in fp32 all three reach the matrix cores' rate and the small ones leave fewer units idle.
+struct TileCost { double tile[3], first, further; };
+constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0}, {{0.57, 0.88, 0}, 6.0, 3.0}, {{0.45, 0.64, 1.0}, 4.0, 3.0}};
+constexpr TileCost kHalfOdd[3] = {{{0, 0, 0}, 0, 0}, {{1.2, 1.27, 0}, 6.0, 3.0}, {{0.9, 1.0, 1.15}, 4.0, 3.0}};
+constexpr TileCost kF32Cost[3] = {{{7.6, 0, 0}, 14.0, 10.0}, {{2.2, 3.8, 0}, 8.0, 4.0}, {{1.3, 2.0, 2.9}, 5.0, 3.0}};
+constexpr TileCost kF32Odd[3] = {{{0, 0, 0}, 0, 0}, {{2.6, 4.4, 0}, 8.0, 4.0}, {{1.6, 2.5, 3.7}, 5.0, 3.0}};
+constexpr int kUnits = 256;  // compute units
+
+// M x N of the result (gated: N columns of y), K the sum's length: the tile and the cut of K with the smallest estimate
+Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es, bool aligned) {
     const int64_t bk = kTileBytes / es, wide = gated ? 2 * N : N;
-    // estimated time of each tile and cut: rounds of work-groups over the compute units times a work-group's k tiles, plus
-    // the partial sums' way through memory
-    static const double kStep[3] = {0.90, 0.30, 0.20};   // us of a k tile, half precision, as many work-groups as fit
-    static const int kFit[3] = {256, 512, 768};
+    const TileCost* const cost = es == 4 ? (aligned ? kF32Cost : kF32Odd) : (aligned ? kHalfCost : kHalfOdd);
     Plan best{};
     double best_t = 1e300;
     for (int tile = aligned ? 0 : 1; tile < 3; ++tile) {
+        const TileCost& c = cost[tile];
         const int64_t tm = div_up(M, kTileM[tile]), tn = div_up(wide, kTileN[tile]);
         const int64_t tiles = tm * tn, steps = div_up(K, bk);
         if (tiles >= (int64_t(1) << 30)) continue;
-        for (int64_t split = 1; split <= 64; ++split) {
-            if (split > 1 && (steps / split < 4 || tiles * split > 2048)) break;
+        const int fit = tile == 0 ? 1 : tile == 1 || lay == L_KK ? 2 : 3;  // work-groups that share a compute unit
+        for (int64_t split = 1; split <= 128; ++split) {
+            if (split > 1 && (steps / split < 2 || tiles * split > 4 * kUnits)) break;
             const int64_t per = div_up(steps, split);
             if (div_up(steps, per) != split) continue;
-            const double rounds = (double)div_up(tiles * split, kFit[tile]);
-            const double fill = (double)(tiles * split) / kFit[tile];
-            const double step = kStep[tile] * (es == 4 ? 8.0 : 1.0);
-            double t = (rounds > 1.0 ? 0.5 * (rounds + fill) : rounds) * ((double)per * step + 2.0);
-            if (split > 1) t += 3.0 + (double)split * (double)M * (double)wide * 8.0 / 4.0e6;
+            const int64_t wgs = tiles * split, full = wgs / (kUnits * fit), rest = wgs % (kUnits * fit);
+            double t = (double)full * ((double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
+            if (rest) t += (double)per * c.tile[div_up(rest, kUnits) - 1] + c.further;
+            // partial sums: a launch, and their way to memory and back
+            if (split > 1) t += 4.0 + (double)split * (double)M * (double)wide * 8.0 / 4.0e6;
             if (t < best_t) {
                 best_t = t;
                 best.tile = tile;
@@ -101,8 +110,8 @@ Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, int es, bool aligned
     return best;
 }
 
-size_t plan_bytes(int64_t M, int64_t N, int64_t K, bool gated, int es) {
-    const size_t a = plan_gemm(M, N, K, gated, es, true).bytes, b = plan_gemm(M, N, K, gated, es, false).bytes;
+size_t plan_bytes(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) {
+    const size_t a = plan_gemm(M, N, K, gated, lay, es, true).bytes, b = plan_gemm(M, N, K, gated, lay, es, false).bytes;
     return a > b ? a : b;
 }
 
@@ -131,8 +140,8 @@ BackPlan plan_back(const Shape& s) {
     b.row_blocks = b.rows_per_block ? (int)div_up(s.M, b.rows_per_block) : 0;
     b.off_sums = a256((size_t)s.M * (size_t)b.ld_dz * (size_t)s.es);
     b.off_part = b.off_sums + a256((size_t)b.row_blocks * (size_t)b.sums_ld * 4);
-    const size_t px = s.M ? plan_bytes(s.M, s.K, wide, false, s.es) : 0;
-    const size_t pw = s.M ? plan_bytes(wide, s.K, s.M, false, s.es) : 0;
+    const size_t px = s.M ? plan_bytes(s.M, s.K, wide, false, L_KT, s.es) : 0;
+    const size_t pw = s.M ? plan_bytes(wide, s.K, s.M, false, L_TT, s.es) : 0;
     b.total = b.off_part + a256(px > pw ? px : pw);
     return b;
 }
@@ -141,12 +150,12 @@ size_t work_bytes_of(const dlc_dense_config* c, bool gated, bool backward) {
     Shape s;
     if (!make_shape(c, gated, &s) || s.M == 0) return 0;
     if (backward) return plan_back(s).total;
-    return few_rows(s) ? 0 : plan_bytes(s.M, s.N, s.K, gated, s.es);
+    return few_rows(s) ? 0 : plan_bytes(s.M, s.N, s.K, gated, L_KK, s.es);
 }
 
 template <typename T>
 int run_gemm(GemmArgs g, Layout lay, bool gated, bool aligned, int es, void* work, hipStream_t st) {
-    const Plan p = plan_gemm(g.M, g.N, g.K, gated, es, aligned);
+    const Plan p = plan_gemm(g.M, g.N, g.K, gated, lay, es, aligned);
     g.kper = p.kper; g.split = p.split; g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_n;
     g.part = static_cast<float*>(work);
     g.part_ld = p.part_ld;

@@ -1,14 +1,19 @@
 // The matrix products of the dense operators, one template for three element types and three operand layouts.
 //
-// C[m][n] = sum over k of A(m, k) B(n, k), tile by tile: a work-group takes BM x BN of C and walks k in tiles of 128 bytes
-// (64 half precision or 32 fp32 elements).  Each k tile of A and B goes from memory to one of two buffers in LDS while the
-// matrix cores work on the other.  A wavefront holds a WM x WN part of C in registers as 16 x 16 blocks.
+// C[m][n] = sum over k of A(m, k) B(n, k), tile by tile: a work-group takes BM x BN of C and walks k tile by tile.  The
+// tiles of A and B go from memory to a ring of slots in LDS, several tiles ahead, without passing through registers; a
+// wavefront holds a part of C in registers as 16 x 16 blocks and takes its fragments of a tile from LDS.
 //
-// LDS layouts (16-byte chunks; chosen so that 16 lanes that read together touch 16 different sixteenths of the banks):
-//   k along a row     row r, chunk c of its 8 at r * 128 + (c ^ ((r >> 1) & 7)) * 16
-//   k down a column   k row r of BM (BN) elements, 32-byte (fp32: 64-byte) units u at u ^ f(r): half precision reads these
-//                     with the transposing LDS read (a group of 16 lanes takes 4 k rows of 16 elements and hands every lane
-//                     the 4 k values of its element), fp32 element by element
+// 256 x 256, eight wavefronts: two groups of four, one of each on every SIMD, work half a phase apart; while one reads its
+// fragments and starts loads, the other multiplies (see the loops).  128 x 128 and 64 x 128, four wavefronts: two or three
+// work-groups share a compute unit and fill each other's gaps.
+//
+// LDS layouts (16-byte chunks):
+//   k along a row     rows of TB bytes of k, chunk c of row r at place c ^ (r >> 1): what the 16 lanes of a quarter of a
+//                     16-byte read touch lies in 16 different sixteenths of the banks (no conflicts counted)
+//   k down a column   k row r of BM (BN) elements, units of 16 elements u at u ^ f(r).  Half precision is read with the
+//                     transposing read: 16 lanes take 4 k rows of 16 elements, every lane gets the 4 k values of one
+//                     element.  fp32 is read element by element.
 // A load to LDS writes 64 consecutive chunks per wavefront, so the permutation is applied to the address that is read.
 #pragma once
 #include "dlc_dense.h"
@@ -16,13 +21,14 @@
 namespace dlc {
 
 typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) char lds_char;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// One 16 x 16 block times 64 bytes of k: rows from `r`, columns from `c`; lane l holds D[(l / 16) * 4 + i][l % 16].
+// One 16 x 16 block times 64 bytes of k: rows from `r`, columns from `c`; lane l gives row (column) l % 16 and the 16 bytes
+// of k from (l / 16) * 16 on, and holds D[(l / 16) * 4 + i][l % 16].  (32 x 32 blocks read half the operands and were 8 %
+// slower on 8192 x 2048 x 8192: large products run at the clock that the power allows, and theirs was lower.)
 template <typename T>
 __device__ __forceinline__ f32x4 mma(const u32x4_t& r, const u32x4_t& c, f32x4 acc) {
     if constexpr (std::is_same<T, float>::value) {
@@ -40,135 +46,284 @@ __device__ __forceinline__ f32x4 mma(const u32x4_t& r, const u32x4_t& c, f32x4 a
 // 16 bytes from an element's boundary
 typedef uint32_t u32x4_by2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_by4 __attribute__((ext_vector_type(4), aligned(4)));
-template <int ES>
-__device__ __forceinline__ u32x4_t load_part(const char* p) {
-    if constexpr (ES == 2) return *reinterpret_cast<const u32x4_by2*>(p);
-    else return *reinterpret_cast<const u32x4_by4*>(p);
+
+// elements 0 .. cnt - 1 of a chunk, 0 behind them
+template <typename T>
+__device__ __forceinline__ u32x4_t load_chunk(const char* p, int cnt) {
+    constexpr int EPC = 16 / sizeof(T);
+    if (cnt >= EPC) {
+        if constexpr (sizeof(T) == 2) return *reinterpret_cast<const u32x4_by2*>(p);
+        else return *reinterpret_cast<const u32x4_by4*>(p);
+    }
+    u32x4_t q = {0u, 0u, 0u, 0u};
+    if (cnt > 0) {
+#pragma unroll
+        for (int j = 0; j < EPC - 1; ++j) {
+            if (j < cnt) {
+                if constexpr (sizeof(T) == 4) q[j] = reinterpret_cast<const uint32_t*>(p)[j];
+                else q[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+            }
+        }
+    }
+    return q;
 }
 
-// permutation of a k row's units where k runs down a column; UNITS of them in a row
+// ---- fragments from LDS ----
+// They are read in blocks that wait for their own results.  To the compiler's knowledge a read may touch whatever a load to
+// LDS in flight writes, and it would wait for all of those before the read; the kernel's own waits and barriers order the two.
+
+// k along a row: N rows PITCH bytes apart, 16 bytes each
+template <int N, int PITCH, int OFF>
+__device__ __forceinline__ void read_rows(u32x4_t* o, uint32_t a) {
+    if constexpr (N == 2) {
+        asm volatile(
+            "ds_read_b128 %0, %2 offset:%3\n\t"
+            "ds_read_b128 %1, %2 offset:%4\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(o[0]), "=&v"(o[1])
+            : "v"(a), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH) : "memory");
+    } else if constexpr (N == 4) {
+        asm volatile(
+            "ds_read_b128 %0, %4 offset:%5\n\t"
+            "ds_read_b128 %1, %4 offset:%6\n\t"
+            "ds_read_b128 %2, %4 offset:%7\n\t"
+            "ds_read_b128 %3, %4 offset:%8\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3])
+            : "v"(a), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH) : "memory");
+    } else if constexpr (N == 8) {
+        asm volatile(
+            "ds_read_b128 %0, %8 offset:%9\n\t"
+            "ds_read_b128 %1, %8 offset:%10\n\t"
+            "ds_read_b128 %2, %8 offset:%11\n\t"
+            "ds_read_b128 %3, %8 offset:%12\n\t"
+            "ds_read_b128 %4, %8 offset:%13\n\t"
+            "ds_read_b128 %5, %8 offset:%14\n\t"
+            "ds_read_b128 %6, %8 offset:%15\n\t"
+            "ds_read_b128 %7, %8 offset:%16\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
+            : "v"(a), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH), "i"(OFF + 4 * PITCH), "i"(OFF + 5 * PITCH), "i"(OFF + 6 * PITCH), "i"(OFF + 7 * PITCH) : "memory");
+    }
+}
+
+// ... of both operands
+template <int NA, int NB, int PITCH, int OFF>
+__device__ __forceinline__ void read_rows2(u32x4_t* x, uint32_t a, u32x4_t* y, uint32_t b) {
+    if constexpr (NA == 2 && NB == 4) {
+        asm volatile(
+            "ds_read_b128 %2, %7 offset:%8\n\t"
+            "ds_read_b128 %3, %7 offset:%9\n\t"
+            "ds_read_b128 %4, %7 offset:%10\n\t"
+            "ds_read_b128 %5, %7 offset:%11\n\t"
+            "ds_read_b128 %0, %6 offset:%8\n\t"
+            "ds_read_b128 %1, %6 offset:%9\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(x[0]), "=&v"(x[1]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+            : "v"(a), "v"(b), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH) : "memory");
+    } else if constexpr (NA == 4 && NB == 4) {
+        asm volatile(
+            "ds_read_b128 %4, %9 offset:%10\n\t"
+            "ds_read_b128 %5, %9 offset:%11\n\t"
+            "ds_read_b128 %6, %9 offset:%12\n\t"
+            "ds_read_b128 %7, %9 offset:%13\n\t"
+            "ds_read_b128 %0, %8 offset:%10\n\t"
+            "ds_read_b128 %1, %8 offset:%11\n\t"
+            "ds_read_b128 %2, %8 offset:%12\n\t"
+            "ds_read_b128 %3, %8 offset:%13\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+            : "v"(a), "v"(b), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH) : "memory");
+    } else if constexpr (NA == 8 && NB == 4) {
+        asm volatile(
+            "ds_read_b128 %8, %13 offset:%14\n\t"
+            "ds_read_b128 %9, %13 offset:%15\n\t"
+            "ds_read_b128 %10, %13 offset:%16\n\t"
+            "ds_read_b128 %11, %13 offset:%17\n\t"
+            "ds_read_b128 %0, %12 offset:%14\n\t"
+            "ds_read_b128 %1, %12 offset:%15\n\t"
+            "ds_read_b128 %2, %12 offset:%16\n\t"
+            "ds_read_b128 %3, %12 offset:%17\n\t"
+            "ds_read_b128 %4, %12 offset:%18\n\t"
+            "ds_read_b128 %5, %12 offset:%19\n\t"
+            "ds_read_b128 %6, %12 offset:%20\n\t"
+            "ds_read_b128 %7, %12 offset:%21\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+            : "v"(a), "v"(b), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH), "i"(OFF + 4 * PITCH), "i"(OFF + 5 * PITCH), "i"(OFF + 6 * PITCH), "i"(OFF + 7 * PITCH) : "memory");
+    }
+}
+
+__device__ __forceinline__ u32x4_t join_halves(s16x4 lo, s16x4 hi) {
+    return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// k down a column, half precision: the transposing read, 4 k rows and the next 4, K4 bytes on
+template <int N, int OFF, int K4>
+__device__ __forceinline__ void read_cols(u32x4_t* o, const uint32_t* a) {
+    if constexpr (N == 2) {
+        s16x4 v0, v1, v2, v3;
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+            "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
+            : "v"(a[0]), "v"(a[1]), "i"(OFF), "i"(OFF + K4) : "memory");
+        o[0] = join_halves(v0, v1);
+        o[1] = join_halves(v2, v3);
+    } else if constexpr (N == 4) {
+        s16x4 v0, v1, v2, v3, v4, v5, v6, v7;
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+            "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3), "=&v"(v4), "=&v"(v5), "=&v"(v6), "=&v"(v7)
+            : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "i"(OFF), "i"(OFF + K4) : "memory");
+        o[0] = join_halves(v0, v1);
+        o[1] = join_halves(v2, v3);
+        o[2] = join_halves(v4, v5);
+        o[3] = join_halves(v6, v7);
+    } else if constexpr (N == 8) {
+        s16x4 v0, v1, v2, v3, v4, v5, v6, v7, v8, v9, v10, v11, v12, v13, v14, v15;
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %16 offset:%24\n\tds_read_b64_tr_b16 %1, %16 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %2, %17 offset:%24\n\tds_read_b64_tr_b16 %3, %17 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %4, %18 offset:%24\n\tds_read_b64_tr_b16 %5, %18 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %6, %19 offset:%24\n\tds_read_b64_tr_b16 %7, %19 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %8, %20 offset:%24\n\tds_read_b64_tr_b16 %9, %20 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %10, %21 offset:%24\n\tds_read_b64_tr_b16 %11, %21 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %12, %22 offset:%24\n\tds_read_b64_tr_b16 %13, %22 offset:%25\n\t"
+            "ds_read_b64_tr_b16 %14, %23 offset:%24\n\tds_read_b64_tr_b16 %15, %23 offset:%25\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3), "=&v"(v4), "=&v"(v5), "=&v"(v6), "=&v"(v7), "=&v"(v8), "=&v"(v9), "=&v"(v10), "=&v"(v11), "=&v"(v12), "=&v"(v13), "=&v"(v14), "=&v"(v15)
+            : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(a[4]), "v"(a[5]), "v"(a[6]), "v"(a[7]), "i"(OFF), "i"(OFF + K4) : "memory");
+        o[0] = join_halves(v0, v1);
+        o[1] = join_halves(v2, v3);
+        o[2] = join_halves(v4, v5);
+        o[3] = join_halves(v6, v7);
+        o[4] = join_halves(v8, v9);
+        o[5] = join_halves(v10, v11);
+        o[6] = join_halves(v12, v13);
+        o[7] = join_halves(v14, v15);
+    }
+}
+
+// k down a column, fp32: element by element, 4 k rows ROW bytes apart
+template <int OFF, int ROW>
+__device__ __forceinline__ void read_cols_f32(u32x4_t& o, uint32_t a) {
+    uint32_t v0, v1, v2, v3;
+    asm volatile(
+        "ds_read_b32 %0, %4 offset:%5\n\tds_read_b32 %1, %4 offset:%6\n\t"
+        "ds_read_b32 %2, %4 offset:%7\n\tds_read_b32 %3, %4 offset:%8\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
+        : "v"(a), "i"(OFF), "i"(OFF + ROW), "i"(OFF + 2 * ROW), "i"(OFF + 3 * ROW) : "memory");
+    o = u32x4_t{v0, v1, v2, v3};
+}
+
+// Permutation of a k row's units where k runs down a column, UNITS of them in a row: the k rows that are read together
+// (half precision: 4 consecutive ones and the 4 that stand 8 further; fp32: 4 that are 4 apart) get different values.
 template <typename T, int UNITS>
 __device__ __forceinline__ int unit_swizzle(int krow) {
     const int f = sizeof(T) == 4 ? (krow >> 2) & 3 : (krow & 3) | (((krow >> 3) & 1) << 2);
     return f & (UNITS - 1);
 }
 
-// One operand's path into LDS.  KT: k runs down a column.  R: rows (columns of C) of the tile.  DUAL: the tile's rows are
-// those of two matrices of `half` rows each, 32 of the first and 32 of the second in turn.
-template <typename T, bool KT, int R, int THREADS, bool ALIGNED, bool DUAL>
+// One operand's path into LDS.  KT: k runs down a column.  R: rows (columns of C) of the tile.  TB: bytes of k of a tile.
+// DUAL: the tile's rows are those of two matrices one behind the other, 32 of the first and 32 of the second in turn.
+template <typename T, bool KT, int R, int TB, int THREADS, bool ALIGNED, bool DUAL>
 struct Operand {
-    static constexpr int EPC = 16 / sizeof(T);          // elements of a chunk
-    static constexpr int BK = kTileBytes / sizeof(T);   // elements of a k tile
-    static constexpr int CPR = KT ? R / EPC : 8;        // chunks of a row in LDS
-    static constexpr int ROWS = KT ? BK : R;            // rows in LDS
-    static constexpr int PASSES = ROWS * CPR / THREADS; // chunks a thread moves
-    static constexpr int RSTEP = THREADS / CPR;         // rows between them
-    static constexpr bool SAME = RSTEP % 16 == 0;       // ... which all have the same permutation
+    static constexpr int EPC = 16 / sizeof(T);           // elements of a chunk
+    static constexpr int BK = TB / sizeof(T);            // k values of a tile
+    static constexpr int CPR = KT ? R / EPC : TB / 16;   // chunks of a row in LDS
+    static constexpr int ROWS = KT ? BK : R;             // rows in LDS
+    static constexpr int PASSES = ROWS * CPR / THREADS;  // chunks a thread moves
+    static constexpr int RSTEP = THREADS / CPR;          // rows between them
     static constexpr int BYTES = ROWS * CPR * 16;
-    static_assert(PASSES * THREADS == ROWS * CPR , "tile and work-group");
+    static_assert(PASSES * THREADS == ROWS * CPR, "tile and work-group");
+    static_assert(KT || RSTEP % 16 == 0, "a thread's chunks are at one place of their rows");
 
-    const char* base;      // of the tile's first row and the current k tile
-    int64_t ld;            // bytes
-    int row0, slot;        // this thread's first row and its place in it
-    int chunk;             // the chunk that stands there
-    int rows_left;         // rows of the matrix from the tile's first on (columns, where k runs down)
-    int k_left;            // k values from the current tile on
-    uint32_t voff;         // byte offset of the thread's first chunk
-    int64_t half_off;      // DUAL: bytes from a row of the first half to the same row of the second
+    // An offset past the buffer's range: the load gives 0.  (The range ends here; a tile's rows span no more than
+    // 256 * 2^22 bytes = 2^30.)
+    static constexpr uint32_t kOut = 0x7FFFFFF0u;
+
+    const char* base;       // of the tile's first row and the current k tile
+    int64_t step;           // bytes to the next k tile
+    int64_t ld;             // bytes
+    int64_t half_off;       // DUAL: bytes from a row of the first matrix to the same row of the second
+    int k_left;             // k values from the current tile on
+    int key;                // the k value in a tile of a thread's first chunk (k along a row: of the chunk's first element)
+    int row0, slot;         // the thread's first row and its place in it
+    int rows_left;          // rows (columns) of the matrix from the tile's first on
+    uint32_t voff[PASSES];  // ALIGNED: offsets of the thread's chunks from base, kOut outside the matrix
     u32x4_t reg[ALIGNED ? 1 : PASSES];
 
-    __device__ __forceinline__ static int chunk_at(int r, int slot) {
+    // the chunk that stands at place `s` of row r
+    __device__ __forceinline__ static int chunk_at(int r, int s) {
         if constexpr (KT) {
             constexpr int UB = sizeof(T) == 4 ? 2 : 1;  // log2 of a unit's chunks
-            return (((slot >> UB) ^ unit_swizzle<T, (CPR >> UB)>(r)) << UB) | (slot & ((1 << UB) - 1));
+            return (((s >> UB) ^ unit_swizzle<T, (CPR >> UB)>(r)) << UB) | (s & ((1 << UB) - 1));
         } else {
-            return slot ^ ((r >> 1) & 7);
+            return s ^ ((r >> 1) & (CPR - 1));
         }
     }
+    __device__ __forceinline__ int chunk_of(int i) const { return chunk_at(row0 + i * RSTEP, slot); }
+    // DUAL: row r of the tile is row f of its matrix
+    __device__ __forceinline__ static int source_row(int r) { return DUAL ? ((r >> 6) << 5) | (r & 31) : r; }
+    __device__ __forceinline__ static bool second(int r) { return DUAL && ((r >> 5) & 1); }
 
-    __device__ __forceinline__ int chunk_of(int i) const { return SAME ? chunk : chunk_at(row0 + i * RSTEP, slot); }
-
-    // row: first row (column) of the tile; rows: of the matrix (DUAL: of one half)
+    // row: first row (column) of the tile; rows: of the matrix (DUAL: of one of the two)
     __device__ __forceinline__ void init(const void* p, int64_t ld_elems, int row, int rows, int k0, int k1, int tid) {
         ld = ld_elems * (int64_t)sizeof(T);
         row0 = tid / CPR;
         slot = tid % CPR;
-        chunk = chunk_at(row0, slot);
         rows_left = rows - row;
         k_left = k1 - k0;
-        if constexpr (KT) base = static_cast<const char*>(p) + (int64_t)row * sizeof(T) + (int64_t)k0 * ld;
-        else base = static_cast<const char*>(p) + (int64_t)row * ld + (int64_t)k0 * sizeof(T);
-        if constexpr (DUAL) half_off = (int64_t)rows * ld;
-        voff = (uint32_t)row0 * (uint32_t)ld + chunk * 16u;
+        const int64_t down = KT ? k0 : row, along = KT ? row : k0;
+        base = static_cast<const char*>(p) + down * ld + along * (int64_t)sizeof(T);
+        step = KT ? (int64_t)BK * ld : (int64_t)TB;
+        half_off = (int64_t)rows * ld;
+        key = KT ? row0 : chunk_of(0) * EPC;
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int r = row0 + i * RSTEP, c = chunk_of(i), f = source_row(r);
+                const bool in = KT ? c * EPC < rows_left : f < rows_left;
+                voff[i] = in ? (uint32_t)f * (uint32_t)ld + (uint32_t)c * 16u : kOut;
+            }
+        }
     }
 
-    // Copies the current k tile to `lds` (ALIGNED), or to registers; then steps to the next.  What lies outside the
-    // matrix becomes 0: by the buffer's range check where rows or k rows end, by an offset past any range where a row does.
+    // Starts the current k tile's loads to `lds` (ALIGNED), or into registers; then steps to the next.  What lies outside
+    // the matrix becomes 0, and so do tiles past the last.
     __device__ __forceinline__ void fetch(char* lds, int tid) {
         if constexpr (ALIGNED) {
-            // (a tile's rows span no more than 256 * 2^22 bytes = 2^30: no range reaches kOut)
-            constexpr uint32_t kOut = 0x7FFFFFF0u;
+            if (k_left < BK) {  // (the last tile; those behind it stay empty)
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) voff[i] = key + (KT ? i * RSTEP : 0) < k_left ? voff[i] : kOut;
+            }
             const int wave_lds = (tid & ~63) * 16;
-            // rows run to the last valid one; where k runs along them its end is the range's end for the last row only
-            const int nrow = KT ? k_left : rows_left, ncol = KT ? rows_left : k_left;
-            // (whole chunks: a row that ends inside one is a row of dz, which is padded with zeros)
-            const int64_t bytes = nrow > 0 && ncol > 0 ? (int64_t)(nrow - 1) * ld + (int64_t)((ncol + EPC - 1) / EPC) * 16 : 0;
-            const int range = bytes < (int64_t)kOut ? (int)bytes : (int)kOut;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 char* const dst = lds + wave_lds + i * THREADS * 16;
-                if constexpr (DUAL) {
-                    const int r = row0 + i * RSTEP;
-                    // (a wavefront's 8 rows are all of one matrix)
-                    const bool second = __builtin_amdgcn_readfirstlane(r >> 5) & 1;
-                    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (second ? half_off : 0)), 0, range, 0x00020000);
-                    const uint32_t f = (uint32_t)(((r >> 6) << 5) | (r & 31));
-                    const uint32_t v = chunk * EPC < ncol ? f * (uint32_t)ld + chunk * 16u : kOut;
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, v, 0, 0, 0);
-                } else {
-                    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, range, 0x00020000);
-                    const int ch = chunk_of(i);
-                    const uint32_t v = ch * EPC < ncol ? voff + (uint32_t)(i * RSTEP) * (uint32_t)ld + (uint32_t)(ch - chunk) * 16u : kOut;
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, v, 0, 0, 0);
-                }
+                // (a wavefront's rows are all of one matrix)
+                const char* const src = base + (DUAL && (__builtin_amdgcn_readfirstlane(row0 + i * RSTEP) >> 5) & 1 ? half_off : 0);
+                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, 0, kOut, 0x00020000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, voff[i], 0, 0, 0);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
-                const int r = row0 + i * RSTEP, chunk = chunk_of(i);
-                const char* p;
-                int cnt;  // elements of the chunk inside the matrix
-                if constexpr (KT) {
-                    p = base + (int64_t)r * ld + chunk * 16;
-                    cnt = r < k_left ? rows_left - chunk * EPC : 0;
-                } else if constexpr (DUAL) {
-                    const int f = ((r >> 6) << 5) | (r & 31);
-                    p = base + ((r >> 5) & 1 ? half_off : 0) + (int64_t)f * ld + chunk * 16;
-                    cnt = f < rows_left ? k_left - chunk * EPC : 0;
-                } else {
-                    p = base + (int64_t)r * ld + chunk * 16;
-                    cnt = r < rows_left ? k_left - chunk * EPC : 0;
-                }
-                reg[i] = load_chunk(p, cnt);
+                const int r = row0 + i * RSTEP, c = chunk_of(i), f = source_row(r);
+                const char* const p = base + (second(r) ? half_off : 0) + (int64_t)f * ld + c * 16;
+                const int cnt = KT ? (r < k_left ? rows_left - c * EPC : 0) : (f < rows_left ? k_left - c * EPC : 0);
+                reg[i] = load_chunk<T>(p, cnt);
             }
         }
         k_left -= BK;
-        base += KT ? (int64_t)BK * ld : (int64_t)kTileBytes;
-    }
-
-    __device__ __forceinline__ static u32x4_t load_chunk(const char* p, int cnt) {
-        if (cnt >= EPC) return load_part<sizeof(T)>(p);
-        u32x4_t q = {0u, 0u, 0u, 0u};
-        if (cnt > 0) {
-#pragma unroll
-            for (int j = 0; j < EPC - 1; ++j) {
-                if (j < cnt) {
-                    if constexpr (sizeof(T) == 4) q[j] = reinterpret_cast<const uint32_t*>(p)[j];
-                    else q[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
-                }
-            }
-        }
-        return q;
+        base += step;
     }
 
     __device__ __forceinline__ void put(char* lds, int tid) const {
@@ -178,29 +333,41 @@ struct Operand {
         }
     }
 
-    // 64 bytes of k (half a k tile, kk = 0, 1) of the 16 rows from `row` on: lane l gets row l % 16, its k values
-    // (l / 16) * 16 bytes on
-    __device__ __forceinline__ static u32x4_t frag(const char* lds, int row, int kk, int lane) {
+    // Where a lane reads in a tile: row (column) `row` + l % 16 of N blocks of 16, its k values (l / 16) * 16 bytes on in
+    // each 64 bytes of k (k along a row: block i stands 16 rows on)
+    template <int N>
+    struct Place {
+        static constexpr int COUNT = KT ? N : TB / 64;
+        uint32_t a[COUNT];
+    };
+    template <int N>
+    __device__ __forceinline__ static void place(Place<N>& p, uint32_t at, int row, int lane) {
         const int g = lane >> 4, j = lane & 15;
         if constexpr (!KT) {
-            const int r = row + j;
-            return *reinterpret_cast<const u32x4_t*>(lds + r * 128 + (((kk * 4 + g) ^ ((r >> 1) & 7)) << 4));
-        } else if constexpr (sizeof(T) == 2) {
-            const int k = kk * 32 + g * 8 + (j >> 2);
-            const int u0 = (row >> 4) ^ unit_swizzle<T, CPR / 2>(k);  // (the same for k + 4)
-            const char* p = lds + k * (CPR * 16) + u0 * 32 + (j & 3) * 8;
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * CPR * 16));
-            return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        } else {
-            u32x4_t q;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = kk * 16 + g * 4 + i;
-                const int u0 = (row >> 4) ^ unit_swizzle<T, CPR / 4>(k);
-                q[i] = *reinterpret_cast<const uint32_t*>(lds + k * (CPR * 16) + u0 * 64 + j * 4);
-            }
-            return q;
+            for (int h = 0; h < TB / 64; ++h)
+                p.a[h] = at + (uint32_t)((row + j) * TB + (((h * 4 + g) ^ ((j >> 1) & (CPR - 1))) << 4));
+        } else if constexpr (sizeof(T) == 2) {
+            const int k = g * 8 + (j >> 2), f = unit_swizzle<T, CPR / 2>(k);  // (the same for k + 4)
+#pragma unroll
+            for (int v = 0; v < N; ++v) p.a[v] = at + (uint32_t)(k * (CPR * 16) + (j & 3) * 8 + ((((row >> 4) + v) ^ f) << 5));
+        } else {
+            const int f = unit_swizzle<T, CPR / 4>(g * 4);  // (the same for the four k rows)
+#pragma unroll
+            for (int v = 0; v < N; ++v) p.a[v] = at + (uint32_t)(g * 4 * (CPR * 16) + j * 4 + ((((row >> 4) + v) ^ f) << 6));
+        }
+    }
+    // Fragments of the N blocks from the tile OFF bytes on (TB = 64)
+    template <int N, int OFF>
+    __device__ __forceinline__ static void frags(u32x4_t (&out)[N], const Place<N>& p) {
+        static_assert(TB == 64, "one block of k");
+        if constexpr (!KT) {
+            read_rows<N, 16 * TB, OFF>(out, p.a[0]);
+        } else if constexpr (sizeof(T) == 2) {
+            read_cols<N, OFF, 4 * CPR * 16>(out, p.a);
+        } else {
+#pragma unroll
+            for (int v = 0; v < N; ++v) read_cols_f32<OFF, CPR * 16>(out[v], p.a[v]);
         }
     }
 };
@@ -212,9 +379,26 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// A barrier that nothing is moved across, and that waits for nothing itself: what has to be there is waited for before it.
+__device__ __forceinline__ void bare_barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// waits until no more than N of this wavefront's loads are in flight
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+    asm volatile("" ::: "memory");
+}
+
 // Work-group -> tile.  Consecutive work-groups go to the 8 XCDs in turn; each XCD gets a stretch of consecutive tiles, and
-// those run down 8 tile rows before the next column, so that the tiles an XCD works on at a time share rows and columns in
-// its L2.
+// those run down 8 tile rows before the next column, so that the 32 tiles an XCD works on at a time share rows and columns
+// in its L2 (nine requests in ten hit).
 __device__ __forceinline__ void tile_of(int wg, int total, int tiles_m, int tiles_n, int& tm, int& tn, int& sp) {
     const int q = total / 8, r = total % 8, x = wg % 8, i = wg / 8;
     int t = x < r ? x * (q + 1) + i : r * (q + 1) + (x - r) * q + i;
@@ -229,16 +413,23 @@ __device__ __forceinline__ void tile_of(int wg, int total, int tiles_m, int tile
 }
 
 template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED, bool GATED>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_gemm(const GemmArgs ga) {
-    constexpr int THREADS = 64 * WAVES_M * WAVES_N;
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmArgs ga) {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass has no use for the body, and does not know its assembly)
+    constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, MI = WM / 16, NJ = WN / 16;
-    constexpr int BK = kTileBytes / sizeof(T);
-    using OpA = Operand<T, LAY == L_TT, BM, THREADS, ALIGNED, false>;
-    using OpB = Operand<T, LAY != L_KK, BN, THREADS, ALIGNED, GATED>;
-    static_assert(!GATED || WN == 64, "a wavefront's columns are 32 of the gate and 32 of the other");
+    constexpr bool PAIRED = WAVES == 8;
+    // With k along both operands' rows a tile has 128 bytes of them: whole cache lines, half the requests, 5 % faster on
+    // 16384 x 2048 x 8192 than 64.  With k down a column a row is long anyway, and tiles of 64 bytes in four slots were
+    // 10 % faster: the loads are spread over all phases.
+    constexpr int TB = LAY == L_KK ? 128 : 64;
+    constexpr int BK = TB / sizeof(T);
+    using OpA = Operand<T, LAY == L_TT, BM, TB, THREADS, ALIGNED, false>;
+    using OpB = Operand<T, LAY != L_KK, BN, TB, THREADS, ALIGNED, GATED>;
+    static_assert(WN == 64, "a wavefront's columns (gated: 32 of the gate and 32 of the other)");
     constexpr int STAGE = OpA::BYTES + OpB::BYTES;
-    __shared__ __attribute__((aligned(16))) char lds0[STAGE];
-    __shared__ __attribute__((aligned(16))) char lds1[STAGE];
+    constexpr int A3 = 3 * OpA::BYTES;  // k along the rows: three slots for A, then two for B
+    constexpr int LDS = LAY == L_KK ? A3 + 2 * OpB::BYTES : 4 * STAGE;
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int tm, tn, sp;
@@ -257,55 +448,177 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_gemm(const GemmArgs 
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    struct { u32x4_t a[MI], b[NJ]; } f;
+    auto multiply = [&] {
+        if constexpr (PAIRED) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(f.b[j], f.a[i], acc[i][j]);
+        if constexpr (PAIRED) __builtin_amdgcn_s_setprio(0);
+    };
+    constexpr std::integral_constant<int, 0> i0{};
+    constexpr std::integral_constant<int, 1> i1{};
+    constexpr std::integral_constant<int, 2> i2{};
+    constexpr std::integral_constant<int, 3> i3{};
+    const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds;
+    const bool late = wave >= WAVES / 2;
 
-    auto compute = [&](const char* lds) {
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            u32x4_t fa[MI], fb[NJ];
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) fb[j] = OpB::frag(lds + OpA::BYTES, wn + j * 16, kk, lane);
-#pragma unroll
-            for (int i = 0; i < MI; ++i) fa[i] = OpA::frag(lds, wm + i * 16, kk, lane);
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
-        }
-    };
-    // one k tile: wait for it, let the other buffer's readers finish, start the next tile's loads into that buffer
-    auto step = [&](char* cur, char* nxt, bool more) {
+    if constexpr (LAY == L_KK) {
+        typename OpA::template Place<MI> pa;
+        typename OpB::template Place<NJ> pb;
+        OpA::template place<MI>(pa, at, wm, lane);
+        OpB::template place<NJ>(pb, at + A3, wn, lane);
+        uint32_t sa = 0, sb = 0;  // slots of the current tiles, in bytes
+        auto read = [&](auto half) {
+            constexpr int H = decltype(half)::value;
+            read_rows2<MI, NJ, 16 * TB, 0>(f.a, pa.a[H] + sa, f.b, pb.a[H] + sb);
+            __builtin_amdgcn_sched_barrier(0);  // (the reads first, the loads behind them)
+        };
+        auto next = [&] {
+            sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
+            sb = OpB::BYTES - sb;
+        };
         if constexpr (ALIGNED) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-            if (more) { oa.fetch(nxt, tid); ob.fetch(nxt + OpA::BYTES, tid); }
-            compute(cur);
+            // A tile of B is started when all have read the one before the last, two of A are on their way
+            auto load_b = [&] { ob.fetch(lds + A3 + (OpB::BYTES - sb), tid); };
+            auto load_a = [&] { oa.fetch(lds + (sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES), tid); };
+            oa.fetch(lds, tid);
+            ob.fetch(lds + A3, tid);
+            oa.fetch(lds + OpA::BYTES, tid);
+            if constexpr (PAIRED) {
+                // The wait for the next tiles stands before the barrier behind which the first group reads them
+                wait_loads<OpA::PASSES>();
+                bare_barrier();
+                if (late) bare_barrier();
+                for (int s = 0; s < steps; ++s) {
+                    read(i0);
+                    load_b();
+                    bare_barrier();
+                    multiply();
+                    bare_barrier();
+                    read(i1);
+                    load_a();
+                    if (late) wait_loads<OpA::PASSES>();
+                    bare_barrier();
+                    multiply();
+                    if (!late) wait_loads<OpA::PASSES>();
+                    bare_barrier();
+                    next();
+                }
+                if (!late) bare_barrier();
+            } else {
+                for (int s = 0; s < steps; ++s) {
+                    wait_loads<OpA::PASSES>();
+                    bare_barrier();
+                    read(i0);
+                    load_b();
+                    multiply();
+                    read(i1);
+                    load_a();
+                    multiply();
+                    next();
+                }
+            }
         } else {
-            oa.put(cur, tid);
-            ob.put(cur + OpA::BYTES, tid);
-            __syncthreads();
-            if (more) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
-            compute(cur);
+            if (steps > 0) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
+            for (int s = 0; s < steps; ++s) {
+                oa.put(lds + sa, tid);
+                ob.put(lds + A3 + sb, tid);
+                __syncthreads();
+                if (s + 1 < steps) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
+                read(i0);
+                multiply();
+                read(i1);
+                multiply();
+                next();
+            }
         }
-    };
-    if (steps > 0) {
-        oa.fetch(lds0, tid);
-        ob.fetch(lds0 + OpA::BYTES, tid);
+    } else {
+        // four slots, each with a tile of A and one of B; a lane's places in the first and in the third
+        typename OpA::template Place<MI> pa[2];
+        typename OpB::template Place<NJ> pb[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            OpA::template place<MI>(pa[h], at + h * 2 * STAGE, wm, lane);
+            OpB::template place<NJ>(pb[h], at + h * 2 * STAGE + OpA::BYTES, wn, lane);
+#pragma unroll
+            for (int i = 0; i < pa[h].COUNT; ++i) asm volatile("" : "+v"(pa[h].a[i]));  // (kept, not made again)
+#pragma unroll
+            for (int i = 0; i < pb[h].COUNT; ++i) asm volatile("" : "+v"(pb[h].a[i]));
+        }
+        auto read = [&](auto slot) {
+            constexpr int H = decltype(slot)::value / 2, OFF = decltype(slot)::value % 2 * STAGE;
+            OpB::template frags<NJ, OFF>(f.b, pb[H]);
+            OpA::template frags<MI, OFF>(f.a, pa[H]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if constexpr (ALIGNED) {
+            constexpr int LOADS = OpA::PASSES + OpB::PASSES;
+            auto load = [&](int slot) {
+                oa.fetch(lds + slot * STAGE, tid);
+                ob.fetch(lds + slot * STAGE + OpA::BYTES, tid);
+            };
+            load(0);
+            load(1);
+            load(2);
+            auto step = [&](auto slot) {
+                constexpr int S = decltype(slot)::value;
+                if constexpr (PAIRED) {
+                    read(slot);
+                    load((S + 3) % 4);
+                    wait_loads<2 * LOADS>();
+                    bare_barrier();
+                    multiply();
+                    bare_barrier();
+                } else {
+                    wait_loads<2 * LOADS>();
+                    bare_barrier();
+                    read(slot);
+                    load((S + 3) % 4);
+                    multiply();
+                }
+            };
+            if constexpr (PAIRED) {
+                wait_loads<2 * LOADS>();
+                bare_barrier();
+                if (late) bare_barrier();
+            }
+            for (int s = 0; s < steps; s += 4) {  // (tiles past the last are zeros)
+                step(i0);
+                step(i1);
+                step(i2);
+                step(i3);
+            }
+            if constexpr (PAIRED) {
+                if (!late) bare_barrier();
+            }
+        } else {
+            auto step = [&](auto slot, bool more) {
+                constexpr int S = decltype(slot)::value;
+                oa.put(lds + S * STAGE, tid);
+                ob.put(lds + S * STAGE + OpA::BYTES, tid);
+                __syncthreads();
+                if (more) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
+                read(slot);
+                multiply();
+            };
+            if (steps > 0) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
+            for (int s = 0; s < steps; s += 2) {
+                step(i0, s + 1 < steps);
+                if (s + 1 < steps) step(i1, s + 2 < steps);
+            }
+        }
     }
-    for (int s = 0; s < steps; s += 2) {
-        step(lds0, lds1, s + 1 < steps);
-        if (s + 1 < steps) step(lds1, lds0, s + 2 < steps);
-    }
+    wait_loads<0>();  // (tiles past the last may still be on their way)
 
     // Epilogue: a wavefront's part goes through its own piece of LDS, so that a lane gets eight consecutive columns; the
     // 16-byte units of a row are permuted by the row
-    constexpr int RM = WM < 64 ? WM : 64;  // rows at a time
-    static_assert(WN == 64 && WM % RM == 0, "a row of the piece has 16 units");
-    static_assert(WAVES_M * WAVES_N * RM * 256 <= 2 * STAGE, "room for the epilogue");
-    constexpr int PER = STAGE / (RM * 256);  // wavefronts whose pieces are in the first buffer
+    constexpr int FIT = LDS / WAVES / 256;                    // rows a wavefront has room for
+    constexpr int RM = FIT >= WM ? WM : FIT >= 64 ? 64 : 32;  // rows at a time
+    static_assert(RM <= FIT && WM % RM == 0, "room for the epilogue");
     __syncthreads();
-    char* const buf = (wave < PER ? lds0 + wave * RM * 256 : lds1 + (wave - PER) * RM * 256);
+    char* const buf = lds + wave * RM * 256;
     const uint64_t offset = full_offset(ga.e.offset, ga.e.d_offset);
     const int g = lane >> 4, c16 = lane & 15;
     constexpr int CH = GATED ? 4 : 8;  // chunks of eight columns in a row
@@ -347,6 +660,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void k_gemm(const GemmArgs 
         }
         wave_sync();
     }
+#endif
 }
 
 // Few rows (at most 16): the product is a pass over B.  A work-group takes 16 columns of C (gated: and the 16 of the other
@@ -365,7 +679,6 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(const GemmArgs ga)
     const T* pu = pb + (int64_t)ga.N * ldb;
     const bool row_ok = j < ga.M;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f}, accu = {0.f, 0.f, 0.f, 0.f};
-    using Op = Operand<T, false, 128, 256, false, false>;
     auto chunk = [&](const T* p, int k) {  // elements k .. k + EPC - 1 of a row, 0 past its end
         const int cnt = ga.K - k - g * EPC;
         if constexpr (ALIGNED) {
@@ -373,7 +686,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(const GemmArgs ga)
             if (cnt > 0) q = *reinterpret_cast<const u32x4_t*>(p + k);
             return q;
         } else {
-            return Op::load_chunk(reinterpret_cast<const char*>(p + k), cnt);
+            return load_chunk<T>(reinterpret_cast<const char*>(p + k), cnt);
         }
     };
     for (int k = wave * KS * UN; k < ga.K; k += kSkinnyWaves * KS * UN) {
@@ -514,22 +827,28 @@ __global__ __launch_bounds__(256) void k_dz(const DzArgs da) {
     }
 }
 
-// bias gradient: the row blocks' sums added up in order
+// bias gradient: the row blocks' sums added up in a fixed order, 32 columns a work-group, 32 rows at a time
 template <typename T>
-__global__ __launch_bounds__(256) void k_sum(const SumArgs sa) {
-    __shared__ float red[8][33];
+__global__ __launch_bounds__(1024) void k_sum(const SumArgs sa) {
+    __shared__ float red[32][33];
     const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + cx, total = sa.n;
-    float s = 0.f;
-    if (c < total)
-        for (int i = ry; i < sa.row_blocks; i += 8) s += sa.sums[(int64_t)i * sa.sums_ld + c];
-    red[ry][cx] = s;
-    __syncthreads();
-    if (ry == 0 && c < total) {
-        s = 0.f;
+    const int c = blockIdx.x * 32 + cx;
+    float s[4] = {};
+    if (c < sa.n) {
+        const float* const p = sa.sums + c;
+        for (int i = ry; i < sa.row_blocks; i += 128) {
 #pragma unroll
-        for (int w = 0; w < 8; ++w) s += red[w][cx];
-        static_cast<T*>(sa.out)[c] = (T)s;
+            for (int u = 0; u < 4; ++u)
+                if (i + 32 * u < sa.row_blocks) s[u] += p[(int64_t)(i + 32 * u) * sa.sums_ld];
+        }
+    }
+    red[ry][cx] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    if (ry == 0 && c < sa.n) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 32; ++w) t += red[w][cx];
+        static_cast<T*>(sa.out)[c] = (T)t;
     }
 }
 
@@ -613,7 +932,7 @@ hipError_t DenseOps<T>::dz(const DzArgs& d, hipStream_t s) {
 
 template <typename T>
 hipError_t DenseOps<T>::sum(const SumArgs& a, hipStream_t s) {
-    k_sum<T><<<dim3((unsigned)((a.n + 31) / 32)), dim3(256), 0, s>>>(a);
+    k_sum<T><<<dim3((unsigned)((a.n + 31) / 32)), dim3(1024), 0, s>>>(a);
     return hipGetLastError();
 }
 
