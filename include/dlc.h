@@ -342,9 +342,10 @@ int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* tot
  *              epilogue are fp32; a result is rounded once, when it is stored.  The backward pass rounds dz (below) to the
  *              type as well, since it is an operand of two products; the bias gradient sums it unrounded.
  *   matrices   row-major, columns one element apart, rows a leading dimension (in elements) apart; a leading dimension of
- *              0 means the row's length.  Pointers lie on an element's boundary.  Rows on 16-byte boundaries (pointer
- *              and leading dimension, and for the products the row's length too) are what the fast kernels want; others
- *              are slower, never refused.
+ *              0 means the row's length.  Pointers lie on an element's boundary.  x and w are read where they stand if
+ *              their rows start and end on 16-byte boundaries; otherwise they are first copied to such rows in the
+ *              workspace (with up to 16 rows a forward call never copies).  Weights that are used often are best kept with
+ *              a leading dimension and a row length on such boundaries.
  *   sizes      rows 0 .. 2^30, features 1 .. 2^20, leading dimensions up to 2^20.  With no rows a forward call does
  *              nothing and a backward call writes zero weight and bias gradients.
  *   drop(v)    of the element in row r and column c: 0 if its 16 random bits are below t = round(65536 p), else
@@ -356,15 +357,22 @@ int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* tot
  *   overlap    d_residual may be d_y; d_x may be d_y in dlc_dropout (with equal leading dimensions).  No other output
  *              may overlap an input, another output or the workspace.
  *   d_work     16-byte aligned, work_bytes at least dlc_*_workspace_bytes of the configuration and direction (else
- *              DLC_ECAPACITY); may be NULL where that is 0.  Not initialised, not kept: calls in order on a stream share it.
+ *              DLC_ECAPACITY); may be NULL where that is 0.  The room for copies of x and w counts in where the row
+ *              length or the leading dimension asks for them; if only a pointer is off a 16-byte boundary, set
+ *              DLC_DENSE_OFF_BOUNDARY, which counts them in for any pointers.  Not initialised, not kept: calls in order on a stream share it.
  * Return values: DLC_OK, DLC_EINVAL (geometry, null or misaligned pointer, p outside [0, 1]), DLC_ECAPACITY, DLC_EHIP.
  */
 enum { DLC_ACT_NONE = 0, DLC_ACT_RELU = 1, DLC_ACT_SIGMOID = 2, DLC_ACT_SILU = 3 /* z sigmoid(z) */,
        DLC_ACT_GELU = 4 /* z/2 (1 + erf(z / sqrt 2)) */ };
 
+/* dlc_dense_config.flags: the workspace is to have room for x and w wherever their pointers lie (below) */
+enum { DLC_DENSE_OFF_BOUNDARY = 1 };
+
 typedef struct {
     int32_t dtype;             /* DLC_F32, DLC_F16 or DLC_BF16 */
     int32_t act;               /* DLC_ACT_* */
+    int32_t flags;             /* 0 or DLC_DENSE_OFF_BOUNDARY */
+    int32_t reserved;          /* 0 */
     int64_t rows;              /* M: samples */
     int64_t in_features;       /* K */
     int64_t out_features;      /* N */
@@ -409,7 +417,7 @@ int dlc_gated_forward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, con
                       void* d_pre, void* d_work, size_t work_bytes, void* stream);
 int dlc_gated_backward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_pre,
                        const void* d_dy, void* d_dx, void* d_dw, void* d_dbias, void* d_work, size_t work_bytes, void* stream);
-/* Workspace of a forward (backward = 0) or backward call with any alignment; 0 also if cfg is invalid. */
+/* Workspace of a forward (backward = 0) or backward call; 0 also if cfg is invalid. */
 size_t dlc_linear_workspace_bytes(const dlc_dense_config* cfg /*HOST*/, int backward);
 size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg /*HOST*/, int backward);
 /*

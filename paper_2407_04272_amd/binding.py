@@ -14,6 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdlc.so")
 
 F32, F16, BF16 = 0, 1, 2  # BF16: dense operators only
+DENSE_OFF_BOUNDARY = 1
 ACT_NONE, ACT_RELU, ACT_SIGMOID, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
 OK, EINVAL, ENOMEM, ECAPACITY, ECORRUPT, EHIP, ESTATE, ELIMIT = 0, -1, -2, -3, -4, -5, -6, -7
 STATIC_MAX_TABLES = 4096
@@ -41,7 +42,8 @@ class ControllerParams(C.Structure):
 
 
 class DenseConfig(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int64),
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("flags", C.c_int32), ("reserved", C.c_int32),
+                ("rows", C.c_int64), ("in_features", C.c_int64),
                 ("out_features", C.c_int64), ("ld_x", C.c_int64), ("ld_w", C.c_int64), ("ld_y", C.c_int64),
                 ("ld_pre", C.c_int64), ("ld_res", C.c_int64), ("ld_dy", C.c_int64), ("ld_dx", C.c_int64),
                 ("ld_dw", C.c_int64), ("dropout_p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64),
@@ -164,11 +166,22 @@ def dlc_decompress_static(cfg: Config, d_comp, comp_bytes, d_payload_out, d_stat
                                        _stream_ptr(stream))
 
 
+_raw_stream = None
+
+
 def _stream_ptr(stream):
-    if stream is None:
+    if stream is not None:
+        return C.c_void_p(int(stream.cuda_stream))
+    # the handle alone, where torch gives it: making its stream object took a third of a small call (2.7 of 7.6 us)
+    global _raw_stream
+    if _raw_stream is None:
         import torch
-        stream = torch.cuda.current_stream()
-    return C.c_void_p(int(stream.cuda_stream))
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            _raw_stream = lambda: raw(torch.cuda.current_device())  # noqa: E731
+        else:
+            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    return C.c_void_p(_raw_stream())
 
 
 def _np_ptr(a):
@@ -177,10 +190,10 @@ def _np_ptr(a):
 
 # ---- dense operators: linear layers, gated blocks, dropout (no context; see include/dlc.h) ----
 def make_dense_config(dtype, rows, in_features, out_features, act=ACT_NONE, dropout_p=0.0, seed=0, offset=0, d_offset=None,
-                      ld_x=0, ld_w=0, ld_y=0, ld_pre=0, ld_res=0, ld_dy=0, ld_dx=0, ld_dw=0) -> DenseConfig:
+                      flags=0, ld_x=0, ld_w=0, ld_y=0, ld_pre=0, ld_res=0, ld_dy=0, ld_dx=0, ld_dw=0) -> DenseConfig:
     """ld_*: elements from row to row, 0 for dense rows.  d_offset: an int64 tensor of one element on the GPU that the
     kernels add to `offset` (a replayed graph counts it up), which has to live as long as the configuration."""
-    return DenseConfig(dtype, act, rows, in_features, out_features, ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw,
+    return DenseConfig(dtype, act, flags, 0, rows, in_features, out_features, ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw,
                        dropout_p, seed, offset, _ptr(d_offset))
 
 

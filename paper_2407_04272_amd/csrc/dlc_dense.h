@@ -24,9 +24,7 @@ struct Epi {
     float scale;      // 65536 / (65536 - thr)
     int32_t act;
     int32_t n;        // columns of y (gated: the gate's half of the sums' columns)
-    uint32_t vec;     // bit 0: y, 1: pre, 2: residual, 3: bias are read and written 16 bytes at a time
 };
-enum { VEC_Y = 1, VEC_PRE = 2, VEC_RES = 4, VEC_BIAS = 8 };
 
 // One product: C[m][n] = sum over k of A(m, k) B(n, k).
 struct GemmArgs {
@@ -41,12 +39,20 @@ struct GemmArgs {
     Epi e;
 };
 
-// Adds up the partial sums of a product and does its epilogue
+// Adds up the partial sums of a product and does its epilogue (M = 0: nothing)
 struct JoinArgs {
     const float* part;
     int64_t part_ld;
     int32_t M, split, gated;
     Epi e;
+};
+
+// Up to two matrices whose rows are copied to 16-byte boundaries: dst is [rows][cols rounded up to whole chunks]
+struct PackArgs {
+    const void* src[2];
+    void* dst[2];
+    int64_t ld[2], rows[2];
+    int32_t cols[2];
 };
 
 // dz = drop(dy) * act'(pre) (gated: both halves) and the partial column sums for the bias gradient
@@ -63,9 +69,9 @@ struct DzArgs {
     float scale;
     uint64_t seed, offset;
     const uint64_t* d_offset;
-    uint32_t vec;         // bit 0: dy, 1: pre, 2: dz
 };
 
+// Adds up the row blocks' sums: the bias gradient (n = 0: nothing)
 struct SumArgs {
     const float* sums;
     int64_t sums_ld;
@@ -83,7 +89,6 @@ struct DropArgs {
     float scale;
     uint64_t seed, offset;
     const uint64_t* d_offset;
-    uint32_t vec;
 };
 
 // operand layouts of a product: both with k along a row (x w'), a with k along a row and b with k down a column (dz w),
@@ -92,11 +97,11 @@ enum Layout { L_KK = 0, L_KT = 1, L_TT = 2 };
 
 template <typename T>
 struct DenseOps {
-    static hipError_t gemm(const GemmArgs& g, Layout lay, bool gated, int tile, bool aligned, hipStream_t s);
+    static hipError_t gemm(const GemmArgs& g, Layout lay, bool gated, int tile, hipStream_t s);
     static hipError_t skinny(const GemmArgs& g, bool gated, bool aligned, hipStream_t s);
-    static hipError_t join(const JoinArgs& j, hipStream_t s);
-    static hipError_t dz(const DzArgs& d, hipStream_t s);
-    static hipError_t sum(const SumArgs& a, hipStream_t s);
+    static hipError_t join(const JoinArgs& j, const SumArgs& a, hipStream_t s);
+    static hipError_t pack(const PackArgs& p, hipStream_t s);
+    static hipError_t dz(const DzArgs& d, const PackArgs& p, hipStream_t s);
     static hipError_t drop(const DropArgs& d, hipStream_t s);
 };
 
@@ -109,7 +114,8 @@ inline __host__ __device__ int64_t round8(int64_t v) { return (v + 7) & ~int64_t
 constexpr int kTileM[] = {256, 128, 64};
 constexpr int kTileN[] = {256, 128, 128};
 constexpr int kTileBytes = 128;  // a cut of k is a multiple of this many bytes of it (a k tile, or two)
-constexpr int kSkinnyRows = 16;
+constexpr int kSkinnyRows = 32, kSkinnyOddRows = 16;  // most rows of a pass over the weights, and where they stand off boundaries
+constexpr int kDzRows = 32;    // rows a work-group of k_dz takes at a time
 
 #if defined(__HIPCC__)
 
@@ -210,20 +216,24 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
     }
 }
 
-// ---- eight consecutive elements of a row ----
+// ---- eight consecutive elements of a row, from an element's boundary ----
+// (16 bytes an access wherever they stand: an access that is not on its own boundary costs a little more, element by element
+// it costs eight times as many)
 template <typename T>
-struct alignas(16) Vec16 { T v[16 / sizeof(T)]; };
+struct Vec8 {
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
 
-// reads elements [0, cnt) of p as fp32; vec: p is on a 16-byte boundary
+// reads elements [0, cnt) of p as fp32, 0 behind them
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int cnt, bool vec, float f[8]) {
-    if (vec && cnt >= 8) {
-        constexpr int V = 16 / sizeof(T);
+__device__ __forceinline__ void load8(const T* p, int cnt, float f[8]) {
+    constexpr int V = 16 / sizeof(T);
+    if (cnt >= 8) {
 #pragma unroll
         for (int i = 0; i < 8 / V; ++i) {
-            const Vec16<T> q = *reinterpret_cast<const Vec16<T>*>(p + i * V);
+            const typename Vec8<T>::type q = *reinterpret_cast<const typename Vec8<T>::type*>(p + i * V);
 #pragma unroll
-            for (int j = 0; j < V; ++j) f[i * V + j] = (float)q.v[j];
+            for (int j = 0; j < V; ++j) f[i * V + j] = (float)q[j];
         }
     } else {
 #pragma unroll
@@ -232,15 +242,15 @@ __device__ __forceinline__ void load8(const T* p, int cnt, bool vec, float f[8])
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T* p, int cnt, bool vec, const float f[8]) {
-    if (vec && cnt >= 8) {
-        constexpr int V = 16 / sizeof(T);
+__device__ __forceinline__ void store8(T* p, int cnt, const float f[8]) {
+    constexpr int V = 16 / sizeof(T);
+    if (cnt >= 8) {
 #pragma unroll
         for (int i = 0; i < 8 / V; ++i) {
-            Vec16<T> q;
+            typename Vec8<T>::type q;
 #pragma unroll
-            for (int j = 0; j < V; ++j) q.v[j] = (T)f[i * V + j];
-            *reinterpret_cast<Vec16<T>*>(p + i * V) = q;
+            for (int j = 0; j < V; ++j) q[j] = (T)f[i * V + j];
+            *reinterpret_cast<typename Vec8<T>::type*>(p + i * V) = q;
         }
     } else {
 #pragma unroll
@@ -262,19 +272,19 @@ __device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t
     if (e.bias) {
         const T* bias = static_cast<const T*>(e.bias);
         float b[8];
-        load8(bias + col, cnt, e.vec & VEC_BIAS, b);
+        load8(bias + col, cnt, b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += b[i];
         if constexpr (GATED) {
-            load8(bias + e.n + col, cnt, (e.vec & VEC_BIAS) && e.n % 8 == 0, b);
+            load8(bias + e.n + col, cnt, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] += b[i];
         }
     }
     if (e.pre) {
         T* p = static_cast<T*>(e.pre) + m * e.ld_pre;
-        store8(p + col, cnt, e.vec & VEC_PRE, s);
-        if constexpr (GATED) store8(p + e.n + col, cnt, (e.vec & VEC_PRE) && e.n % 8 == 0, u);
+        store8(p + col, cnt, s);
+        if constexpr (GATED) store8(p + e.n + col, cnt, u);
     }
     act_values(e.act, s);
     if constexpr (GATED) {
@@ -288,11 +298,11 @@ __device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t
     }
     if (e.res) {
         float r[8];
-        load8(static_cast<const T*>(e.res) + m * e.ld_res + col, cnt, e.vec & VEC_RES, r);
+        load8(static_cast<const T*>(e.res) + m * e.ld_res + col, cnt, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += r[i];
     }
-    store8(static_cast<T*>(e.y) + m * e.ld_y + col, cnt, e.vec & VEC_Y, s);
+    store8(static_cast<T*>(e.y) + m * e.ld_y + col, cnt, s);
 }
 
 #endif  // __HIPCC__

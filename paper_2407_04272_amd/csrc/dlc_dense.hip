@@ -8,7 +8,7 @@ namespace {
 struct Shape {
     int64_t M, K, N;  // gated: N columns of y, 2 N rows of w
     int64_t ldx, ldw, ldy, ldpre, ldres, lddy, lddx, lddw;
-    bool gated;
+    bool gated, off_boundary;
     int es;
     uint32_t thr;
     float scale;
@@ -40,6 +40,8 @@ bool make_shape(const dlc_dense_config* c, bool gated, Shape* s) {
     s->ldres = c->ld_res; s->lddy = c->ld_dy; s->lddx = c->ld_dx; s->lddw = c->ld_dw;
     if (!good_ld(s->ldx, s->K) || !good_ld(s->ldw, s->K) || !good_ld(s->lddx, s->K) || !good_ld(s->lddw, s->K)) return false;
     if (!good_ld(s->ldy, s->N) || !good_ld(s->ldpre, wide) || !good_ld(s->ldres, s->N) || !good_ld(s->lddy, s->N)) return false;
+    if (c->flags & ~(int32_t)DLC_DENSE_OFF_BOUNDARY || c->reserved != 0) return false;
+    s->off_boundary = (c->flags & DLC_DENSE_OFF_BOUNDARY) != 0;
     s->gated = gated;
     s->es = c->dtype == DLC_F32 ? 4 : 2;
     // a launch's work-groups are counted in 31 bits, 64 x 128 elements of the result each at least
@@ -69,18 +71,16 @@ struct Plan {
 // the longest start and end; in fp32 all three reach the matrix cores' rate and the small ones leave fewer units idle.
 struct TileCost { double tile[3], first, further; };
 constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0}, {{0.57, 0.88, 0}, 6.0, 3.0}, {{0.45, 0.64, 1.0}, 4.0, 3.0}};
-constexpr TileCost kHalfOdd[3] = {{{0, 0, 0}, 0, 0}, {{1.2, 1.27, 0}, 6.0, 3.0}, {{0.9, 1.0, 1.15}, 4.0, 3.0}};
 constexpr TileCost kF32Cost[3] = {{{7.6, 0, 0}, 14.0, 10.0}, {{2.2, 3.8, 0}, 8.0, 4.0}, {{1.3, 2.0, 2.9}, 5.0, 3.0}};
-constexpr TileCost kF32Odd[3] = {{{0, 0, 0}, 0, 0}, {{2.6, 4.4, 0}, 8.0, 4.0}, {{1.6, 2.5, 3.7}, 5.0, 3.0}};
 constexpr int kUnits = 256;  // compute units
 
 // M x N of the result (gated: N columns of y), K the sum's length: the tile and the cut of K with the smallest estimate
-Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es, bool aligned) {
+Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) {
     const int64_t bk = kTileBytes / es, wide = gated ? 2 * N : N;
-    const TileCost* const cost = es == 4 ? (aligned ? kF32Cost : kF32Odd) : (aligned ? kHalfCost : kHalfOdd);
+    const TileCost* const cost = es == 4 ? kF32Cost : kHalfCost;
     Plan best{};
     double best_t = 1e300;
-    for (int tile = aligned ? 0 : 1; tile < 3; ++tile) {
+    for (int tile = 0; tile < 3; ++tile) {
         const TileCost& c = cost[tile];
         const int64_t tm = div_up(M, kTileM[tile]), tn = div_up(wide, kTileN[tile]);
         const int64_t tiles = tm * tn, steps = div_up(K, bk);
@@ -110,20 +110,44 @@ Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es, 
     return best;
 }
 
-size_t plan_bytes(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) {
-    const size_t a = plan_gemm(M, N, K, gated, lay, es, true).bytes, b = plan_gemm(M, N, K, gated, lay, es, false).bytes;
-    return a > b ? a : b;
+// A matrix of the call that the products read where it stands, or packed (pack_rows)
+struct Source {
+    const void* p;
+    int64_t ld;
+};
+bool good_rows(int64_t ld, int64_t cols, int es) { return (ld * es) % 16 == 0 && (cols * es) % 16 == 0; }
+int64_t packed_ld(int64_t cols, int es) { return div_up(cols * es, 16) * 16 / es; }
+size_t packed_bytes(int64_t rows, int64_t cols, int es) { return a256((size_t)rows * (size_t)packed_ld(cols, es) * (size_t)es); }
+
+// Room for packed x and w: where their rows are off 16-byte boundaries, or their pointers may be (flags)
+size_t pack_room(const Shape& s) {
+    const int64_t wide = s.gated ? 2 * s.N : s.N;
+    return (s.off_boundary || !good_rows(s.ldx, s.K, s.es) ? packed_bytes(s.M, s.K, s.es) : 0) +
+           (s.off_boundary || !good_rows(s.ldw, s.K, s.es) ? packed_bytes(wide, s.K, s.es) : 0);
 }
 
-// few rows: the forward product is a pass over the weights
-bool few_rows(const Shape& s) { return s.M <= kSkinnyRows; }
+// Where x and w are read by the products, packing those that have to be into `room`; returns the bytes used
+size_t place_operands(const Shape& s, const void* x, const void* w, char* room, PackArgs* pk, Source* sx, Source* sw) {
+    size_t used = 0;
+    const int64_t wide = s.gated ? 2 * s.N : s.N;
+    const auto place = [&](int i, const void* p, int64_t ld, int64_t rows, Source* out) {
+        *out = Source{p, ld};
+        if (!p || (on(p, 16) && good_rows(ld, s.K, s.es))) return;
+        pk->src[i] = p; pk->dst[i] = room + used; pk->ld[i] = ld; pk->rows[i] = rows; pk->cols[i] = (int)s.K;
+        *out = Source{room + used, packed_ld(s.K, s.es)};
+        used += packed_bytes(rows, s.K, s.es);
+    };
+    place(0, x, s.ldx, s.M, sx);
+    place(1, w, s.ldw, wide, sw);
+    return used;
+}
 
-// workspace of a backward call: dz, the bias gradient's partial sums, one product's partial sums at a time
+// workspace of a backward call: dz, the bias gradient's partial sums, one product's partial sums at a time, packed operands
 struct BackPlan {
     int64_t ld_dz;
     int row_blocks, rows_per_block;
     int64_t sums_ld;
-    size_t off_sums, off_part, total;
+    size_t off_sums, off_part, off_pack, total;
 };
 
 BackPlan plan_back(const Shape& s) {
@@ -132,44 +156,49 @@ BackPlan plan_back(const Shape& s) {
     b.ld_dz = round8(wide);
     b.sums_ld = b.ld_dz;
     const int64_t cols = div_up(s.N, 256);
-    int64_t blocks = div_up(2048, cols);
-    if (blocks > div_up(s.M, 8)) blocks = div_up(s.M, 8);
-    if (blocks > 512) blocks = 512;
+    // about four work-groups a compute unit; few blocks of rows, since the last launch has their sums to add up
+    int64_t blocks = div_up(1024, cols);
+    if (blocks > 128) blocks = 128;
+    if (blocks > div_up(s.M, kDzRows)) blocks = div_up(s.M, kDzRows);
     if (blocks < 1) blocks = 1;
-    b.rows_per_block = (int)(div_up(div_up(s.M, blocks), 8) * 8);
+    b.rows_per_block = (int)(div_up(div_up(s.M, blocks), kDzRows) * kDzRows);
     b.row_blocks = b.rows_per_block ? (int)div_up(s.M, b.rows_per_block) : 0;
     b.off_sums = a256((size_t)s.M * (size_t)b.ld_dz * (size_t)s.es);
     b.off_part = b.off_sums + a256((size_t)b.row_blocks * (size_t)b.sums_ld * 4);
-    const size_t px = s.M ? plan_bytes(s.M, s.K, wide, false, L_KT, s.es) : 0;
-    const size_t pw = s.M ? plan_bytes(wide, s.K, s.M, false, L_TT, s.es) : 0;
-    b.total = b.off_part + a256(px > pw ? px : pw);
+    const size_t px = s.M ? plan_gemm(s.M, s.K, wide, false, L_KT, s.es).bytes : 0;
+    const size_t pw = s.M ? plan_gemm(wide, s.K, s.M, false, L_TT, s.es).bytes : 0;
+    b.off_pack = b.off_part + a256(px > pw ? px : pw);
+    b.total = b.off_pack + pack_room(s);
     return b;
 }
 
-size_t work_bytes_of(const dlc_dense_config* c, bool gated, bool backward) {
-    Shape s;
-    if (!make_shape(c, gated, &s) || s.M == 0) return 0;
+// a forward call's: the product's partial sums, packed operands (a pass over few rows takes them as they are)
+size_t forward_part(const Shape& s) { return a256(plan_gemm(s.M, s.N, s.K, s.gated, L_KK, s.es).bytes); }
+
+size_t work_bytes_of(const Shape& s, bool backward) {
+    if (s.M == 0) return 0;
     if (backward) return plan_back(s).total;
-    return few_rows(s) ? 0 : plan_bytes(s.M, s.N, s.K, gated, L_KK, s.es);
+    return s.M <= kSkinnyOddRows ? 0 : forward_part(s) + pack_room(s);
 }
 
+// The product; sums: what the last launch adds up besides (n = 0: nothing)
 template <typename T>
-int run_gemm(GemmArgs g, Layout lay, bool gated, bool aligned, int es, void* work, hipStream_t st) {
-    const Plan p = plan_gemm(g.M, g.N, g.K, gated, lay, es, aligned);
+int run_gemm(GemmArgs g, Layout lay, bool gated, int es, void* work, const SumArgs& sums, hipStream_t st) {
+    const Plan p = plan_gemm(g.M, g.N, g.K, gated, lay, es);
     g.kper = p.kper; g.split = p.split; g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_n;
     g.part = static_cast<float*>(work);
     g.part_ld = p.part_ld;
-    if (DenseOps<T>::gemm(g, lay, gated, p.tile, aligned, st) != hipSuccess) return DLC_EHIP;
-    if (p.split > 1) {
-        const JoinArgs j{g.part, g.part_ld, g.M, p.split, gated ? 1 : 0, g.e};
-        if (DenseOps<T>::join(j, st) != hipSuccess) return DLC_EHIP;
+    if (DenseOps<T>::gemm(g, lay, gated, p.tile, st) != hipSuccess) return DLC_EHIP;
+    if (p.split > 1 || sums.n > 0) {
+        const JoinArgs j{g.part, g.part_ld, p.split > 1 ? g.M : 0, p.split, gated ? 1 : 0, g.e};
+        if (DenseOps<T>::join(j, sums, st) != hipSuccess) return DLC_EHIP;
     }
     return DLC_OK;
 }
 
 template <typename T>
 int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* bias, const void* res, void* y,
-            void* pre, void* work, hipStream_t st) {
+            void* pre, void* work, size_t work_bytes, hipStream_t st) {
     GemmArgs g{};
     g.a = x; g.b = w; g.lda = s.ldx; g.ldb = s.ldw;
     g.M = (int)s.M; g.N = (int)s.N; g.K = (int)s.K;
@@ -179,16 +208,24 @@ int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void
     e.ld_y = s.ldy; e.ld_pre = s.ldpre; e.ld_res = s.ldres;
     e.seed = c->seed; e.offset = c->offset; e.d_offset = c->d_offset;
     e.thr = s.thr; e.scale = s.scale; e.act = c->act; e.n = (int)s.N;
-    e.vec = (rows16(y, s.ldy, s.es) ? VEC_Y : 0) | (rows16(pre, s.ldpre, s.es) ? VEC_PRE : 0) |
-            (rows16(res, s.ldres, s.es) ? VEC_RES : 0) | (on(bias, 16) ? VEC_BIAS : 0);
-    const bool aligned = rows16(x, s.ldx, s.es) && rows16(w, s.ldw, s.es) && (s.K * s.es) % 16 == 0;
-    if (few_rows(s)) return DenseOps<T>::skinny(g, s.gated, aligned, st) == hipSuccess ? DLC_OK : DLC_EHIP;
-    return run_gemm<T>(g, L_KK, s.gated, aligned, s.es, work, st);
+    // few rows: a pass over the weights (32 rows of 2048 -> 4096 bf16: 10.3 us in tiles)
+    if (s.M <= kSkinnyRows) {
+        const bool aligned = on(x, 16) && on(w, 16) && good_rows(s.ldx, s.K, s.es) && good_rows(s.ldw, s.K, s.es);
+        if (aligned || s.M <= kSkinnyOddRows) return DenseOps<T>::skinny(g, s.gated, aligned, st) == hipSuccess ? DLC_OK : DLC_EHIP;
+    }
+    const size_t part = forward_part(s);
+    PackArgs pk{};
+    Source sx, sw;
+    const size_t used = place_operands(s, x, w, static_cast<char*>(work) + part, &pk, &sx, &sw);
+    if (part + used > work_bytes) return DLC_ECAPACITY;
+    if (used && DenseOps<T>::pack(pk, st) != hipSuccess) return DLC_EHIP;
+    g.a = sx.p; g.lda = sx.ld; g.b = sw.p; g.ldb = sw.ld;
+    return run_gemm<T>(g, L_KK, s.gated, s.es, work, SumArgs{}, st);
 }
 
 template <typename T>
 int backward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* pre, const void* dy, void* dx,
-             void* dw, void* dbias, void* work, hipStream_t st) {
+             void* dw, void* dbias, void* work, size_t work_bytes, hipStream_t st) {
     const BackPlan b = plan_back(s);
     char* const wk = static_cast<char*>(work);
     const int64_t wide = s.gated ? 2 * s.N : s.N;
@@ -196,7 +233,16 @@ int backward(const dlc_dense_config* c, const Shape& s, const void* x, const voi
     const bool direct = same && rows16(dy, s.lddy, s.es) && (s.N * s.es) % 16 == 0;
     const bool products = (dx || dw) && s.M > 0;
     float* const sums = reinterpret_cast<float*>(wk + b.off_sums);
-    if (s.M > 0 && (dbias || (products && !direct))) {
+    PackArgs pk{};
+    Source sx{}, sw{};
+    size_t used = 0;
+    if (products) {
+        used = place_operands(s, dw ? x : nullptr, dx ? w : nullptr, wk + b.off_pack, &pk, &sx, &sw);
+        if (b.off_pack + used > work_bytes) return DLC_ECAPACITY;
+    }
+    const bool elementwise = s.M > 0 && (dbias || (products && !direct));
+    if (used && !elementwise && DenseOps<T>::pack(pk, st) != hipSuccess) return DLC_EHIP;
+    if (elementwise) {
         DzArgs d{};
         d.dy = dy; d.pre = same ? nullptr : pre;
         if (!s.gated && c->act == DLC_ACT_NONE) d.pre = nullptr;
@@ -206,47 +252,42 @@ int backward(const dlc_dense_config* c, const Shape& s, const void* x, const voi
         d.M = s.M; d.n = (int)s.N; d.gated = s.gated; d.act = c->act;
         d.row_blocks = b.row_blocks; d.rows_per_block = b.rows_per_block;
         d.thr = s.thr; d.scale = s.scale; d.seed = c->seed; d.offset = c->offset; d.d_offset = c->d_offset;
-        d.vec = (rows16(dy, s.lddy, s.es) ? 1u : 0u) | (rows16(pre, s.ldpre, s.es) ? 2u : 0u);
-        if (DenseOps<T>::dz(d, st) != hipSuccess) return DLC_EHIP;
+        if (DenseOps<T>::dz(d, pk, st) != hipSuccess) return DLC_EHIP;
     }
-    if (dbias) {
-        const SumArgs a{sums, b.sums_ld, s.M > 0 ? b.row_blocks : 0, (int)wide, dbias};
-        if (DenseOps<T>::sum(a, st) != hipSuccess) return DLC_EHIP;
-    }
+    // the bias gradient's sums are put together by the call's last launch, whichever it is
+    const SumArgs sum = dbias ? SumArgs{sums, b.sums_ld, s.M > 0 ? b.row_blocks : 0, (int)wide, dbias} : SumArgs{};
     const void* const dz = direct ? dy : work;
     const int64_t lddz = direct ? s.lddy : b.ld_dz;
-    const bool w16 = rows16(w, s.ldw, s.es) && (s.K * s.es) % 16 == 0;
-    const bool x16 = rows16(x, s.ldx, s.es) && (s.K * s.es) % 16 == 0;
     if (dx && s.M > 0) {
         GemmArgs g{};
-        g.a = dz; g.b = w; g.lda = lddz; g.ldb = s.ldw;
+        g.a = dz; g.b = sw.p; g.lda = lddz; g.ldb = sw.ld;
         g.M = (int)s.M; g.N = (int)s.K; g.K = (int)wide;
-        g.e.y = dx; g.e.ld_y = s.lddx; g.e.n = (int)s.K; g.e.vec = rows16(dx, s.lddx, s.es) ? VEC_Y : 0;
-        if (const int rc = run_gemm<T>(g, L_KT, false, w16, s.es, wk + b.off_part, st); rc != DLC_OK) return rc;
+        g.e.y = dx; g.e.ld_y = s.lddx; g.e.n = (int)s.K;
+        if (const int rc = run_gemm<T>(g, L_KT, false, s.es, wk + b.off_part, dw ? SumArgs{} : sum, st); rc != DLC_OK) return rc;
     }
     if (dw) {
         GemmArgs g{};
-        g.a = dz; g.b = x; g.lda = lddz; g.ldb = s.ldx;
+        g.a = dz; g.b = sx.p; g.lda = lddz; g.ldb = sx.ld;
         g.M = (int)wide; g.N = (int)s.K; g.K = (int)s.M;
-        g.e.y = dw; g.e.ld_y = s.lddw; g.e.n = (int)s.K; g.e.vec = rows16(dw, s.lddw, s.es) ? VEC_Y : 0;
+        g.e.y = dw; g.e.ld_y = s.lddw; g.e.n = (int)s.K;
         if (s.M == 0) {  // the empty sum
             const JoinArgs j{nullptr, 0, g.M, 0, 0, g.e};
-            if (DenseOps<T>::join(j, st) != hipSuccess) return DLC_EHIP;
-        } else if (const int rc = run_gemm<T>(g, L_TT, false, x16, s.es, wk + b.off_part, st); rc != DLC_OK) {
-            return rc;
+            return DenseOps<T>::join(j, sum, st) == hipSuccess ? DLC_OK : DLC_EHIP;
         }
+        return run_gemm<T>(g, L_TT, false, s.es, wk + b.off_part, sum, st);
     }
+    if (dbias && !(dx && s.M > 0)) return DenseOps<T>::join(JoinArgs{}, sum, st) == hipSuccess ? DLC_OK : DLC_EHIP;
     return DLC_OK;
 }
 
 // d is there if `need`, and lies on an element's boundary
 bool good_ptr(const void* d, int es, bool need) { return d ? on(d, es) : !need; }
 
-int check_work(const dlc_dense_config* c, bool gated, bool backward, const void* work, size_t bytes) {
-    const size_t need = work_bytes_of(c, gated, backward);
-    if (need == 0) return DLC_OK;
-    if (!work || !on(work, 16)) return DLC_EINVAL;
-    return bytes >= need ? DLC_OK : DLC_ECAPACITY;
+int check_work(const Shape& s, bool backward, const void* work, size_t* bytes) {
+    if (!on(work, 16)) return DLC_EINVAL;
+    const size_t need = work_bytes_of(s, backward);
+    if (!work) *bytes = 0;
+    return *bytes >= need ? DLC_OK : work ? DLC_ECAPACITY : DLC_EINVAL;
 }
 
 int forward_any(const dlc_dense_config* c, bool gated, const void* x, const void* w, const void* bias, const void* res, void* y,
@@ -257,12 +298,12 @@ int forward_any(const dlc_dense_config* c, bool gated, const void* x, const void
     if (!good_ptr(x, s.es, need) || !good_ptr(w, s.es, need) || !good_ptr(bias, s.es, false) || !good_ptr(res, s.es, false) ||
         !good_ptr(y, s.es, need) || !good_ptr(pre, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
     if (!need) return DLC_OK;
-    if (const int rc = check_work(c, gated, false, work, bytes); rc != DLC_OK) return rc;
+    if (const int rc = check_work(s, false, work, &bytes); rc != DLC_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
     switch (c->dtype) {
-        case DLC_F32: return forward<float>(c, s, x, w, bias, res, y, pre, work, st);
-        case DLC_F16: return forward<f16_t>(c, s, x, w, bias, res, y, pre, work, st);
-        default: return forward<bf16_t>(c, s, x, w, bias, res, y, pre, work, st);
+        case DLC_F32: return forward<float>(c, s, x, w, bias, res, y, pre, work, bytes, st);
+        case DLC_F16: return forward<f16_t>(c, s, x, w, bias, res, y, pre, work, bytes, st);
+        default: return forward<bf16_t>(c, s, x, w, bias, res, y, pre, work, bytes, st);
     }
 }
 
@@ -274,19 +315,23 @@ int backward_any(const dlc_dense_config* c, bool gated, const void* x, const voi
     if (!good_ptr(x, s.es, some && dw) || !good_ptr(w, s.es, some && dx) || !good_ptr(dy, s.es, some) ||
         !good_ptr(pre, s.es, some && (gated || c->act != DLC_ACT_NONE)) || !good_ptr(dx, s.es, false) || !good_ptr(dw, s.es, false) ||
         !good_ptr(dbias, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
-    if (const int rc = check_work(c, gated, true, work, bytes); rc != DLC_OK) return rc;
+    if (const int rc = check_work(s, true, work, &bytes); rc != DLC_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
     switch (c->dtype) {
-        case DLC_F32: return backward<float>(c, s, x, w, pre, dy, dx, dw, dbias, work, st);
-        case DLC_F16: return backward<f16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, st);
-        default: return backward<bf16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, st);
+        case DLC_F32: return backward<float>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, st);
+        case DLC_F16: return backward<f16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, st);
+        default: return backward<bf16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, st);
     }
 }
 
 }  // namespace
 
-extern "C" size_t dlc_linear_workspace_bytes(const dlc_dense_config* cfg, int backward) { return work_bytes_of(cfg, false, backward != 0); }
-extern "C" size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg, int backward) { return work_bytes_of(cfg, true, backward != 0); }
+static size_t workspace(const dlc_dense_config* cfg, bool gated, int backward) {
+    Shape s;
+    return make_shape(cfg, gated, &s) ? work_bytes_of(s, backward != 0) : 0;
+}
+extern "C" size_t dlc_linear_workspace_bytes(const dlc_dense_config* cfg, int backward) { return workspace(cfg, false, backward); }
+extern "C" size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg, int backward) { return workspace(cfg, true, backward); }
 
 extern "C" int dlc_linear_forward(const dlc_dense_config* cfg, const void* x, const void* w, const void* bias, const void* res, void* y,
                                   void* pre, void* work, size_t bytes, void* stream) {
@@ -327,7 +372,6 @@ extern "C" int dlc_dropout(const dlc_dropout_config* c, const void* x, const voi
     if (!need) return DLC_OK;
     d.x = x; d.res = res; d.y = y;
     d.seed = c->seed; d.offset = c->offset; d.d_offset = c->d_offset;
-    d.vec = (rows16(x, d.ld_x, es) ? 1u : 0u) | (rows16(y, d.ld_y, es) ? 2u : 0u) | (rows16(res, d.ld_res, es) ? 4u : 0u);
     hipStream_t st = (hipStream_t)stream;
     hipError_t rc;
     switch (c->dtype) {

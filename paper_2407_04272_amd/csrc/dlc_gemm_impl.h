@@ -154,6 +154,36 @@ __device__ __forceinline__ void read_rows2(u32x4_t* x, uint32_t a, u32x4_t* y, u
     }
 }
 
+// ... both halves of N slots' rows, PITCH bytes apart (at a and b)
+template <int N, int PITCH>
+__device__ __forceinline__ void read_halves(u32x4_t* o, uint32_t a, uint32_t b) {
+    if constexpr (N == 2) {
+        asm volatile(
+            "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\t"
+            "ds_read_b128 %2, %4 offset:%6\n\tds_read_b128 %3, %5 offset:%6\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]) : "v"(a), "v"(b), "i"(PITCH) : "memory");
+    } else if constexpr (N == 4) {
+        asm volatile(
+            "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\t"
+            "ds_read_b128 %2, %8 offset:%10\n\tds_read_b128 %3, %9 offset:%10\n\t"
+            "ds_read_b128 %4, %8 offset:%11\n\tds_read_b128 %5, %9 offset:%11\n\t"
+            "ds_read_b128 %6, %8 offset:%12\n\tds_read_b128 %7, %9 offset:%12\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5]), "=&v"(o[6]), "=&v"(o[7])
+            : "v"(a), "v"(b), "i"(PITCH), "i"(2 * PITCH), "i"(3 * PITCH) : "memory");
+    } else {
+        static_assert(N == 3, "");
+        asm volatile(
+            "ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\t"
+            "ds_read_b128 %2, %6 offset:%8\n\tds_read_b128 %3, %7 offset:%8\n\t"
+            "ds_read_b128 %4, %6 offset:%9\n\tds_read_b128 %5, %7 offset:%9\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(o[0]), "=&v"(o[1]), "=&v"(o[2]), "=&v"(o[3]), "=&v"(o[4]), "=&v"(o[5])
+            : "v"(a), "v"(b), "i"(PITCH), "i"(2 * PITCH) : "memory");
+    }
+}
+
 __device__ __forceinline__ u32x4_t join_halves(s16x4 lo, s16x4 hi) {
     return __builtin_bit_cast(u32x4_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
@@ -233,7 +263,8 @@ __device__ __forceinline__ int unit_swizzle(int krow) {
 
 // One operand's path into LDS.  KT: k runs down a column.  R: rows (columns of C) of the tile.  TB: bytes of k of a tile.
 // DUAL: the tile's rows are those of two matrices one behind the other, 32 of the first and 32 of the second in turn.
-template <typename T, bool KT, int R, int TB, int THREADS, bool ALIGNED, bool DUAL>
+// Rows start on 16-byte boundaries, and what stands between a row's end and the next boundary is zeros or outside the sum.
+template <typename T, bool KT, int R, int TB, int THREADS, bool DUAL>
 struct Operand {
     static constexpr int EPC = 16 / sizeof(T);           // elements of a chunk
     static constexpr int BK = TB / sizeof(T);            // k values of a tile
@@ -256,9 +287,7 @@ struct Operand {
     int k_left;             // k values from the current tile on
     int key;                // the k value in a tile of a thread's first chunk (k along a row: of the chunk's first element)
     int row0, slot;         // the thread's first row and its place in it
-    int rows_left;          // rows (columns) of the matrix from the tile's first on
-    uint32_t voff[PASSES];  // ALIGNED: offsets of the thread's chunks from base, kOut outside the matrix
-    u32x4_t reg[ALIGNED ? 1 : PASSES];
+    uint32_t voff[PASSES];  // offsets of the thread's chunks from base, kOut outside the matrix
 
     // the chunk that stands at place `s` of row r
     __device__ __forceinline__ static int chunk_at(int r, int s) {
@@ -272,65 +301,45 @@ struct Operand {
     __device__ __forceinline__ int chunk_of(int i) const { return chunk_at(row0 + i * RSTEP, slot); }
     // DUAL: row r of the tile is row f of its matrix
     __device__ __forceinline__ static int source_row(int r) { return DUAL ? ((r >> 6) << 5) | (r & 31) : r; }
-    __device__ __forceinline__ static bool second(int r) { return DUAL && ((r >> 5) & 1); }
 
     // row: first row (column) of the tile; rows: of the matrix (DUAL: of one of the two)
     __device__ __forceinline__ void init(const void* p, int64_t ld_elems, int row, int rows, int k0, int k1, int tid) {
         ld = ld_elems * (int64_t)sizeof(T);
         row0 = tid / CPR;
         slot = tid % CPR;
-        rows_left = rows - row;
+        const int rows_left = rows - row;
         k_left = k1 - k0;
         const int64_t down = KT ? k0 : row, along = KT ? row : k0;
         base = static_cast<const char*>(p) + down * ld + along * (int64_t)sizeof(T);
         step = KT ? (int64_t)BK * ld : (int64_t)TB;
         half_off = (int64_t)rows * ld;
         key = KT ? row0 : chunk_of(0) * EPC;
-        if constexpr (ALIGNED) {
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int r = row0 + i * RSTEP, c = chunk_of(i), f = source_row(r);
-                const bool in = KT ? c * EPC < rows_left : f < rows_left;
-                voff[i] = in ? (uint32_t)f * (uint32_t)ld + (uint32_t)c * 16u : kOut;
-            }
+        for (int i = 0; i < PASSES; ++i) {
+            const int r = row0 + i * RSTEP, c = chunk_of(i), f = source_row(r);
+            const bool in = KT ? c * EPC < rows_left : f < rows_left;
+            voff[i] = in ? (uint32_t)f * (uint32_t)ld + (uint32_t)c * 16u : kOut;
         }
     }
 
-    // Starts the current k tile's loads to `lds` (ALIGNED), or into registers; then steps to the next.  What lies outside
-    // the matrix becomes 0, and so do tiles past the last.
+    // Starts the current k tile's loads to `lds`; then steps to the next.  What lies outside the matrix becomes 0, and so do
+    // tiles past the last.
     __device__ __forceinline__ void fetch(char* lds, int tid) {
-        if constexpr (ALIGNED) {
-            if (k_left < BK) {  // (the last tile; those behind it stay empty)
+        if (k_left < BK) {  // (the last tile; those behind it stay empty)
 #pragma unroll
-                for (int i = 0; i < PASSES; ++i) voff[i] = key + (KT ? i * RSTEP : 0) < k_left ? voff[i] : kOut;
-            }
-            const int wave_lds = (tid & ~63) * 16;
+            for (int i = 0; i < PASSES; ++i) voff[i] = key + (KT ? i * RSTEP : 0) < k_left ? voff[i] : kOut;
+        }
+        const int wave_lds = (tid & ~63) * 16;
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                char* const dst = lds + wave_lds + i * THREADS * 16;
-                // (a wavefront's rows are all of one matrix)
-                const char* const src = base + (DUAL && (__builtin_amdgcn_readfirstlane(row0 + i * RSTEP) >> 5) & 1 ? half_off : 0);
-                const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, 0, kOut, 0x00020000);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, voff[i], 0, 0, 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int r = row0 + i * RSTEP, c = chunk_of(i), f = source_row(r);
-                const char* const p = base + (second(r) ? half_off : 0) + (int64_t)f * ld + c * 16;
-                const int cnt = KT ? (r < k_left ? rows_left - c * EPC : 0) : (f < rows_left ? k_left - c * EPC : 0);
-                reg[i] = load_chunk<T>(p, cnt);
-            }
+        for (int i = 0; i < PASSES; ++i) {
+            char* const dst = lds + wave_lds + i * THREADS * 16;
+            // (a wavefront's rows are all of one matrix)
+            const char* const src = base + (DUAL && (__builtin_amdgcn_readfirstlane(row0 + i * RSTEP) >> 5) & 1 ? half_off : 0);
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, 0, kOut, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, voff[i], 0, 0, 0);
         }
         k_left -= BK;
         base += step;
-    }
-
-    __device__ __forceinline__ void put(char* lds, int tid) const {
-        if constexpr (!ALIGNED) {
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) *reinterpret_cast<u32x4_t*>(lds + (tid + i * THREADS) * 16) = reg[i];
-        }
     }
 
     // Where a lane reads in a tile: row (column) `row` + l % 16 of N blocks of 16, its k values (l / 16) * 16 bytes on in
@@ -412,7 +421,7 @@ __device__ __forceinline__ void tile_of(int wg, int total, int tiles_m, int tile
     tn = t / h;
 }
 
-template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED, bool GATED>
+template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool GATED>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmArgs ga) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass has no use for the body, and does not know its assembly)
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
@@ -423,8 +432,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
     // 10 % faster: the loads are spread over all phases.
     constexpr int TB = LAY == L_KK ? 128 : 64;
     constexpr int BK = TB / sizeof(T);
-    using OpA = Operand<T, LAY == L_TT, BM, TB, THREADS, ALIGNED, false>;
-    using OpB = Operand<T, LAY != L_KK, BN, TB, THREADS, ALIGNED, GATED>;
+    using OpA = Operand<T, LAY == L_TT, BM, TB, THREADS, false>;
+    using OpB = Operand<T, LAY != L_KK, BN, TB, THREADS, GATED>;
     static_assert(WN == 64, "a wavefront's columns (gated: 32 of the gate and 32 of the other)");
     constexpr int STAGE = OpA::BYTES + OpB::BYTES;
     constexpr int A3 = 3 * OpA::BYTES;  // k along the rows: three slots for A, then two for B
@@ -479,57 +488,42 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
             sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
             sb = OpB::BYTES - sb;
         };
-        if constexpr (ALIGNED) {
-            // A tile of B is started when all have read the one before the last, two of A are on their way
-            auto load_b = [&] { ob.fetch(lds + A3 + (OpB::BYTES - sb), tid); };
-            auto load_a = [&] { oa.fetch(lds + (sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES), tid); };
-            oa.fetch(lds, tid);
-            ob.fetch(lds + A3, tid);
-            oa.fetch(lds + OpA::BYTES, tid);
-            if constexpr (PAIRED) {
-                // The wait for the next tiles stands before the barrier behind which the first group reads them
+        // A tile of B is started when all have read the one before the last, two of A are on their way
+        auto load_b = [&] { ob.fetch(lds + A3 + (OpB::BYTES - sb), tid); };
+        auto load_a = [&] { oa.fetch(lds + (sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES), tid); };
+        oa.fetch(lds, tid);
+        ob.fetch(lds + A3, tid);
+        oa.fetch(lds + OpA::BYTES, tid);
+        if constexpr (PAIRED) {
+            // The wait for the next tiles stands before the barrier behind which the first group reads them
+            wait_loads<OpA::PASSES>();
+            bare_barrier();
+            if (late) bare_barrier();
+            for (int s = 0; s < steps; ++s) {
+                read(i0);
+                load_b();
+                bare_barrier();
+                multiply();
+                bare_barrier();
+                read(i1);
+                load_a();
+                if (late) wait_loads<OpA::PASSES>();
+                bare_barrier();
+                multiply();
+                if (!late) wait_loads<OpA::PASSES>();
+                bare_barrier();
+                next();
+            }
+            if (!late) bare_barrier();
+        } else {
+            for (int s = 0; s < steps; ++s) {
                 wait_loads<OpA::PASSES>();
                 bare_barrier();
-                if (late) bare_barrier();
-                for (int s = 0; s < steps; ++s) {
-                    read(i0);
-                    load_b();
-                    bare_barrier();
-                    multiply();
-                    bare_barrier();
-                    read(i1);
-                    load_a();
-                    if (late) wait_loads<OpA::PASSES>();
-                    bare_barrier();
-                    multiply();
-                    if (!late) wait_loads<OpA::PASSES>();
-                    bare_barrier();
-                    next();
-                }
-                if (!late) bare_barrier();
-            } else {
-                for (int s = 0; s < steps; ++s) {
-                    wait_loads<OpA::PASSES>();
-                    bare_barrier();
-                    read(i0);
-                    load_b();
-                    multiply();
-                    read(i1);
-                    load_a();
-                    multiply();
-                    next();
-                }
-            }
-        } else {
-            if (steps > 0) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
-            for (int s = 0; s < steps; ++s) {
-                oa.put(lds + sa, tid);
-                ob.put(lds + A3 + sb, tid);
-                __syncthreads();
-                if (s + 1 < steps) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
                 read(i0);
+                load_b();
                 multiply();
                 read(i1);
+                load_a();
                 multiply();
                 next();
             }
@@ -553,61 +547,44 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
             OpA::template frags<MI, OFF>(f.a, pa[H]);
             __builtin_amdgcn_sched_barrier(0);
         };
-        if constexpr (ALIGNED) {
-            constexpr int LOADS = OpA::PASSES + OpB::PASSES;
-            auto load = [&](int slot) {
-                oa.fetch(lds + slot * STAGE, tid);
-                ob.fetch(lds + slot * STAGE + OpA::BYTES, tid);
-            };
-            load(0);
-            load(1);
-            load(2);
-            auto step = [&](auto slot) {
-                constexpr int S = decltype(slot)::value;
-                if constexpr (PAIRED) {
-                    read(slot);
-                    load((S + 3) % 4);
-                    wait_loads<2 * LOADS>();
-                    bare_barrier();
-                    multiply();
-                    bare_barrier();
-                } else {
-                    wait_loads<2 * LOADS>();
-                    bare_barrier();
-                    read(slot);
-                    load((S + 3) % 4);
-                    multiply();
-                }
-            };
+        constexpr int LOADS = OpA::PASSES + OpB::PASSES;
+        auto load = [&](int slot) {
+            oa.fetch(lds + slot * STAGE, tid);
+            ob.fetch(lds + slot * STAGE + OpA::BYTES, tid);
+        };
+        load(0);
+        load(1);
+        load(2);
+        auto step = [&](auto slot) {
+            constexpr int S = decltype(slot)::value;
             if constexpr (PAIRED) {
+                read(slot);
+                load((S + 3) % 4);
                 wait_loads<2 * LOADS>();
                 bare_barrier();
-                if (late) bare_barrier();
-            }
-            for (int s = 0; s < steps; s += 4) {  // (tiles past the last are zeros)
-                step(i0);
-                step(i1);
-                step(i2);
-                step(i3);
-            }
-            if constexpr (PAIRED) {
-                if (!late) bare_barrier();
-            }
-        } else {
-            auto step = [&](auto slot, bool more) {
-                constexpr int S = decltype(slot)::value;
-                oa.put(lds + S * STAGE, tid);
-                ob.put(lds + S * STAGE + OpA::BYTES, tid);
-                __syncthreads();
-                if (more) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
-                read(slot);
                 multiply();
-            };
-            if (steps > 0) { oa.fetch(nullptr, tid); ob.fetch(nullptr, tid); }
-            for (int s = 0; s < steps; s += 2) {
-                step(i0, s + 1 < steps);
-                if (s + 1 < steps) step(i1, s + 2 < steps);
+                bare_barrier();
+            } else {
+                wait_loads<2 * LOADS>();
+                bare_barrier();
+                read(slot);
+                load((S + 3) % 4);
+                multiply();
             }
+        };
+        if constexpr (PAIRED) {
+            wait_loads<2 * LOADS>();
+            bare_barrier();
+            if (late) bare_barrier();
+        }
+        for (int s = 0; s < steps; s += 4) {  // (tiles past the last are zeros)
+            step(i0);
+            step(i1);
+            step(i2);
+            step(i3);
+        }
+        if constexpr (PAIRED) {
+            if (!late) bare_barrier();
         }
     }
     wait_loads<0>();  // (tiles past the last may still be on their way)
@@ -663,13 +640,127 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
 #endif
 }
 
-// Few rows (at most 16): the product is a pass over B.  A work-group takes 16 columns of C (gated: and the 16 of the other
-// half), its wavefronts take stretches of k in turn straight from memory, and their sums meet in LDS.
+// The wavefronts' sums of 16 x 16 elements (gated: of both halves) added up in order, and the epilogue
 constexpr int kSkinnyWaves = 8;
 
-template <typename T, bool ALIGNED, bool GATED>
+template <typename T, bool GATED>
+__device__ __forceinline__ void skinny_end(const GemmArgs& ga, int m0, int n0, const float (*sums)[GATED ? 2 : 1][16][20], int tid) {
+    const int row = tid >> 1, ch = tid & 1;
+    if (tid >= 32 || m0 + row >= ga.M) return;
+    float s[8], u[8];
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+        s[v] = 0.f;
+        u[v] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kSkinnyWaves; ++w) {
+            s[v] += sums[w][0][row][ch * 8 + v];
+            if constexpr (GATED) u[v] += sums[w][1][row][ch * 8 + v];
+        }
+    }
+    epilogue8<T, GATED>(ga.e, full_offset(ga.e.offset, ga.e.d_offset), m0 + row, n0 + ch * 8, s, u);
+}
+
+// Few rows (at most 32): the product is a pass over B.  A work-group takes 16 columns of C (gated: and the 16 of the other
+// half); its wavefronts take 128 bytes of k in turn, each on its own, and their sums meet in LDS.
+//
+// A wavefront loads 8 rows of 128 bytes at a time, whole cache lines from neighbouring lanes, to its two slots in LDS and
+// reads its fragments from there; with two slots two work-groups share a compute unit (more slots were slower).  Fragments
+// loaded straight from memory take 16 bytes of 16 rows from neighbouring lanes: 16 rows of 8192 -> 1024 bf16 16.7 us that
+// way, 7.7 us (2.2 TB/s) this way; 2048 -> 8192 12.4 and 10.4 us (3.2 TB/s), gated 2048 -> 4096 13.0 and 11.0 us.
+
+// One operand of a wavefront: 16 rows, 128 bytes of k of each in a slot, chunk c of row r at place c ^ (r >> 1)
+template <typename T>
+struct SkinnyRows {
+    static constexpr int EPC = 16 / sizeof(T), BK = 128 / sizeof(T);
+    static constexpr uint32_t kOut = 0x7FFFFFF0u;
+    static constexpr int BYTES = 2048, LOADS = 2;
+    const char* base;  // of the first row and the wavefront's next 128 bytes
+    uint32_t voff[2];
+    int k[2];          // first k value of the lane's chunks
+    __device__ __forceinline__ void init(const void* p, int64_t ld, int row, int rows, int k0, int lane) {
+        base = static_cast<const char*>(p) + ((int64_t)row * ld + k0) * (int64_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = (lane >> 3) + 8 * i, c = (lane & 7) ^ ((r >> 1) & 7);
+            voff[i] = row + r < rows ? (uint32_t)r * (uint32_t)(ld * (int64_t)sizeof(T)) + (uint32_t)c * 16u : kOut;
+            k[i] = c * EPC;
+        }
+    }
+    __device__ __forceinline__ void fetch(char* lds, int k_left, int step) {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, kOut, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + i * 1024), 16, k[i] < k_left ? voff[i] : kOut, 0, 0, 0);
+        base += step;
+    }
+};
+
+// MT: blocks of 16 rows of A
+template <typename T, bool GATED, int MT>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(const GemmArgs ga) {
-    constexpr int EPC = 16 / sizeof(T), KS = 64 / sizeof(T), UN = 4;
+#if defined(__HIP_DEVICE_COMPILE__)
+    using Rows = SkinnyRows<T>;
+    constexpr int OB = GATED ? 2 : 1, OPS = OB + MT, SLOT = OPS * Rows::BYTES, SLOTS = 2, LOADS = OPS * Rows::LOADS;
+    constexpr int BK = Rows::BK;
+    __shared__ __attribute__((aligned(16))) char lds[kSkinnyWaves * SLOTS * SLOT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, j = lane & 15;
+    const int n0 = blockIdx.x * 16, k0 = wave * BK;
+    char* const mine = lds + wave * (SLOTS * SLOT);
+    Rows op[OPS];  // B (gated: both halves), then A's blocks
+#pragma unroll
+    for (int i = 0; i < OPS; ++i) {
+        if (i < OB) op[i].init(static_cast<const T*>(ga.b) + (int64_t)i * ga.N * ga.ldb, ga.ldb, n0, ga.N, k0, lane);
+        else op[i].init(ga.a, ga.lda, (i - OB) * 16, ga.M, k0, lane);
+    }
+    f32x4 acc[OB][MT];
+#pragma unroll
+    for (int i = 0; i < OB; ++i)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[i][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int ahead = ga.K - k0;  // k values from the next tile to fetch on
+    auto fetch = [&](char* slot) {
+#pragma unroll
+        for (int i = 0; i < OPS; ++i) op[i].fetch(slot + i * Rows::BYTES, ahead, kSkinnyWaves * 128);
+        ahead -= kSkinnyWaves * BK;
+    };
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) fetch(mine + i * SLOT);
+    const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)mine + (uint32_t)(j * 128);
+    const uint32_t c0 = (uint32_t)((g ^ ((j >> 1) & 7)) << 4), c1 = c0 ^ 64u;  // the lane's chunk in each half
+    int slot = 0;
+    for (int k = k0; k < ga.K; k += kSkinnyWaves * BK) {
+        wait_loads<(SLOTS - 1) * LOADS>();
+        u32x4_t f[2 * OPS];
+        const uint32_t s = at + (uint32_t)(slot * SLOT);
+        read_halves<OPS, Rows::BYTES>(f, s + c0, s + c1);
+        fetch(mine + slot * SLOT);
+        slot ^= 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < OB; ++i)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[i][m] = mma<T>(f[2 * i + h], f[2 * (OB + m) + h], acc[i][m]);
+    }
+    wait_loads<0>();
+    __syncthreads();
+    typedef float Sums[OB][16][20];
+    Sums* const sums = reinterpret_cast<Sums*>(lds);  // [MT][wavefronts]
+    static_assert(sizeof(Sums) * MT * kSkinnyWaves <= sizeof(lds), "room for the sums");
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < OB; ++i) *reinterpret_cast<f32x4*>(&sums[m * kSkinnyWaves + wave][i][j][g * 4]) = acc[i][m];
+    __syncthreads();
+    if (wave < MT) skinny_end<T, GATED>(ga, wave * 16, n0, sums + wave * kSkinnyWaves, lane);
+#endif
+}
+
+// ... at most 16 rows, of operands that are off 16-byte boundaries: fragments straight from memory
+template <typename T, bool GATED>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny_odd(const GemmArgs ga) {
+    constexpr int EPC = 16 / sizeof(T), KS = 64 / sizeof(T), UN = 8;
     __shared__ __attribute__((aligned(16))) float sums[kSkinnyWaves][GATED ? 2 : 1][16][20];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, j = lane & 15;
     const int n0 = blockIdx.x * 16;
@@ -680,14 +771,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(const GemmArgs ga)
     const bool row_ok = j < ga.M;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f}, accu = {0.f, 0.f, 0.f, 0.f};
     auto chunk = [&](const T* p, int k) {  // elements k .. k + EPC - 1 of a row, 0 past its end
-        const int cnt = ga.K - k - g * EPC;
-        if constexpr (ALIGNED) {
-            u32x4_t q = {0u, 0u, 0u, 0u};
-            if (cnt > 0) q = *reinterpret_cast<const u32x4_t*>(p + k);
-            return q;
-        } else {
-            return load_chunk<T>(reinterpret_cast<const char*>(p + k), cnt);
-        }
+        return load_chunk<T>(reinterpret_cast<const char*>(p + k), ga.K - k - g * EPC);
     };
     for (int k = wave * KS * UN; k < ga.K; k += kSkinnyWaves * KS * UN) {
         u32x4_t fa[UN], fb[UN], fu[UN];
@@ -707,35 +791,46 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny(const GemmArgs ga)
     *reinterpret_cast<f32x4*>(&sums[wave][0][j][g * 4]) = acc;
     if constexpr (GATED) *reinterpret_cast<f32x4*>(&sums[wave][1][j][g * 4]) = accu;
     __syncthreads();
-    if (tid < 32) {
-        const int row = tid >> 1, ch = tid & 1;
-        if (row < ga.M) {
-            float s[8], u[8];
-#pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                s[v] = 0.f;
-                u[v] = 0.f;
-                for (int w = 0; w < kSkinnyWaves; ++w) {
-                    s[v] += sums[w][0][row][ch * 8 + v];
-                    if constexpr (GATED) u[v] += sums[w][1][row][ch * 8 + v];
-                }
-            }
-            epilogue8<T, GATED>(ga.e, full_offset(ga.e.offset, ga.e.d_offset), row, n0 + ch * 8, s, u);
-        }
-    }
+    skinny_end<T, GATED>(ga, 0, n0, sums, tid);
 }
 
-// Adds up the partial sums of a product whose k was cut, in the order of the cuts, and does the epilogue
+// The last launch of a call.  The first sum_wgs work-groups add up the row blocks' sums of the bias gradient, 32 columns
+// each, 8 rows at a time; the others add up the partial sums of a product whose k was cut, in the order of the cuts, and do
+// its epilogue.  Every sum has a fixed order.
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_join(const JoinArgs ja) {
+__global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const SumArgs sa, int sum_wgs) {
+    if ((int)blockIdx.x < sum_wgs) {
+        __shared__ float red[8][33];
+        const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
+        const int c = blockIdx.x * 32 + cx;
+        float s[8] = {};
+        if (c < sa.n) {
+            const float* const p = sa.sums + c;
+            for (int i = ry; i < sa.row_blocks; i += 64) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (i + 8 * u < sa.row_blocks) s[u] += p[(int64_t)(i + 8 * u) * sa.sums_ld];
+            }
+        }
+        red[ry][cx] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        __syncthreads();
+        if (ry == 0 && c < sa.n) {
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) t += red[w][cx];
+            static_cast<T*>(sa.out)[c] = (T)t;
+        }
+        return;
+    }
     const int chunks = (ja.e.n + 7) / 8;
-    const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t idx = (int64_t)((int)blockIdx.x - sum_wgs) * 256 + threadIdx.x;
     if (idx >= (int64_t)chunks * ja.M) return;
     const int m = (int)(idx / chunks), col = (int)(idx % chunks) * 8;
     float s[8] = {}, u[8] = {};
     const float* p = ja.part + (int64_t)m * ja.part_ld + col;
     const int64_t slab = (int64_t)ja.M * ja.part_ld;
     const int up = (ja.e.n + 7) & ~7;
+#pragma unroll 4
     for (int i = 0; i < ja.split; ++i, p += slab) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -752,11 +847,41 @@ __global__ __launch_bounds__(256) void k_join(const JoinArgs ja) {
     epilogue8<T, GATED>(ja.e, full_offset(ja.e.offset, ja.e.d_offset), m, col, s, u);
 }
 
+// Rows that do not start on 16-byte boundaries, or end inside a chunk, copied to rows that do, zeros behind their ends: the
+// products load whole chunks straight to LDS.  (Products that took such rows through registers cost 1.6 times as much with
+// k along the rows, 4 times with k down a column: 4096 x 2047 -> 2047 f16.)
+template <typename T>
+__device__ __forceinline__ void pack_rows(const PackArgs& pk, int64_t first, int64_t step) {
+    constexpr int EPC = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t cpr = (uint32_t)(pk.cols[i] + EPC - 1) / EPC;
+        const int64_t total = (int64_t)cpr * pk.rows[i];
+        for (int64_t c = first; c < total; c += step) {
+            // (a 64-bit division takes longer than the copy)
+            const int64_t r = total < (int64_t(1) << 32) ? (int64_t)((uint32_t)c / cpr) : c / cpr;
+            const int k = (int)(c - r * cpr) * EPC;
+            const char* const p = static_cast<const char*>(pk.src[i]) + (r * pk.ld[i] + k) * (int64_t)sizeof(T);
+            static_cast<u32x4_t*>(pk.dst[i])[c] = load_chunk<T>(p, pk.cols[i] - k);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack(const PackArgs pk) {
+    pack_rows<T>(pk, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+}
+
 // dz and the bias gradient's partial sums: a work-group takes 256 columns and rows_per_block rows, 32 lanes side by side
-// with eight columns each, 8 rows at a time
+// with eight columns each, kDzRows rows at a time.  The work-groups behind those copy rows for the products (pack_rows).
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_dz(const DzArgs da) {
-    __shared__ float red[8][256 + 8];
+__global__ __launch_bounds__(32 * kDzRows) void k_dz(const DzArgs da, const PackArgs pk) {
+    __shared__ float red[kDzRows][256 + 8];
+    if ((int)blockIdx.y >= da.row_blocks) {
+        const int64_t wg = (int64_t)(blockIdx.y - da.row_blocks) * gridDim.x + blockIdx.x, wgs = (int64_t)(gridDim.y - da.row_blocks) * gridDim.x;
+        pack_rows<T>(pk, wg * (32 * kDzRows) + threadIdx.x, wgs * (32 * kDzRows));
+        return;
+    }
     const int tid = threadIdx.x, cx = tid & 31, ry = tid >> 5;
     const int col = (blockIdx.x * 32 + cx) * 8;
     const int64_t r0 = (int64_t)blockIdx.y * da.rows_per_block, r1 = min(da.M, r0 + da.rows_per_block);
@@ -766,9 +891,9 @@ __global__ __launch_bounds__(256) void k_dz(const DzArgs da) {
     const int last = GATED ? 2 * da.n : da.n;
     float sum[GATED ? 2 : 1][8] = {};
     if (cnt > 0) {
-        for (int64_t r = r0 + ry; r < r1; r += 8) {
+        for (int64_t r = r0 + ry; r < r1; r += kDzRows) {
             float d[8], z[8], u[8];
-            load8(static_cast<const T*>(da.dy) + r * da.ld_dy + col, cnt, da.vec & 1, d);
+            load8(static_cast<const T*>(da.dy) + r * da.ld_dy + col, cnt, d);
             if (da.thr) {
                 const uint32_t keep = keep_mask((uint32_t)col >> 3, (uint32_t)r, da.seed, offset, da.thr);
 #pragma unroll
@@ -776,8 +901,8 @@ __global__ __launch_bounds__(256) void k_dz(const DzArgs da) {
             }
             if (da.pre) {
                 const T* p = static_cast<const T*>(da.pre) + r * da.ld_pre + col;
-                load8(p, cnt, da.vec & 2, z);
-                if constexpr (GATED) load8(p + da.n, cnt, (da.vec & 2) && da.n % 8 == 0, u);
+                load8(p, cnt, z);
+                if constexpr (GATED) load8(p + da.n, cnt, u);
                 float slope[8];
                 act_both(da.act, z, slope);
 #pragma unroll
@@ -801,12 +926,12 @@ __global__ __launch_bounds__(256) void k_dz(const DzArgs da) {
             if (da.dz) {
                 T* q = static_cast<T*>(da.dz) + r * da.ld_dz + col;
                 if constexpr (GATED) {
-                    store8(q, cnt, true, d);
-                    store8(q + da.n, cnt, da.n % 8 == 0, u);
+                    store8(q, cnt, d);
+                    store8(q + da.n, cnt, u);
                     if (cnt <= 8)
                         for (int i = cnt; i < cnt + (8 - last % 8) % 8; ++i) q[da.n + i] = (T)0.0f;
                 } else {
-                    store8(q, 8, true, d);
+                    store8(q, 8, d);
                 }
             }
         }
@@ -818,37 +943,14 @@ __global__ __launch_bounds__(256) void k_dz(const DzArgs da) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) red[ry][cx * 8 + i] = sum[h][i];
             __syncthreads();
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) s += red[w][tid];
             const int c = blockIdx.x * 256 + tid;
-            if (c < da.n) da.sums[(int64_t)blockIdx.y * da.sums_ld + (h ? da.n : 0) + c] = s;
-        }
-    }
-}
-
-// bias gradient: the row blocks' sums added up in a fixed order, 32 columns a work-group, 32 rows at a time
-template <typename T>
-__global__ __launch_bounds__(1024) void k_sum(const SumArgs sa) {
-    __shared__ float red[32][33];
-    const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + cx;
-    float s[4] = {};
-    if (c < sa.n) {
-        const float* const p = sa.sums + c;
-        for (int i = ry; i < sa.row_blocks; i += 128) {
+            if (tid < 256 && c < da.n) {
+                float s = 0.f;
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (i + 32 * u < sa.row_blocks) s[u] += p[(int64_t)(i + 32 * u) * sa.sums_ld];
+                for (int w = 0; w < kDzRows; ++w) s += red[w][tid];
+                da.sums[(int64_t)blockIdx.y * da.sums_ld + (h ? da.n : 0) + c] = s;
+            }
         }
-    }
-    red[ry][cx] = (s[0] + s[1]) + (s[2] + s[3]);
-    __syncthreads();
-    if (ry == 0 && c < sa.n) {
-        float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < 32; ++w) t += red[w][cx];
-        static_cast<T*>(sa.out)[c] = (T)t;
     }
 }
 
@@ -861,7 +963,7 @@ __global__ __launch_bounds__(256) void k_drop(const DropArgs da) {
         const int64_t row = idx / chunks;
         const int col = (int)(idx - row * chunks) * 8, cnt = da.cols - col;
         float s[8];
-        load8(static_cast<const T*>(da.x) + row * da.ld_x + col, cnt, da.vec & 1, s);
+        load8(static_cast<const T*>(da.x) + row * da.ld_x + col, cnt, s);
         if (da.thr) {
             const uint32_t keep = keep_mask((uint32_t)(col >> 3), (uint32_t)row, da.seed, offset, da.thr);
 #pragma unroll
@@ -869,70 +971,86 @@ __global__ __launch_bounds__(256) void k_drop(const DropArgs da) {
         }
         if (da.res) {
             float r[8];
-            load8(static_cast<const T*>(da.res) + row * da.ld_res + col, cnt, da.vec & 4, r);
+            load8(static_cast<const T*>(da.res) + row * da.ld_res + col, cnt, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] += r[i];
         }
-        store8(static_cast<T*>(da.y) + row * da.ld_y + col, cnt, da.vec & 2, s);
+        store8(static_cast<T*>(da.y) + row * da.ld_y + col, cnt, s);
     }
 }
 
 // ---- launches -----------------------------------------------------------------------------------
-template <typename T, int LAY, int BM, int BN, int WM, int WN, bool AL, bool GT>
+template <typename T, int LAY, int BM, int BN, int WM, int WN, bool GT>
 static hipError_t gemm_go(const GemmArgs& g, hipStream_t s) {
-    k_gemm<T, LAY, BM, BN, WM, WN, AL, GT><<<dim3((unsigned)(g.tiles_m * g.tiles_n * g.split)), dim3(64 * WM * WN), 0, s>>>(g);
+    k_gemm<T, LAY, BM, BN, WM, WN, GT><<<dim3((unsigned)(g.tiles_m * g.tiles_n * g.split)), dim3(64 * WM * WN), 0, s>>>(g);
     return hipGetLastError();
 }
 
 template <typename T, int LAY, bool GT>
-static hipError_t gemm_tile(const GemmArgs& g, int tile, bool aligned, hipStream_t s) {
-    if (!aligned) return tile == 2 ? gemm_go<T, LAY, 64, 128, 2, 2, false, GT>(g, s) : gemm_go<T, LAY, 128, 128, 2, 2, false, GT>(g, s);
-    if (tile == 0) return gemm_go<T, LAY, 256, 256, 2, 4, true, GT>(g, s);
-    if (tile == 1) return gemm_go<T, LAY, 128, 128, 2, 2, true, GT>(g, s);
-    return gemm_go<T, LAY, 64, 128, 2, 2, true, GT>(g, s);
+static hipError_t gemm_tile(const GemmArgs& g, int tile, hipStream_t s) {
+    if (tile == 0) return gemm_go<T, LAY, 256, 256, 2, 4, GT>(g, s);
+    if (tile == 1) return gemm_go<T, LAY, 128, 128, 2, 2, GT>(g, s);
+    return gemm_go<T, LAY, 64, 128, 2, 2, GT>(g, s);
 }
 
 template <typename T>
-hipError_t DenseOps<T>::gemm(const GemmArgs& g, Layout lay, bool gated, int tile, bool aligned, hipStream_t s) {
-    if (gated) return gemm_tile<T, L_KK, true>(g, tile, aligned, s);
-    if (lay == L_KK) return gemm_tile<T, L_KK, false>(g, tile, aligned, s);
-    if (lay == L_KT) return gemm_tile<T, L_KT, false>(g, tile, aligned, s);
-    return gemm_tile<T, L_TT, false>(g, tile, aligned, s);
+hipError_t DenseOps<T>::gemm(const GemmArgs& g, Layout lay, bool gated, int tile, hipStream_t s) {
+    if (gated) return gemm_tile<T, L_KK, true>(g, tile, s);
+    if (lay == L_KK) return gemm_tile<T, L_KK, false>(g, tile, s);
+    if (lay == L_KT) return gemm_tile<T, L_KT, false>(g, tile, s);
+    return gemm_tile<T, L_TT, false>(g, tile, s);
+}
+
+template <typename T, bool GT>
+static void skinny_go(const GemmArgs& g, bool aligned, hipStream_t s) {
+    const dim3 grid((unsigned)((g.N + 15) / 16)), block(64 * kSkinnyWaves);
+    if (!aligned) k_skinny_odd<T, GT><<<grid, block, 0, s>>>(g);
+    else if (g.M <= 16) k_skinny<T, GT, 1><<<grid, block, 0, s>>>(g);
+    else k_skinny<T, GT, 2><<<grid, block, 0, s>>>(g);
 }
 
 template <typename T>
 hipError_t DenseOps<T>::skinny(const GemmArgs& g, bool gated, bool aligned, hipStream_t s) {
-    const dim3 grid((unsigned)((g.N + 15) / 16)), block(64 * kSkinnyWaves);
-    if (gated) {
-        if (aligned) k_skinny<T, true, true><<<grid, block, 0, s>>>(g);
-        else k_skinny<T, false, true><<<grid, block, 0, s>>>(g);
-    } else {
-        if (aligned) k_skinny<T, true, false><<<grid, block, 0, s>>>(g);
-        else k_skinny<T, false, false><<<grid, block, 0, s>>>(g);
-    }
+    if (gated) skinny_go<T, true>(g, aligned, s);
+    else skinny_go<T, false>(g, aligned, s);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t DenseOps<T>::join(const JoinArgs& j, hipStream_t s) {
+hipError_t DenseOps<T>::join(const JoinArgs& j, const SumArgs& a, hipStream_t s) {
     const int64_t n = (int64_t)((j.e.n + 7) / 8) * j.M;
-    const dim3 grid((unsigned)((n + 255) / 256));
-    if (j.gated) k_join<T, true><<<grid, dim3(256), 0, s>>>(j);
-    else k_join<T, false><<<grid, dim3(256), 0, s>>>(j);
+    const int sum_wgs = (a.n + 31) / 32;
+    const dim3 grid((unsigned)((n + 255) / 256 + sum_wgs));
+    if (j.gated) k_join<T, true><<<grid, dim3(256), 0, s>>>(j, a, sum_wgs);
+    else k_join<T, false><<<grid, dim3(256), 0, s>>>(j, a, sum_wgs);
+    return hipGetLastError();
+}
+
+// work-groups of `threads` for the chunks to copy, at most `most`
+template <typename T>
+static int pack_wgs(const PackArgs& pk, int threads, int most) {
+    constexpr int EPC = 16 / sizeof(T);
+    int64_t n = 0;
+    for (int i = 0; i < 2; ++i) n += (pk.cols[i] + EPC - 1) / EPC * pk.rows[i];
+    const int64_t w = (n + threads - 1) / threads;
+    return (int)(w < most ? w : most);
+}
+
+template <typename T>
+hipError_t DenseOps<T>::pack(const PackArgs& pk, hipStream_t s) {
+    const int wgs = pack_wgs<T>(pk, 256, 4096);
+    if (wgs == 0) return hipSuccess;
+    k_pack<T><<<dim3((unsigned)wgs), dim3(256), 0, s>>>(pk);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t DenseOps<T>::dz(const DzArgs& d, hipStream_t s) {
-    const dim3 grid((unsigned)((d.n + 255) / 256), (unsigned)d.row_blocks);
-    if (d.gated) k_dz<T, true><<<grid, dim3(256), 0, s>>>(d);
-    else k_dz<T, false><<<grid, dim3(256), 0, s>>>(d);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t DenseOps<T>::sum(const SumArgs& a, hipStream_t s) {
-    k_sum<T><<<dim3((unsigned)((a.n + 31) / 32)), dim3(1024), 0, s>>>(a);
+hipError_t DenseOps<T>::dz(const DzArgs& d, const PackArgs& pk, hipStream_t s) {
+    const unsigned cols = (unsigned)((d.n + 255) / 256);
+    const unsigned more = ((unsigned)pack_wgs<T>(pk, 32 * kDzRows, 1024) + cols - 1) / cols;
+    const dim3 grid(cols, (unsigned)d.row_blocks + more);
+    if (d.gated) k_dz<T, true><<<grid, dim3(32 * kDzRows), 0, s>>>(d, pk);
+    else k_dz<T, false><<<grid, dim3(32 * kDzRows), 0, s>>>(d, pk);
     return hipGetLastError();
 }
 

@@ -131,7 +131,7 @@ def _backward(op, dtype, M, K, N, name, p, how, seed=2):
 
 # rows, in, out: single tokens, the largest batch of the few-rows kernel and one past it, ragged and whole tiles, one
 # column, one k, long sums that are cut, several tiles of every size
-FORWARD = [(1, 1664, 1024), (3, 13, 1), (16, 520, 40), (17, 64, 128), (5, 1, 7), (40, 259, 129), (130, 72, 200),
+FORWARD = [(1, 1664, 1024), (3, 13, 1), (16, 520, 40), (17, 64, 128), (5, 1, 7), (32, 72, 24), (31, 1000, 130), (33, 64, 64), (40, 259, 129), (130, 72, 200),
            (777, 515, 103), (64, 8192, 64), (2048, 256, 1024), (300, 4096, 256), (1030, 200, 2000)]
 BACKWARD = [(1, 64, 32), (2, 13, 1), (17, 100, 40), (1, 1, 1), (259, 37, 129), (1000, 264, 72), (4096, 64, 128),
             (2999, 259, 129), (2048, 1024, 512), (1025, 520, 1000)]
@@ -438,6 +438,38 @@ def test_on_another_stream():
 
 
 @pytest.mark.gpu
+def test_pointers_off_the_boundary():
+    """Rows whose length and pitch are fine behind pointers that are not: the flag makes room for copies, without it the
+    call says that there is too little; the results are those of the same rows elsewhere."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    for M, back in ((300, False), (300, True), (5, False)):
+        t = _inputs(29, "bf16", x=((M, 128), 1.0), w=((72, 128), 0.1), dy=((M, 72), 1.0))
+        off = {k: Guarded(*t[k].shape, "bf16", shift=3).set(t[k]) for k in ("x", "w")}
+        outs = []
+        for x, w, flags in ((t["x"], t["w"], 0), (off["x"].view, off["w"].view, b.DENSE_OFF_BOUNDARY), (off["x"].view, t["w"], b.DENSE_OFF_BOUNDARY)):
+            cfg = b.make_dense_config(b.BF16, M, 128, 72, flags=flags)
+            work = torch.full((max(16, b.dlc_linear_workspace_bytes(cfg, back)),), 0xFF, dtype=torch.uint8, device="cuda")
+            y, dx, dw = torch.zeros_like(t["dy"]), torch.zeros_like(t["x"]), torch.zeros_like(t["w"])
+            if back:
+                b.dlc_linear_backward(cfg, x, w, None, t["dy"], dx, dw, None, work)
+            else:
+                b.dlc_linear_forward(cfg, x, w, None, None, y, None, work)
+            outs.append((y, dx, dw))
+        for o in outs[1:]:
+            assert all(torch.equal(a, c) for a, c in zip(outs[0], o))
+        cfg = b.make_dense_config(b.BF16, M, 128, 72)
+        work = torch.empty(b.dlc_linear_workspace_bytes(cfg, back), dtype=torch.uint8, device="cuda")
+        if back or M > 16:
+            with pytest.raises(b.DlcError) as err:
+                if back:
+                    b.dlc_linear_backward(cfg, off["x"].view, off["w"].view, None, t["dy"], dx, dw, None, work)
+                else:
+                    b.dlc_linear_forward(cfg, off["x"].view, off["w"].view, None, None, y, None, work)
+            assert err.value.status == b.ECAPACITY
+
+
+@pytest.mark.gpu
 def test_offsets_past_32_bits():
     """Operands of more than 2^32 bytes: rows past that point, forward and backward."""
     import torch
@@ -488,7 +520,7 @@ def test_invalid_geometry_has_no_workspace():
     assert b.dlc_linear_workspace_bytes(mk(b.F32, 512, 64, 64), True) > 0
     for bad in (mk(3, 512, 64, 64), mk(-1, 512, 64, 64), mk(b.F32, -1, 64, 64), mk(b.F32, 512, 0, 64), mk(b.F32, 512, 64, 0),
                 mk(b.F32, 512, 64, 64, act=5), mk(b.F32, 512, 64, 64, act=-1), mk(b.F32, 512, 64, 64, dropout_p=1.5),
-                mk(b.F32, 512, 64, 64, dropout_p=-0.1), mk(b.F32, 512, 64, 64, dropout_p=float("nan")),
+                mk(b.F32, 512, 64, 64, dropout_p=-0.1), mk(b.F32, 512, 64, 64, dropout_p=float("nan")), mk(b.F32, 512, 64, 64, flags=2),
                 mk(b.F32, 512, 64, 64, ld_x=63), mk(b.F32, 512, 64, 64, ld_dw=-1), mk(b.F32, (1 << 30) + 1, 64, 64),
                 mk(b.F32, 512, (1 << 20) + 1, 64), mk(b.F32, 512, 64, (1 << 20) + 1), mk(b.F32, 512, 64, 64, ld_w=1 << 40),
                 mk(b.F32, 1 << 30, 1 << 20, 64)):
