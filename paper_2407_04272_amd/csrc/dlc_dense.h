@@ -115,7 +115,7 @@ constexpr int kTileM[] = {256, 128, 64};
 constexpr int kTileN[] = {256, 128, 128};
 constexpr int kTileBytes = 128;  // a cut of k is a multiple of this many bytes of it (a k tile, or two)
 constexpr int kSkinnyRows = 32, kSkinnyOddRows = 16;  // most rows of a pass over the weights, and where they stand off boundaries
-constexpr int kDzRows = 32;    // rows a work-group of k_dz takes at a time
+constexpr int kDzRows = 16;    // rows a work-group of k_dz takes at a time
 
 #if defined(__HIPCC__)
 
@@ -150,10 +150,43 @@ __device__ __forceinline__ uint32_t keep_mask(uint32_t col8, uint32_t row, uint6
 }
 
 // ---- activations, in fp32 ----
-// The exponentials overflow to infinity for very negative arguments, and 1 / infinity is the limit 0 that is wanted;
-// silu's product with it, (-large) * 0, is too.
-__device__ __forceinline__ float sigmoidf(float z) { return 1.0f / (1.0f + expf(-z)); }
+// FAST (results of half precision): the hardware's exponential and reciprocal, off by a few 2^-24 of the result, and a
+// polynomial for erfc, where a full division, expf and erfcf took 8 us of every 256 x 256 tile's epilogue.  An exponential
+// that overflows gives 1 / infinity = 0, the limit that is wanted.
+template <bool FAST>
+__device__ __forceinline__ float sigmoidf(float z) {
+    if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+    else return 1.0f / (1.0f + expf(-z));
+}
 
+// The normal distribution function at z, and (phi) its density.  FAST: erfc(x) = exp(-x^2) t P(t) with t = 1 / (1 + 0.45 x);
+// P is a least-squares fit of exp(x^2) erfc(x) / t over all x >= 0, reweighted towards equal relative errors: 1.4e-7 at most.
+template <bool FAST>
+__device__ __forceinline__ float normal_cdf(float z, float* phi) {
+    if constexpr (FAST) {
+        const float x = __builtin_fabsf(z) * 0.70710678f;
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.45f, x, 1.0f));
+        const float e = __builtin_amdgcn_exp2f(x * x * -1.44269504f);
+        float p = -0.04207083582878113f;
+        p = __builtin_fmaf(p, t, 0.19364100694656372f);
+        p = __builtin_fmaf(p, t, -0.3059483766555786f);
+        p = __builtin_fmaf(p, t, 0.14769354462623596f);
+        p = __builtin_fmaf(p, t, -0.025435185059905052f);
+        p = __builtin_fmaf(p, t, 0.12102247029542923f);
+        p = __builtin_fmaf(p, t, 0.17503467202186584f);
+        p = __builtin_fmaf(p, t, 0.22829535603523254f);
+        p = __builtin_fmaf(p, t, 0.2538819909095764f);
+        p = __builtin_fmaf(p, t, 0.25388532876968384f);
+        const float h = 0.5f * (e * (t * p));
+        if (phi) *phi = e * 0.39894228f;
+        return z < 0.0f ? h : 1.0f - h;
+    } else {
+        if (phi) *phi = expf(-0.5f * z * z) * 0.39894228040143268f;
+        return 0.5f * erfcf(z * -0.70710678118654752f);
+    }
+}
+
+template <bool FAST>
 __device__ __forceinline__ void act_values(int act, float z[8]) {
     switch (act) {
         case DLC_ACT_RELU:
@@ -162,21 +195,22 @@ __device__ __forceinline__ void act_values(int act, float z[8]) {
             break;
         case DLC_ACT_SIGMOID:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = sigmoidf(z[i]);
+            for (int i = 0; i < 8; ++i) z[i] = sigmoidf<FAST>(z[i]);
             break;
         case DLC_ACT_SILU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= sigmoidf(z[i]);
+            for (int i = 0; i < 8; ++i) z[i] *= sigmoidf<FAST>(z[i]);
             break;
         case DLC_ACT_GELU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= 0.5f * erfcf(z[i] * -0.70710678118654752f);
+            for (int i = 0; i < 8; ++i) z[i] *= normal_cdf<FAST>(z[i], nullptr);
             break;
         default: break;
     }
 }
 
 // values (into z) and slopes at z
+template <bool FAST>
 __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
     switch (act) {
         case DLC_ACT_RELU:
@@ -189,7 +223,7 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
         case DLC_ACT_SIGMOID:
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float q = sigmoidf(z[i]);
+                const float q = sigmoidf<FAST>(z[i]);
                 z[i] = q;
                 d[i] = q * (1.0f - q);
             }
@@ -197,7 +231,7 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
         case DLC_ACT_SILU:
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float q = sigmoidf(z[i]);
+                const float q = sigmoidf<FAST>(z[i]);
                 d[i] = q * (1.0f + z[i] * (1.0f - q));
                 z[i] *= q;
             }
@@ -205,8 +239,9 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
         case DLC_ACT_GELU:
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float c = 0.5f * erfcf(z[i] * -0.70710678118654752f);
-                d[i] = c + z[i] * (expf(-0.5f * z[i] * z[i]) * 0.39894228040143268f);
+                float phi;
+                const float c = normal_cdf<FAST>(z[i], &phi);
+                d[i] = c + z[i] * phi;
                 z[i] *= c;
             }
             break;
@@ -286,7 +321,7 @@ __device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t
         store8(p + col, cnt, s);
         if constexpr (GATED) store8(p + e.n + col, cnt, u);
     }
-    act_values(e.act, s);
+    act_values<sizeof(T) == 2>(e.act, s);
     if constexpr (GATED) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] *= u[i];

@@ -18,7 +18,7 @@ constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 20;
 
 bool good_ld(int64_t& ld, int64_t row) {
     if (ld == 0) ld = row;
-    return ld >= row && ld <= (row > kMaxDim ? row : kMaxDim);
+    return ld >= row && ld <= kMaxDim;
 }
 
 bool dropout_params(double p, uint32_t* thr, float* scale) {
@@ -35,6 +35,7 @@ bool make_shape(const dlc_dense_config* c, bool gated, Shape* s) {
     if (c->rows < 0 || c->rows > kMaxRows) return false;
     if (c->in_features < 1 || c->in_features > kMaxDim || c->out_features < 1 || c->out_features > kMaxDim) return false;
     const int64_t wide = gated ? 2 * c->out_features : c->out_features;
+    if (wide > kMaxDim) return false;  // (a tile's 256 rows of dz span less than 2^31 bytes)
     s->M = c->rows; s->K = c->in_features; s->N = c->out_features;
     s->ldx = c->ld_x; s->ldw = c->ld_w; s->ldy = c->ld_y; s->ldpre = c->ld_pre;
     s->ldres = c->ld_res; s->lddy = c->ld_dy; s->lddx = c->ld_dx; s->lddw = c->ld_dw;
@@ -156,9 +157,10 @@ BackPlan plan_back(const Shape& s) {
     b.ld_dz = round8(wide);
     b.sums_ld = b.ld_dz;
     const int64_t cols = div_up(s.N, 256);
-    // about four work-groups a compute unit; few blocks of rows, since the last launch has their sums to add up
-    int64_t blocks = div_up(1024, cols);
-    if (blocks > 128) blocks = 128;
+    // about eight work-groups of eight wavefronts a compute unit; no more than 256 blocks of rows, whose sums the last launch
+    // adds up with all loads in flight
+    int64_t blocks = div_up(2048, cols);
+    if (blocks > 256) blocks = 256;
     if (blocks > div_up(s.M, kDzRows)) blocks = div_up(s.M, kDzRows);
     if (blocks < 1) blocks = 1;
     b.rows_per_block = (int)(div_up(div_up(s.M, blocks), kDzRows) * kDzRows);

@@ -794,30 +794,34 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny_odd(const GemmArgs
     skinny_end<T, GATED>(ga, 0, n0, sums, tid);
 }
 
-// The last launch of a call.  The first sum_wgs work-groups add up the row blocks' sums of the bias gradient, 32 columns
-// each, 8 rows at a time; the others add up the partial sums of a product whose k was cut, in the order of the cuts, and do
+constexpr int kSumCols = 16;
+
+// The last launch of a call.  The first sum_wgs work-groups add up the row blocks' sums of the bias gradient, 16 columns
+// each, all loads in flight at once; the others add up the partial sums of a product whose k was cut, in the order of the cuts, and do
 // its epilogue.  Every sum has a fixed order.
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const SumArgs sa, int sum_wgs) {
     if ((int)blockIdx.x < sum_wgs) {
-        __shared__ float red[8][33];
-        const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
-        const int c = blockIdx.x * 32 + cx;
-        float s[8] = {};
+        __shared__ float red[16][17];
+        const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
+        const int c = blockIdx.x * kSumCols + cx;
+        float s = 0.f;
         if (c < sa.n) {
             const float* const p = sa.sums + c;
-            for (int i = ry; i < sa.row_blocks; i += 64) {
+            for (int i = ry; i < sa.row_blocks; i += 256) {
+                float v[16];
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (i + 8 * u < sa.row_blocks) s[u] += p[(int64_t)(i + 8 * u) * sa.sums_ld];
+                for (int u = 0; u < 16; ++u) v[u] = i + 16 * u < sa.row_blocks ? p[(int64_t)(i + 16 * u) * sa.sums_ld] : 0.f;
+#pragma unroll
+                for (int u = 0; u < 16; ++u) s += v[u];
             }
         }
-        red[ry][cx] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+        red[ry][cx] = s;
         __syncthreads();
         if (ry == 0 && c < sa.n) {
             float t = 0.f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) t += red[w][cx];
+            for (int w = 0; w < 16; ++w) t += red[w][cx];
             static_cast<T*>(sa.out)[c] = (T)t;
         }
         return;
@@ -904,7 +908,7 @@ __global__ __launch_bounds__(32 * kDzRows) void k_dz(const DzArgs da, const Pack
                 load8(p, cnt, z);
                 if constexpr (GATED) load8(p + da.n, cnt, u);
                 float slope[8];
-                act_both(da.act, z, slope);
+                act_both<sizeof(T) == 2>(da.act, z, slope);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if constexpr (GATED) {
@@ -1019,7 +1023,7 @@ hipError_t DenseOps<T>::skinny(const GemmArgs& g, bool gated, bool aligned, hipS
 template <typename T>
 hipError_t DenseOps<T>::join(const JoinArgs& j, const SumArgs& a, hipStream_t s) {
     const int64_t n = (int64_t)((j.e.n + 7) / 8) * j.M;
-    const int sum_wgs = (a.n + 31) / 32;
+    const int sum_wgs = (a.n + kSumCols - 1) / kSumCols;
     const dim3 grid((unsigned)((n + 255) / 256 + sum_wgs));
     if (j.gated) k_join<T, true><<<grid, dim3(256), 0, s>>>(j, a, sum_wgs);
     else k_join<T, false><<<grid, dim3(256), 0, s>>>(j, a, sum_wgs);

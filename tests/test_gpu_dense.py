@@ -527,6 +527,8 @@ def test_invalid_geometry_has_no_workspace():
         assert b.dlc_linear_workspace_bytes(bad, True) == 0 and b.dlc_gated_workspace_bytes(bad, True) == 0
         assert b.dlc_linear_workspace_bytes(bad) == 0 and b.dlc_gated_workspace_bytes(bad) == 0
     assert b.dlc_gated_workspace_bytes(mk(b.F32, 512, 64, 64, ld_pre=127), True) == 0
+    assert b.dlc_gated_workspace_bytes(mk(b.F32, 512, 64, (1 << 19) + 1), True) == 0
+    assert b.dlc_gated_workspace_bytes(mk(b.F32, 512, 64, 1 << 19), True) > 0
     assert b.dlc_linear_workspace_bytes(mk(b.F32, 512, 64, 64, ld_pre=127), True) > 0
 
 
