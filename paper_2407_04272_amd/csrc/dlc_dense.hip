@@ -95,7 +95,7 @@ Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) 
             double t = (double)full * ((double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
             if (rest) t += (double)per * c.tile[div_up(rest, kUnits) - 1] + c.further;
             // partial sums: a launch, and their way to memory and back
-            if (split > 1) t += 4.0 + (double)split * (double)M * (double)wide * 8.0 / 4.0e6;
+            if (split > 1) t += 4.0 + (double)split * (double)M * (double)wide * 8.0 / 8.0e6;
             if (t < best_t) {
                 best_t = t;
                 best.tile = tile;
