@@ -99,7 +99,8 @@ template <typename T>
 struct DenseOps {
     static hipError_t gemm(const GemmArgs& g, Layout lay, bool gated, int tile, hipStream_t s);
     static hipError_t skinny(const GemmArgs& g, bool gated, bool aligned, hipStream_t s);
-    static hipError_t join(const JoinArgs& j, const SumArgs& a, hipStream_t s);
+    static hipError_t back(const GemmArgs& gx, const GemmArgs& gw, const SumArgs& a, int tile, hipStream_t s);
+    static hipError_t join(const JoinArgs& ja, const JoinArgs& jb, const SumArgs& a, hipStream_t s);
     static hipError_t pack(const PackArgs& p, hipStream_t s);
     static hipError_t dz(const DzArgs& d, const PackArgs& p, hipStream_t s);
     static hipError_t drop(const DropArgs& d, hipStream_t s);

@@ -64,6 +64,7 @@ struct Plan {
     int tiles_m, tiles_n;
     int64_t part_ld;
     size_t bytes;  // of the partial sums
+    double t;      // the estimate, us
 };
 
 // What a k tile (128 bytes of k) costs with 1, 2 and 3 work-groups on a compute unit, in us, and what a work-group costs
@@ -75,40 +76,102 @@ constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0}, {{0.57, 0.88, 0}, 
 constexpr TileCost kF32Cost[3] = {{{7.6, 0, 0}, 14.0, 10.0}, {{2.2, 3.8, 0}, 8.0, 4.0}, {{1.3, 2.0, 2.9}, 5.0, 3.0}};
 constexpr int kUnits = 256;  // compute units
 
+// cuts of k that are looked at
+constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+
+// a product: M x wide of the result, K the sum's length in k tiles
+struct Product {
+    int64_t M, wide, steps;
+};
+
+// the partial sums' launch, and their way to the caches and back
+double join_cost(const Product& p, int64_t split) { return split > 1 ? (double)split * (double)p.M * (double)p.wide * 8.0 / 8.0e6 : 0.0; }
+
+void set_cut(Plan* plan, const Product& p, int tile, int64_t split, int64_t per, int64_t part_ld, int64_t bk) {
+    plan->tile = tile;
+    plan->split = (int)split;
+    plan->kper = (int)(per * bk);
+    plan->tiles_m = (int)div_up(p.M, kTileM[tile]);
+    plan->tiles_n = (int)div_up(p.wide, kTileN[tile]);
+    plan->part_ld = part_ld;
+    plan->bytes = split > 1 ? (size_t)split * (size_t)p.M * (size_t)part_ld * 4 : 0;
+}
+
 // M x N of the result (gated: N columns of y), K the sum's length: the tile and the cut of K with the smallest estimate
 Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) {
-    const int64_t bk = kTileBytes / es, wide = gated ? 2 * N : N;
+    const int64_t bk = kTileBytes / es;
+    const Product p{M, gated ? 2 * N : N, div_up(K, bk)};
+    const int64_t part_ld = gated ? 2 * round8(N) : round8(N);
     const TileCost* const cost = es == 4 ? kF32Cost : kHalfCost;
     Plan best{};
-    double best_t = 1e300;
+    best.t = 1e300;
     for (int tile = 0; tile < 3; ++tile) {
         const TileCost& c = cost[tile];
-        const int64_t tm = div_up(M, kTileM[tile]), tn = div_up(wide, kTileN[tile]);
-        const int64_t tiles = tm * tn, steps = div_up(K, bk);
-        if (tiles >= (int64_t(1) << 30)) continue;
+        const int64_t tiles = div_up(p.M, kTileM[tile]) * div_up(p.wide, kTileN[tile]);
         const int fit = tile == 0 ? 1 : tile == 1 || lay == L_KK ? 2 : 3;  // work-groups that share a compute unit
-        for (int64_t split = 1; split <= 128; ++split) {
-            if (split > 1 && (steps / split < 2 || tiles * split > 4 * kUnits)) break;
-            const int64_t per = div_up(steps, split);
-            if (div_up(steps, per) != split) continue;
+        for (const int cut : kCuts) {
+            if (cut > 1 && (p.steps < 2 * cut || tiles * cut > 4 * kUnits)) break;
+            const int64_t per = div_up(p.steps, cut), split = div_up(p.steps, per);
             const int64_t wgs = tiles * split, full = wgs / (kUnits * fit), rest = wgs % (kUnits * fit);
             double t = (double)full * ((double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
-            if (rest) t += (double)per * c.tile[div_up(rest, kUnits) - 1] + c.further;
-            // partial sums: a launch, and their way to memory and back
-            if (split > 1) t += 4.0 + (double)split * (double)M * (double)wide * 8.0 / 8.0e6;
-            if (t < best_t) {
-                best_t = t;
-                best.tile = tile;
-                best.split = (int)split;
-                best.kper = (int)(per * bk);
-                best.tiles_m = (int)tm;
-                best.tiles_n = (int)tn;
+            if (rest) t += (double)per * c.tile[(rest - 1) / kUnits] + c.further;
+            if (split > 1) t += 4.0 + join_cost(p, split);
+            if (t < best.t) {
+                best.t = t;
+                set_cut(&best, p, tile, split, per, part_ld, bk);
             }
         }
     }
-    best.part_ld = gated ? 2 * round8(N) : round8(N);
-    best.bytes = best.split > 1 ? (size_t)best.split * (size_t)M * (size_t)best.part_ld * 4 : 0;
     return best;
+}
+
+// na jobs of `a` us, then nb of `b` us, each on the place that is free first
+double makespan(int64_t places, int64_t na, double a, int64_t nb, double b) {
+    const int64_t full = na / places, rest = na % places;  // `rest` places take one more of the first kind
+    const double late = (double)(full + (rest > 0)) * a, early = (double)full * a;
+    double end = late;
+    int64_t on_early = 0, on_late = 0;  // jobs of the second kind that one place has taken
+    while (nb > 0) {
+        const bool to_early = early + (double)on_early * b <= late + (double)on_late * b;
+        nb -= to_early ? places - rest : rest;
+        const double t = to_early ? early + (double)++on_early * b : late + (double)++on_late * b;
+        end = t > end ? t : end;
+    }
+    return end;
+}
+
+// Both products of a backward call in one launch: one tile for both, cut so that no work-group walks over more than a given
+// number of k tiles.  True, and the plans, if that is estimated to take less than one launch after the other.
+bool plan_pair(const Product& px, const Product& pw, int64_t part_ld, int es, Plan* x, Plan* w) {
+    const int64_t bk = kTileBytes / es;
+    const TileCost* const cost = es == 4 ? kF32Cost : kHalfCost;
+    double best = x->t + w->t;
+    bool found = false;
+    for (int tile = 1; tile < 3; ++tile) {
+        const TileCost& c = cost[tile];
+        const int fit = tile == 1 ? 2 : 3;
+        const int64_t tx = div_up(px.M, kTileM[tile]) * div_up(px.wide, kTileN[tile]);
+        const int64_t tw = div_up(pw.M, kTileM[tile]) * div_up(pw.wide, kTileN[tile]);
+        for (const int most : kCuts) {
+            const int64_t sx = div_up(px.steps, most), sw = div_up(pw.steps, most);
+            if (most == 1 || sx > 128 || sw > 128 || tx * sx + tw * sw > 6 * kUnits) continue;
+            const int64_t lx = div_up(px.steps, sx), lw = div_up(pw.steps, sw);
+            const int64_t wgs = tx * sx + tw * sw;
+            const int64_t res = div_up(wgs, kUnits) < fit ? div_up(wgs, kUnits) : fit;
+            // dW's work-groups come first, dX's fill the places as they fall free
+            const double per_tile = c.tile[res - 1];
+            double t = makespan(kUnits * res, tw * sw, (double)lw * per_tile + c.further, tx * sx, (double)lx * per_tile + c.further);
+            t += c.first - c.further;
+            if (sx > 1 || sw > 1) t += 4.0 + join_cost(px, sx) + join_cost(pw, sw);
+            if (t < best) {
+                best = t;
+                found = true;
+                set_cut(x, px, tile, sx, lx, part_ld, bk);
+                set_cut(w, pw, tile, sw, lw, part_ld, bk);
+            }
+        }
+    }
+    return found;
 }
 
 // A matrix of the call that the products read where it stands, or packed (pack_rows)
@@ -148,6 +211,9 @@ struct BackPlan {
     int64_t ld_dz;
     int row_blocks, rows_per_block;
     int64_t sums_ld;
+    Plan x, w;     // one launch after the other, in one piece of the workspace
+    bool both;     // in one launch, in two pieces
+    Plan bx, bw;
     size_t off_sums, off_part, off_pack, total;
 };
 
@@ -167,40 +233,42 @@ BackPlan plan_back(const Shape& s) {
     b.row_blocks = b.rows_per_block ? (int)div_up(s.M, b.rows_per_block) : 0;
     b.off_sums = a256((size_t)s.M * (size_t)b.ld_dz * (size_t)s.es);
     b.off_part = b.off_sums + a256((size_t)b.row_blocks * (size_t)b.sums_ld * 4);
-    const size_t px = s.M ? plan_gemm(s.M, s.K, wide, false, L_KT, s.es).bytes : 0;
-    const size_t pw = s.M ? plan_gemm(wide, s.K, s.M, false, L_TT, s.es).bytes : 0;
-    b.off_pack = b.off_part + a256(px > pw ? px : pw);
+    b.x = plan_gemm(s.M, s.K, wide, false, L_KT, s.es);
+    b.w = plan_gemm(wide, s.K, s.M, false, L_TT, s.es);
+    b.bx = b.x;
+    b.bw = b.w;
+    const int64_t bk = kTileBytes / s.es;
+    b.both = plan_pair(Product{s.M, s.K, div_up(wide, bk)}, Product{wide, s.K, div_up(s.M, bk)}, round8(s.K), s.es, &b.bx, &b.bw);
+    const size_t one = a256(b.x.bytes > b.w.bytes ? b.x.bytes : b.w.bytes), two = b.both ? a256(b.bx.bytes) + a256(b.bw.bytes) : 0;
+    b.off_pack = b.off_part + (one > two ? one : two);
     b.total = b.off_pack + pack_room(s);
     return b;
 }
 
-// a forward call's: the product's partial sums, packed operands (a pass over few rows takes them as they are)
-size_t forward_part(const Shape& s) { return a256(plan_gemm(s.M, s.N, s.K, s.gated, L_KK, s.es).bytes); }
+void set_plan(GemmArgs* g, const Plan& p, void* part) {
+    g->kper = p.kper; g->split = p.split; g->tiles_m = p.tiles_m; g->tiles_n = p.tiles_n;
+    g->part = static_cast<float*>(part);
+    g->part_ld = p.part_ld;
+}
 
-size_t work_bytes_of(const Shape& s, bool backward) {
-    if (s.M == 0) return 0;
-    if (backward) return plan_back(s).total;
-    return s.M <= kSkinnyOddRows ? 0 : forward_part(s) + pack_room(s);
+// the product's partial sums to put together (none if k was not cut)
+JoinArgs join_of(const GemmArgs& g, bool gated) {
+    return g.split > 1 ? JoinArgs{g.part, g.part_ld, g.M, g.split, gated ? 1 : 0, g.e} : JoinArgs{};
 }
 
 // The product; sums: what the last launch adds up besides (n = 0: nothing)
 template <typename T>
-int run_gemm(GemmArgs g, Layout lay, bool gated, int es, void* work, const SumArgs& sums, hipStream_t st) {
-    const Plan p = plan_gemm(g.M, g.N, g.K, gated, lay, es);
-    g.kper = p.kper; g.split = p.split; g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_n;
-    g.part = static_cast<float*>(work);
-    g.part_ld = p.part_ld;
+int run_gemm(GemmArgs g, const Plan& p, Layout lay, bool gated, void* part, const SumArgs& sums, hipStream_t st) {
+    set_plan(&g, p, part);
     if (DenseOps<T>::gemm(g, lay, gated, p.tile, st) != hipSuccess) return DLC_EHIP;
-    if (p.split > 1 || sums.n > 0) {
-        const JoinArgs j{g.part, g.part_ld, p.split > 1 ? g.M : 0, p.split, gated ? 1 : 0, g.e};
-        if (DenseOps<T>::join(j, sums, st) != hipSuccess) return DLC_EHIP;
-    }
+    if (g.split > 1 || sums.n > 0)
+        if (DenseOps<T>::join(join_of(g, gated), JoinArgs{}, sums, st) != hipSuccess) return DLC_EHIP;
     return DLC_OK;
 }
 
 template <typename T>
 int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* bias, const void* res, void* y,
-            void* pre, void* work, size_t work_bytes, hipStream_t st) {
+            void* pre, void* work, size_t work_bytes, const Plan& plan, hipStream_t st) {
     GemmArgs g{};
     g.a = x; g.b = w; g.lda = s.ldx; g.ldb = s.ldw;
     g.M = (int)s.M; g.N = (int)s.N; g.K = (int)s.K;
@@ -215,20 +283,19 @@ int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void
         const bool aligned = on(x, 16) && on(w, 16) && good_rows(s.ldx, s.K, s.es) && good_rows(s.ldw, s.K, s.es);
         if (aligned || s.M <= kSkinnyOddRows) return DenseOps<T>::skinny(g, s.gated, aligned, st) == hipSuccess ? DLC_OK : DLC_EHIP;
     }
-    const size_t part = forward_part(s);
+    const size_t part = a256(plan.bytes);
     PackArgs pk{};
     Source sx, sw;
     const size_t used = place_operands(s, x, w, static_cast<char*>(work) + part, &pk, &sx, &sw);
     if (part + used > work_bytes) return DLC_ECAPACITY;
     if (used && DenseOps<T>::pack(pk, st) != hipSuccess) return DLC_EHIP;
     g.a = sx.p; g.lda = sx.ld; g.b = sw.p; g.ldb = sw.ld;
-    return run_gemm<T>(g, L_KK, s.gated, s.es, work, SumArgs{}, st);
+    return run_gemm<T>(g, plan, L_KK, s.gated, work, SumArgs{}, st);
 }
 
 template <typename T>
 int backward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* pre, const void* dy, void* dx,
-             void* dw, void* dbias, void* work, size_t work_bytes, hipStream_t st) {
-    const BackPlan b = plan_back(s);
+             void* dw, void* dbias, void* work, size_t work_bytes, const BackPlan& b, hipStream_t st) {
     char* const wk = static_cast<char*>(work);
     const int64_t wide = s.gated ? 2 * s.N : s.N;
     const bool same = !s.gated && c->act == DLC_ACT_NONE && s.thr == 0;  // dz is dy
@@ -260,34 +327,42 @@ int backward(const dlc_dense_config* c, const Shape& s, const void* x, const voi
     const SumArgs sum = dbias ? SumArgs{sums, b.sums_ld, s.M > 0 ? b.row_blocks : 0, (int)wide, dbias} : SumArgs{};
     const void* const dz = direct ? dy : work;
     const int64_t lddz = direct ? s.lddy : b.ld_dz;
-    if (dx && s.M > 0) {
-        GemmArgs g{};
-        g.a = dz; g.b = sw.p; g.lda = lddz; g.ldb = sw.ld;
-        g.M = (int)s.M; g.N = (int)s.K; g.K = (int)wide;
-        g.e.y = dx; g.e.ld_y = s.lddx; g.e.n = (int)s.K;
-        if (const int rc = run_gemm<T>(g, L_KT, false, s.es, wk + b.off_part, dw ? SumArgs{} : sum, st); rc != DLC_OK) return rc;
+    GemmArgs gx{}, gw{};
+    gx.a = dz; gx.b = sw.p; gx.lda = lddz; gx.ldb = sw.ld;
+    gx.M = (int)s.M; gx.N = (int)s.K; gx.K = (int)wide;
+    gx.e.y = dx; gx.e.ld_y = s.lddx; gx.e.n = (int)s.K;
+    gw.a = dz; gw.b = sx.p; gw.lda = lddz; gw.ldb = sx.ld;
+    gw.M = (int)wide; gw.N = (int)s.K; gw.K = (int)s.M;
+    gw.e.y = dw; gw.e.ld_y = s.lddw; gw.e.n = (int)s.K;
+    const auto join = [&](const JoinArgs& ja, const JoinArgs& jb) { return DenseOps<T>::join(ja, jb, sum, st) == hipSuccess ? DLC_OK : DLC_EHIP; };
+    if (s.M == 0) {  // (an empty sum: a product with no cut at all)
+        JoinArgs j{};
+        if (dw) j = JoinArgs{nullptr, 0, gw.M, 0, 0, gw.e};
+        return dw || dbias ? join(j, JoinArgs{}) : DLC_OK;
     }
-    if (dw) {
-        GemmArgs g{};
-        g.a = dz; g.b = sx.p; g.lda = lddz; g.ldb = sx.ld;
-        g.M = (int)wide; g.N = (int)s.K; g.K = (int)s.M;
-        g.e.y = dw; g.e.ld_y = s.lddw; g.e.n = (int)s.K;
-        if (s.M == 0) {  // the empty sum
-            const JoinArgs j{nullptr, 0, g.M, 0, 0, g.e};
-            return DenseOps<T>::join(j, sum, st) == hipSuccess ? DLC_OK : DLC_EHIP;
-        }
-        return run_gemm<T>(g, L_TT, false, s.es, wk + b.off_part, sum, st);
+    if (dx && dw && b.both) {
+        set_plan(&gx, b.bx, wk + b.off_part);
+        set_plan(&gw, b.bw, wk + b.off_part + a256(b.bx.bytes));
+        const bool cut = gx.split > 1 || gw.split > 1;
+        if (DenseOps<T>::back(gx, gw, cut ? SumArgs{} : sum, b.bx.tile, st) != hipSuccess) return DLC_EHIP;
+        return cut ? join(join_of(gx, false), join_of(gw, false)) : DLC_OK;
     }
-    if (dbias && !(dx && s.M > 0)) return DenseOps<T>::join(JoinArgs{}, sum, st) == hipSuccess ? DLC_OK : DLC_EHIP;
-    return DLC_OK;
+    if (dx)
+        if (const int rc = run_gemm<T>(gx, b.x, L_KT, false, wk + b.off_part, dw ? SumArgs{} : sum, st); rc != DLC_OK) return rc;
+    if (dw) return run_gemm<T>(gw, b.w, L_TT, false, wk + b.off_part, sum, st);
+    return dbias && !dx ? join(JoinArgs{}, JoinArgs{}) : DLC_OK;
 }
 
 // d is there if `need`, and lies on an element's boundary
 bool good_ptr(const void* d, int es, bool need) { return d ? on(d, es) : !need; }
 
-int check_work(const Shape& s, bool backward, const void* work, size_t* bytes) {
+// the workspace a forward call needs: the product's partial sums, packed operands (a pass over few rows takes them as they are)
+size_t forward_bytes(const Shape& s, const Plan& p) { return s.M <= kSkinnyOddRows ? 0 : a256(p.bytes) + pack_room(s); }
+
+Plan plan_forward(const Shape& s) { return s.M <= kSkinnyOddRows ? Plan{} : plan_gemm(s.M, s.N, s.K, s.gated, L_KK, s.es); }
+
+int check_work(size_t need, const void* work, size_t* bytes) {
     if (!on(work, 16)) return DLC_EINVAL;
-    const size_t need = work_bytes_of(s, backward);
     if (!work) *bytes = 0;
     return *bytes >= need ? DLC_OK : work ? DLC_ECAPACITY : DLC_EINVAL;
 }
@@ -300,12 +375,13 @@ int forward_any(const dlc_dense_config* c, bool gated, const void* x, const void
     if (!good_ptr(x, s.es, need) || !good_ptr(w, s.es, need) || !good_ptr(bias, s.es, false) || !good_ptr(res, s.es, false) ||
         !good_ptr(y, s.es, need) || !good_ptr(pre, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
     if (!need) return DLC_OK;
-    if (const int rc = check_work(s, false, work, &bytes); rc != DLC_OK) return rc;
+    const Plan p = plan_forward(s);
+    if (const int rc = check_work(forward_bytes(s, p), work, &bytes); rc != DLC_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
     switch (c->dtype) {
-        case DLC_F32: return forward<float>(c, s, x, w, bias, res, y, pre, work, bytes, st);
-        case DLC_F16: return forward<f16_t>(c, s, x, w, bias, res, y, pre, work, bytes, st);
-        default: return forward<bf16_t>(c, s, x, w, bias, res, y, pre, work, bytes, st);
+        case DLC_F32: return forward<float>(c, s, x, w, bias, res, y, pre, work, bytes, p, st);
+        case DLC_F16: return forward<f16_t>(c, s, x, w, bias, res, y, pre, work, bytes, p, st);
+        default: return forward<bf16_t>(c, s, x, w, bias, res, y, pre, work, bytes, p, st);
     }
 }
 
@@ -317,12 +393,13 @@ int backward_any(const dlc_dense_config* c, bool gated, const void* x, const voi
     if (!good_ptr(x, s.es, some && dw) || !good_ptr(w, s.es, some && dx) || !good_ptr(dy, s.es, some) ||
         !good_ptr(pre, s.es, some && (gated || c->act != DLC_ACT_NONE)) || !good_ptr(dx, s.es, false) || !good_ptr(dw, s.es, false) ||
         !good_ptr(dbias, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
-    if (const int rc = check_work(s, true, work, &bytes); rc != DLC_OK) return rc;
+    const BackPlan p = some ? plan_back(s) : BackPlan{};
+    if (const int rc = check_work(p.total, work, &bytes); rc != DLC_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
     switch (c->dtype) {
-        case DLC_F32: return backward<float>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, st);
-        case DLC_F16: return backward<f16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, st);
-        default: return backward<bf16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, st);
+        case DLC_F32: return backward<float>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, p, st);
+        case DLC_F16: return backward<f16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, p, st);
+        default: return backward<bf16_t>(c, s, x, w, pre, dy, dx, dw, dbias, work, bytes, p, st);
     }
 }
 
@@ -330,7 +407,8 @@ int backward_any(const dlc_dense_config* c, bool gated, const void* x, const voi
 
 static size_t workspace(const dlc_dense_config* cfg, bool gated, int backward) {
     Shape s;
-    return make_shape(cfg, gated, &s) ? work_bytes_of(s, backward != 0) : 0;
+    if (!make_shape(cfg, gated, &s) || s.M == 0) return 0;
+    return backward ? plan_back(s).total : forward_bytes(s, plan_forward(s));
 }
 extern "C" size_t dlc_linear_workspace_bytes(const dlc_dense_config* cfg, int backward) { return workspace(cfg, false, backward); }
 extern "C" size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg, int backward) { return workspace(cfg, true, backward); }

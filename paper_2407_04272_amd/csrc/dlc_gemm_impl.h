@@ -422,9 +422,15 @@ __device__ __forceinline__ void tile_of(int wg, int total, int tiles_m, int tile
     tn = t / h;
 }
 
+// LDS of a work-group: with k along the rows three slots for A and two for B, otherwise four for both
+template <typename T, int LAY, int BM, int BN>
+constexpr int gemm_lds() {
+    return LAY == L_KK ? 3 * BM * 128 + 2 * BN * 128 : 4 * (BM + BN) * 64;
+}
+
+// Tile `wg` of `total` of a product (the tiles of every cut of k)
 template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool GATED>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmArgs ga) {
-#if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass has no use for the body, and does not know its assembly)
+__device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total, char* const lds) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, MI = WM / 16, NJ = WN / 16;
     constexpr bool PAIRED = WAVES == 8;
@@ -437,13 +443,13 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
     using OpB = Operand<T, LAY != L_KK, BN, TB, THREADS, GATED>;
     static_assert(WN == 64, "a wavefront's columns (gated: 32 of the gate and 32 of the other)");
     constexpr int STAGE = OpA::BYTES + OpB::BYTES;
-    constexpr int A3 = 3 * OpA::BYTES;  // k along the rows: three slots for A, then two for B
-    constexpr int LDS = LAY == L_KK ? A3 + 2 * OpB::BYTES : 4 * STAGE;
-    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    constexpr int A3 = 3 * OpA::BYTES;  // k along the rows: where B's slots start
+    constexpr int LDS = gemm_lds<T, LAY, BM, BN>();
+    static_assert(LDS == (LAY == L_KK ? A3 + 2 * OpB::BYTES : 4 * STAGE), "slots");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int tm, tn, sp;
-    tile_of(blockIdx.x, gridDim.x, ga.tiles_m, ga.tiles_n, tm, tn, sp);
+    tile_of(wg, total, ga.tiles_m, ga.tiles_n, tm, tn, sp);
     const int m0 = tm * BM, n0 = tn * (GATED ? BN / 2 : BN);
     const int k0 = sp * ga.kper, k1 = min(ga.K, k0 + ga.kper);
     OpA oa;
@@ -638,8 +644,65 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
         }
         wave_sync();
     }
+}
+
+template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool GATED>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmArgs ga) {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass has no use for the body, and does not know its assembly)
+    __shared__ __attribute__((aligned(16))) char lds[gemm_lds<T, LAY, BM, BN>()];
+    gemm_tile<T, LAY, BM, BN, WAVES_M, WAVES_N, GATED>(ga, blockIdx.x, gridDim.x, lds);
 #endif
 }
+
+// sum_cols columns' row blocks' sums of the bias gradient added up in a fixed order, by 256 threads with all loads in flight
+constexpr int kSumCols = 16;
+
+template <typename T>
+__device__ __forceinline__ void sum_columns(const SumArgs& sa, int wg, float (*red)[17]) {
+    const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
+    const int c = wg * kSumCols + cx;
+    float s = 0.f;
+    if (c < sa.n) {
+        const float* const p = sa.sums + c;
+        for (int i = ry; i < sa.row_blocks; i += 256) {
+            float v[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) v[u] = i + 16 * u < sa.row_blocks ? p[(int64_t)(i + 16 * u) * sa.sums_ld] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 16; ++u) s += v[u];
+        }
+    }
+    red[ry][cx] = s;
+    __syncthreads();
+    if (ry == 0 && c < sa.n) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) t += red[w][cx];
+        static_cast<T*>(sa.out)[c] = (T)t;
+    }
+}
+
+// Both products of a backward call in one launch, and the bias gradient if nothing comes behind: small products leave most
+// compute units idle one by one.  The work-groups of each start at a multiple of 8, so that tile_of's XCDs are the real ones.
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__(256, 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ __attribute__((aligned(16))) char lds[gemm_lds<T, L_TT, BM, BN>()];
+    const int nw8 = (nw + 7) & ~7, nx8 = (nx + 7) & ~7;
+    int b = blockIdx.x;
+    if (b < nw8) {
+        if (b < nw) gemm_tile<T, L_TT, BM, BN, 2, 2, false>(gw, b, nw, lds);
+        return;
+    }
+    b -= nw8;
+    if (b < nx8) {
+        if (b < nx) gemm_tile<T, L_KT, BM, BN, 2, 2, false>(gx, b, nx, lds);
+        return;
+    }
+    sum_columns<T>(sa, b - nx8, reinterpret_cast<float(*)[17]>(lds));
+#endif
+}
+
 
 // The wavefronts' sums of 16 x 16 elements (gated: of both halves) added up in order, and the epilogue
 constexpr int kSkinnyWaves = 8;
@@ -795,40 +858,10 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_skinny_odd(const GemmArgs
     skinny_end<T, GATED>(ga, 0, n0, sums, tid);
 }
 
-constexpr int kSumCols = 16;
-
-// The last launch of a call.  The first sum_wgs work-groups add up the row blocks' sums of the bias gradient, 16 columns
-// each, all loads in flight at once; the others add up the partial sums of a product whose k was cut, in the order of the cuts, and do
-// its epilogue.  Every sum has a fixed order.
+// eight columns of a product whose k was cut: the partial sums added up in the order of the cuts, and the epilogue
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const SumArgs sa, int sum_wgs) {
-    if ((int)blockIdx.x < sum_wgs) {
-        __shared__ float red[16][17];
-        const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
-        const int c = blockIdx.x * kSumCols + cx;
-        float s = 0.f;
-        if (c < sa.n) {
-            const float* const p = sa.sums + c;
-            for (int i = ry; i < sa.row_blocks; i += 256) {
-                float v[16];
-#pragma unroll
-                for (int u = 0; u < 16; ++u) v[u] = i + 16 * u < sa.row_blocks ? p[(int64_t)(i + 16 * u) * sa.sums_ld] : 0.f;
-#pragma unroll
-                for (int u = 0; u < 16; ++u) s += v[u];
-            }
-        }
-        red[ry][cx] = s;
-        __syncthreads();
-        if (ry == 0 && c < sa.n) {
-            float t = 0.f;
-#pragma unroll
-            for (int w = 0; w < 16; ++w) t += red[w][cx];
-            static_cast<T*>(sa.out)[c] = (T)t;
-        }
-        return;
-    }
+__device__ __forceinline__ void join_chunk(const JoinArgs& ja, int64_t idx) {
     const int chunks = (ja.e.n + 7) / 8;
-    const int64_t idx = (int64_t)((int)blockIdx.x - sum_wgs) * 256 + threadIdx.x;
     if (idx >= (int64_t)chunks * ja.M) return;
     const int m = (int)(idx / chunks), col = (int)(idx % chunks) * 8;
     float s[8] = {}, u[8] = {};
@@ -850,6 +883,17 @@ __global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const SumArgs s
         }
     }
     epilogue8<T, GATED>(ja.e, full_offset(ja.e.offset, ja.e.d_offset), m, col, s, u);
+}
+
+// The last launch of a call: the bias gradient, then the partial sums of up to two products
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const JoinArgs jb, const SumArgs sa, int sum_wgs, int ja_wgs) {
+    __shared__ float red[16][17];
+    int b = blockIdx.x;
+    if (b < sum_wgs) return sum_columns<T>(sa, b, red);
+    b -= sum_wgs;
+    if (b < ja_wgs) return join_chunk<T, GATED>(ja, (int64_t)b * 256 + threadIdx.x);
+    if constexpr (!GATED) join_chunk<T, false>(jb, (int64_t)(b - ja_wgs) * 256 + threadIdx.x);
 }
 
 // Rows that do not start on 16-byte boundaries, or end inside a chunk, copied to rows that do, zeros behind their ends: the
@@ -992,7 +1036,7 @@ static hipError_t gemm_go(const GemmArgs& g, hipStream_t s) {
 }
 
 template <typename T, int LAY, bool GT>
-static hipError_t gemm_tile(const GemmArgs& g, int tile, hipStream_t s) {
+static hipError_t gemm_pick(const GemmArgs& g, int tile, hipStream_t s) {
     if (tile == 0) return gemm_go<T, LAY, 256, 256, 2, 4, GT>(g, s);
     if (tile == 1) return gemm_go<T, LAY, 128, 128, 2, 2, GT>(g, s);
     return gemm_go<T, LAY, 64, 128, 2, 2, GT>(g, s);
@@ -1000,10 +1044,10 @@ static hipError_t gemm_tile(const GemmArgs& g, int tile, hipStream_t s) {
 
 template <typename T>
 hipError_t DenseOps<T>::gemm(const GemmArgs& g, Layout lay, bool gated, int tile, hipStream_t s) {
-    if (gated) return gemm_tile<T, L_KK, true>(g, tile, s);
-    if (lay == L_KK) return gemm_tile<T, L_KK, false>(g, tile, s);
-    if (lay == L_KT) return gemm_tile<T, L_KT, false>(g, tile, s);
-    return gemm_tile<T, L_TT, false>(g, tile, s);
+    if (gated) return gemm_pick<T, L_KK, true>(g, tile, s);
+    if (lay == L_KK) return gemm_pick<T, L_KK, false>(g, tile, s);
+    if (lay == L_KT) return gemm_pick<T, L_KT, false>(g, tile, s);
+    return gemm_pick<T, L_TT, false>(g, tile, s);
 }
 
 template <typename T, bool GT>
@@ -1022,12 +1066,21 @@ hipError_t DenseOps<T>::skinny(const GemmArgs& g, bool gated, bool aligned, hipS
 }
 
 template <typename T>
-hipError_t DenseOps<T>::join(const JoinArgs& j, const SumArgs& a, hipStream_t s) {
-    const int64_t n = (int64_t)((j.e.n + 7) / 8) * j.M;
+hipError_t DenseOps<T>::back(const GemmArgs& gx, const GemmArgs& gw, const SumArgs& a, int tile, hipStream_t s) {
+    const int nx = gx.tiles_m * gx.tiles_n * gx.split, nw = gw.tiles_m * gw.tiles_n * gw.split;
+    const dim3 grid((unsigned)(((nx + 7) & ~7) + ((nw + 7) & ~7) + (a.n + kSumCols - 1) / kSumCols));
+    if (tile == 1) k_back<T, 128, 128><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    else k_back<T, 64, 128><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t DenseOps<T>::join(const JoinArgs& ja, const JoinArgs& jb, const SumArgs& a, hipStream_t s) {
+    const auto wgs = [](const JoinArgs& j) { return ((int64_t)((j.e.n + 7) / 8) * j.M + 255) / 256; };
     const int sum_wgs = (a.n + kSumCols - 1) / kSumCols;
-    const dim3 grid((unsigned)((n + 255) / 256 + sum_wgs));
-    if (j.gated) k_join<T, true><<<grid, dim3(256), 0, s>>>(j, a, sum_wgs);
-    else k_join<T, false><<<grid, dim3(256), 0, s>>>(j, a, sum_wgs);
+    const dim3 grid((unsigned)(sum_wgs + wgs(ja) + wgs(jb)));
+    if (ja.gated) k_join<T, true><<<grid, dim3(256), 0, s>>>(ja, jb, a, sum_wgs, (int)wgs(ja));
+    else k_join<T, false><<<grid, dim3(256), 0, s>>>(ja, jb, a, sum_wgs, (int)wgs(ja));
     return hipGetLastError();
 }
 
