@@ -67,17 +67,17 @@ struct Plan {
     double t;      // the estimate, us
 };
 
-// What a k tile (128 bytes of k) costs with 1, 2 and 3 work-groups on a compute unit, in us, and what a work-group costs
-// besides, measured with all three layouts on full and half full cards (0: no third work-group fits).  256 x 256 is the
+// What a k tile (128 bytes of k) costs with 1, 2 and 3 work-groups on a compute unit, in us, what a work-group costs
+// besides, and what it costs more to write partial sums, measured with all three layouts on full and half full cards (0: no third work-group fits).  256 x 256 is the
 // fastest per product in half precision (1560 TFLOP/s against 1280 and 850 of the other two, all compute units busy) and has
 // the longest start and end; in fp32 all three reach the matrix cores' rate and the small ones leave fewer units idle.
-struct TileCost { double tile[3], first, further; };
-constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0}, {{0.57, 0.88, 0}, 6.0, 3.0}, {{0.45, 0.64, 1.0}, 4.0, 3.0}};
-constexpr TileCost kF32Cost[3] = {{{7.6, 0, 0}, 14.0, 10.0}, {{2.2, 3.8, 0}, 8.0, 4.0}, {{1.3, 2.0, 2.9}, 5.0, 3.0}};
+struct TileCost { double tile[3], first, further, part; };
+constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0, 5.0}, {{0.57, 0.88, 0}, 6.0, 3.0, 0}, {{0.45, 0.64, 1.0}, 4.0, 3.0, 0}};
+constexpr TileCost kF32Cost[3] = {{{7.6, 0, 0}, 14.0, 10.0, 5.0}, {{2.2, 3.8, 0}, 8.0, 4.0, 0}, {{1.3, 2.0, 2.9}, 5.0, 3.0, 0}};
 constexpr int kUnits = 256;  // compute units
 
 // cuts of k that are looked at
-constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512};
 
 // a product: M x wide of the result, K the sum's length in k tiles
 struct Product {
@@ -115,7 +115,7 @@ Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) 
             const int64_t wgs = tiles * split, full = wgs / (kUnits * fit), rest = wgs % (kUnits * fit);
             double t = (double)full * ((double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
             if (rest) t += (double)per * c.tile[(rest - 1) / kUnits] + c.further;
-            if (split > 1) t += 4.0 + join_cost(p, split);
+            if (split > 1) t += 4.0 + c.part + join_cost(p, split);
             if (t < best.t) {
                 best.t = t;
                 set_cut(&best, p, tile, split, per, part_ld, bk);
@@ -147,9 +147,9 @@ bool plan_pair(const Product& px, const Product& pw, int64_t part_ld, int es, Pl
     const TileCost* const cost = es == 4 ? kF32Cost : kHalfCost;
     double best = x->t + w->t;
     bool found = false;
-    for (int tile = 1; tile < 3; ++tile) {
+    for (int tile = es == 4 ? 1 : 0; tile < 3; ++tile) {  // (256 x 256 does not pay in fp32)
         const TileCost& c = cost[tile];
-        const int fit = tile == 1 ? 2 : 3;
+        const int fit = tile + 1;
         const int64_t tx = div_up(px.M, kTileM[tile]) * div_up(px.wide, kTileN[tile]);
         const int64_t tw = div_up(pw.M, kTileM[tile]) * div_up(pw.wide, kTileN[tile]);
         for (const int most : kCuts) {
@@ -160,7 +160,8 @@ bool plan_pair(const Product& px, const Product& pw, int64_t part_ld, int es, Pl
             const int64_t res = div_up(wgs, kUnits) < fit ? div_up(wgs, kUnits) : fit;
             // dW's work-groups come first, dX's fill the places as they fall free
             const double per_tile = c.tile[res - 1];
-            double t = makespan(kUnits * res, tw * sw, (double)lw * per_tile + c.further, tx * sx, (double)lx * per_tile + c.further);
+            double t = makespan(kUnits * res, tw * sw, (double)lw * per_tile + c.further + (sw > 1 ? c.part : 0.0),
+                                tx * sx, (double)lx * per_tile + c.further + (sx > 1 ? c.part : 0.0));
             t += c.first - c.further;
             if (sx > 1 || sw > 1) t += 4.0 + join_cost(px, sx) + join_cost(pw, sw);
             if (t < best) {

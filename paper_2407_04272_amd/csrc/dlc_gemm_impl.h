@@ -654,20 +654,21 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmAr
 #endif
 }
 
-// sum_cols columns' row blocks' sums of the bias gradient added up in a fixed order, by 256 threads with all loads in flight
+// kSumCols columns of the bias gradient from the row blocks' sums, added up in a fixed order by 16 x LANES threads with all
+// loads in flight
 constexpr int kSumCols = 16;
 
-template <typename T>
+template <typename T, int LANES>
 __device__ __forceinline__ void sum_columns(const SumArgs& sa, int wg, float (*red)[17]) {
     const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
     const int c = wg * kSumCols + cx;
     float s = 0.f;
     if (c < sa.n) {
         const float* const p = sa.sums + c;
-        for (int i = ry; i < sa.row_blocks; i += 256) {
+        for (int i = ry; i < sa.row_blocks; i += 16 * LANES) {
             float v[16];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) v[u] = i + 16 * u < sa.row_blocks ? p[(int64_t)(i + 16 * u) * sa.sums_ld] : 0.f;
+            for (int u = 0; u < 16; ++u) v[u] = i + LANES * u < sa.row_blocks ? p[(int64_t)(i + LANES * u) * sa.sums_ld] : 0.f;
 #pragma unroll
             for (int u = 0; u < 16; ++u) s += v[u];
         }
@@ -677,29 +678,29 @@ __device__ __forceinline__ void sum_columns(const SumArgs& sa, int wg, float (*r
     if (ry == 0 && c < sa.n) {
         float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) t += red[w][cx];
+        for (int w = 0; w < LANES; ++w) t += red[w][cx];
         static_cast<T*>(sa.out)[c] = (T)t;
     }
 }
 
 // Both products of a backward call in one launch, and the bias gradient if nothing comes behind: small products leave most
 // compute units idle one by one.  The work-groups of each start at a multiple of 8, so that tile_of's XCDs are the real ones.
-template <typename T, int BM, int BN>
-__global__ __launch_bounds__(256, 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
+template <typename T, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ __attribute__((aligned(16))) char lds[gemm_lds<T, L_TT, BM, BN>()];
     const int nw8 = (nw + 7) & ~7, nx8 = (nx + 7) & ~7;
     int b = blockIdx.x;
     if (b < nw8) {
-        if (b < nw) gemm_tile<T, L_TT, BM, BN, 2, 2, false>(gw, b, nw, lds);
+        if (b < nw) gemm_tile<T, L_TT, BM, BN, WAVES_M, WAVES_N, false>(gw, b, nw, lds);
         return;
     }
     b -= nw8;
     if (b < nx8) {
-        if (b < nx) gemm_tile<T, L_KT, BM, BN, 2, 2, false>(gx, b, nx, lds);
+        if (b < nx) gemm_tile<T, L_KT, BM, BN, WAVES_M, WAVES_N, false>(gx, b, nx, lds);
         return;
     }
-    sum_columns<T>(sa, b - nx8, reinterpret_cast<float(*)[17]>(lds));
+    sum_columns<T, 4 * WAVES_M * WAVES_N>(sa, b - nx8, reinterpret_cast<float(*)[17]>(lds));
 #endif
 }
 
@@ -890,7 +891,7 @@ template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const JoinArgs jb, const SumArgs sa, int sum_wgs, int ja_wgs) {
     __shared__ float red[16][17];
     int b = blockIdx.x;
-    if (b < sum_wgs) return sum_columns<T>(sa, b, red);
+    if (b < sum_wgs) return sum_columns<T, 16>(sa, b, red);
     b -= sum_wgs;
     if (b < ja_wgs) return join_chunk<T, GATED>(ja, (int64_t)b * 256 + threadIdx.x);
     if constexpr (!GATED) join_chunk<T, false>(jb, (int64_t)(b - ja_wgs) * 256 + threadIdx.x);
@@ -1069,8 +1070,9 @@ template <typename T>
 hipError_t DenseOps<T>::back(const GemmArgs& gx, const GemmArgs& gw, const SumArgs& a, int tile, hipStream_t s) {
     const int nx = gx.tiles_m * gx.tiles_n * gx.split, nw = gw.tiles_m * gw.tiles_n * gw.split;
     const dim3 grid((unsigned)(((nx + 7) & ~7) + ((nw + 7) & ~7) + (a.n + kSumCols - 1) / kSumCols));
-    if (tile == 1) k_back<T, 128, 128><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
-    else k_back<T, 64, 128><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    if (tile == 1) k_back<T, 128, 128, 2, 2><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    else if (tile == 2) k_back<T, 64, 128, 2, 2><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    else if constexpr (sizeof(T) == 2) k_back<T, 256, 256, 2, 4><<<grid, dim3(512), 0, s>>>(gx, gw, a, nx, nw);
     return hipGetLastError();
 }
 

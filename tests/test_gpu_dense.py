@@ -176,6 +176,19 @@ def test_gated_backward(dtype, shape):
         _backward("gated", dtype, *shape, ACTS[(i + 2) % 5], p=0.3 if i % 2 else 0.0, how=how)
 
 
+# both products in one launch on the largest tiles: nothing cut and the bias gradient in the same launch, the gradient of w
+# cut; one launch after the other, the gradient of x cut
+BACKWARD_LARGE = [("linear", (8200, 4100, 2056), "odd"), ("linear", (8192, 2048, 2048), "dense"), ("linear", (300, 4000, 2000), "pitch"),
+                  ("gated", (1000, 2000, 4000), "dense"), ("gated", (2100, 700, 600), "odd")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("op,shape,how", BACKWARD_LARGE)
+def test_large_backward(dtype, op, shape, how):
+    _backward(op, dtype, *shape, "relu" if op == "linear" else "silu", p=0.0, how=how)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("op", ["linear", "gated"])
