@@ -187,25 +187,19 @@ __device__ __forceinline__ float normal_cdf(float z, float* phi) {
     }
 }
 
-template <bool FAST>
-__device__ __forceinline__ void act_values(int act, float z[8]) {
+template <bool FAST, int U>
+__device__ __forceinline__ void act_values(int act, float (&z)[U][8]) {
+    const auto each = [&](auto f) {
+#pragma unroll
+        for (int r = 0; r < U; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[r][i] = f(z[r][i]);
+    };
     switch (act) {
-        case DLC_ACT_RELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];  // (NaN stays NaN)
-            break;
-        case DLC_ACT_SIGMOID:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = sigmoidf<FAST>(z[i]);
-            break;
-        case DLC_ACT_SILU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= sigmoidf<FAST>(z[i]);
-            break;
-        case DLC_ACT_GELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= normal_cdf<FAST>(z[i], nullptr);
-            break;
+        case DLC_ACT_RELU: return each([](float v) { return v < 0.0f ? 0.0f : v; });  // (NaN stays NaN)
+        case DLC_ACT_SIGMOID: return each([](float v) { return sigmoidf<FAST>(v); });
+        case DLC_ACT_SILU: return each([](float v) { return v * sigmoidf<FAST>(v); });
+        case DLC_ACT_GELU: return each([](float v) { return v * normal_cdf<FAST>(v, nullptr); });
         default: break;
     }
 }
@@ -299,46 +293,62 @@ __device__ __forceinline__ uint64_t full_offset(uint64_t offset, const uint64_t*
     return d_offset ? offset + *d_offset : offset;
 }
 
-// Epilogue of eight columns col .. col+7 (col a multiple of 8) of row m: s the sums; gated: s the gate's, u the other's.
-// Everything is fp32 up to the one rounding at the store.
-template <typename T, bool GATED>
-__device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t m, int col, float s[8], float u[8]) {
+// Epilogue of eight columns col .. col+7 (col a multiple of 8) of the rows m, m + STEP, ..., of which those below m + rows
+// exist: s the sums; gated: s the gate's, u the other's.  Everything is fp32 up to the one rounding at the store.
+template <typename T, bool GATED, int U, int STEP>
+__device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t m, int rows, int col, float (&s)[U][8], float (&u)[U][8]) {
     const int cnt = e.n - col;
     if (cnt <= 0) return;
     if (e.bias) {
         const T* bias = static_cast<const T*>(e.bias);
-        float b[8];
+        float b[8], c[8];
         load8(bias + col, cnt, b);
+        if constexpr (GATED) load8(bias + e.n + col, cnt, c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += b[i];
-        if constexpr (GATED) {
-            load8(bias + e.n + col, cnt, b);
+        for (int r = 0; r < U; ++r)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) u[i] += b[i];
-        }
+            for (int i = 0; i < 8; ++i) {
+                s[r][i] += b[i];
+                if constexpr (GATED) u[r][i] += c[i];
+            }
     }
     if (e.pre) {
-        T* p = static_cast<T*>(e.pre) + m * e.ld_pre;
-        store8(p + col, cnt, s);
-        if constexpr (GATED) store8(p + e.n + col, cnt, u);
+#pragma unroll
+        for (int r = 0; r < U; ++r) {
+            if (r * STEP >= rows) continue;
+            T* p = static_cast<T*>(e.pre) + (m + r * STEP) * e.ld_pre;
+            store8(p + col, cnt, s[r]);
+            if constexpr (GATED) store8(p + e.n + col, cnt, u[r]);
+        }
     }
     act_values<sizeof(T) == 2>(e.act, s);
     if constexpr (GATED) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] *= u[i];
+        for (int r = 0; r < U; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[r][i] *= u[r][i];
     }
     if (e.thr) {
-        const uint32_t keep = keep_mask((uint32_t)col >> 3, (uint32_t)m, e.seed, offset, e.thr);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = (keep >> i) & 1u ? s[i] * e.scale : 0.0f;
+        for (int r = 0; r < U; ++r) {
+            const uint32_t keep = keep_mask((uint32_t)col >> 3, (uint32_t)(m + r * STEP), e.seed, offset, e.thr);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[r][i] = (keep >> i) & 1u ? s[r][i] * e.scale : 0.0f;
+        }
     }
     if (e.res) {
-        float r[8];
-        load8(static_cast<const T*>(e.res) + m * e.ld_res + col, cnt, r);
+        float x[U][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += r[i];
+        for (int r = 0; r < U; ++r)
+            if (r * STEP < rows) load8(static_cast<const T*>(e.res) + (m + r * STEP) * e.ld_res + col, cnt, x[r]);
+#pragma unroll
+        for (int r = 0; r < U; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[r][i] += x[r][i];
     }
-    store8(static_cast<T*>(e.y) + m * e.ld_y + col, cnt, s);
+#pragma unroll
+    for (int r = 0; r < U; ++r)
+        if (r * STEP < rows) store8(static_cast<T*>(e.y) + (m + r * STEP) * e.ld_y + col, cnt, s[r]);
 }
 
 #endif  // __HIPCC__

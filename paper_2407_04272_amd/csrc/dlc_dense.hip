@@ -68,12 +68,13 @@ struct Plan {
 };
 
 // What a k tile (128 bytes of k) costs with 1, 2 and 3 work-groups on a compute unit, in us, what a work-group costs
-// besides, and what it costs more to write partial sums, measured with all three layouts on full and half full cards (0: no third work-group fits).  256 x 256 is the
-// fastest per product in half precision (1560 TFLOP/s against 1280 and 850 of the other two, all compute units busy) and has
-// the longest start and end; in fp32 all three reach the matrix cores' rate and the small ones leave fewer units idle.
+// besides, and what it costs more to write partial sums, measured with all three layouts on full and half full cards (0: no
+// further work-group fits).  256 x 256 is the fastest per product in half precision (1500 TFLOP/s against 1280 and 850 of
+// the other two, all compute units busy) and has the longest start and end; in fp32 the small tiles reach the matrix cores'
+// rate and leave fewer units idle: there is no large one.
 struct TileCost { double tile[3], first, further, part; };
 constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0, 5.0}, {{0.57, 0.88, 0}, 6.0, 3.0, 0}, {{0.45, 0.64, 1.0}, 4.0, 3.0, 0}};
-constexpr TileCost kF32Cost[3] = {{{7.6, 0, 0}, 14.0, 10.0, 5.0}, {{2.2, 3.8, 0}, 8.0, 4.0, 0}, {{1.3, 2.0, 2.9}, 5.0, 3.0, 0}};
+constexpr TileCost kF32Cost[3] = {{}, {{2.2, 3.8, 0}, 8.0, 4.0, 0}, {{1.3, 2.0, 2.9}, 5.0, 3.0, 0}};
 constexpr int kUnits = 256;  // compute units
 
 // cuts of k that are looked at
@@ -105,7 +106,7 @@ Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) 
     const TileCost* const cost = es == 4 ? kF32Cost : kHalfCost;
     Plan best{};
     best.t = 1e300;
-    for (int tile = 0; tile < 3; ++tile) {
+    for (int tile = es == 4 ? 1 : 0; tile < 3; ++tile) {
         const TileCost& c = cost[tile];
         const int64_t tiles = div_up(p.M, kTileM[tile]) * div_up(p.wide, kTileN[tile]);
         const int fit = tile == 0 ? 1 : tile == 1 || lay == L_KK ? 2 : 3;  // work-groups that share a compute unit
@@ -147,7 +148,7 @@ bool plan_pair(const Product& px, const Product& pw, int64_t part_ld, int es, Pl
     const TileCost* const cost = es == 4 ? kF32Cost : kHalfCost;
     double best = x->t + w->t;
     bool found = false;
-    for (int tile = es == 4 ? 1 : 0; tile < 3; ++tile) {  // (256 x 256 does not pay in fp32)
+    for (int tile = es == 4 ? 1 : 0; tile < 3; ++tile) {
         const TileCost& c = cost[tile];
         const int fit = tile + 1;
         const int64_t tx = div_up(px.M, kTileM[tile]) * div_up(px.wide, kTileN[tile]);

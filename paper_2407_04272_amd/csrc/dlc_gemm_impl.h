@@ -4,9 +4,13 @@
 // tiles of A and B go from memory to a ring of slots in LDS, several tiles ahead, without passing through registers; a
 // wavefront holds a part of C in registers as 16 x 16 blocks and takes its fragments of a tile from LDS.
 //
-// 256 x 256, eight wavefronts: two groups of four, one of each on every SIMD, work half a phase apart; while one reads its
-// fragments and starts loads, the other multiplies (see the loops).  128 x 128 and 64 x 128, four wavefronts: two or three
-// work-groups share a compute unit and fill each other's gaps.
+// 256 x 256 (half precision): four wavefronts, one on each SIMD, with 128 x 128 each (gemm_wide).  A byte read from LDS is
+// used for twice the products of a 64 x 64 part, which leaves LDS idle four fifths of the time and the clock higher than
+// eight wavefronts of 128 x 64 in two alternating groups did (the card is bound by power, 1.9 to 2.0 GHz here, with the
+// matrix cores busy 75 % of the time).  bf16, without an epilogue, k along both rows, down one's and down both's columns:
+// 8192 x 2048 x 8192 184, 186 and 187 us = 1495, 1478 and 1465 TFLOP/s (eight wavefronts: 193, 204 and 206; a library 171 to
+// 185), 16384 x 8192 x 2048 400, 405 and 408 (421, 439 and 446).
+// 128 x 128 and 64 x 128, four wavefronts: two or three work-groups share a compute unit and fill each other's gaps.
 //
 // LDS layouts (16-byte chunks):
 //   k along a row     rows of TB bytes of k, chunk c of row r at place c ^ (r >> 1): what the 16 lanes of a quarter of a
@@ -110,7 +114,8 @@ __device__ __forceinline__ void read_rows(u32x4_t* o, uint32_t a) {
 // ... of both operands
 template <int NA, int NB, int PITCH, int OFF>
 __device__ __forceinline__ void read_rows2(u32x4_t* x, uint32_t a, u32x4_t* y, uint32_t b) {
-    if constexpr (NA == 2 && NB == 4) {
+    static_assert((NA == 2 || NA == 4) && NB == 4, "");
+    if constexpr (NA == 2) {
         asm volatile(
             "ds_read_b128 %2, %7 offset:%8\n\t"
             "ds_read_b128 %3, %7 offset:%9\n\t"
@@ -121,7 +126,7 @@ __device__ __forceinline__ void read_rows2(u32x4_t* x, uint32_t a, u32x4_t* y, u
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(x[0]), "=&v"(x[1]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
             : "v"(a), "v"(b), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH) : "memory");
-    } else if constexpr (NA == 4 && NB == 4) {
+    } else {
         asm volatile(
             "ds_read_b128 %4, %9 offset:%10\n\t"
             "ds_read_b128 %5, %9 offset:%11\n\t"
@@ -134,23 +139,6 @@ __device__ __forceinline__ void read_rows2(u32x4_t* x, uint32_t a, u32x4_t* y, u
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
             : "v"(a), "v"(b), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH) : "memory");
-    } else if constexpr (NA == 8 && NB == 4) {
-        asm volatile(
-            "ds_read_b128 %8, %13 offset:%14\n\t"
-            "ds_read_b128 %9, %13 offset:%15\n\t"
-            "ds_read_b128 %10, %13 offset:%16\n\t"
-            "ds_read_b128 %11, %13 offset:%17\n\t"
-            "ds_read_b128 %0, %12 offset:%14\n\t"
-            "ds_read_b128 %1, %12 offset:%15\n\t"
-            "ds_read_b128 %2, %12 offset:%16\n\t"
-            "ds_read_b128 %3, %12 offset:%17\n\t"
-            "ds_read_b128 %4, %12 offset:%18\n\t"
-            "ds_read_b128 %5, %12 offset:%19\n\t"
-            "ds_read_b128 %6, %12 offset:%20\n\t"
-            "ds_read_b128 %7, %12 offset:%21\n\t"
-            "s_waitcnt lgkmcnt(0)"
-            : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
-            : "v"(a), "v"(b), "i"(OFF + 0 * PITCH), "i"(OFF + 1 * PITCH), "i"(OFF + 2 * PITCH), "i"(OFF + 3 * PITCH), "i"(OFF + 4 * PITCH), "i"(OFF + 5 * PITCH), "i"(OFF + 6 * PITCH), "i"(OFF + 7 * PITCH) : "memory");
     }
 }
 
@@ -253,6 +241,91 @@ __device__ __forceinline__ void read_cols_f32(u32x4_t& o, uint32_t a) {
     o = u32x4_t{v0, v1, v2, v3};
 }
 
+// ---- the inner loop of the 256 x 256 tile ----
+// 16 products of 16 x 16 x 32, while four fragments of the next step are read from LDS and two loads to LDS are started.  It
+// is one block of assembly because a wavefront has its SIMD to itself: whatever else it issues has to stand between the
+// products, or the matrix cores wait.  The block waits for its own reads; the loads write no register.  The sums are kept
+// in the second half of the register file ("a"), which leaves the first to two steps' fragments.
+struct LoadTo {
+    uint32_t v0, v1;  // offsets
+    u32x4_t s0, s1;   // sources
+    uint32_t at;      // where in LDS the wavefront's first load of the tile goes
+};
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is the compiler's to set before each use: none lives across)
+#define DLC_MFMA(TY, ACC, B, A) "v_mfma_f32_16x16x32_" TY " %" #ACC ", %" #B ", %" #A ", %" #ACC "\n\t"
+#define DLC_CHUNK_ROWS(TY) \
+    asm volatile( \
+    DLC_MFMA(TY, 4, 22, 20) "ds_read_b128 %0, %30 offset:%31\n\t" DLC_MFMA(TY, 5, 23, 20) \
+    "ds_read_b128 %1, %30 offset:%32\n\t" DLC_MFMA(TY, 6, 24, 20) "ds_read_b128 %2, %30 offset:%33\n\t" \
+    DLC_MFMA(TY, 7, 25, 20) "ds_read_b128 %3, %30 offset:%34\n\t" DLC_MFMA(TY, 8, 26, 20) DLC_MFMA(TY, 9, 27, 20) \
+    "s_add_u32 m0, %39, %40\n\t" DLC_MFMA(TY, 10, 28, 20) "buffer_load_dwordx4 %35, %37, 0 offen lds\n\t" \
+    DLC_MFMA(TY, 11, 29, 20) DLC_MFMA(TY, 12, 22, 21) DLC_MFMA(TY, 13, 23, 21) DLC_MFMA(TY, 14, 24, 21) \
+    "s_add_u32 m0, %39, %41\n\t" DLC_MFMA(TY, 15, 25, 21) "buffer_load_dwordx4 %36, %38, 0 offen lds\n\t" \
+    DLC_MFMA(TY, 16, 26, 21) DLC_MFMA(TY, 17, 27, 21) DLC_MFMA(TY, 18, 28, 21) DLC_MFMA(TY, 19, 29, 21) \
+    "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(next[0]), "=&v"(next[1]), "=&v"(next[2]), "=&v"(next[3]), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc0[4]), "+a"(acc0[5]), "+a"(acc0[6]), "+a"(acc0[7]), \
+      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]), "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), \
+      "v"(from[0]), "i"(OFF), "i"(OFF + STEP), "i"(OFF + 2 * STEP), "i"(OFF + 3 * STEP), \
+      "v"(to.v0), "v"(to.v1), "s"(to.s0), "s"(to.s1), "s"(to.at), "i"(I * 8192), "i"(I * 8192 + 4096) \
+    : "memory", "m0", "scc")
+#define DLC_CHUNK_COLS(TY) \
+    asm volatile( \
+    DLC_MFMA(TY, 8, 26, 24) "ds_read_b64_tr_b16 %0, %34 offset:%38\n\t" DLC_MFMA(TY, 9, 27, 24) \
+    "ds_read_b64_tr_b16 %1, %34 offset:%39\n\t" DLC_MFMA(TY, 10, 28, 24) "ds_read_b64_tr_b16 %2, %35 offset:%38\n\t" \
+    DLC_MFMA(TY, 11, 29, 24) "ds_read_b64_tr_b16 %3, %35 offset:%39\n\t" DLC_MFMA(TY, 12, 30, 24) \
+    "ds_read_b64_tr_b16 %4, %36 offset:%38\n\t" DLC_MFMA(TY, 13, 31, 24) "ds_read_b64_tr_b16 %5, %36 offset:%39\n\t" \
+    DLC_MFMA(TY, 14, 32, 24) "ds_read_b64_tr_b16 %6, %37 offset:%38\n\t" DLC_MFMA(TY, 15, 33, 24) \
+    "ds_read_b64_tr_b16 %7, %37 offset:%39\n\t" DLC_MFMA(TY, 16, 26, 25) "s_add_u32 m0, %44, %45\n\t" \
+    DLC_MFMA(TY, 17, 27, 25) "buffer_load_dwordx4 %40, %42, 0 offen lds\n\t" DLC_MFMA(TY, 18, 28, 25) \
+    DLC_MFMA(TY, 19, 29, 25) "s_add_u32 m0, %44, %46\n\t" DLC_MFMA(TY, 20, 30, 25) \
+    "buffer_load_dwordx4 %41, %43, 0 offen lds\n\t" DLC_MFMA(TY, 21, 31, 25) DLC_MFMA(TY, 22, 32, 25) \
+    DLC_MFMA(TY, 23, 33, 25) "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(h0), "=&v"(h1), "=&v"(h2), "=&v"(h3), "=&v"(h4), "=&v"(h5), "=&v"(h6), "=&v"(h7), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc0[4]), "+a"(acc0[5]), "+a"(acc0[6]), "+a"(acc0[7]), \
+      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]), "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), \
+      "v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]), "i"(OFF), "i"(OFF + STEP), \
+      "v"(to.v0), "v"(to.v1), "s"(to.s0), "s"(to.s1), "s"(to.at), "i"(I * 8192), "i"(I * 8192 + 4096) \
+    : "memory", "m0", "scc")
+
+// acc0, acc1: rows of blocks, a0 and a1 times b.  COLS: the fragments read have k down a column (from: four addresses, STEP
+// to the second half), else along a row (from: one, STEP from block to block).  I: the loads are numbers 2 I and 2 I + 1.
+template <typename T, bool COLS, int OFF, int STEP, int I>
+__device__ __forceinline__ void chunk16(f32x4* acc0, f32x4* acc1, const u32x4_t& a0, const u32x4_t& a1, const u32x4_t* b, u32x4_t* next,
+                                        const uint32_t* from, const LoadTo& to) {
+    constexpr bool F16 = std::is_same<T, f16_t>::value;
+    if constexpr (!COLS) {
+        if constexpr (F16) DLC_CHUNK_ROWS("f16");
+        else DLC_CHUNK_ROWS("bf16");
+    } else {
+        s16x4 h0, h1, h2, h3, h4, h5, h6, h7;
+        if constexpr (F16) DLC_CHUNK_COLS("f16");
+        else DLC_CHUNK_COLS("bf16");
+        next[0] = join_halves(h0, h1);
+        next[1] = join_halves(h2, h3);
+        next[2] = join_halves(h4, h5);
+        next[3] = join_halves(h6, h7);
+    }
+}
+#undef DLC_CHUNK_ROWS
+#undef DLC_CHUNK_COLS
+#undef DLC_MFMA
+#pragma clang diagnostic pop
+
+// The sums are in their registers: products that assembly started are not known to the compiler
+template <int MI, int NJ>
+__device__ __forceinline__ void settle(f32x4 (&acc)[MI][NJ]) {
+    asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+}
+
 // Permutation of a k row's units where k runs down a column, UNITS of them in a row: the k rows that are read together
 // (half precision: 4 consecutive ones and the 4 that stand 8 further; fp32: 4 that are 4 apart) get different values.
 template <typename T, int UNITS>
@@ -322,24 +395,42 @@ struct Operand {
         }
     }
 
-    // Starts the current k tile's loads to `lds`; then steps to the next.  What lies outside the matrix becomes 0, and so do
-    // tiles past the last.
-    __device__ __forceinline__ void fetch(char* lds, int tid) {
+    // Before a k tile's loads: what lies outside the matrix becomes 0, and so do tiles past the last.
+    __device__ __forceinline__ void mask() {
         if (k_left < BK) {  // (the last tile; those behind it stay empty)
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) voff[i] = key + (KT ? i * RSTEP : 0) < k_left ? voff[i] : kOut;
         }
+    }
+    // What a thread's chunks i with i % 2 = odd are loaded from (DUAL: its rows 32 .. 63 of each 64 are the second matrix's)
+    __device__ __forceinline__ u32x4_t source(int odd) const {
+        static_assert(!DUAL || RSTEP == 32, "a pass's rows are all of one matrix");
+        const uint64_t p = (uint64_t)(uintptr_t)(base + (DUAL && odd ? half_off : 0));
+        return u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32) & 0xFFFFu), kOut,
+                       0x00020000u};
+    }
+    // Behind them: on to the next k tile
+    __device__ __forceinline__ void advance() {
+        k_left -= BK;
+        base += step;
+    }
+    // Starts loads FROM .. FROM + N - 1 of the current k tile to `lds`
+    template <int FROM, int N>
+    __device__ __forceinline__ void load(char* lds, int tid) const {
         const int wave_lds = (tid & ~63) * 16;
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
+        for (int i = FROM; i < FROM + N; ++i) {
             char* const dst = lds + wave_lds + i * THREADS * 16;
-            // (a wavefront's rows are all of one matrix)
-            const char* const src = base + (DUAL && (__builtin_amdgcn_readfirstlane(row0 + i * RSTEP) >> 5) & 1 ? half_off : 0);
+            const char* const src = base + (DUAL && i % 2 ? half_off : 0);
             const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, 0, kOut, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, voff[i], 0, 0, 0);
         }
-        k_left -= BK;
-        base += step;
+    }
+    // All of them
+    __device__ __forceinline__ void fetch(char* lds, int tid) {
+        mask();
+        load<0, PASSES>(lds, tid);
+        advance();
     }
 
     // Where a lane reads in a tile: row (column) `row` + l % 16 of N blocks of 16, its k values (l / 16) * 16 bytes on in
@@ -422,21 +513,82 @@ __device__ __forceinline__ void tile_of(int wg, int total, int tiles_m, int tile
     tn = t / h;
 }
 
+// RM x 64 of a wavefront's sums (acc[RM / 16][j0 .. j0 + 3]) through a piece of LDS of its own, so that a lane gets eight
+// consecutive columns, and the epilogue.  The 16-byte units of a row are permuted by the row.  m0, n0: the first row and
+// column of y
+template <typename T, bool GATED, int RM, int NJ>
+__device__ __forceinline__ void write_block(const GemmArgs& ga, const f32x4 (*acc)[NJ], int j0, char* buf, int m0, int n0, int sp, int lane) {
+    const uint64_t offset = full_offset(ga.e.offset, ga.e.d_offset);
+    const int g = lane >> 4, c16 = lane & 15;
+    constexpr int CH = GATED ? 4 : 8;  // chunks of eight columns in a row
+#pragma unroll
+    for (int i = 0; i < RM / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<f32x4*>(buf + (i * 16 + c16) * 256 + (((j * 4 + g) ^ c16) << 4)) = acc[i][j0 + j];
+    wave_sync();
+    constexpr int STEP = 64 / CH;  // a lane's rows are so far apart, its columns the same
+    // Rows at a time, whose residuals and results are on their way together: one by one, 16384 x 2048 x 2048 backward took 260
+    // us for 247, 8192 x 1024 x 512 41 for 37 (gated, four: too many registers on the small tiles, 20 us for 17.5)
+    constexpr int AT_ONCE = GATED ? 2 : 4;
+    const int ch = lane % CH, row0 = lane / CH, col = n0 + ch * 8;
+#pragma unroll 1
+    for (int q = 0; q < RM; q += STEP * AT_ONCE) {
+        float s[AT_ONCE][8], u[AT_ONCE][8];
+        const int m = m0 + q + row0;
+#pragma unroll
+        for (int r = 0; r < AT_ONCE; ++r) {
+            const int row = q + r * STEP + row0;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                *reinterpret_cast<f32x4*>(s[r] + v * 4) = *reinterpret_cast<const f32x4*>(buf + row * 256 + (((ch * 2 + v) ^ (row & 15)) << 4));
+                if constexpr (GATED)
+                    *reinterpret_cast<f32x4*>(u[r] + v * 4) = *reinterpret_cast<const f32x4*>(buf + row * 256 + (((8 + ch * 2 + v) ^ (row & 15)) << 4));
+            }
+        }
+        if (m >= ga.M) continue;
+        if (ga.split == 1) {
+            epilogue8<T, GATED, AT_ONCE, STEP>(ga.e, offset, m, ga.M - m, col, s, u);
+        } else if (col < ga.N) {  // (the pitch of the partial sums has room for whole chunks)
+#pragma unroll
+            for (int r = 0; r < AT_ONCE; ++r) {
+                if (m + r * STEP >= ga.M) continue;
+                float* p = ga.part + ((int64_t)sp * ga.M + m + r * STEP) * ga.part_ld + col;
+                *reinterpret_cast<f32x4*>(p) = *reinterpret_cast<f32x4*>(s[r]);
+                *reinterpret_cast<f32x4*>(p + 4) = *reinterpret_cast<f32x4*>(s[r] + 4);
+                if constexpr (GATED) {
+                    float* p2 = p + ((ga.N + 7) & ~7);
+                    *reinterpret_cast<f32x4*>(p2) = *reinterpret_cast<f32x4*>(u[r]);
+                    *reinterpret_cast<f32x4*>(p2 + 4) = *reinterpret_cast<f32x4*>(u[r] + 4);
+                }
+            }
+        }
+    }
+    wave_sync();
+}
+
+// a lane's places are kept in registers, not made again
+template <typename P>
+__device__ __forceinline__ void keep(P& p) {
+#pragma unroll
+    for (int i = 0; i < P::COUNT; ++i) asm volatile("" : "+v"(p.a[i]));
+}
+
+constexpr int kWideLds = 160 * 1024;  // all of a compute unit's
+
 // LDS of a work-group: with k along the rows three slots for A and two for B, otherwise four for both
 template <typename T, int LAY, int BM, int BN>
 constexpr int gemm_lds() {
     return LAY == L_KK ? 3 * BM * 128 + 2 * BN * 128 : 4 * (BM + BN) * 64;
 }
 
-// Tile `wg` of `total` of a product (the tiles of every cut of k)
-template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool GATED>
+// Tile `wg` of `total` of a product (the tiles of every cut of k), 128 x 128 or 64 x 128
+template <typename T, int LAY, int BM, int BN, bool GATED>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total, char* const lds) {
-    constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
-    constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, MI = WM / 16, NJ = WN / 16;
-    constexpr bool PAIRED = WAVES == 8;
-    // With k along both operands' rows a tile has 128 bytes of them: whole cache lines, half the requests, 5 % faster on
-    // 16384 x 2048 x 8192 than 64.  With k down a column a row is long anyway, and tiles of 64 bytes in four slots were
-    // 10 % faster: the loads are spread over all phases.
+    constexpr int WAVES = 4, THREADS = 256;
+    constexpr int WM = BM / 2, WN = BN / 2, MI = WM / 16, NJ = WN / 16;
+    // With k along both operands' rows a tile has 128 bytes of them: whole cache lines, half the requests.  With k down a
+    // column a row is long anyway, and tiles of 64 bytes in four slots spread the loads over the phases.
     constexpr int TB = LAY == L_KK ? 128 : 64;
     constexpr int BK = TB / sizeof(T);
     using OpA = Operand<T, LAY == L_TT, BM, TB, THREADS, false>;
@@ -457,7 +609,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
     oa.init(ga.a, ga.lda, m0, ga.M, k0, k1, tid);
     ob.init(ga.b, ga.ldb, n0, ga.N, k0, k1, tid);
     const int steps = (k1 - k0 + BK - 1) / BK;
-    const int wm = (wave / WAVES_N) * WM, wn = (wave % WAVES_N) * WN;
+    const int wm = (wave / 2) * WM, wn = (wave % 2) * WN;
 
     f32x4 acc[MI][NJ];
 #pragma unroll
@@ -466,19 +618,16 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     struct { u32x4_t a[MI], b[NJ]; } f;
     auto multiply = [&] {
-        if constexpr (PAIRED) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) acc[i][j] = mma<T>(f.b[j], f.a[i], acc[i][j]);
-        if constexpr (PAIRED) __builtin_amdgcn_s_setprio(0);
     };
     constexpr std::integral_constant<int, 0> i0{};
     constexpr std::integral_constant<int, 1> i1{};
     constexpr std::integral_constant<int, 2> i2{};
     constexpr std::integral_constant<int, 3> i3{};
     const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds;
-    const bool late = wave >= WAVES / 2;
 
     if constexpr (LAY == L_KK) {
         typename OpA::template Place<MI> pa;
@@ -491,49 +640,21 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
             read_rows2<MI, NJ, 16 * TB, 0>(f.a, pa.a[H] + sa, f.b, pb.a[H] + sb);
             __builtin_amdgcn_sched_barrier(0);  // (the reads first, the loads behind them)
         };
-        auto next = [&] {
-            sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
-            sb = OpB::BYTES - sb;
-        };
-        // A tile of B is started when all have read the one before the last, two of A are on their way
-        auto load_b = [&] { ob.fetch(lds + A3 + (OpB::BYTES - sb), tid); };
-        auto load_a = [&] { oa.fetch(lds + (sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES), tid); };
         oa.fetch(lds, tid);
         ob.fetch(lds + A3, tid);
         oa.fetch(lds + OpA::BYTES, tid);
-        if constexpr (PAIRED) {
-            // The wait for the next tiles stands before the barrier behind which the first group reads them
+        for (int s = 0; s < steps; ++s) {
+            // a tile of B is started when all have read the one before the last, two of A are on their way
             wait_loads<OpA::PASSES>();
             bare_barrier();
-            if (late) bare_barrier();
-            for (int s = 0; s < steps; ++s) {
-                read(i0);
-                load_b();
-                bare_barrier();
-                multiply();
-                bare_barrier();
-                read(i1);
-                load_a();
-                if (late) wait_loads<OpA::PASSES>();
-                bare_barrier();
-                multiply();
-                if (!late) wait_loads<OpA::PASSES>();
-                bare_barrier();
-                next();
-            }
-            if (!late) bare_barrier();
-        } else {
-            for (int s = 0; s < steps; ++s) {
-                wait_loads<OpA::PASSES>();
-                bare_barrier();
-                read(i0);
-                load_b();
-                multiply();
-                read(i1);
-                load_a();
-                multiply();
-                next();
-            }
+            read(i0);
+            ob.fetch(lds + A3 + (OpB::BYTES - sb), tid);
+            multiply();
+            read(i1);
+            oa.fetch(lds + (sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES), tid);
+            multiply();
+            sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
+            sb = OpB::BYTES - sb;
         }
     } else {
         // four slots, each with a tile of A and one of B; a lane's places in the first and in the third
@@ -543,18 +664,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
         for (int h = 0; h < 2; ++h) {
             OpA::template place<MI>(pa[h], at + h * 2 * STAGE, wm, lane);
             OpB::template place<NJ>(pb[h], at + h * 2 * STAGE + OpA::BYTES, wn, lane);
-#pragma unroll
-            for (int i = 0; i < pa[h].COUNT; ++i) asm volatile("" : "+v"(pa[h].a[i]));  // (kept, not made again)
-#pragma unroll
-            for (int i = 0; i < pb[h].COUNT; ++i) asm volatile("" : "+v"(pb[h].a[i]));
+            keep(pa[h]);
+            keep(pb[h]);
         }
-        auto read = [&](auto slot) {
-            constexpr int H = decltype(slot)::value / 2, OFF = decltype(slot)::value % 2 * STAGE;
-            OpB::template frags<NJ, OFF>(f.b, pb[H]);
-            OpA::template frags<MI, OFF>(f.a, pa[H]);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        constexpr int LOADS = OpA::PASSES + OpB::PASSES;
         auto load = [&](int slot) {
             oa.fetch(lds + slot * STAGE, tid);
             ob.fetch(lds + slot * STAGE + OpA::BYTES, tid);
@@ -563,112 +675,251 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
         load(1);
         load(2);
         auto step = [&](auto slot) {
-            constexpr int S = decltype(slot)::value;
-            if constexpr (PAIRED) {
-                read(slot);
-                load((S + 3) % 4);
-                wait_loads<2 * LOADS>();
-                bare_barrier();
-                multiply();
-                bare_barrier();
-            } else {
-                wait_loads<2 * LOADS>();
-                bare_barrier();
-                read(slot);
-                load((S + 3) % 4);
-                multiply();
-            }
-        };
-        if constexpr (PAIRED) {
-            wait_loads<2 * LOADS>();
+            constexpr int S = decltype(slot)::value, H = S / 2, OFF = S % 2 * STAGE;
+            wait_loads<2 * (OpA::PASSES + OpB::PASSES)>();
             bare_barrier();
-            if (late) bare_barrier();
-        }
+            OpB::template frags<NJ, OFF>(f.b, pb[H]);
+            OpA::template frags<MI, OFF>(f.a, pa[H]);
+            __builtin_amdgcn_sched_barrier(0);
+            load((S + 3) % 4);
+            multiply();
+        };
         for (int s = 0; s < steps; s += 4) {  // (tiles past the last are zeros)
             step(i0);
             step(i1);
             step(i2);
             step(i3);
         }
-        if constexpr (PAIRED) {
-            if (!late) bare_barrier();
-        }
     }
     wait_loads<0>();  // (tiles past the last may still be on their way)
 
-    // Epilogue: a wavefront's part goes through its own piece of LDS, so that a lane gets eight consecutive columns; the
-    // 16-byte units of a row are permuted by the row
     constexpr int FIT = LDS / WAVES / 256;                    // rows a wavefront has room for
     constexpr int RM = FIT >= WM ? WM : FIT >= 64 ? 64 : 32;  // rows at a time
     static_assert(RM <= FIT && WM % RM == 0, "room for the epilogue");
     __syncthreads();
-    char* const buf = lds + wave * RM * 256;
-    const uint64_t offset = full_offset(ga.e.offset, ga.e.d_offset);
-    const int g = lane >> 4, c16 = lane & 15;
-    constexpr int CH = GATED ? 4 : 8;  // chunks of eight columns in a row
 #pragma unroll
-    for (int h = 0; h < WM / RM; ++h) {
-#pragma unroll
-        for (int i = 0; i < RM / 16; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                *reinterpret_cast<f32x4*>(buf + (i * 16 + c16) * 256 + (((j * 4 + g) ^ c16) << 4)) = acc[h * (RM / 16) + i][j];
-        wave_sync();
-#pragma unroll 1
-        for (int q = 0; q < RM * CH / 64; ++q) {
-            const int idx = q * 64 + lane, row = idx / CH, ch = idx % CH;
-            const int m = m0 + wm + h * RM + row, col = n0 + (GATED ? wn / 2 : wn) + ch * 8;
-            float s[8], u[8];
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                *reinterpret_cast<f32x4*>(s + v * 4) = *reinterpret_cast<const f32x4*>(buf + row * 256 + (((ch * 2 + v) ^ (row & 15)) << 4));
-                if constexpr (GATED)
-                    *reinterpret_cast<f32x4*>(u + v * 4) = *reinterpret_cast<const f32x4*>(buf + row * 256 + (((8 + ch * 2 + v) ^ (row & 15)) << 4));
-            }
-            if (m < ga.M) {
-                if (ga.split > 1) {
-                    if (col < ga.N) {  // (the pitch of the partial sums has room for whole chunks)
-                        float* p = ga.part + ((int64_t)sp * ga.M + m) * ga.part_ld + col;
-                        *reinterpret_cast<f32x4*>(p) = *reinterpret_cast<f32x4*>(s);
-                        *reinterpret_cast<f32x4*>(p + 4) = *reinterpret_cast<f32x4*>(s + 4);
-                        if constexpr (GATED) {
-                            float* p2 = p + ((ga.N + 7) & ~7);
-                            *reinterpret_cast<f32x4*>(p2) = *reinterpret_cast<f32x4*>(u);
-                            *reinterpret_cast<f32x4*>(p2 + 4) = *reinterpret_cast<f32x4*>(u + 4);
-                        }
-                    }
-                } else {
-                    epilogue8<T, GATED>(ga.e, offset, m, col, s, u);
-                }
-            }
-        }
-        wave_sync();
-    }
+    for (int h = 0; h < WM / RM; ++h)
+        write_block<T, GATED, RM>(ga, &acc[h * (RM / 16)], 0, lds + wave * RM * 256, m0 + wm + h * RM, n0 + (GATED ? wn / 2 : wn), sp, lane);
 }
 
-template <typename T, int LAY, int BM, int BN, int WAVES_M, int WAVES_N, bool GATED>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_gemm(const GemmArgs ga) {
+// The same with 256 x 256 of C, half precision: four wavefronts, one on each SIMD, with 128 x 128 each.  While a step's (32
+// k values) fragments are multiplied the next step's are read; a step's loads go to the slots that all have read.
+template <typename T, int LAY, bool GATED>
+__device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total, char* const lds) {
+    constexpr int THREADS = 256, W = 256, MI = 8, NJ = 8;
+    // k along a row: tiles of 128 bytes of it (whole cache lines), two steps each; down a column: of 64
+    constexpr bool CA = LAY == L_TT, CB = LAY != L_KK;
+    constexpr int TA = CA ? 64 : 128, TBB = CB ? 64 : 128;
+    using OpA = Operand<T, CA, W, TA, THREADS, false>;
+    using OpB = Operand<T, CB, W, TBB, THREADS, GATED>;
+    constexpr int SLOTS_A = CA ? 4 : 3, SLOTS_B = CB ? 4 : 2;
+    constexpr int A0 = 0, B0 = SLOTS_A * OpA::BYTES;
+    static_assert(B0 + SLOTS_B * OpB::BYTES <= kWideLds, "slots");
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tm, tn, sp;
+    tile_of(wg, total, ga.tiles_m, ga.tiles_n, tm, tn, sp);
+    const int m0 = tm * W, n0 = tn * (GATED ? W / 2 : W);
+    const int k0 = sp * ga.kper, k1 = min(ga.K, k0 + ga.kper);
+    OpA oa;
+    OpB ob;
+    oa.init(ga.a, ga.lda, m0, ga.M, k0, k1, tid);
+    ob.init(ga.b, ga.ldb, n0, ga.N, k0, k1, tid);
+    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
+
+    f32x4 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    struct { u32x4_t a[MI], b[NJ]; } f[2];
+    const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds, mine = at + (uint32_t)wave * 1024u;
+    constexpr int SA = CA ? 4 * OpA::CPR * 16 : 16 * TA, SB = CB ? 4 * OpB::CPR * 16 : 16 * TBB;
+    constexpr int RA = CA ? 0 : 4 * SA, RB = CB ? 0 : 4 * SB;  // to the second four blocks (columns: at addresses of their own)
+    constexpr int NA = CA ? 4 : 0, NB = CB ? 4 : 0;
+    typename OpA::template Place<MI> pa[CA ? 2 : 1];
+    typename OpB::template Place<NJ> pb[CB ? 2 : 1];
+#pragma unroll
+    for (int h = 0; h < (CA ? 2 : 1); ++h) {
+        OpA::template place<MI>(pa[h], at + A0 + h * 2 * OpA::BYTES, wm, lane);
+        keep(pa[h]);
+    }
+#pragma unroll
+    for (int h = 0; h < (CB ? 2 : 1); ++h) {
+        OpB::template place<NJ>(pb[h], at + B0 + h * 2 * OpB::BYTES, wn, lane);
+        keep(pb[h]);
+    }
+    // 64 products with c's fragments, and n's read; the loads are numbers IA .. IA + NLA - 1 of A, then the same of B
+    auto multiply = [&](auto& c, auto& n, const uint32_t* ra, const uint32_t* rb, auto off_a, auto off_b, const auto& l0, const auto& l1,
+                        const auto& l2, const auto& l3, auto w0, auto w1, auto w2, auto w3) {
+        constexpr int OA = decltype(off_a)::value, OB = decltype(off_b)::value;
+        chunk16<T, CB, OB, SB, decltype(w0)::value>(acc[0], acc[1], c.a[0], c.a[1], c.b, n.b, rb, l0);
+        chunk16<T, CB, OB + RB, SB, decltype(w1)::value>(acc[2], acc[3], c.a[2], c.a[3], c.b, n.b + 4, rb + NB, l1);
+        chunk16<T, CA, OA, SA, decltype(w2)::value>(acc[4], acc[5], c.a[4], c.a[5], c.b, n.a, ra, l2);
+        chunk16<T, CA, OA + RA, SA, decltype(w3)::value>(acc[6], acc[7], c.a[6], c.a[7], c.b, n.a + 4, ra + NA, l3);
+    };
+    constexpr std::integral_constant<int, 0> i0{};
+    constexpr std::integral_constant<int, 1> i1{};
+    constexpr std::integral_constant<int, 2> i2{};
+    constexpr std::integral_constant<int, 3> i3{};
+    // loads 2 i and 2 i + 1 of the operand's current tile to the slot at `slot`
+    auto to = [&](const auto& o, int i, uint32_t slot) { return LoadTo{o.voff[2 * i], o.voff[2 * i + 1], o.source(0), o.source(1), mine + slot}; };
+
+    if constexpr (LAY == L_KK) {
+        const int tiles = (k1 - k0 + OpA::BK - 1) / OpA::BK;
+        uint32_t sa = 0, sb = 0;  // slots of the current tiles, in bytes
+        oa.fetch(lds, tid);
+        ob.fetch(lds + B0, tid);
+        oa.fetch(lds + OpA::BYTES, tid);
+        ob.fetch(lds + B0 + OpB::BYTES, tid);
+        wait_loads<OpA::PASSES + OpB::PASSES>();
+        bare_barrier();
+        read_rows<NJ, SB, 0>(f[0].b, pb[0].a[0]);
+        read_rows<MI, SA, 0>(f[0].a, pa[0].a[0]);
+        settle(acc);
+        for (int s = 0; s < tiles; ++s) {
+            // the tile's first half; A's tile after the next goes where the one before was
+            const uint32_t slot_a = sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES;
+            uint32_t ra = pa[0].a[1] + sa, rb = pb[0].a[1] + sb;
+            oa.mask();
+            multiply(f[0], f[1], &ra, &rb, i0, i0, to(oa, 0, slot_a), to(oa, 1, slot_a), to(oa, 2, slot_a), to(oa, 3, slot_a), i0, i1, i2, i3);
+            oa.advance();
+            // the next tiles have come, and all have read this one: B's after the next takes its place
+            wait_loads<OpA::PASSES>();
+            bare_barrier();
+            const uint32_t slot_b = B0 + sb;
+            sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
+            sb = OpB::BYTES - sb;
+            ra = pa[0].a[0] + sa;
+            rb = pb[0].a[0] + sb;
+            ob.mask();
+            multiply(f[1], f[0], &ra, &rb, i0, i0, to(ob, 0, slot_b), to(ob, 1, slot_b), to(ob, 2, slot_b), to(ob, 3, slot_b), i0, i1, i2, i3);
+            ob.advance();
+        }
+    } else if constexpr (LAY == L_KT) {
+        // a tile of A lasts two steps, half of its loads in each
+        const int steps = (k1 - k0 + OpB::BK - 1) / OpB::BK;
+        uint32_t sa = 0;
+        oa.mask();
+        oa.template load<0, 4>(lds, tid);
+        ob.fetch(lds + B0, tid);
+        oa.template load<4, 4>(lds, tid);
+        oa.advance();
+        ob.fetch(lds + B0 + OpB::BYTES, tid);
+        oa.mask();
+        oa.template load<0, 4>(lds + OpA::BYTES, tid);
+        ob.fetch(lds + B0 + 2 * OpB::BYTES, tid);
+        oa.template load<4, 4>(lds + OpA::BYTES, tid);
+        oa.advance();
+        ob.fetch(lds + B0 + 3 * OpB::BYTES, tid);
+        wait_loads<20>();
+        bare_barrier();
+        OpB::template frags<NJ, 0>(f[0].b, pb[0]);
+        read_rows<MI, SA, 0>(f[0].a, pa[0].a[0]);
+        settle(acc);
+        auto step = [&](auto slot) {
+            constexpr int S = decltype(slot)::value, X = (S + 1) % 4;
+            constexpr std::integral_constant<int, X % 2 * OpB::BYTES> off{};
+            constexpr uint32_t slot_b = B0 + S * OpB::BYTES;
+            if constexpr (S % 2 == 0) {
+                wait_loads<16>();
+                bare_barrier();
+                const uint32_t slot_a = sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES;
+                const uint32_t ra = pa[0].a[1] + sa;
+                oa.mask();
+                ob.mask();
+                multiply(f[0], f[1], &ra, pb[X / 2].a, i0, off, to(oa, 0, slot_a), to(oa, 1, slot_a), to(ob, 0, slot_b), to(ob, 1, slot_b), i0, i1, i0, i1);
+            } else {
+                wait_loads<12>();
+                bare_barrier();
+                const uint32_t slot_a = sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES;
+                sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
+                const uint32_t ra = pa[0].a[0] + sa;
+                ob.mask();
+                multiply(f[1], f[0], &ra, pb[X / 2].a, i0, off, to(oa, 2, slot_a), to(oa, 3, slot_a), to(ob, 0, slot_b), to(ob, 1, slot_b), i2, i3, i0, i1);
+                oa.advance();
+            }
+            ob.advance();
+        };
+        for (int s = 0; s < steps; s += 4) {  // (tiles past the last are zeros)
+            step(i0);
+            step(i1);
+            step(i2);
+            step(i3);
+        }
+    } else {
+        const int steps = (k1 - k0 + OpB::BK - 1) / OpB::BK;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            oa.fetch(lds + i * OpA::BYTES, tid);
+            ob.fetch(lds + B0 + i * OpB::BYTES, tid);
+        }
+        constexpr int LOADS = OpA::PASSES + OpB::PASSES;
+        wait_loads<3 * LOADS>();
+        bare_barrier();
+        OpB::template frags<NJ, 0>(f[0].b, pb[0]);
+        OpA::template frags<MI, 0>(f[0].a, pa[0]);
+        settle(acc);
+        auto step = [&](auto slot) {
+            constexpr int S = decltype(slot)::value, X = (S + 1) % 4;
+            constexpr std::integral_constant<int, X % 2 * OpA::BYTES> off_a{};
+            constexpr std::integral_constant<int, X % 2 * OpB::BYTES> off_b{};
+            wait_loads<2 * LOADS>();
+            bare_barrier();
+            oa.mask();
+            ob.mask();
+            multiply(f[S % 2], f[1 - S % 2], pa[X / 2].a, pb[X / 2].a, off_a, off_b, to(oa, 0, S * OpA::BYTES), to(oa, 1, S * OpA::BYTES),
+                     to(ob, 0, B0 + S * OpB::BYTES), to(ob, 1, B0 + S * OpB::BYTES), i0, i1, i0, i1);
+            oa.advance();
+            ob.advance();
+        };
+        for (int s = 0; s < steps; s += 4) {
+            step(i0);
+            step(i1);
+            step(i2);
+            step(i3);
+        }
+    }
+    wait_loads<0>();  // (tiles past the last may still be on their way)
+    settle(acc);
+    __syncthreads();
+    static_assert(4 * 128 * 256 <= kWideLds, "room for the epilogue");
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        write_block<T, GATED, 128>(ga, acc, h * 4, lds + wave * 128 * 256, m0 + wm, n0 + (GATED ? wn / 2 + h * 32 : wn + h * 64), sp, lane);
+}
+
+template <typename T, int LAY, int BM, int BN, bool GATED>
+__global__ __launch_bounds__(256, 2) void k_gemm(const GemmArgs ga) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host's pass has no use for the body, and does not know its assembly)
     __shared__ __attribute__((aligned(16))) char lds[gemm_lds<T, LAY, BM, BN>()];
-    gemm_tile<T, LAY, BM, BN, WAVES_M, WAVES_N, GATED>(ga, blockIdx.x, gridDim.x, lds);
+    gemm_tile<T, LAY, BM, BN, GATED>(ga, blockIdx.x, gridDim.x, lds);
 #endif
 }
 
-// kSumCols columns of the bias gradient from the row blocks' sums, added up in a fixed order by 16 x LANES threads with all
-// loads in flight
+template <typename T, int LAY, bool GATED>
+__global__ __launch_bounds__(256, 1) void k_gemm_wide(const GemmArgs ga) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ __attribute__((aligned(16))) char lds[kWideLds];
+    gemm_wide<T, LAY, GATED>(ga, blockIdx.x, gridDim.x, lds);
+#endif
+}
+
+// kSumCols columns of the bias gradient from the row blocks' sums, added up in a fixed order by 256 threads with all loads in
+// flight
 constexpr int kSumCols = 16;
 
-template <typename T, int LANES>
+template <typename T>
 __device__ __forceinline__ void sum_columns(const SumArgs& sa, int wg, float (*red)[17]) {
     const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
     const int c = wg * kSumCols + cx;
     float s = 0.f;
     if (c < sa.n) {
         const float* const p = sa.sums + c;
-        for (int i = ry; i < sa.row_blocks; i += 16 * LANES) {
+        for (int i = ry; i < sa.row_blocks; i += 256) {
             float v[16];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) v[u] = i + LANES * u < sa.row_blocks ? p[(int64_t)(i + LANES * u) * sa.sums_ld] : 0.f;
+            for (int u = 0; u < 16; ++u) v[u] = i + 16 * u < sa.row_blocks ? p[(int64_t)(i + 16 * u) * sa.sums_ld] : 0.f;
 #pragma unroll
             for (int u = 0; u < 16; ++u) s += v[u];
         }
@@ -678,29 +929,34 @@ __device__ __forceinline__ void sum_columns(const SumArgs& sa, int wg, float (*r
     if (ry == 0 && c < sa.n) {
         float t = 0.f;
 #pragma unroll
-        for (int w = 0; w < LANES; ++w) t += red[w][cx];
+        for (int w = 0; w < 16; ++w) t += red[w][cx];
         static_cast<T*>(sa.out)[c] = (T)t;
     }
 }
 
 // Both products of a backward call in one launch, and the bias gradient if nothing comes behind: small products leave most
 // compute units idle one by one.  The work-groups of each start at a multiple of 8, so that tile_of's XCDs are the real ones.
-template <typename T, int BM, int BN, int WAVES_M, int WAVES_N>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
+template <typename T, int TILE>
+__global__ __launch_bounds__(256, TILE == 0 ? 1 : 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ __attribute__((aligned(16))) char lds[gemm_lds<T, L_TT, BM, BN>()];
+    constexpr int BM = kTileM[TILE], BN = kTileN[TILE];
+    __shared__ __attribute__((aligned(16))) char lds[TILE == 0 ? kWideLds : gemm_lds<T, L_TT, BM, BN>()];
     const int nw8 = (nw + 7) & ~7, nx8 = (nx + 7) & ~7;
     int b = blockIdx.x;
     if (b < nw8) {
-        if (b < nw) gemm_tile<T, L_TT, BM, BN, WAVES_M, WAVES_N, false>(gw, b, nw, lds);
+        if (b >= nw) return;
+        if constexpr (TILE == 0) gemm_wide<T, L_TT, false>(gw, b, nw, lds);
+        else gemm_tile<T, L_TT, BM, BN, false>(gw, b, nw, lds);
         return;
     }
     b -= nw8;
     if (b < nx8) {
-        if (b < nx) gemm_tile<T, L_KT, BM, BN, WAVES_M, WAVES_N, false>(gx, b, nx, lds);
+        if (b >= nx) return;
+        if constexpr (TILE == 0) gemm_wide<T, L_KT, false>(gx, b, nx, lds);
+        else gemm_tile<T, L_KT, BM, BN, false>(gx, b, nx, lds);
         return;
     }
-    sum_columns<T, 4 * WAVES_M * WAVES_N>(sa, b - nx8, reinterpret_cast<float(*)[17]>(lds));
+    sum_columns<T>(sa, b - nx8, reinterpret_cast<float(*)[17]>(lds));
 #endif
 }
 
@@ -712,18 +968,18 @@ template <typename T, bool GATED>
 __device__ __forceinline__ void skinny_end(const GemmArgs& ga, int m0, int n0, const float (*sums)[GATED ? 2 : 1][16][20], int tid) {
     const int row = tid >> 1, ch = tid & 1;
     if (tid >= 32 || m0 + row >= ga.M) return;
-    float s[8], u[8];
+    float s[1][8], u[1][8];
 #pragma unroll
     for (int v = 0; v < 8; ++v) {
-        s[v] = 0.f;
-        u[v] = 0.f;
+        s[0][v] = 0.f;
+        u[0][v] = 0.f;
 #pragma unroll
         for (int w = 0; w < kSkinnyWaves; ++w) {
-            s[v] += sums[w][0][row][ch * 8 + v];
-            if constexpr (GATED) u[v] += sums[w][1][row][ch * 8 + v];
+            s[0][v] += sums[w][0][row][ch * 8 + v];
+            if constexpr (GATED) u[0][v] += sums[w][1][row][ch * 8 + v];
         }
     }
-    epilogue8<T, GATED>(ga.e, full_offset(ga.e.offset, ga.e.d_offset), m0 + row, n0 + ch * 8, s, u);
+    epilogue8<T, GATED, 1, 1>(ga.e, full_offset(ga.e.offset, ga.e.d_offset), m0 + row, 1, n0 + ch * 8, s, u);
 }
 
 // Few rows (at most 32): the product is a pass over B.  A work-group takes 16 columns of C (gated: and the 16 of the other
@@ -865,7 +1121,7 @@ __device__ __forceinline__ void join_chunk(const JoinArgs& ja, int64_t idx) {
     const int chunks = (ja.e.n + 7) / 8;
     if (idx >= (int64_t)chunks * ja.M) return;
     const int m = (int)(idx / chunks), col = (int)(idx % chunks) * 8;
-    float s[8] = {}, u[8] = {};
+    float s[1][8] = {}, u[1][8] = {};
     const float* p = ja.part + (int64_t)m * ja.part_ld + col;
     const int64_t slab = (int64_t)ja.M * ja.part_ld;
     const int up = (ja.e.n + 7) & ~7;
@@ -875,15 +1131,15 @@ __device__ __forceinline__ void join_chunk(const JoinArgs& ja, int64_t idx) {
         for (int h = 0; h < 2; ++h) {
             const f32x4 q = *reinterpret_cast<const f32x4*>(p + h * 4);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) s[h * 4 + v] += q[v];
+            for (int v = 0; v < 4; ++v) s[0][h * 4 + v] += q[v];
             if constexpr (GATED) {
                 const f32x4 r = *reinterpret_cast<const f32x4*>(p + up + h * 4);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) u[h * 4 + v] += r[v];
+                for (int v = 0; v < 4; ++v) u[0][h * 4 + v] += r[v];
             }
         }
     }
-    epilogue8<T, GATED>(ja.e, full_offset(ja.e.offset, ja.e.d_offset), m, col, s, u);
+    epilogue8<T, GATED, 1, 1>(ja.e, full_offset(ja.e.offset, ja.e.d_offset), m, 1, col, s, u);
 }
 
 // The last launch of a call: the bias gradient, then the partial sums of up to two products
@@ -891,7 +1147,7 @@ template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_join(const JoinArgs ja, const JoinArgs jb, const SumArgs sa, int sum_wgs, int ja_wgs) {
     __shared__ float red[16][17];
     int b = blockIdx.x;
-    if (b < sum_wgs) return sum_columns<T, 16>(sa, b, red);
+    if (b < sum_wgs) return sum_columns<T>(sa, b, red);
     b -= sum_wgs;
     if (b < ja_wgs) return join_chunk<T, GATED>(ja, (int64_t)b * 256 + threadIdx.x);
     if constexpr (!GATED) join_chunk<T, false>(jb, (int64_t)(b - ja_wgs) * 256 + threadIdx.x);
@@ -1030,17 +1286,13 @@ __global__ __launch_bounds__(256) void k_drop(const DropArgs da) {
 }
 
 // ---- launches -----------------------------------------------------------------------------------
-template <typename T, int LAY, int BM, int BN, int WM, int WN, bool GT>
-static hipError_t gemm_go(const GemmArgs& g, hipStream_t s) {
-    k_gemm<T, LAY, BM, BN, WM, WN, GT><<<dim3((unsigned)(g.tiles_m * g.tiles_n * g.split)), dim3(64 * WM * WN), 0, s>>>(g);
-    return hipGetLastError();
-}
-
 template <typename T, int LAY, bool GT>
 static hipError_t gemm_pick(const GemmArgs& g, int tile, hipStream_t s) {
-    if (tile == 0) return gemm_go<T, LAY, 256, 256, 2, 4, GT>(g, s);
-    if (tile == 1) return gemm_go<T, LAY, 128, 128, 2, 2, GT>(g, s);
-    return gemm_go<T, LAY, 64, 128, 2, 2, GT>(g, s);
+    const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * g.split)), block(256);
+    if (tile == 1) k_gemm<T, LAY, kTileM[1], kTileN[1], GT><<<grid, block, 0, s>>>(g);
+    else if (tile == 2) k_gemm<T, LAY, kTileM[2], kTileN[2], GT><<<grid, block, 0, s>>>(g);
+    else if constexpr (sizeof(T) == 2) k_gemm_wide<T, LAY, GT><<<grid, block, 0, s>>>(g);
+    return hipGetLastError();
 }
 
 template <typename T>
@@ -1070,9 +1322,9 @@ template <typename T>
 hipError_t DenseOps<T>::back(const GemmArgs& gx, const GemmArgs& gw, const SumArgs& a, int tile, hipStream_t s) {
     const int nx = gx.tiles_m * gx.tiles_n * gx.split, nw = gw.tiles_m * gw.tiles_n * gw.split;
     const dim3 grid((unsigned)(((nx + 7) & ~7) + ((nw + 7) & ~7) + (a.n + kSumCols - 1) / kSumCols));
-    if (tile == 1) k_back<T, 128, 128, 2, 2><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
-    else if (tile == 2) k_back<T, 64, 128, 2, 2><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
-    else if constexpr (sizeof(T) == 2) k_back<T, 256, 256, 2, 4><<<grid, dim3(512), 0, s>>>(gx, gw, a, nx, nw);
+    if (tile == 1) k_back<T, 1><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    else if (tile == 2) k_back<T, 2><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
+    else if constexpr (sizeof(T) == 2) k_back<T, 0><<<grid, dim3(256), 0, s>>>(gx, gw, a, nx, nw);
     return hipGetLastError();
 }
 

@@ -176,6 +176,17 @@ def test_gated_backward(dtype, shape):
         _backward("gated", dtype, *shape, ACTS[(i + 2) % 5], p=0.3 if i % 2 else 0.0, how=how)
 
 
+# the largest tiles in half precision, whole and ragged
+FORWARD_LARGE = [("gated", (4096, 1024, 2048), "dense"), ("gated", (4090, 1030, 2050), "pitch"), ("linear", (8190, 1000, 4001), "odd")]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("op,shape,how", FORWARD_LARGE)
+def test_large_forward(dtype, op, shape, how):
+    _forward(op, dtype, *shape, "silu", bias=True, residual=op == "linear", save=True, p=0.0, how=how)
+
+
 # both products in one launch on the largest tiles: nothing cut and the bias gradient in the same launch, the gradient of w
 # cut; one launch after the other, the gradient of x cut
 BACKWARD_LARGE = [("linear", (8200, 4100, 2056), "odd"), ("linear", (8192, 2048, 2048), "dense"), ("linear", (300, 4000, 2000), "pitch"),
