@@ -576,10 +576,10 @@ __device__ __forceinline__ void keep(P& p) {
 
 constexpr int kWideLds = 160 * 1024;  // all of a compute unit's
 
-// LDS of a work-group: with k along the rows three slots for A and two for B, otherwise four for both
+// LDS of a work-group: with k along the rows three slots for A and two or three for B, otherwise four for both
 template <typename T, int LAY, int BM, int BN>
 constexpr int gemm_lds() {
-    return LAY == L_KK ? 3 * BM * 128 + 2 * BN * 128 : 4 * (BM + BN) * 64;
+    return LAY == L_KK ? 3 * BM * 128 + (BM == 64 ? 3 : 2) * BN * 128 : 4 * (BM + BN) * 64;
 }
 
 // Tile `wg` of `total` of a product (the tiles of every cut of k), 128 x 128 or 64 x 128
@@ -596,8 +596,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
     static_assert(WN == 64, "a wavefront's columns (gated: 32 of the gate and 32 of the other)");
     constexpr int STAGE = OpA::BYTES + OpB::BYTES;
     constexpr int A3 = 3 * OpA::BYTES;  // k along the rows: where B's slots start
+    constexpr bool DEEP = BM == 64;     // there is room for a third (128 x 4096 x 4096 in bf16 19.0 -> 16.4 us)
     constexpr int LDS = gemm_lds<T, LAY, BM, BN>();
-    static_assert(LDS == (LAY == L_KK ? A3 + 2 * OpB::BYTES : 4 * STAGE), "slots");
+    static_assert(LDS == (LAY == L_KK ? A3 + (DEEP ? 3 : 2) * OpB::BYTES : 4 * STAGE), "slots");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int tm, tn, sp;
@@ -643,18 +644,19 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
         oa.fetch(lds, tid);
         ob.fetch(lds + A3, tid);
         oa.fetch(lds + OpA::BYTES, tid);
+        if constexpr (DEEP) ob.fetch(lds + A3 + OpB::BYTES, tid);
         for (int s = 0; s < steps; ++s) {
-            // a tile of B is started when all have read the one before the last, two of A are on their way
-            wait_loads<OpA::PASSES>();
+            // tiles are started when all have read those whose places they take: two ahead, of B one ahead if it has two slots
+            wait_loads<OpA::PASSES + (DEEP ? OpB::PASSES : 0)>();
             bare_barrier();
             read(i0);
-            ob.fetch(lds + A3 + (OpB::BYTES - sb), tid);
+            ob.fetch(lds + A3 + (!DEEP ? OpB::BYTES - sb : sb == 0 ? 2 * OpB::BYTES : sb - OpB::BYTES), tid);
             multiply();
             read(i1);
             oa.fetch(lds + (sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES), tid);
             multiply();
             sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
-            sb = OpB::BYTES - sb;
+            sb = !DEEP ? OpB::BYTES - sb : sb == 2 * OpB::BYTES ? 0 : sb + OpB::BYTES;
         }
     } else {
         // four slots, each with a tile of A and one of B; a lane's places in the first and in the third
