@@ -70,11 +70,11 @@ struct Plan {
 // What a k tile (128 bytes of k) costs with 1, 2 and 3 work-groups on a compute unit, in us, what a work-group costs
 // besides, and what it costs more to write partial sums, measured with all three layouts on full and half full cards (0: no
 // further work-group fits).  256 x 256 is the fastest per product in half precision (1500 TFLOP/s against 1280 and 850 of
-// the other two, all compute units busy) and has the longest start and end; in fp32 the small tiles reach the matrix cores'
-// rate and leave fewer units idle: there is no large one.
+// the other two, all compute units busy) and has the longest start and end; in fp32 128 x 128 and 64 x 128 reach 150 and 138
+// TFLOP/s and there is no larger one.
 struct TileCost { double tile[3], first, further, part; };
 constexpr TileCost kHalfCost[3] = {{{1.38, 0, 0}, 12.0, 9.0, 5.0}, {{0.57, 0.88, 0}, 6.0, 3.0, 0}, {{0.45, 0.64, 1.0}, 4.0, 3.0, 0}};
-constexpr TileCost kF32Cost[3] = {{}, {{2.2, 3.8, 0}, 8.0, 4.0, 0}, {{1.3, 2.0, 2.9}, 5.0, 3.0, 0}};
+constexpr TileCost kF32Cost[3] = {{}, {{1.80, 3.58, 0}, 10.0, 4.5, 0}, {{1.25, 1.95, 2.9}, 6.5, 3.0, 0}};
 constexpr int kUnits = 256;  // compute units
 
 // cuts of k that are looked at

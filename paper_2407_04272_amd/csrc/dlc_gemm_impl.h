@@ -4,13 +4,17 @@
 // tiles of A and B go from memory to a ring of slots in LDS, several tiles ahead, without passing through registers; a
 // wavefront holds a part of C in registers as 16 x 16 blocks and takes its fragments of a tile from LDS.
 //
-// 256 x 256 (half precision): four wavefronts, one on each SIMD, with 128 x 128 each (gemm_wide).  A byte read from LDS is
+// 256 x 256 in half precision, 128 x 128 in fp32 (gemm_wide): four wavefronts, each with a quarter, read a step's fragments
+// while they multiply the one before.  Half precision has one of them on each SIMD with 128 x 128: a byte read from LDS is
 // used for twice the products of a 64 x 64 part, which leaves LDS idle four fifths of the time and the clock higher than
 // eight wavefronts of 128 x 64 in two alternating groups did (the card is bound by power, 1.9 to 2.0 GHz here, with the
 // matrix cores busy 75 % of the time).  bf16, without an epilogue, k along both rows, down one's and down both's columns:
 // 8192 x 2048 x 8192 184, 186 and 187 us = 1495, 1478 and 1465 TFLOP/s (eight wavefronts: 193, 204 and 206; a library 171 to
-// 185), 16384 x 8192 x 2048 400, 405 and 408 (421, 439 and 446).
-// 128 x 128 and 64 x 128, four wavefronts: two or three work-groups share a compute unit and fill each other's gaps.
+// 185), 16384 x 8192 x 2048 400, 405 and 408 (421, 439 and 446).  fp32 4096 x 4096 x 4096 926, 941 and 945 us = 148, 146 and
+// 145 TFLOP/s, the matrix cores busy 94 % at 2.4 GHz (reads and products in turn: 970, 1004 and 984); 4096 x 1024 x 1664,
+// one work-group a compute unit, 112, 110 and 110 us (120, 127 and 136).
+// 128 x 128 in half precision and 64 x 128, four wavefronts: two or three work-groups share a compute unit and fill each
+// other's gaps (gemm_tile).
 //
 // LDS layouts (16-byte chunks):
 //   k along a row     rows of TB bytes of k, chunk c of row r at place c ^ (r >> 1): what the 16 lanes of a quarter of a
@@ -314,6 +318,60 @@ __device__ __forceinline__ void chunk16(f32x4* acc0, f32x4* acc1, const u32x4_t&
 #undef DLC_CHUNK_ROWS
 #undef DLC_CHUNK_COLS
 #undef DLC_MFMA
+
+#define DLC_MFMA_F32(ACC, B, A) "v_mfma_f32_16x16x4_f32 %" #ACC ", %" #B ", %" #A ", %" #ACC "\n\t"
+#define DLC_CHUNK_ROWS_F32 \
+    asm volatile( \
+    DLC_MFMA_F32(2, 22, 18) "ds_read_b128 %0, %26 offset:%27\n\t" DLC_MFMA_F32(3, 23, 18) \
+    "ds_read_b128 %1, %26 offset:%28\n\t" DLC_MFMA_F32(4, 24, 18) DLC_MFMA_F32(5, 25, 18) DLC_MFMA_F32(6, 22, 19) \
+    "s_add_u32 m0, %31, %32\n\t" DLC_MFMA_F32(7, 23, 19) "buffer_load_dwordx4 %29, %30, 0 offen lds\n\t" \
+    DLC_MFMA_F32(8, 24, 19) DLC_MFMA_F32(9, 25, 19) DLC_MFMA_F32(10, 22, 20) DLC_MFMA_F32(11, 23, 20) \
+    DLC_MFMA_F32(12, 24, 20) DLC_MFMA_F32(13, 25, 20) DLC_MFMA_F32(14, 22, 21) DLC_MFMA_F32(15, 23, 21) \
+    DLC_MFMA_F32(16, 24, 21) DLC_MFMA_F32(17, 25, 21) "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(next[0]), "=&v"(next[1]), \
+      "+a"(acc[0][0]), "+a"(acc[0][1]), "+a"(acc[0][2]), "+a"(acc[0][3]), \
+      "+a"(acc[1][0]), "+a"(acc[1][1]), "+a"(acc[1][2]), "+a"(acc[1][3]), \
+      "+a"(acc[2][0]), "+a"(acc[2][1]), "+a"(acc[2][2]), "+a"(acc[2][3]), \
+      "+a"(acc[3][0]), "+a"(acc[3][1]), "+a"(acc[3][2]), "+a"(acc[3][3]) \
+    : "v"(a[0][K]), "v"(a[1][K]), "v"(a[2][K]), "v"(a[3][K]), "v"(b[0][K]), "v"(b[1][K]), "v"(b[2][K]), "v"(b[3][K]), \
+      "v"(from[0]), "i"(OFF), "i"(OFF + STEP), "v"(to.v0), "s"(to.s0), "s"(to.at), "i"(I * 4096) \
+    : "memory", "m0", "scc")
+#define DLC_CHUNK_COLS_F32 \
+    asm volatile( \
+    DLC_MFMA_F32(8, 28, 24) "ds_read_b32 %0, %32 offset:%34\n\t" DLC_MFMA_F32(9, 29, 24) \
+    "ds_read_b32 %1, %32 offset:%35\n\t" DLC_MFMA_F32(10, 30, 24) "ds_read_b32 %2, %32 offset:%36\n\t" \
+    DLC_MFMA_F32(11, 31, 24) "ds_read_b32 %3, %32 offset:%37\n\t" DLC_MFMA_F32(12, 28, 25) \
+    "ds_read_b32 %4, %33 offset:%34\n\t" DLC_MFMA_F32(13, 29, 25) "ds_read_b32 %5, %33 offset:%35\n\t" \
+    DLC_MFMA_F32(14, 30, 25) "ds_read_b32 %6, %33 offset:%36\n\t" DLC_MFMA_F32(15, 31, 25) \
+    "ds_read_b32 %7, %33 offset:%37\n\t" DLC_MFMA_F32(16, 28, 26) DLC_MFMA_F32(17, 29, 26) \
+    "s_add_u32 m0, %40, %41\n\t" DLC_MFMA_F32(18, 30, 26) "buffer_load_dwordx4 %38, %39, 0 offen lds\n\t" \
+    DLC_MFMA_F32(19, 31, 26) DLC_MFMA_F32(20, 28, 27) DLC_MFMA_F32(21, 29, 27) DLC_MFMA_F32(22, 30, 27) \
+    DLC_MFMA_F32(23, 31, 27) "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(h0), "=&v"(h1), "=&v"(h2), "=&v"(h3), "=&v"(h4), "=&v"(h5), "=&v"(h6), "=&v"(h7), \
+      "+a"(acc[0][0]), "+a"(acc[0][1]), "+a"(acc[0][2]), "+a"(acc[0][3]), \
+      "+a"(acc[1][0]), "+a"(acc[1][1]), "+a"(acc[1][2]), "+a"(acc[1][3]), \
+      "+a"(acc[2][0]), "+a"(acc[2][1]), "+a"(acc[2][2]), "+a"(acc[2][3]), \
+      "+a"(acc[3][0]), "+a"(acc[3][1]), "+a"(acc[3][2]), "+a"(acc[3][3]) \
+    : "v"(a[0][K]), "v"(a[1][K]), "v"(a[2][K]), "v"(a[3][K]), "v"(b[0][K]), "v"(b[1][K]), "v"(b[2][K]), "v"(b[3][K]), \
+      "v"(from[0]), "v"(from[1]), "i"(OFF), "i"(OFF + STEP), "i"(OFF + 2 * STEP), "i"(OFF + 3 * STEP), "v"(to.v0), "s"(to.s0), "s"(to.at), "i"(I * 4096) \
+    : "memory", "m0", "scc")
+
+// fp32: 16 products of 16 x 16 x 4, of value K of every fragment; two fragments are read and load I is started
+template <bool COLS, int K, int OFF, int STEP, int I>
+__device__ __forceinline__ void chunk16_f32(f32x4 (&acc)[4][4], const u32x4_t* a, const u32x4_t* b, u32x4_t* next, const uint32_t* from,
+                                            const LoadTo& to) {
+    if constexpr (!COLS) {
+        DLC_CHUNK_ROWS_F32;
+    } else {
+        uint32_t h0, h1, h2, h3, h4, h5, h6, h7;
+        DLC_CHUNK_COLS_F32;
+        next[0] = u32x4_t{h0, h1, h2, h3};
+        next[1] = u32x4_t{h4, h5, h6, h7};
+    }
+}
+#undef DLC_CHUNK_ROWS_F32
+#undef DLC_CHUNK_COLS_F32
+#undef DLC_MFMA_F32
 #pragma clang diagnostic pop
 
 // The sums are in their registers: products that assembly started are not known to the compiler
@@ -574,7 +632,11 @@ __device__ __forceinline__ void keep(P& p) {
     for (int i = 0; i < P::COUNT; ++i) asm volatile("" : "+v"(p.a[i]));
 }
 
-constexpr int kWideLds = 160 * 1024;  // all of a compute unit's
+// ... and of gemm_wide's: all of a compute unit's, in fp32 half of it
+template <typename T>
+constexpr int wide_lds() {
+    return sizeof(T) == 2 ? 160 * 1024 : 80 * 1024;
+}
 
 // LDS of a work-group: with k along the rows three slots for A and two or three for B, otherwise four for both
 template <typename T, int LAY, int BM, int BN>
@@ -582,7 +644,7 @@ constexpr int gemm_lds() {
     return LAY == L_KK ? 3 * BM * 128 + (BM == 64 ? 3 : 2) * BN * 128 : 4 * (BM + BN) * 64;
 }
 
-// Tile `wg` of `total` of a product (the tiles of every cut of k), 128 x 128 or 64 x 128
+// Tile `wg` of `total` of a product (the tiles of every cut of k), 128 x 128 (half precision) or 64 x 128
 template <typename T, int LAY, int BM, int BN, bool GATED>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total, char* const lds) {
     constexpr int WAVES = 4, THREADS = 256;
@@ -704,13 +766,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& ga, int wg, int total,
         write_block<T, GATED, RM>(ga, &acc[h * (RM / 16)], 0, lds + wave * RM * 256, m0 + wm + h * RM, n0 + (GATED ? wn / 2 : wn), sp, lane);
 }
 
-// The same with 256 x 256 of C, half precision: four wavefronts, one on each SIMD, with 128 x 128 each.  While a step's (32
-// k values) fragments are multiplied the next step's are read; a step's loads go to the slots that all have read.  One
+// The same with 256 x 256 of C in half precision, 128 x 128 in fp32: four wavefronts, each with a quarter.  While a step's (64
+// bytes of k) fragments are multiplied the next step's are read; a step's loads go to the slots that all have read.  One
 // barrier a step (k along both rows: every two): it stands behind a wait for the tile that is read next, whose loads were
 // started two to four steps before.
 template <typename T, int LAY, bool GATED>
 __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total, char* const lds) {
-    constexpr int THREADS = 256, W = 256, MI = 8, NJ = 8;
+    constexpr bool F32 = std::is_same<T, float>::value;
+    constexpr int THREADS = 256, W = F32 ? 128 : 256, P = W / 2, MI = P / 16, NJ = MI;
+    constexpr int D = F32 ? 1 : 2;  // loads a chunk
     // k along a row: tiles of 128 bytes of it (whole cache lines), two steps each; down a column: of 64
     constexpr bool CA = LAY == L_TT, CB = LAY != L_KK;
     constexpr int TA = CA ? 64 : 128, TBB = CB ? 64 : 128;
@@ -718,7 +782,8 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
     using OpB = Operand<T, CB, W, TBB, THREADS, GATED>;
     constexpr int SLOTS_A = CA ? 4 : 3, SLOTS_B = CB ? 4 : 2;
     constexpr int A0 = 0, B0 = SLOTS_A * OpA::BYTES;
-    static_assert(B0 + SLOTS_B * OpB::BYTES <= kWideLds, "slots");
+    static_assert(B0 + SLOTS_B * OpB::BYTES <= wide_lds<T>(), "slots");
+    static_assert((CA ? 2 : 4) * D == OpA::PASSES && (CB ? 2 : 4) * D == OpB::PASSES, "loads");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn, sp;
@@ -729,7 +794,7 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
     OpB ob;
     oa.init(ga.a, ga.lda, m0, ga.M, k0, k1, tid);
     ob.init(ga.b, ga.ldb, n0, ga.N, k0, k1, tid);
-    const int wm = (wave >> 1) * 128, wn = (wave & 1) * 128;
+    const int wm = (wave >> 1) * P, wn = (wave & 1) * P;
 
     f32x4 acc[MI][NJ];
 #pragma unroll
@@ -738,9 +803,9 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     struct { u32x4_t a[MI], b[NJ]; } f[2];
     const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds, mine = at + (uint32_t)wave * 1024u;
-    constexpr int SA = CA ? 4 * OpA::CPR * 16 : 16 * TA, SB = CB ? 4 * OpB::CPR * 16 : 16 * TBB;
-    constexpr int RA = CA ? 0 : 4 * SA, RB = CB ? 0 : 4 * SB;  // to the second four blocks (columns: at addresses of their own)
-    constexpr int NA = CA ? 4 : 0, NB = CB ? 4 : 0;
+    constexpr int SA = CA ? (F32 ? 1 : 4) * OpA::CPR * 16 : 16 * TA, SB = CB ? (F32 ? 1 : 4) * OpB::CPR * 16 : 16 * TBB;
+    constexpr int R = MI / 2;  // blocks whose fragments a chunk reads; to the next ones: (columns: at addresses of their own)
+    constexpr int RA = CA ? 0 : R * SA, RB = CB ? 0 : R * SB, NA = CA ? R : 0, NB = CB ? R : 0;
     typename OpA::template Place<MI> pa[CA ? 2 : 1];
     typename OpB::template Place<NJ> pb[CB ? 2 : 1];
 #pragma unroll
@@ -753,22 +818,31 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
         OpB::template place<NJ>(pb[h], at + B0 + h * 2 * OpB::BYTES, wn, lane);
         keep(pb[h]);
     }
-    // 64 products with c's fragments, while n's are read from ra and rb; l0 .. l3: where the four chunks' loads go, w0 .. w3:
+    // A step's products with c's fragments, while n's are read from ra and rb; l0 .. l3: where the four chunks' loads go, w0 .. w3:
     // which of their tile's they are
     auto multiply = [&](auto& c, auto& n, const uint32_t* ra, const uint32_t* rb, auto off_a, auto off_b, const auto& l0, const auto& l1,
                         const auto& l2, const auto& l3, auto w0, auto w1, auto w2, auto w3) {
         constexpr int OA = decltype(off_a)::value, OB = decltype(off_b)::value;
-        chunk16<T, CB, OB, SB, decltype(w0)::value>(acc[0], acc[1], c.a[0], c.a[1], c.b, n.b, rb, l0);
-        chunk16<T, CB, OB + RB, SB, decltype(w1)::value>(acc[2], acc[3], c.a[2], c.a[3], c.b, n.b + 4, rb + NB, l1);
-        chunk16<T, CA, OA, SA, decltype(w2)::value>(acc[4], acc[5], c.a[4], c.a[5], c.b, n.a, ra, l2);
-        chunk16<T, CA, OA + RA, SA, decltype(w3)::value>(acc[6], acc[7], c.a[6], c.a[7], c.b, n.a + 4, ra + NA, l3);
+        if constexpr (F32) {
+            chunk16_f32<CB, 0, OB, SB, decltype(w0)::value>(acc, c.a, c.b, n.b, rb, l0);
+            chunk16_f32<CB, 1, OB + RB, SB, decltype(w1)::value>(acc, c.a, c.b, n.b + R, rb + NB, l1);
+            chunk16_f32<CA, 2, OA, SA, decltype(w2)::value>(acc, c.a, c.b, n.a, ra, l2);
+            chunk16_f32<CA, 3, OA + RA, SA, decltype(w3)::value>(acc, c.a, c.b, n.a + R, ra + NA, l3);
+        } else {
+            chunk16<T, CB, OB, SB, decltype(w0)::value>(acc[0], acc[1], c.a[0], c.a[1], c.b, n.b, rb, l0);
+            chunk16<T, CB, OB + RB, SB, decltype(w1)::value>(acc[2], acc[3], c.a[2], c.a[3], c.b, n.b + R, rb + NB, l1);
+            chunk16<T, CA, OA, SA, decltype(w2)::value>(acc[4], acc[5], c.a[4], c.a[5], c.b, n.a, ra, l2);
+            chunk16<T, CA, OA + RA, SA, decltype(w3)::value>(acc[6], acc[7], c.a[6], c.a[7], c.b, n.a + R, ra + NA, l3);
+        }
     };
     constexpr std::integral_constant<int, 0> i0{};
     constexpr std::integral_constant<int, 1> i1{};
     constexpr std::integral_constant<int, 2> i2{};
     constexpr std::integral_constant<int, 3> i3{};
-    // loads 2 i and 2 i + 1 of the operand's current tile to the slot at `slot`
-    auto to = [&](const auto& o, int i, uint32_t slot) { return LoadTo{o.voff[2 * i], o.voff[2 * i + 1], o.source(0), o.source(1), mine + slot}; };
+    // a chunk's loads, D i to D i + D - 1 of the operand's current tile, to the slot at `slot` (fp32: one, of either source)
+    auto to = [&](const auto& o, int i, uint32_t slot) {
+        return LoadTo{o.voff[D * i], o.voff[D * i + D - 1], o.source(D == 1 ? i % 2 : 0), o.source(1), mine + slot};
+    };
 
     if constexpr (LAY == L_KK) {
         const int tiles = (k1 - k0 + OpA::BK - 1) / OpA::BK;
@@ -806,18 +880,18 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
         const int steps = (k1 - k0 + OpB::BK - 1) / OpB::BK;
         uint32_t sa = 0;
         oa.mask();
-        oa.template load<0, 4>(lds, tid);
+        oa.template load<0, 2 * D>(lds, tid);
         ob.fetch(lds + B0, tid);
-        oa.template load<4, 4>(lds, tid);
+        oa.template load<2 * D, 2 * D>(lds, tid);
         oa.advance();
         ob.fetch(lds + B0 + OpB::BYTES, tid);
         oa.mask();
-        oa.template load<0, 4>(lds + OpA::BYTES, tid);
+        oa.template load<0, 2 * D>(lds + OpA::BYTES, tid);
         ob.fetch(lds + B0 + 2 * OpB::BYTES, tid);
-        oa.template load<4, 4>(lds + OpA::BYTES, tid);
+        oa.template load<2 * D, 2 * D>(lds + OpA::BYTES, tid);
         oa.advance();
         ob.fetch(lds + B0 + 3 * OpB::BYTES, tid);
-        wait_loads<20>();
+        wait_loads<10 * D>();
         bare_barrier();
         OpB::template frags<NJ, 0>(f[0].b, pb[0]);
         read_rows<MI, SA, 0>(f[0].a, pa[0].a[0]);
@@ -827,7 +901,7 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
             constexpr std::integral_constant<int, X % 2 * OpB::BYTES> off{};
             constexpr uint32_t slot_b = B0 + S * OpB::BYTES;
             if constexpr (S % 2 == 0) {
-                wait_loads<16>();
+                wait_loads<8 * D>();
                 bare_barrier();
                 const uint32_t slot_a = sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES;
                 const uint32_t ra = pa[0].a[1] + sa;
@@ -835,7 +909,7 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
                 ob.mask();
                 multiply(f[0], f[1], &ra, pb[X / 2].a, i0, off, to(oa, 0, slot_a), to(oa, 1, slot_a), to(ob, 0, slot_b), to(ob, 1, slot_b), i0, i1, i0, i1);
             } else {
-                wait_loads<12>();
+                wait_loads<6 * D>();
                 bare_barrier();
                 const uint32_t slot_a = sa == 0 ? 2 * OpA::BYTES : sa - OpA::BYTES;
                 sa = sa == 2 * OpA::BYTES ? 0 : sa + OpA::BYTES;
@@ -888,11 +962,15 @@ __device__ __forceinline__ void gemm_wide(const GemmArgs& ga, int wg, int total,
     wait_loads<0>();  // (tiles past the last may still be on their way)
     settle(acc);
     __syncthreads();
-    static_assert(4 * 128 * 256 <= kWideLds, "room for the epilogue");
+    static_assert(4 * P * 256 <= wide_lds<T>(), "room for the epilogue");
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-        write_block<T, GATED, 128>(ga, acc, h * 4, lds + wave * 128 * 256, m0 + wm, n0 + (GATED ? wn / 2 + h * 32 : wn + h * 64), sp, lane);
+    for (int h = 0; h < P / 64; ++h)
+        write_block<T, GATED, P>(ga, acc, h * 4, lds + wave * P * 256, m0 + wm, n0 + (GATED ? wn / 2 + h * 32 : wn + h * 64), sp, lane);
 }
+
+// which of the tiles are gemm_wide's
+template <typename T, int TILE>
+constexpr bool kWide = TILE == (sizeof(T) == 2 ? 0 : 1);
 
 template <typename T, int LAY, int BM, int BN, bool GATED>
 __global__ __launch_bounds__(256, 2) void k_gemm(const GemmArgs ga) {
@@ -903,9 +981,9 @@ __global__ __launch_bounds__(256, 2) void k_gemm(const GemmArgs ga) {
 }
 
 template <typename T, int LAY, bool GATED>
-__global__ __launch_bounds__(256, 1) void k_gemm_wide(const GemmArgs ga) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 1 : 2) void k_gemm_wide(const GemmArgs ga) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ __attribute__((aligned(16))) char lds[kWideLds];
+    __shared__ __attribute__((aligned(16))) char lds[wide_lds<T>()];
     gemm_wide<T, LAY, GATED>(ga, blockIdx.x, gridDim.x, lds);
 #endif
 }
@@ -948,19 +1026,19 @@ template <typename T, int TILE>
 __global__ __launch_bounds__(256, TILE == 0 ? 1 : 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int BM = kTileM[TILE], BN = kTileN[TILE];
-    __shared__ __attribute__((aligned(16))) char lds[TILE == 0 ? kWideLds : gemm_lds<T, L_TT, BM, BN>()];
+    __shared__ __attribute__((aligned(16))) char lds[kWide<T, TILE> ? wide_lds<T>() : gemm_lds<T, L_TT, BM, BN>()];
     const int nw8 = (nw + 7) & ~7, nx8 = (nx + 7) & ~7;
     int b = blockIdx.x;
     if (b < nw8) {
         if (b >= nw) return;
-        if constexpr (TILE == 0) gemm_wide<T, L_TT, false>(gw, b, nw, lds);
+        if constexpr (kWide<T, TILE>) gemm_wide<T, L_TT, false>(gw, b, nw, lds);
         else gemm_tile<T, L_TT, BM, BN, false>(gw, b, nw, lds);
         return;
     }
     b -= nw8;
     if (b < nx8) {
         if (b >= nx) return;
-        if constexpr (TILE == 0) gemm_wide<T, L_KT, false>(gx, b, nx, lds);
+        if constexpr (kWide<T, TILE>) gemm_wide<T, L_KT, false>(gx, b, nx, lds);
         else gemm_tile<T, L_KT, BM, BN, false>(gx, b, nx, lds);
         return;
     }
@@ -1304,9 +1382,9 @@ __global__ __launch_bounds__(256) void k_drop(const DropArgs da) {
 template <typename T, int LAY, bool GT>
 static hipError_t gemm_pick(const GemmArgs& g, int tile, hipStream_t s) {
     const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * g.split)), block(256);
-    if (tile == 1) k_gemm<T, LAY, kTileM[1], kTileN[1], GT><<<grid, block, 0, s>>>(g);
+    if (tile == (sizeof(T) == 2 ? 0 : 1)) k_gemm_wide<T, LAY, GT><<<grid, block, 0, s>>>(g);
     else if (tile == 2) k_gemm<T, LAY, kTileM[2], kTileN[2], GT><<<grid, block, 0, s>>>(g);
-    else if constexpr (sizeof(T) == 2) k_gemm_wide<T, LAY, GT><<<grid, block, 0, s>>>(g);
+    else if constexpr (sizeof(T) == 2) k_gemm<T, LAY, kTileM[1], kTileN[1], GT><<<grid, block, 0, s>>>(g);
     return hipGetLastError();
 }
 
