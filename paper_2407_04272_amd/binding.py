@@ -176,12 +176,13 @@ def _stream_ptr(stream):
     global _raw_stream
     if _raw_stream is None:
         import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         if raw is not None:
-            _raw_stream = lambda: raw(torch.cuda.current_device())  # noqa: E731
+            torch.cuda.init()
+            _raw_stream = lambda: raw(device())  # noqa: E731
         else:
             _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
-    return C.c_void_p(_raw_stream())
+    return _raw_stream()
 
 
 def _np_ptr(a):
