@@ -404,7 +404,9 @@ int dlc_linear_forward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, co
  * Its backward pass:   dz = drop(dy) act'(z);   dx = dz w;   dw = dz' x;   dbias = column sums of dz
  *   d_pre as the forward call stored it (not read, may be NULL, if act is DLC_ACT_NONE)   d_dy [M][N]
  *   d_dx [M][K]   d_dw [N][K]   d_dbias [N]: each may be NULL and is then not computed.  The residual's gradient is dy.
- *   relu's slope at 0 is 0, and what is not finite in dy does not pass where the slope is 0.
+ *   relu's slope at 0 is 0.  A product with a factor of 0 -- a dropped element, a dy of 0, a slope of 0 -- is 0 whatever the
+ *   other factor holds, and values and slopes at infinite z are their limits: a z past the type's range, which d_pre holds
+ *   as an infinity, spoils nothing (but act(g) or u that are infinite themselves are factors of what they meet).
  */
 int dlc_linear_backward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_pre,
                         const void* d_dy, void* d_dx, void* d_dw, void* d_dbias, void* d_work, size_t work_bytes, void* stream);
@@ -412,7 +414,8 @@ int dlc_linear_backward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, c
  * Gated block:   [g | u] = x w' + bias;   y = drop(act(g) * u)
  *   d_w [2N][K]: the gate's N rows, then the other N   d_bias [2N] or NULL   d_y [M][N]   d_pre [M][2N] or NULL: [g | u]
  * Backward:   dh = drop(dy);   dz = [dh u act'(g) | dh act(g)];   dx = dz w;   dw = dz' x;   dbias = column sums of dz
- *   d_pre is required; d_dw [2N][K], d_dbias [2N]; outputs may be NULL as above
+ *   d_pre is required; d_dw [2N][K], d_dbias [2N]; outputs may be NULL, and factors of 0 and infinite pre-activations are
+ *   treated, as above
  */
 int dlc_gated_forward(const dlc_dense_config* cfg /*HOST*/, const void* d_x, const void* d_w, const void* d_bias, void* d_y,
                       void* d_pre, void* d_work, size_t work_bytes, void* stream);

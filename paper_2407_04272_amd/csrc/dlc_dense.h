@@ -204,6 +204,11 @@ __device__ __forceinline__ void act_values(int act, float (&z)[U][8]) {
     }
 }
 
+// A product that is 0 where a factor is, whatever the other one holds.  The backward pass is made of these: what a dropped or
+// closed element holds does not get out (in half precision a sum past the type's range is saved as an infinity), and values and
+// slopes at infinity come out as their limits.
+__device__ __forceinline__ float mul0(float a, float b) { return a == 0.0f || b == 0.0f ? 0.0f : a * b; }
+
 // values (into z) and slopes at z
 template <bool FAST>
 __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
@@ -227,8 +232,8 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float q = sigmoidf<FAST>(z[i]);
-                d[i] = q * (1.0f + z[i] * (1.0f - q));
-                z[i] *= q;
+                d[i] = mul0(q, 1.0f + mul0(z[i], 1.0f - q));
+                z[i] = mul0(z[i], q);
             }
             break;
         case DLC_ACT_GELU:
@@ -236,8 +241,8 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
             for (int i = 0; i < 8; ++i) {
                 float phi;
                 const float c = normal_cdf<FAST>(z[i], &phi);
-                d[i] = c + z[i] * phi;
-                z[i] *= c;
+                d[i] = c + mul0(z[i], phi);
+                z[i] = mul0(z[i], c);
             }
             break;
         default:

@@ -1307,10 +1307,10 @@ __global__ __launch_bounds__(32 * kDzRows) void k_dz(const DzArgs da, const Pack
                 for (int i = 0; i < 8; ++i) {
                     if constexpr (GATED) {
                         const float dh = d[i];
-                        d[i] = dh * u[i] * slope[i];
-                        u[i] = dh * z[i];
+                        d[i] = mul0(mul0(dh, u[i]), slope[i]);
+                        u[i] = mul0(dh, z[i]);
                     } else {
-                        d[i] = slope[i] == 0.0f ? 0.0f : d[i] * slope[i];  // (a gradient that is not finite does not pass a closed unit)
+                        d[i] = mul0(d[i], slope[i]);
                     }
                 }
             }
