@@ -160,6 +160,23 @@ __device__ __forceinline__ float sigmoidf(float z) {
     else return 1.0f / (1.0f + expf(-z));
 }
 
+// ... and its slope, which is even: e / (1 + e)^2 with e = exp(-|z|).  (q (1 - q) cancels: 6 % off at z = 16, 0 from 17 on.)
+template <bool FAST>
+__device__ __forceinline__ float sigmoid_both(float z, float* slope) {
+    const float x = __builtin_fabsf(z);
+    float e, r;
+    if constexpr (FAST) {
+        e = __builtin_amdgcn_exp2f(x * -1.44269504f);
+        r = __builtin_amdgcn_rcpf(1.0f + e);
+    } else {
+        e = expf(-x);
+        r = 1.0f / (1.0f + e);
+    }
+    const float p = e * r;  // sigmoid(-|z|)
+    *slope = p * r;
+    return z < 0.0f ? p : r;
+}
+
 // The normal distribution function at z, and (phi) its density.  FAST: erfc(x) = exp(-x^2) t P(t) with t = 1 / (1 + 0.45 x);
 // P is a least-squares fit of exp(x^2) erfc(x) / t over all x >= 0, reweighted towards equal relative errors: 1.4e-7 at most.
 template <bool FAST>
@@ -222,17 +239,14 @@ __device__ __forceinline__ void act_both(int act, float z[8], float d[8]) {
             break;
         case DLC_ACT_SIGMOID:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float q = sigmoidf<FAST>(z[i]);
-                z[i] = q;
-                d[i] = q * (1.0f - q);
-            }
+            for (int i = 0; i < 8; ++i) z[i] = sigmoid_both<FAST>(z[i], &d[i]);
             break;
         case DLC_ACT_SILU:
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float q = sigmoidf<FAST>(z[i]);
-                d[i] = mul0(q, 1.0f + mul0(z[i], 1.0f - q));
+                float slope;
+                const float q = sigmoid_both<FAST>(z[i], &slope);
+                d[i] = q + mul0(z[i], slope);
                 z[i] = mul0(z[i], q);
             }
             break;

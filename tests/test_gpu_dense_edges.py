@@ -186,3 +186,42 @@ def test_what_is_kept_shows():
     dy[7, 6] = -inf
     db = _call_backward("linear", "f32", "gelu", 0.0, x, w, pre, dy)[2]
     assert (~torch.isfinite(db)).nonzero().flatten().tolist() == [4, 6] and float(db[6]) == -inf
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("op", ["linear", "gated"])
+def test_slope_of_a_saturated_sigmoid(op, dtype):
+    """The slope e / (1 + e)^2, e = exp(-|z|), is even and keeps its digits far out.  Relative bound: the exponential's argument
+    is off by 2 units of 2^-24 of |z| log2 e (44 at most), the exponential and the reciprocal by 2 units each (the latter counts
+    twice), three products and a sum by one: 2 * 44 + 2 + 4 + 5 < 128.  One row, so that the bias gradient is dz itself."""
+    import torch
+    N = 1 << 13
+    lin = torch.linspace(0, 30, N // 2, device="cuda")
+    z = torch.cat((lin, -lin))[None].to(torch_type(dtype))
+    g = _gen(47)
+    dy = (_normal(g, dtype, 1, N, scale=0.1).float().abs() + 1).to(torch_type(dtype)) * 256
+    if op == "gated":
+        up = torch.full((1, N), 1.0, dtype=z.dtype, device="cuda")
+        z2 = torch.cat((z, up), 1)
+    x = torch.ones((1, 8), dtype=z.dtype, device="cuda")
+    w = torch.zeros((2 * N if op == "gated" else N, 8), dtype=z.dtype, device="cuda")
+    dx, dw, db = _call_backward(op, dtype, "sigmoid", 0.0, x, w, z2 if op == "gated" else z, dy)
+    e = torch.exp(-z[0].double().abs())
+    dz = dy[0].double() * e / (1 + e) ** 2
+    err = 128 * F32 * dz
+    assert_close(db[:N], dz, rounded(dz, err, dtype), f"{op} {dtype} dbias")
+    # (dw holds dz rounded to the type, times one)
+    assert_close(dw[:N, 0], dz, rounded(dz, err + rounded(dz, err, dtype), dtype), f"{op} {dtype} dw")
+    if op == "gated":
+        q = torch.sigmoid(z[0].double())
+        v = dy[0].double() * q
+        assert_close(db[N:], v, rounded(v, 128 * F32 * v, dtype), f"{op} {dtype} dbias of u")
+
+
+def test_a_saturated_sigmoid_is_not_closed():
+    """Its slope at 20 is 2e-9, not 0: what is not finite in dy shows."""
+    import torch
+    z, dy = torch.full((1, 8), 20.0, device="cuda"), torch.full((1, 8), float("inf"), device="cuda")
+    z[0, 4:] *= -1
+    x, w = torch.ones((1, 8), device="cuda"), torch.ones((8, 8), device="cuda")
+    assert bool(torch.isinf(_call_backward("linear", "f32", "sigmoid", 0.0, x, w, z, dy)[2]).all())
