@@ -192,18 +192,24 @@ def _np_ptr(a):
 # ---- dense operators: linear layers, gated blocks, dropout (no context; see include/dlc.h) ----
 def make_dense_config(dtype, rows, in_features, out_features, act=ACT_NONE, dropout_p=0.0, seed=0, offset=0, d_offset=None,
                       flags=0, ld_x=0, ld_w=0, ld_y=0, ld_pre=0, ld_res=0, ld_dy=0, ld_dx=0, ld_dw=0) -> DenseConfig:
-    """ld_*: elements from row to row, 0 for dense rows.  d_offset: an int64 tensor of one element on the GPU that the
-    kernels add to `offset` (a replayed graph counts it up), which has to live as long as the configuration."""
+    """ld_*: elements from row to row, 0 for dense rows.  d_offset: an int64 tensor on the GPU whose first element the kernels
+    add to `offset` (a replayed graph counts it up), which has to live as long as the configuration.  Raises DlcError."""
     return DenseConfig(dtype, act, flags, 0, rows, in_features, out_features, ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw,
-                       dropout_p, seed, offset, _ptr(d_offset))
+                       dropout_p, seed, offset, _counter(d_offset))
 
 
 def make_dropout_config(dtype, rows, cols, p, seed=0, offset=0, d_offset=None, ld_x=0, ld_res=0, ld_y=0) -> DropoutConfig:
-    return DropoutConfig(dtype, 0, rows, cols, ld_x, ld_res, ld_y, p, seed, offset, _ptr(d_offset))
+    return DropoutConfig(dtype, 0, rows, cols, ld_x, ld_res, ld_y, p, seed, offset, _counter(d_offset))
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _counter(t):
+    """The address of a counter that kernels read; None stays None."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype not in (torch.int64, torch.uint64) or not t.is_cuda or t.numel() < 1:
+        raise DlcError(EINVAL, f"d_offset: {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def dlc_linear_workspace_bytes(cfg: DenseConfig, backward: bool = False) -> int:
