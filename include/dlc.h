@@ -334,7 +334,8 @@ int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* tot
  * dlc_compress takes next -- linear layers with bias, activation, dropout and residual in the product's epilogue, gated
  * blocks, and dropout by itself, each with its backward pass.
  *
- * They take no context and keep no state.  Buffers, the workspace among them, are the caller's; a call only enqueues
+ * They take no context and keep no state.  Buffers, the workspace among them, are the caller's, on the GPU of `stream` (NULL:
+ * the current one; the Python binding refuses tensors of another); a call only enqueues
  * kernels on `stream` and may be recorded into a HIP graph.  Results do not depend on the run: sums that are cut are put
  * together in a fixed order, there are no floating-point atomics.
  *

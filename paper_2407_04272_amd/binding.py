@@ -48,12 +48,14 @@ class DenseConfig(C.Structure):
                 ("ld_pre", C.c_int64), ("ld_res", C.c_int64), ("ld_dy", C.c_int64), ("ld_dx", C.c_int64),
                 ("ld_dw", C.c_int64), ("dropout_p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64),
                 ("d_offset", C.c_void_p)]
+    counter = None  # the tensor behind d_offset
 
 
 class DropoutConfig(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
                 ("ld_x", C.c_int64), ("ld_res", C.c_int64), ("ld_y", C.c_int64), ("dropout_p", C.c_double),
                 ("seed", C.c_uint64), ("offset", C.c_uint64), ("d_offset", C.c_void_p)]
+    counter = None
 
 
 EXPORTS = ["dlc_create", "dlc_destroy", "dlc_compress_bound", "dlc_workspace_bytes", "dlc_stats",
@@ -166,23 +168,37 @@ def dlc_decompress_static(cfg: Config, d_comp, comp_bytes, d_payload_out, d_stat
                                        _stream_ptr(stream))
 
 
-_raw_stream = None
+def _find_current():
+    # the handle alone, where torch gives it: making its stream object took a third of a small call (2.7 of 7.6 us)
+    global _current
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    if raw is not None:
+        torch.cuda.init()
+
+        def _current():
+            d = device()
+            return d, raw(d)
+    else:
+        def _current():
+            s = torch.cuda.current_stream()
+            return s.device_index, s.cuda_stream
+    return _current()
+
+
+_current = _find_current  # () -> the current GPU, the handle of its current stream
+
+
+def _launch(stream):
+    """The GPU that a call on the stream (None: the current one) goes to, and the stream's handle"""
+    if stream is None:
+        return _current()
+    device = getattr(stream, "device_index", None)  # (an object with a handle alone: the current GPU's)
+    return _current()[0] if device is None else device, int(stream.cuda_stream)
 
 
 def _stream_ptr(stream):
-    if stream is not None:
-        return C.c_void_p(int(stream.cuda_stream))
-    # the handle alone, where torch gives it: making its stream object took a third of a small call (2.7 of 7.6 us)
-    global _raw_stream
-    if _raw_stream is None:
-        import torch
-        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-        if raw is not None:
-            torch.cuda.init()
-            _raw_stream = lambda: raw(device())  # noqa: E731
-        else:
-            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
-    return _raw_stream()
+    return _current()[1] if stream is None else C.c_void_p(int(stream.cuda_stream))
 
 
 def _np_ptr(a):
@@ -193,13 +209,17 @@ def _np_ptr(a):
 def make_dense_config(dtype, rows, in_features, out_features, act=ACT_NONE, dropout_p=0.0, seed=0, offset=0, d_offset=None,
                       flags=0, ld_x=0, ld_w=0, ld_y=0, ld_pre=0, ld_res=0, ld_dy=0, ld_dx=0, ld_dw=0) -> DenseConfig:
     """ld_*: elements from row to row, 0 for dense rows.  d_offset: an int64 tensor on the GPU whose first element the kernels
-    add to `offset` (a replayed graph counts it up), which has to live as long as the configuration.  Raises DlcError."""
-    return DenseConfig(dtype, act, flags, 0, rows, in_features, out_features, ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw,
-                       dropout_p, seed, offset, _counter(d_offset))
+    add to `offset` (a replayed graph counts it up).  Raises DlcError."""
+    cfg = DenseConfig(dtype, act, flags, 0, rows, in_features, out_features, ld_x, ld_w, ld_y, ld_pre, ld_res, ld_dy, ld_dx, ld_dw,
+                      dropout_p, seed, offset, _counter(d_offset))
+    cfg.counter = d_offset
+    return cfg
 
 
 def make_dropout_config(dtype, rows, cols, p, seed=0, offset=0, d_offset=None, ld_x=0, ld_res=0, ld_y=0) -> DropoutConfig:
-    return DropoutConfig(dtype, 0, rows, cols, ld_x, ld_res, ld_y, p, seed, offset, _counter(d_offset))
+    cfg = DropoutConfig(dtype, 0, rows, cols, ld_x, ld_res, ld_y, p, seed, offset, _counter(d_offset))
+    cfg.counter = d_offset
+    return cfg
 
 
 def _counter(t):
@@ -223,23 +243,29 @@ def dlc_gated_workspace_bytes(cfg: DenseConfig, backward: bool = False) -> int:
 _torch_types = ()
 
 
-def _dense_type(cfg):
-    """The torch type of the configuration's matrices."""
+def _where(cfg, stream):
+    """What a call's tensors have to be: the type of the configuration's matrices and the GPU that the call goes to; and the
+    stream's handle."""
     global _torch_types
     if not _torch_types:
         import torch
         _torch_types = (torch.float32, torch.float16, torch.bfloat16)
-    if not 0 <= cfg.dtype < len(_torch_types):
-        raise DlcError(EINVAL, f"dtype {cfg.dtype}")
-    return _torch_types[cfg.dtype]
+    dtype, counter = cfg.dtype, cfg.counter
+    if not 0 <= dtype < 3:
+        raise DlcError(EINVAL, f"dtype {dtype}")
+    device, handle = _current() if stream is None else _launch(stream)
+    if counter is not None and counter.get_device() != device:
+        raise DlcError(EINVAL, f"d_offset: on {counter.device}, not on GPU {device}")
+    return (_torch_types[dtype], device), handle
 
 
-def _matrix(name, t, dtype, rows, cols, ld):
+def _matrix(name, t, want, rows, cols, ld):
     """The tensor's address; None stays None.  What the configuration says of it has to be true of it."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda:
-        raise DlcError(EINVAL, f"{name}: {t.dtype} on {t.device}")
+    dtype, device = want
+    if t.dtype is not dtype or t.get_device() != device:
+        raise DlcError(EINVAL, f"{name}: {t.dtype} on {t.device}, not {dtype} on GPU {device}")
     if t.shape != (rows, cols):
         raise DlcError(EINVAL, f"{name}: shape {tuple(t.shape)}, not {(rows, cols)}")
     if ld in (0, cols) and t.is_contiguous():
@@ -251,54 +277,54 @@ def _matrix(name, t, dtype, rows, cols, ld):
     return t.data_ptr()
 
 
-def _vector(name, t, dtype, n):
+def _vector(name, t, want, n):
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_cuda or t.shape != (n,) or not t.is_contiguous():
+    if t.dtype is not want[0] or t.get_device() != want[1] or t.shape != (n,) or not t.is_contiguous():
         raise DlcError(EINVAL, f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _work(t):
+def _work(t, want):
     if t is None:
         return None, 0
-    if not t.is_cuda or not t.is_contiguous():
-        raise DlcError(EINVAL, "workspace: not a contiguous tensor on the GPU")
+    if t.get_device() != want[1] or not t.is_contiguous():
+        raise DlcError(EINVAL, f"workspace: not a contiguous tensor on GPU {want[1]}")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
 def dlc_linear_forward(cfg: DenseConfig, x, w, bias, residual, y, pre=None, work=None, stream=None):
     """y = drop(act(x w' + bias)) + residual; pre, if given, gets x w' + bias.  Raises DlcError."""
-    ty = _dense_type(cfg)
+    ty, st = _where(cfg, stream)
     M, K, N = cfg.rows, cfg.in_features, cfg.out_features
-    wk, nb = _work(work)
+    wk, nb = _work(work, ty)
     _check(lib().dlc_linear_forward(
         C.byref(cfg), _matrix("x", x, ty, M, K, cfg.ld_x), _matrix("w", w, ty, N, K, cfg.ld_w),
         _vector("bias", bias, ty, N), _matrix("residual", residual, ty, M, N, cfg.ld_res),
-        _matrix("y", y, ty, M, N, cfg.ld_y), _matrix("pre", pre, ty, M, N, cfg.ld_pre), wk, nb, _stream_ptr(stream)),
+        _matrix("y", y, ty, M, N, cfg.ld_y), _matrix("pre", pre, ty, M, N, cfg.ld_pre), wk, nb, st),
         "dlc_linear_forward")
 
 
 def dlc_gated_forward(cfg: DenseConfig, x, w, bias, y, pre=None, work=None, stream=None):
     """[g | u] = x w' + bias; y = drop(act(g) u); pre, if given, gets [g | u].  Raises DlcError."""
-    ty = _dense_type(cfg)
+    ty, st = _where(cfg, stream)
     M, K, N = cfg.rows, cfg.in_features, cfg.out_features
-    wk, nb = _work(work)
+    wk, nb = _work(work, ty)
     _check(lib().dlc_gated_forward(
         C.byref(cfg), _matrix("x", x, ty, M, K, cfg.ld_x), _matrix("w", w, ty, 2 * N, K, cfg.ld_w),
         _vector("bias", bias, ty, 2 * N), _matrix("y", y, ty, M, N, cfg.ld_y),
-        _matrix("pre", pre, ty, M, 2 * N, cfg.ld_pre), wk, nb, _stream_ptr(stream)), "dlc_gated_forward")
+        _matrix("pre", pre, ty, M, 2 * N, cfg.ld_pre), wk, nb, st), "dlc_gated_forward")
 
 
 def _dense_backward(name, cfg, wide, x, w, pre, dy, dx, dw, dbias, work, stream):
-    ty = _dense_type(cfg)
+    ty, st = _where(cfg, stream)
     M, K, N = cfg.rows, cfg.in_features, cfg.out_features
-    wk, nb = _work(work)
+    wk, nb = _work(work, ty)
     _check(getattr(lib(), name)(
         C.byref(cfg), _matrix("x", x, ty, M, K, cfg.ld_x), _matrix("w", w, ty, wide, K, cfg.ld_w),
         _matrix("pre", pre, ty, M, wide, cfg.ld_pre), _matrix("dy", dy, ty, M, N, cfg.ld_dy),
         _matrix("dx", dx, ty, M, K, cfg.ld_dx), _matrix("dw", dw, ty, wide, K, cfg.ld_dw),
-        _vector("dbias", dbias, ty, wide), wk, nb, _stream_ptr(stream)), name)
+        _vector("dbias", dbias, ty, wide), wk, nb, st), name)
 
 
 def dlc_linear_backward(cfg: DenseConfig, x, w, pre, dy, dx, dw, dbias, work=None, stream=None):
@@ -313,11 +339,11 @@ def dlc_gated_backward(cfg: DenseConfig, x, w, pre, dy, dx, dw, dbias, work=None
 
 def dlc_dropout(cfg: DropoutConfig, x, residual, y, stream=None):
     """y = drop(x) + residual (None: without); the gradient is the same call on the gradient of y.  Raises DlcError."""
-    ty = _dense_type(cfg)
+    ty, st = _where(cfg, stream)
     M, N = cfg.rows, cfg.cols
     _check(lib().dlc_dropout(C.byref(cfg), _matrix("x", x, ty, M, N, cfg.ld_x),
                              _matrix("residual", residual, ty, M, N, cfg.ld_res), _matrix("y", y, ty, M, N, cfg.ld_y),
-                             _stream_ptr(stream)), "dlc_dropout")
+                             st), "dlc_dropout")
 
 
 class Context:
