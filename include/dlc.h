@@ -348,8 +348,8 @@ int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* tot
  *              workspace (with up to 16 rows a forward call never copies).  Weights that are used often are best kept with
  *              a leading dimension and a row length on such boundaries.
  *   sizes      rows 0 .. 2^30, features 1 .. 2^20 (a gated block's out_features to 2^19), leading dimensions up to 2^20;
- *              results of fewer than 2^41 elements.  With no rows a forward call does
- *              nothing and a backward call writes zero weight and bias gradients.
+ *              results of fewer than 2^24 tiles of 128 x 128 elements (half precision: 256 x 256).  With no rows a forward
+ *              call does nothing and a backward call writes zero weight and bias gradients.
  *   drop(v)    of the element in row r and column c: 0 if its 16 random bits are below t = round(65536 p), else
  *              v * 65536 / (65536 - t).  The bits are half words, low half first, of Philox4x32-10 (Salmon et al., SC 2011)
  *              with key `seed` and counter (c / 8, r, offset low, offset high): half word c % 8.  No mask is stored; a

@@ -15,6 +15,10 @@ struct Shape {
 };
 
 constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 20;
+// a launch's threads, work-groups of 256, are counted in 32 bits
+constexpr int64_t kMaxGroups = int64_t(1) << 24;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 bool good_ld(int64_t& ld, int64_t row) {
     if (ld == 0) ld = row;
@@ -45,16 +49,15 @@ bool make_shape(const dlc_dense_config* c, bool gated, Shape* s) {
     s->off_boundary = (c->flags & DLC_DENSE_OFF_BOUNDARY) != 0;
     s->gated = gated;
     s->es = c->dtype == DLC_F32 ? 4 : 2;
-    // a launch's work-groups are counted in 31 bits, 64 x 128 elements of the result each at least
-    const int64_t wmax = wide > s->K ? wide : s->K;
-    if ((s->M / 64 + 1) * (wmax / 128 + 1) >= (int64_t(1) << 28)) return false;
+    // the results of every product fit a launch with the type's largest tile (plan_gemm leaves tiles out that do not)
+    const int64_t side = kTileM[s->es == 4 ? 1 : 0], tm = div_up(s->M, side), tk = div_up(s->K, side), tw = div_up(wide, side);
+    if (tm * tw >= kMaxGroups || tm * tk >= kMaxGroups || tw * tk >= kMaxGroups) return false;
     return dropout_params(c->dropout_p, &s->thr, &s->scale);
 }
 
 bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 bool rows16(const void* p, int64_t ld, int es) { return on(p, 16) && (ld * es) % 16 == 0; }
 
-int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t a256(size_t v) { return (v + 255) & ~size_t(255); }
 
 // ---- choice of tile and cut ---------------------------------------------------------------------
@@ -109,6 +112,7 @@ Plan plan_gemm(int64_t M, int64_t N, int64_t K, bool gated, Layout lay, int es) 
     for (int tile = es == 4 ? 1 : 0; tile < 3; ++tile) {
         const TileCost& c = cost[tile];
         const int64_t tiles = div_up(p.M, kTileM[tile]) * div_up(p.wide, kTileN[tile]);
+        if (tiles >= kMaxGroups) continue;
         const int fit = tile == 0 ? 1 : tile == 1 || lay == L_KK ? 2 : 3;  // work-groups that share a compute unit
         for (const int cut : kCuts) {
             if (cut > 1 && (p.steps < 2 * cut || tiles * cut > 4 * kUnits)) break;
@@ -337,10 +341,14 @@ int backward(const dlc_dense_config* c, const Shape& s, const void* x, const voi
     gw.M = (int)wide; gw.N = (int)s.K; gw.K = (int)s.M;
     gw.e.y = dw; gw.e.ld_y = s.lddw; gw.e.n = (int)s.K;
     const auto join = [&](const JoinArgs& ja, const JoinArgs& jb) { return DenseOps<T>::join(ja, jb, sum, st) == hipSuccess ? DLC_OK : DLC_EHIP; };
-    if (s.M == 0) {  // (an empty sum: a product with no cut at all)
-        JoinArgs j{};
-        if (dw) j = JoinArgs{nullptr, 0, gw.M, 0, 0, gw.e};
-        return dw || dbias ? join(j, JoinArgs{}) : DLC_OK;
+    if (s.M == 0) {  // (an empty sum: a product with no cut at all, as many rows at a time as a launch has threads for)
+        const int64_t most = kMaxGroups / 2 * 256 / div_up(s.K, 8);
+        for (int64_t r = 0; dw && r < wide; r += most) {
+            JoinArgs j{nullptr, 0, (int)(wide - r < most ? wide - r : most), 0, 0, gw.e};
+            j.e.y = static_cast<char*>(dw) + r * s.lddw * s.es;
+            if (DenseOps<T>::join(j, JoinArgs{}, SumArgs{}, st) != hipSuccess) return DLC_EHIP;
+        }
+        return dbias ? join(JoinArgs{}, JoinArgs{}) : DLC_OK;
     }
     if (dx && dw && b.both) {
         set_plan(&gx, b.bx, wk + b.off_part);

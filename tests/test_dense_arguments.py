@@ -125,3 +125,11 @@ def test_a_counter_on_another_gpu():
                 _refused(call)
             else:
                 call()
+
+
+def test_results_that_no_launch_covers():
+    from paper_2407_04272_amd import binding as b
+    mk, size = b.make_dense_config, b.dlc_linear_workspace_bytes
+    assert size(mk(b.F32, 1 << 30, 4, 128), True) > 0 and size(mk(b.F32, 1 << 30, 4, 129), True) == 0
+    assert size(mk(b.F16, 1 << 30, 4, 768), True) > 0 and size(mk(b.F16, 1 << 30, 4, 769), True) == 0
+    assert size(mk(b.F16, 64, 1 << 20, 1 << 20), True) == 0
