@@ -356,13 +356,13 @@ int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* tot
  *              backward call with the same seed and offset drops the same elements.  A dropped element is 0 whatever
  *              its value.  d_offset, if not NULL, is a DEVICE word that the kernels read and add to `offset`: a graph that
  *              is replayed takes other bits by counting it up.
- *   overlap    d_residual may be d_y; d_x may be d_y in dlc_dropout (with equal leading dimensions).  No other output
- *              may overlap an input, another output or the workspace.
+ *   overlap    d_residual may be d_y, and d_x in dlc_dropout, with equal leading dimensions (else DLC_EINVAL).  No other
+ *              output may overlap an input, another output or the workspace.
  *   d_work     16-byte aligned, work_bytes at least dlc_*_workspace_bytes of the configuration and direction (else
  *              DLC_ECAPACITY); may be NULL where that is 0.  The room for copies of x and w counts in where the row
  *              length or the leading dimension asks for them; if only a pointer is off a 16-byte boundary, set
  *              DLC_DENSE_OFF_BOUNDARY, which counts them in for any pointers.  Not initialised, not kept: calls in order on a stream share it.
- * Return values: DLC_OK, DLC_EINVAL (geometry, null or misaligned pointer, p outside [0, 1]), DLC_ECAPACITY, DLC_EHIP.
+ * Return values: DLC_OK, DLC_EINVAL (geometry, null or misaligned pointer, p outside [0, 1], overlap as above), DLC_ECAPACITY, DLC_EHIP.
  */
 enum { DLC_ACT_NONE = 0, DLC_ACT_RELU = 1, DLC_ACT_SIGMOID = 2, DLC_ACT_SILU = 3 /* z sigmoid(z) */,
        DLC_ACT_GELU = 4 /* z/2 (1 + erf(z / sqrt 2)) */ };

@@ -366,6 +366,9 @@ int backward(const dlc_dense_config* c, const Shape& s, const void* x, const voi
 // d is there if `need`, and lies on an element's boundary
 bool good_ptr(const void* d, int es, bool need) { return d ? on(d, es) : !need; }
 
+// y may take the place of `in` element for element, not with other distances from row to row
+bool good_place(const void* in, int64_t ld_in, const void* y, int64_t ld_y, int64_t rows) { return in != y || ld_in == ld_y || rows <= 1; }
+
 // the workspace a forward call needs: the product's partial sums, packed operands (a pass over few rows takes them as they are)
 size_t forward_bytes(const Shape& s, const Plan& p) { return s.M <= kSkinnyOddRows ? 0 : a256(p.bytes) + pack_room(s); }
 
@@ -385,6 +388,7 @@ int forward_any(const dlc_dense_config* c, bool gated, const void* x, const void
     if (!good_ptr(x, s.es, need) || !good_ptr(w, s.es, need) || !good_ptr(bias, s.es, false) || !good_ptr(res, s.es, false) ||
         !good_ptr(y, s.es, need) || !good_ptr(pre, s.es, false) || !on(c->d_offset, 8)) return DLC_EINVAL;
     if (!need) return DLC_OK;
+    if (!good_place(res, s.ldres, y, s.ldy, s.M)) return DLC_EINVAL;
     const Plan p = plan_forward(s);
     if (const int rc = check_work(forward_bytes(s, p), work, &bytes); rc != DLC_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
@@ -460,6 +464,7 @@ extern "C" int dlc_dropout(const dlc_dropout_config* c, const void* x, const voi
     const bool need = c->rows > 0;
     if (!good_ptr(x, es, need) || !good_ptr(res, es, false) || !good_ptr(y, es, need) || !on(c->d_offset, 8)) return DLC_EINVAL;
     if (!need) return DLC_OK;
+    if (!good_place(x, d.ld_x, y, d.ld_y, c->rows) || !good_place(res, d.ld_res, y, d.ld_y, c->rows)) return DLC_EINVAL;
     d.x = x; d.res = res; d.y = y;
     d.seed = c->seed; d.offset = c->offset; d.d_offset = c->d_offset;
     hipStream_t st = (hipStream_t)stream;
