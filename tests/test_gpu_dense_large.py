@@ -51,3 +51,58 @@ def test_no_rows_behind_many_weights():
     assert bool((db == 0).all())
     for r in range(0, N, 1 << 10):
         assert not bool(dw[r:r + (1 << 10)].any()), r
+
+
+def _far_rows(M, row_bytes, gen):
+    """A few rows at the start, and a few hundred of those that begin more than 2^32 bytes behind it"""
+    import torch
+    first = 2 ** 32 // row_bytes
+    assert first + 1000 < M
+    far = first + torch.randperm(M - first, generator=gen)[:200]
+    return torch.cat((torch.randperm(1000, generator=gen)[:20], far))
+
+
+def _signs(gen, *shape):
+    import torch
+    return torch.randint(0, 2, shape, generator=gen).mul_(2).sub_(1).float()
+
+
+def _check_far_weights(M, K, N, far_is_x):
+    """The gradient of w from few rows that are not 0, with values +-1: every sum is a whole number of at most 220, which bf16
+    holds.  Rows that are left out, or read 2^32 bytes before their place, give other whole numbers."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    gen = torch.Generator()
+    gen.manual_seed(53)
+    rows = _far_rows(M, 2 * (K if far_is_x else N), gen)
+    xs, ds = _signs(gen, len(rows), K), _signs(gen, len(rows), N)
+    want = ds.t() @ xs
+    # what a wrong address would give: the sum without the far rows, and with others in their place
+    near = ds[:20].t() @ xs[:20]
+    other = near + (ds[20:].t() @ _signs(gen, len(rows) - 20, K) if far_is_x else _signs(gen, N, len(rows) - 20) @ xs[20:])
+    for wrong in (near, other):
+        assert float((wrong != want).float().mean()) > 0.9
+    x, dy = torch.empty((M, K), dtype=torch.bfloat16, device="cuda"), torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")
+    for r in range(0, M, 1 << 18):   # +-1 everywhere in x: a wrong row is a wrong sum
+        x[r:r + (1 << 18)].random_(0, 2).mul_(2).sub_(1)
+    at = rows.cuda()
+    x[at], dy[at] = xs.cuda().bfloat16(), ds.cuda().bfloat16()
+    w = _signs(gen, N, K).cuda().bfloat16()
+    cfg = b.make_dense_config(b.BF16, M, K, N)
+    work = torch.empty(b.dlc_linear_workspace_bytes(cfg, True), dtype=torch.uint8, device="cuda")
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, dtype=torch.bfloat16, device="cuda")
+    b.dlc_linear_backward(cfg, x, w, None, dy, dx, dw, db, work)
+    assert torch.equal(dw.float().cpu(), want)
+    assert torch.equal(db.float().cpu(), ds.sum(0))
+    # dx: sums of at most N signs, rounded once; 0 elsewhere
+    assert torch.equal(dx[at].float().cpu(), (ds @ w.float().cpu()).bfloat16().float())
+    dx[at] = 0.0
+    assert not bool(dx.any())
+
+
+def test_weight_gradient_of_rows_of_x_past_32_bits():
+    _check_far_weights(2_300_003, 1024, 8, far_is_x=True)
+
+
+def test_weight_gradient_of_rows_of_dy_past_32_bits():
+    _check_far_weights(2_300_003, 8, 1024, far_is_x=False)
