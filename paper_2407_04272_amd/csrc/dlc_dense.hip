@@ -189,6 +189,11 @@ bool good_rows(int64_t ld, int64_t cols, int es) { return (ld * es) % 16 == 0 &&
 int64_t packed_ld(int64_t cols, int es) { return div_up(cols * es, 16) * 16 / es; }
 size_t packed_bytes(int64_t rows, int64_t cols, int es) { return a256((size_t)rows * (size_t)packed_ld(cols, es) * (size_t)es); }
 
+bool on_boundaries(const Shape& s) { return good_rows(s.ldx, s.K, s.es) && good_rows(s.ldw, s.K, s.es); }
+
+// A forward call that is a pass over the weights, unless pointers are off 16-byte boundaries and the flag did not say so
+bool no_plan(const Shape& s) { return s.M <= kSkinnyOddRows || (s.M <= kSkinnyRows && !s.off_boundary && on_boundaries(s)); }
+
 // Room for packed x and w: where their rows are off 16-byte boundaries, or their pointers may be (flags)
 size_t pack_room(const Shape& s) {
     const int64_t wide = s.gated ? 2 * s.N : s.N;
@@ -274,7 +279,7 @@ int run_gemm(GemmArgs g, const Plan& p, Layout lay, bool gated, void* part, cons
 
 template <typename T>
 int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void* w, const void* bias, const void* res, void* y,
-            void* pre, void* work, size_t work_bytes, const Plan& plan, hipStream_t st) {
+            void* pre, void* work, size_t work_bytes, Plan plan, hipStream_t st) {
     GemmArgs g{};
     g.a = x; g.b = w; g.lda = s.ldx; g.ldb = s.ldw;
     g.M = (int)s.M; g.N = (int)s.N; g.K = (int)s.K;
@@ -286,8 +291,9 @@ int forward(const dlc_dense_config* c, const Shape& s, const void* x, const void
     e.thr = s.thr; e.scale = s.scale; e.act = c->act; e.n = (int)s.N;
     // few rows: a pass over the weights (32 rows of 2048 -> 4096 bf16: 10.3 us in tiles)
     if (s.M <= kSkinnyRows) {
-        const bool aligned = on(x, 16) && on(w, 16) && good_rows(s.ldx, s.K, s.es) && good_rows(s.ldw, s.K, s.es);
+        const bool aligned = on(x, 16) && on(w, 16) && on_boundaries(s);
         if (aligned || s.M <= kSkinnyOddRows) return DenseOps<T>::skinny(g, s.gated, aligned, st) == hipSuccess ? DLC_OK : DLC_EHIP;
+        if (no_plan(s)) plan = plan_gemm(s.M, s.N, s.K, s.gated, L_KK, s.es);  // (only the pointers are off, and no flag said so)
     }
     const size_t part = a256(plan.bytes);
     PackArgs pk{};
@@ -370,9 +376,9 @@ bool good_ptr(const void* d, int es, bool need) { return d ? on(d, es) : !need; 
 bool good_place(const void* in, int64_t ld_in, const void* y, int64_t ld_y, int64_t rows) { return in != y || ld_in == ld_y || rows <= 1; }
 
 // the workspace a forward call needs: the product's partial sums, packed operands (a pass over few rows takes them as they are)
-size_t forward_bytes(const Shape& s, const Plan& p) { return s.M <= kSkinnyOddRows ? 0 : a256(p.bytes) + pack_room(s); }
+size_t forward_bytes(const Shape& s, const Plan& p) { return no_plan(s) ? 0 : a256(p.bytes) + pack_room(s); }
 
-Plan plan_forward(const Shape& s) { return s.M <= kSkinnyOddRows ? Plan{} : plan_gemm(s.M, s.N, s.K, s.gated, L_KK, s.es); }
+Plan plan_forward(const Shape& s) { return no_plan(s) ? Plan{} : plan_gemm(s.M, s.N, s.K, s.gated, L_KK, s.es); }
 
 int check_work(size_t need, const void* work, size_t* bytes) {
     if (!on(work, 16)) return DLC_EINVAL;

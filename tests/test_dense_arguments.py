@@ -133,3 +133,15 @@ def test_results_that_no_launch_covers():
     assert size(mk(b.F32, 1 << 30, 4, 128), True) > 0 and size(mk(b.F32, 1 << 30, 4, 129), True) == 0
     assert size(mk(b.F16, 1 << 30, 4, 768), True) > 0 and size(mk(b.F16, 1 << 30, 4, 769), True) == 0
     assert size(mk(b.F16, 64, 1 << 20, 1 << 20), True) == 0
+
+
+def test_few_rows_on_boundaries_need_no_workspace():
+    """Up to 32 rows, operands whose rows are on 16-byte boundaries: one pass over the weights, which has no partial sums."""
+    from paper_2407_04272_amd import binding as b
+    mk = b.make_dense_config
+    for size in (b.dlc_linear_workspace_bytes, b.dlc_gated_workspace_bytes):
+        for rows in (1, 16, 17, 32):
+            assert size(mk(b.BF16, rows, 4096, 512)) == 0 and size(mk(b.F32, rows, 4096, 512, ld_x=4100, ld_w=4104)) == 0
+            assert (size(mk(b.BF16, rows, 4096, 512, flags=b.DENSE_OFF_BOUNDARY)) > 0) == (rows > 16)
+            assert (size(mk(b.BF16, rows, 4095, 512)) > 0) == (rows > 16) and (size(mk(b.BF16, rows, 4096, 512, ld_w=4099)) > 0) == (rows > 16)
+        assert size(mk(b.BF16, 33, 4096, 512)) > 0
