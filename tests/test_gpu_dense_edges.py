@@ -225,3 +225,62 @@ def test_a_saturated_sigmoid_is_not_closed():
     z[0, 4:] *= -1
     x, w = torch.ones((1, 8), device="cuda"), torch.ones((8, 8), device="cuda")
     assert bool(torch.isinf(_call_backward("linear", "f32", "sigmoid", 0.0, x, w, z, dy)[2]).all())
+
+
+def _values(dtype):
+    """Pre-activations from tiny to past where every exponential overflows"""
+    import torch
+    v = torch.cat((torch.linspace(0, 40, 2001, dtype=torch.float64), torch.logspace(1.5, 4.5, 200, dtype=torch.float64),
+                   torch.tensor([65504.0]), torch.logspace(-7, 0, 100, dtype=torch.float64)))
+    if dtype != "f16":
+        v = torch.cat((v, torch.logspace(5, 38, 200, dtype=torch.float64)))
+    v = torch.cat((v, -v)).to(torch_type(dtype))
+    return v[torch.isfinite(v)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ACTS)
+@pytest.mark.parametrize("rows", [1, 40])
+def test_activations_far_out(name, dtype, rows):
+    """y = act(z) for one z a column (x is 1 in one place, w holds z there): relative to the value, where that can be asked
+    for.  The exponential's argument is off by a unit of 2^-24 of itself or two, which is 2 |z| units of the result (gelu:
+    z^2 / 2 is the argument, rounded four times, the quotient's argument once, and erfc's fit is off by 3 units); a few
+    roundings more.  A value that a normal fp32 number does not hold may be 0; its factor z comes after."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    v = _values(dtype)
+    N = v.numel()
+    x = torch.zeros((rows, 16), dtype=v.dtype, device="cuda")
+    x[:, 3] = 1.0
+    w = torch.zeros((N, 16), dtype=v.dtype, device="cuda")
+    w[:, 3] = v.cuda()
+    y, pre = torch.empty((rows, N), dtype=v.dtype, device="cuda"), torch.empty((rows, N), dtype=v.dtype, device="cuda")
+    cfg = b.make_dense_config(code(dtype), rows, 16, N, act=ACTS.index(name))
+    work = torch.empty(max(16, b.dlc_linear_workspace_bytes(cfg)), dtype=torch.uint8, device="cuda")
+    b.dlc_linear_forward(cfg, x, w, None, None, y, pre, work)
+    z = v.double().cuda()
+    assert torch.equal(pre, v.cuda().expand(rows, N))
+    if name in ("none", "relu"):
+        assert torch.equal(y, (v.clamp(min=0) if name == "relu" else v).cuda().expand(rows, N))
+        return
+    want = act(name, z)[0]
+    units = 16 + (4 * z * z if name == "gelu" else 4 * z.abs())
+    units = torch.where(z > 0, torch.full_like(z, 16.0), units)       # (1 - something small, or 0.5 and more)
+    err = units.clamp(max=2.0 ** 24) * F32 * want.abs() + 2.0 ** -126 * z.abs().clamp(min=1)
+    assert_close(y, want.expand(rows, N), rounded(want, err, dtype).expand(rows, N), f"{name} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_activations_at_infinity(dtype):
+    import torch
+    from paper_2407_04272_amd import binding as b
+    inf = float("inf")
+    x = torch.ones((1, 8), dtype=torch_type(dtype), device="cuda")
+    w = torch.zeros((4, 8), dtype=torch_type(dtype), device="cuda")
+    w[0, 0], w[1, 0], w[2, 0], w[3, 0] = inf, -inf, float("nan"), 1.0
+    for name, high, low in (("none", inf, -inf), ("relu", inf, 0.0), ("sigmoid", 1.0, 0.0), ("silu", inf, None), ("gelu", inf, None)):
+        y = torch.empty((1, 4), dtype=x.dtype, device="cuda")
+        b.dlc_linear_forward(b.make_dense_config(code(dtype), 1, 8, 4, act=ACTS.index(name)), x, w, None, None, y)
+        assert float(y[0, 0]) == high and bool(torch.isnan(y[0, 2])) and bool(torch.isfinite(y[0, 3])), name
+        if low is not None:
+            assert float(y[0, 1]) == low, name
