@@ -221,10 +221,12 @@ __device__ __forceinline__ void act_values(int act, float (&z)[U][8]) {
     }
 }
 
-// A product that is 0 where a factor is, whatever the other one holds.  The backward pass is made of these: what a dropped or
-// closed element holds does not get out (in half precision a sum past the type's range is saved as an infinity), and values and
-// slopes at infinity come out as their limits.
-__device__ __forceinline__ float mul0(float a, float b) { return a == 0.0f || b == 0.0f ? 0.0f : a * b; }
+// A product that is 0 where a factor is, whatever the other one holds; otherwise the ordinary one, subnormals included.  The
+// backward pass is made of these: what a dropped or closed element holds does not get out (in half precision a sum past the
+// type's range is saved as an infinity), and values and slopes at infinity come out as their limits.  The instruction
+// v_mul_legacy_f32 is that product; comparing and selecting takes 72 us for 66 in k_dz of gated 8192 x 4096 bf16.
+extern "C" __device__ float dlc_mul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float mul0(float a, float b) { return dlc_mul_legacy(a, b); }
 
 // values (into z) and slopes at z
 template <bool FAST>
