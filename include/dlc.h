@@ -341,7 +341,8 @@ int dlc_profile_read(dlc_ctx* ctx, int max_slots, const char** names, float* tot
  *
  *   types      DLC_F32, DLC_F16, DLC_BF16: every matrix, bias and gradient of a call has the one type.  Sums and the
  *              epilogue are fp32; a result is rounded once, when it is stored.  The backward pass rounds dz (below) to the
- *              type as well, since it is an operand of two products; the bias gradient sums it unrounded.
+ *              type as well, since it is an operand of two products; the bias gradient sums it unrounded.  In DLC_F16 a dz
+ *              below 2^-25 is lost and one above 65504 becomes an infinity: scale the loss so that gradients lie between.
  *   matrices   row-major, columns one element apart, rows a leading dimension (in elements) apart; a leading dimension of
  *              0 means the row's length.  Pointers lie on an element's boundary.  x and w are read where they stand if
  *              their rows start and end on 16-byte boundaries; otherwise they are first copied to such rows in the

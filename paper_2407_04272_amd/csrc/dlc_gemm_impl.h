@@ -12,7 +12,8 @@
 // 8192 x 2048 x 8192 184, 186 and 187 us = 1495, 1478 and 1465 TFLOP/s (eight wavefronts: 193, 204 and 206; a library 171 to
 // 185), 16384 x 8192 x 2048 400, 405 and 408 (421, 439 and 446).  fp32 4096 x 4096 x 4096 926, 941 and 945 us = 148, 146 and
 // 145 TFLOP/s, the matrix cores busy 94 % at 2.4 GHz (reads and products in turn: 970, 1004 and 984); 4096 x 1024 x 1664,
-// one work-group a compute unit, 112, 110 and 110 us (120, 127 and 136).
+// one work-group a compute unit, 104, 107 and 108 us with warm clocks (116 to 122 over the first hundred calls from idle; reads
+// and products in turn took 7, 15 and 24 % longer).
 // 128 x 128 in half precision and 64 x 128, four wavefronts: two or three work-groups share a compute unit and fill each
 // other's gaps (gemm_tile).
 //
@@ -1021,7 +1022,7 @@ __device__ __forceinline__ void sum_columns(const SumArgs& sa, int wg, float (*r
 // compute units idle one by one, and of large ones the last round of tiles is shared.  dW's work-groups come first: they are
 // the longer ones.  Each product's start at a multiple of 8, so that tile_of's XCDs are the real ones.  bf16, rows x in x
 // out, the whole call against one launch after the other: 64 x 1024 x 1024 15.3 us for 20.1, 2048 x 512 x 2048 28 for 46,
-// 8192 x 8192 x 1024 244 for 301; 16384 x 2048 x 2048 takes 198 us in this kernel, 1390 TFLOP/s.
+// 8192 x 8192 x 1024 244 for 301; 16384 x 2048 x 2048 takes 205 us in this kernel, 1340 TFLOP/s.
 template <typename T, int TILE>
 __global__ __launch_bounds__(256, TILE == 0 ? 1 : 2) void k_back(const GemmArgs gx, const GemmArgs gw, const SumArgs sa, int nx, int nw) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -1270,7 +1271,7 @@ __global__ __launch_bounds__(256) void k_pack(const PackArgs pk) {
 
 // dz and the bias gradient's partial sums: a work-group takes 256 columns and rows_per_block rows, 32 lanes side by side
 // with eight columns each, kDzRows rows at a time.  The work-groups behind those copy rows for the products (pack_rows).
-// Bound by memory: 16384 x 2048 in bf16 with dropout 41 us (4.9 TB/s), gated 8192 x 4096 65 (5.1).  (128 row blocks for the
+// Bound by memory: 16384 x 2048 in bf16 with dropout 41 us (4.9 TB/s), gated 8192 x 4096 67 (5.0).  (128 row blocks for the
 // first: 32, 16 and 8 rows at a time 59, 52 and 47 us.)
 template <typename T, bool GATED>
 __global__ __launch_bounds__(32 * kDzRows) void k_dz(const DzArgs da, const PackArgs pk) {
@@ -1353,7 +1354,7 @@ __global__ __launch_bounds__(32 * kDzRows) void k_dz(const DzArgs da, const Pack
 }
 
 // y = drop(x) + residual, eight columns a thread: one Philox block each.  Bound by memory: 16384 x 8192 bf16 with a residual
-// 134 us, 6.0 TB/s; 256 x 16 is all launch (1.7 us in the kernel).
+// 134 us, 6.0 TB/s; 256 x 16 is all launch (1.9 us in the kernel).
 template <typename T>
 __global__ __launch_bounds__(256) void k_drop(const DropArgs da) {
     const int64_t chunks = ((int64_t)da.cols + 7) / 8, total = chunks * da.rows;
