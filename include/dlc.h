@@ -432,6 +432,122 @@ size_t dlc_gated_workspace_bytes(const dlc_dense_config* cfg /*HOST*/, int backw
  */
 int dlc_dropout(const dlc_dropout_config* cfg /*HOST*/, const void* d_x, const void* d_residual, void* d_y, void* stream);
 
+/*
+ * Around the products: the norm in front of them, operands in microscaled form for serving, and the gradients' norm with
+ * clipping in front of the update.  What is said above of context, streams, buffers, graphs, leading dimensions and return
+ * values holds here too: no state is kept, a call only enqueues kernels, results do not depend on the run.
+ *
+ * Microscaled form of a matrix [rows][cols] (OCP Microscaling Formats, elements E2M1 or E4M3, scales E8M0): 32 columns of a
+ * row share a scale 2^e, e the smallest integer from -127 on with the block's largest magnitude at most 6 (E2M1) or 448
+ * (E4M3) times 2^e -- no element is ever cut off, and one that is not below the format's normal range is off by at most
+ * half a step (relative to itself 2^-2, E4M3 2^-4).  An element is its value over the scale, rounded to the nearest, ties
+ * to even.  A block that holds a NaN or an infinity has the scale NaN, and all of it stands for NaN.
+ *   elements   [rows][row bytes], a row filled up with zeros to a multiple of 128 columns, two E2M1 elements a byte (the
+ *              lower half first).  16-byte aligned
+ *   scales     e + 127, a byte each, [groups of 512 columns][rows][16]: byte 4 g + s of the 16 is that of the group's block
+ *              4 s + g (a lane of the matrix cores takes four steps' scales as one word); blocks past the last are 0.  16-byte aligned
+ * The library's calls write and expect all of it, filling included.
+ */
+enum { DLC_MX_E2M1 = 4, DLC_MX_E4M3 = 8 /* bits of an element */ };
+
+typedef struct {
+    int32_t dtype;             /* of the ordinary matrices: DLC_F32, DLC_F16 or DLC_BF16 */
+    int32_t elem;              /* DLC_MX_* */
+    int64_t rows, cols;        /* rows 0 .. 2^30, cols 1 .. 2^20 */
+    int64_t ld_x, ld_y;        /* leading dimensions, any that hold the row; 0: the row's length */
+} dlc_mx_config;
+
+/* Bytes of a matrix in microscaled form: its elements, its scales; 0 also if cfg is invalid */
+size_t dlc_mx_data_bytes(const dlc_mx_config* cfg /*HOST*/);
+size_t dlc_mx_scale_bytes(const dlc_mx_config* cfg /*HOST*/);
+/*
+ * d_x [rows][cols] -> d_q, d_scale, and back (exact but for the type's own range and rounding: E4M3 has fewer bits than any
+ * type here, a scale may lie outside DLC_F16's range and then gives its limits).  No overlap.
+ */
+int dlc_mx_quantize(const dlc_mx_config* cfg /*HOST*/, const void* d_x, void* d_q, void* d_scale, void* stream);
+int dlc_mx_dequantize(const dlc_mx_config* cfg /*HOST*/, const void* d_q, const void* d_scale, void* d_y, void* stream);
+
+/*
+ * Linear layer for serving, its operands in microscaled form:   y = act(x w' + bias) + residual
+ *   d_xq, d_xs   x [M][K], elements elem_x     d_wq, d_ws   w [N][K], elements E2M1
+ *   d_bias [N] or NULL   d_residual [M][N] or NULL   d_y [M][N], all of type dtype.  d_residual may be d_y, with equal leading
+ *   dimensions (else DLC_EINVAL)
+ * Products are exact, sums and the epilogue fp32, the result is rounded once.
+ *   sizes        rows 0 .. 2^30, features 1 .. 2^20, leading dimensions up to 2^20; results of fewer than 2^24 tiles of 256 x 256
+ *   d_work       as above, dlc_mx_linear_workspace_bytes
+ */
+typedef struct {
+    int32_t dtype;
+    int32_t act;               /* DLC_ACT_* */
+    int32_t elem_x;            /* DLC_MX_* */
+    int32_t reserved;          /* 0 */
+    int64_t rows;              /* M */
+    int64_t in_features;       /* K */
+    int64_t out_features;      /* N */
+    int64_t ld_y, ld_res;
+} dlc_mx_linear_config;
+
+int dlc_mx_linear_forward(const dlc_mx_linear_config* cfg /*HOST*/, const void* d_xq, const void* d_xs, const void* d_wq, const void* d_ws,
+                          const void* d_bias, const void* d_residual, void* d_y, void* d_work, size_t work_bytes, void* stream);
+size_t dlc_mx_linear_workspace_bytes(const dlc_mx_linear_config* cfg /*HOST*/);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition:
+ *   s = x + residual;   r = (mean of s^2 over the row + eps)^(-1/2);   y = s r weight
+ *   d_x [rows][cols]   d_residual [rows][cols] or NULL   d_weight [cols] or NULL (ones)
+ *   d_sum [rows][cols] or NULL: s, which goes on around the next layer and which the backward pass reads (without a residual
+ *         that is x itself).  May be d_x or d_residual, with equal leading dimensions (else DLC_EINVAL)
+ *   d_y [rows][cols], or d_q and d_scale (y in microscaled form with E4M3 elements, as a product takes it; both or neither),
+ *         or all three.  d_y may be d_x, with equal leading dimensions, unless d_sum is.  No other overlap
+ * s, sums and y are fp32 up to the one rounding of each output; r is made of the unrounded s.  A row whose squares' sum passes
+ * fp32's range (values from about 1.8e19 / sqrt(cols) on) has r = 0.
+ * Backward, of y's gradient and (d_ds, or NULL) the gradient that comes back along s:
+ *   g = dy weight;   dx = r (g - s r^2 mean of g s over the row) + ds;   dweight = sum over rows of dy s r
+ *   d_s as the forward call stored it (r is made again from it)   d_dx: the gradient of x and of the residual; may be d_dy or
+ *   d_ds, with equal leading dimensions   d_dweight [cols]; d_dx and d_dweight may be NULL and are then not computed.
+ *   No rows: dweight is zeros.
+ *   d_work  as above, dlc_norm_workspace_bytes (only the backward call takes one; 0 without d_dweight's sums to put together)
+ * rows 0 .. 2^30, cols 1 .. 2^20, leading dimensions any that hold the row.
+ */
+typedef struct {
+    int32_t dtype;
+    int32_t reserved;          /* 0 */
+    int64_t rows, cols;
+    int64_t ld_x, ld_res, ld_sum, ld_y, ld_dy, ld_ds, ld_dx; /* 0: the row's length (backward: d_s has ld_sum) */
+    double eps;                /* 2^-126 .. 2^126 */
+} dlc_norm_config;
+
+int dlc_norm_forward(const dlc_norm_config* cfg /*HOST*/, const void* d_x, const void* d_residual, const void* d_weight, void* d_sum,
+                     void* d_y, void* d_q, void* d_scale, void* stream);
+int dlc_norm_backward(const dlc_norm_config* cfg /*HOST*/, const void* d_s, const void* d_weight, const void* d_dy, const void* d_ds,
+                      void* d_dx, void* d_dweight, void* d_work, size_t work_bytes, void* stream);
+size_t dlc_norm_workspace_bytes(const dlc_norm_config* cfg /*HOST*/);
+
+/*
+ * The norm of all gradients together, and clipping: two calls, so that a program can add up the sums of several GPUs between
+ * them (and leave out what they share).
+ *   list      HOST    `count` tensors, 0 .. 2^20 of them; types may differ; none overlaps another.  Read during the call only
+ *   d_sum     DEVICE  double[1]: dlc_gradient_norm writes the sum of all squares (in 64 bits throughout), dlc_gradient_clip
+ *                     reads it
+ *   d_norm    DEVICE  float[1] or NULL: gets n = sqrt(*d_sum)
+ *   out       HOST    as `list`, the same types and sizes: gets every element times f = min(1, max_norm / n), rounded once; the
+ *                     same tensors (with the same ld) for clipping in place, which writes nothing where f is 1
+ *   max_norm          >= 0.  If n is not finite f is 1: the gradients stay as they are, and *d_norm tells
+ *   d_work            as above, dlc_gradient_workspace_bytes
+ * Returns DLC_ELIMIT for more than 2^40 elements in a tensor or 2^44 in all.
+ */
+typedef struct {
+    void* p;                   /* DEVICE, on an element's boundary; may be NULL if there are no elements */
+    int64_t rows, cols, ld;    /* [rows][cols], rows ld elements apart (0: dense) */
+    int32_t dtype;
+    int32_t reserved;          /* 0 */
+} dlc_tensor;
+
+int dlc_gradient_norm(const dlc_tensor* list /*HOST*/, int64_t count, double* d_sum, void* d_work, size_t work_bytes, void* stream);
+int dlc_gradient_clip(const dlc_tensor* list /*HOST*/, int64_t count, const double* d_sum, double max_norm, float* d_norm,
+                      const dlc_tensor* out /*HOST*/, void* stream);
+size_t dlc_gradient_workspace_bytes(const dlc_tensor* list /*HOST*/, int64_t count);
+
 const char* dlc_strerror(int status);
 
 #ifdef __cplusplus

@@ -13,7 +13,8 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdlc.so")
 
-F32, F16, BF16 = 0, 1, 2  # BF16: dense operators only
+F32, F16, BF16 = 0, 1, 2  # BF16: not for payloads
+MX_E2M1, MX_E4M3 = 4, 8  # elements of matrices in microscaled form, by their bits
 DENSE_OFF_BOUNDARY = 1
 ACT_NONE, ACT_RELU, ACT_SIGMOID, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
 OK, EINVAL, ENOMEM, ECAPACITY, ECORRUPT, EHIP, ESTATE, ELIMIT = 0, -1, -2, -3, -4, -5, -6, -7
@@ -58,20 +59,48 @@ class DropoutConfig(C.Structure):
     counter = None
 
 
+class MxConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("elem", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("ld_x", C.c_int64),
+                ("ld_y", C.c_int64)]
+    counter = None
+
+
+class MxLinearConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("elem_x", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64),
+                ("in_features", C.c_int64), ("out_features", C.c_int64), ("ld_y", C.c_int64), ("ld_res", C.c_int64)]
+    counter = None
+
+
+class NormConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("ld_x", C.c_int64),
+                ("ld_res", C.c_int64), ("ld_sum", C.c_int64), ("ld_y", C.c_int64), ("ld_dy", C.c_int64), ("ld_ds", C.c_int64),
+                ("ld_dx", C.c_int64), ("eps", C.c_double)]
+    counter = None
+
+
+class Tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 EXPORTS = ["dlc_create", "dlc_destroy", "dlc_compress_bound", "dlc_workspace_bytes", "dlc_stats",
            "dlc_set_error_bounds", "dlc_compress", "dlc_decompress", "dlc_sync_status", "dlc_quantize",
            "dlc_read_histogram", "dlc_read_codebook", "dlc_read_row_refs", "dlc_set_row_match", "dlc_speedup_estimate",
            "dlc_select_compressors", "dlc_set_row_hash_multipliers", "dlc_decompress_static",
            "dlc_linear_forward", "dlc_linear_backward", "dlc_gated_forward", "dlc_gated_backward",
            "dlc_linear_workspace_bytes", "dlc_gated_workspace_bytes", "dlc_dropout",
+           "dlc_mx_data_bytes", "dlc_mx_scale_bytes", "dlc_mx_quantize", "dlc_mx_dequantize", "dlc_mx_linear_forward",
+           "dlc_mx_linear_workspace_bytes", "dlc_norm_forward", "dlc_norm_backward", "dlc_norm_workspace_bytes",
+           "dlc_gradient_norm", "dlc_gradient_clip", "dlc_gradient_workspace_bytes",
            "dlc_profile_enable", "dlc_profile_read", "dlc_strerror"]
 
 _lib = None
+_uint8 = _float64 = _float32 = None  # torch's, once the library is loaded
 
 
 def lib():
     """Loads libdlc.so (built beforehand by ``paper_2407_04272_amd.build`` / ``__graft_entry__.build``)."""
-    global _lib
+    global _lib, _uint8, _float64, _float32
     if _lib is None:
         if not os.path.exists(_LIB_PATH):
             raise RuntimeError(f"{_LIB_PATH} is missing: build it with `python -m paper_2407_04272_amd.build` "
@@ -81,6 +110,7 @@ def lib():
         import torch
         if torch.cuda.is_available():
             torch.cuda.init()
+        _uint8, _float64, _float32 = torch.uint8, torch.float64, torch.float32
         L = C.CDLL(_LIB_PATH)
         vp, i32, i64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
         L.dlc_create.argtypes = [C.POINTER(vp), C.POINTER(Config)]
@@ -116,6 +146,22 @@ def lib():
             f.argtypes = [dense, i32]
             f.restype = sz
         L.dlc_dropout.argtypes = [C.POINTER(DropoutConfig)] + [vp] * 4
+        mx, tensors = C.POINTER(MxConfig), C.POINTER(Tensor)
+        for f in (L.dlc_mx_data_bytes, L.dlc_mx_scale_bytes):
+            f.argtypes = [mx]
+            f.restype = sz
+        L.dlc_mx_quantize.argtypes = L.dlc_mx_dequantize.argtypes = [mx] + [vp] * 4
+        L.dlc_mx_linear_forward.argtypes = [C.POINTER(MxLinearConfig)] + [vp] * 8 + [sz, vp]
+        L.dlc_mx_linear_workspace_bytes.argtypes = [C.POINTER(MxLinearConfig)]
+        L.dlc_mx_linear_workspace_bytes.restype = sz
+        L.dlc_norm_forward.argtypes = [C.POINTER(NormConfig)] + [vp] * 8
+        L.dlc_norm_backward.argtypes = [C.POINTER(NormConfig)] + [vp] * 7 + [sz, vp]
+        L.dlc_norm_workspace_bytes.argtypes = [C.POINTER(NormConfig)]
+        L.dlc_norm_workspace_bytes.restype = sz
+        L.dlc_gradient_norm.argtypes = [tensors, i64, vp, vp, sz, vp]
+        L.dlc_gradient_clip.argtypes = [tensors, i64, vp, C.c_double, vp, tensors, vp]
+        L.dlc_gradient_workspace_bytes.argtypes = [tensors, i64]
+        L.dlc_gradient_workspace_bytes.restype = sz
         L.dlc_strerror.argtypes = [i32]
         L.dlc_strerror.restype = C.c_char_p
         _lib = L
@@ -344,6 +390,185 @@ def dlc_dropout(cfg: DropoutConfig, x, residual, y, stream=None):
     _check(lib().dlc_dropout(C.byref(cfg), _matrix("x", x, ty, M, N, cfg.ld_x),
                              _matrix("residual", residual, ty, M, N, cfg.ld_res), _matrix("y", y, ty, M, N, cfg.ld_y),
                              st), "dlc_dropout")
+
+
+# ---- around the products: norm, microscaled operands, gradient clipping (no context; see include/dlc.h) ----
+def make_norm_config(dtype, rows, cols, eps=1e-6, ld_x=0, ld_res=0, ld_sum=0, ld_y=0, ld_dy=0, ld_ds=0, ld_dx=0) -> NormConfig:
+    """ld_*: elements from row to row, 0 for dense rows (backward: s has ld_sum)."""
+    return NormConfig(dtype, 0, rows, cols, ld_x, ld_res, ld_sum, ld_y, ld_dy, ld_ds, ld_dx, eps)
+
+
+def dlc_norm_workspace_bytes(cfg: NormConfig) -> int:
+    return int(lib().dlc_norm_workspace_bytes(C.byref(cfg)))
+
+
+def dlc_norm_forward(cfg: NormConfig, x, residual, weight, sum, y, q=None, scale=None, stream=None):
+    """s = x + residual; y = s (mean s^2 + eps)^-1/2 weight.  sum, if given, gets s; q and scale get y with E4M3 elements (buffers
+    as dlc_mx_data_shape and dlc_mx_scale_shape say); a None is left out.  Raises DlcError."""
+    ty, st = _where(cfg, stream)
+    M, N = cfg.rows, cfg.cols
+    _check(lib().dlc_norm_forward(
+        C.byref(cfg), _matrix("x", x, ty, M, N, cfg.ld_x), _matrix("residual", residual, ty, M, N, cfg.ld_res),
+        _vector("weight", weight, ty, N), _matrix("sum", sum, ty, M, N, cfg.ld_sum), _matrix("y", y, ty, M, N, cfg.ld_y),
+        _bytes("q", q, ty, _mx_data_shape(MX_E4M3, M, N)), _bytes("scale", scale, ty, _mx_scale_shape(M, N)), st), "dlc_norm_forward")
+
+
+def dlc_norm_backward(cfg: NormConfig, s, weight, dy, ds, dx, dweight, work=None, stream=None):
+    """The gradients of dlc_norm_forward from s, y's gradient and (or None) the gradient along s; a None is not computed.
+    Raises DlcError."""
+    ty, st = _where(cfg, stream)
+    M, N = cfg.rows, cfg.cols
+    wk, nb = _work(work, ty)
+    _check(lib().dlc_norm_backward(
+        C.byref(cfg), _matrix("s", s, ty, M, N, cfg.ld_sum), _vector("weight", weight, ty, N), _matrix("dy", dy, ty, M, N, cfg.ld_dy),
+        _matrix("ds", ds, ty, M, N, cfg.ld_ds), _matrix("dx", dx, ty, M, N, cfg.ld_dx), _vector("dweight", dweight, ty, N), wk, nb, st),
+        "dlc_norm_backward")
+
+
+def make_mx_config(dtype, elem, rows, cols, ld_x=0, ld_y=0) -> MxConfig:
+    """elem: MX_E2M1 or MX_E4M3.  ld_x: of dlc_mx_quantize's matrix, ld_y: of dlc_mx_dequantize's."""
+    return MxConfig(dtype, elem, rows, cols, ld_x, ld_y)
+
+
+def _mx_data_shape(elem, rows, cols):
+    return rows, (cols + 127) // 128 * 16 * elem
+
+
+def _mx_scale_shape(rows, cols):
+    return (cols + 511) // 512, rows, 16
+
+
+def dlc_mx_data_shape(cfg: MxConfig):
+    """(rows, row bytes) of the elements' uint8 tensor"""
+    return _mx_data_shape(cfg.elem, cfg.rows, cfg.cols)
+
+
+def dlc_mx_scale_shape(cfg: MxConfig):
+    """(groups of 512 columns, rows, 16) of the scales' uint8 tensor"""
+    return _mx_scale_shape(cfg.rows, cfg.cols)
+
+
+def _bytes(name, t, want, shape):
+    """The address of a contiguous uint8 tensor of that shape; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not _uint8 or t.get_device() != want[1] or t.shape != shape or not t.is_contiguous():
+        raise DlcError(EINVAL, f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not contiguous uint8 {shape} on GPU {want[1]}")
+    return t.data_ptr()
+
+
+def dlc_mx_quantize(cfg: MxConfig, x, q, scale, stream=None):
+    """x to microscaled form.  Raises DlcError."""
+    ty, st = _where(cfg, stream)
+    _check(lib().dlc_mx_quantize(
+        C.byref(cfg), _matrix("x", x, ty, cfg.rows, cfg.cols, cfg.ld_x), _bytes("q", q, ty, dlc_mx_data_shape(cfg)),
+        _bytes("scale", scale, ty, dlc_mx_scale_shape(cfg)), st), "dlc_mx_quantize")
+
+
+def dlc_mx_dequantize(cfg: MxConfig, q, scale, y, stream=None):
+    """The values that a matrix in microscaled form stands for.  Raises DlcError."""
+    ty, st = _where(cfg, stream)
+    _check(lib().dlc_mx_dequantize(
+        C.byref(cfg), _bytes("q", q, ty, dlc_mx_data_shape(cfg)), _bytes("scale", scale, ty, dlc_mx_scale_shape(cfg)),
+        _matrix("y", y, ty, cfg.rows, cfg.cols, cfg.ld_y), st), "dlc_mx_dequantize")
+
+
+def make_mx_linear_config(dtype, elem_x, rows, in_features, out_features, act=ACT_NONE, ld_y=0, ld_res=0) -> MxLinearConfig:
+    return MxLinearConfig(dtype, act, elem_x, 0, rows, in_features, out_features, ld_y, ld_res)
+
+
+def dlc_mx_linear_workspace_bytes(cfg: MxLinearConfig) -> int:
+    return int(lib().dlc_mx_linear_workspace_bytes(C.byref(cfg)))
+
+
+def dlc_mx_linear_forward(cfg: MxLinearConfig, xq, xs, wq, ws, bias, residual, y, work=None, stream=None):
+    """y = act(x w' + bias) + residual; x (elements cfg.elem_x) and w (E2M1) in microscaled form.  Raises DlcError."""
+    ty, st = _where(cfg, stream)
+    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
+    wk, nb = _work(work, ty)
+    _check(lib().dlc_mx_linear_forward(
+        C.byref(cfg), _bytes("xq", xq, ty, _mx_data_shape(cfg.elem_x, M, K)), _bytes("xs", xs, ty, _mx_scale_shape(M, K)),
+        _bytes("wq", wq, ty, _mx_data_shape(MX_E2M1, N, K)), _bytes("ws", ws, ty, _mx_scale_shape(N, K)), _vector("bias", bias, ty, N),
+        _matrix("residual", residual, ty, M, N, cfg.ld_res), _matrix("y", y, ty, M, N, cfg.ld_y), wk, nb, st), "dlc_mx_linear_forward")
+
+
+class GradientList:
+    """Tensors of dlc_gradient_norm and dlc_gradient_clip, checked and described once: of one or two dimensions, columns one
+    element apart, or contiguous; all on one GPU, none twice.  Holds the tensors; make another when a program's gradients move
+    (a tensor's memory is read again in every call, its address is not)."""
+
+    def __init__(self, tensors):
+        import torch
+        codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+        self.tensors = list(tensors)
+        self.device = None
+        self.shapes = [(t.dtype, tuple(t.shape)) for t in self.tensors]
+        self.entries = (Tensor * len(self.tensors))()
+        seen = set()
+        for i, t in enumerate(self.tensors):
+            if t.dtype not in codes or not t.is_cuda:
+                raise DlcError(EINVAL, f"tensor {i}: {t.dtype} on {t.device}")
+            if self.device is None:
+                self.device = t.get_device()
+            if t.get_device() != self.device:
+                raise DlcError(EINVAL, f"tensor {i}: on {t.device}, not on GPU {self.device}")
+            n, shape = t.numel(), t.shape
+            if len(shape) == 2 and n > 0 and (shape[1] == 1 or t.stride(1) == 1) and (shape[0] == 1 or t.stride(0) >= shape[1]):
+                rows, cols, ld = shape[0], shape[1], t.stride(0) if shape[0] > 1 else 0
+            elif len(shape) == 1 and n > 0 and (n == 1 or t.stride(0) > 0):
+                rows, cols, ld = n, 1, t.stride(0) if n > 1 else 0
+            elif t.is_contiguous():
+                rows, cols, ld = 1, n, 0
+            else:
+                raise DlcError(EINVAL, f"tensor {i}: strides {t.stride()} of {tuple(shape)}")
+            if n > 0:
+                if t.data_ptr() in seen:
+                    raise DlcError(EINVAL, f"tensor {i}: in the list twice")
+                seen.add(t.data_ptr())
+            self.entries[i] = Tensor(t.data_ptr(), rows, cols, ld, codes[t.dtype], 0)
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _word(name, t, dtype, device):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or t.numel() < 1:
+        raise DlcError(EINVAL, f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, not {dtype} on GPU {device}")
+    return t.data_ptr()
+
+
+def _gradients(lst, stream):
+    """The GPU and the stream of a call on the list's tensors"""
+    device, handle = _launch(stream)
+    if lst.device is not None and lst.device != device:
+        raise DlcError(EINVAL, f"gradients: on GPU {lst.device}, not on GPU {device}")
+    return device, handle
+
+
+def dlc_gradient_workspace_bytes(lst: GradientList) -> int:
+    return int(lib().dlc_gradient_workspace_bytes(lst.entries, len(lst)))
+
+
+def dlc_gradient_norm(lst: GradientList, sum, work=None, stream=None):
+    """sum (float64 on the GPU) gets the sum of all squares.  Raises DlcError."""
+    device, st = _gradients(lst, stream)
+    wk, nb = _work(work, (None, device))
+    _check(lib().dlc_gradient_norm(lst.entries, len(lst), _word("sum", sum, _float64, device), wk, nb, st), "dlc_gradient_norm")
+
+
+def dlc_gradient_clip(lst: GradientList, sum, max_norm, norm=None, out: GradientList | None = None, stream=None):
+    """Every element times min(1, max_norm / sqrt(sum)), in place or to the tensors of `out`; norm (float32 on the GPU), if given,
+    gets sqrt(sum).  Raises DlcError."""
+    device, st = _gradients(lst, stream)
+    out = lst if out is None else out
+    if out is not lst:
+        _gradients(out, stream)
+        if out.shapes != lst.shapes:
+            raise DlcError(EINVAL, "out: other types or shapes than the gradients")
+    _check(lib().dlc_gradient_clip(lst.entries, len(lst), _word("sum", sum, _float64, device), float(max_norm),
+                                   _word("norm", norm, _float32, device), out.entries, st), "dlc_gradient_clip")
 
 
 class Context:

@@ -1,0 +1,178 @@
+// Matrices to microscaled form and back, and the host side of the product of microscaled operands.
+#include "dlc_mx_gemm.h"
+
+using namespace dlc;
+
+namespace {
+
+struct MxArgs {
+    const void* x;       // the ordinary matrix (back: y)
+    uint8_t* q;
+    uint8_t* scale;
+    int64_t rows, ld, tiles;
+    int32_t cols, groups;
+};
+
+constexpr int kTileRows = 16;  // rows of a work-group's tile: four a wavefront, whose loads are on their way together
+
+// A tile is a group of 512 columns, eight a lane, of 16 rows: their scales are 256 bytes side by side.  Bound by memory.
+template <typename T, int ELEM>
+__global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {
+    constexpr int R = kTileRows / 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const int64_t band = tile / a.groups, row0 = band * kTileRows + wave * R;
+        const int col = (int)(tile - band * a.groups) * kMxGroup + lane * 8;
+        float f[R][8];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            load8(static_cast<const T*>(a.x) + (row0 + i) * a.ld + col, row0 + i < a.rows ? a.cols - col : 0, f[i]);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (row0 + i < a.rows) mx_store8<ELEM>(f[i], row0 + i, col, a.cols, a.rows, a.q, a.scale);
+    }
+}
+
+template <typename T, int ELEM>
+__global__ __launch_bounds__(256) void k_mx_dequantize(const MxArgs a) {
+    constexpr int R = kTileRows / 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row_bytes = mx_row_bytes(a.cols, ELEM);
+    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const int64_t band = tile / a.groups, row0 = band * kTileRows + wave * R;
+        const int group = (int)(tile - band * a.groups), col = group * kMxGroup + lane * 8, cnt = a.cols - col;
+        if (cnt <= 0) continue;
+        MxWords<ELEM> w[R];
+        uint32_t byte[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int64_t row = row0 + i < a.rows ? row0 + i : a.rows - 1;
+            w[i] = *reinterpret_cast<const MxWords<ELEM>*>(a.q + row * row_bytes + col * ELEM / 8);
+            byte[i] = a.scale[((int64_t)group * a.rows + row) * 16 + mx_scale_place(lane >> 2)];
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (row0 + i >= a.rows) continue;
+            float f[8];
+            mx_decode8<ELEM>(w[i], byte[i], f);
+            store8(static_cast<T*>(const_cast<void*>(a.x)) + (row0 + i) * a.ld + col, cnt, f);
+        }
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 20;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+bool good(const void* p, int es, bool need) { return p ? on(p, es) : !need; }
+bool good_type(int t) { return t == DLC_F32 || t == DLC_F16 || t == DLC_BF16; }
+bool good_elem(int e) { return e == DLC_MX_E2M1 || e == DLC_MX_E4M3; }
+
+bool good_mx(const dlc_mx_config* c) {
+    if (!c || !good_type(c->dtype) || !good_elem(c->elem)) return false;
+    if (c->rows < 0 || c->rows > kMaxRows || c->cols < 1 || c->cols > kMaxDim) return false;
+    const int64_t lim = c->rows > 0 ? (int64_t(1) << 60) / c->rows : int64_t(1) << 60;  // (a buffer's last byte has a 64-bit address)
+    for (const int64_t ld : {c->ld_x, c->ld_y})
+        if (ld != 0 && (ld < c->cols || ld > lim)) return false;
+    return true;
+}
+
+template <typename T>
+void convert(const MxArgs& a, int elem, bool back, hipStream_t st) {
+    const dim3 grid((unsigned)(a.tiles < (int64_t(1) << 20) ? a.tiles : int64_t(1) << 20)), block(256);
+    if (back) {
+        if (elem == DLC_MX_E4M3) k_mx_dequantize<T, 8><<<grid, block, 0, st>>>(a);
+        else k_mx_dequantize<T, 4><<<grid, block, 0, st>>>(a);
+    } else {
+        if (elem == DLC_MX_E4M3) k_mx_quantize<T, 8><<<grid, block, 0, st>>>(a);
+        else k_mx_quantize<T, 4><<<grid, block, 0, st>>>(a);
+    }
+}
+
+int convert_any(const dlc_mx_config* c, const void* x, const void* q, const void* scale, bool back, void* stream) {
+    if (!good_mx(c)) return DLC_EINVAL;
+    const int es = c->dtype == DLC_F32 ? 4 : 2;
+    const bool need = c->rows > 0;
+    if (!good(x, es, need) || !good(q, 16, need) || !good(scale, 16, need)) return DLC_EINVAL;
+    if (!need) return DLC_OK;
+    MxArgs a{};
+    a.x = x; a.q = static_cast<uint8_t*>(const_cast<void*>(q)); a.scale = static_cast<uint8_t*>(const_cast<void*>(scale));
+    a.rows = c->rows; a.cols = (int)c->cols;
+    a.ld = back ? c->ld_y : c->ld_x;
+    if (a.ld == 0) a.ld = c->cols;
+    a.groups = (int)mx_groups(c->cols);
+    a.tiles = div_up(c->rows, kTileRows) * a.groups;
+    hipStream_t st = (hipStream_t)stream;
+    switch (c->dtype) {
+        case DLC_F32: convert<float>(a, c->elem, back, st); break;
+        case DLC_F16: convert<f16_t>(a, c->elem, back, st); break;
+        default: convert<bf16_t>(a, c->elem, back, st); break;
+    }
+    return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
+}
+
+// ---- the product ---------------------------------------------------------------------------------
+struct Shape {
+    int64_t M, K, N, ldy, ldres;
+    int elem, es;
+};
+
+bool make_shape(const dlc_mx_linear_config* c, Shape* s) {
+    if (!c || !good_type(c->dtype) || !good_elem(c->elem_x) || c->act < DLC_ACT_NONE || c->act > DLC_ACT_GELU || c->reserved != 0) return false;
+    if (c->rows < 0 || c->rows > kMaxRows) return false;
+    if (c->in_features < 1 || c->in_features > kMaxDim || c->out_features < 1 || c->out_features > kMaxDim) return false;
+    s->M = c->rows; s->K = c->in_features; s->N = c->out_features;
+    s->ldy = c->ld_y ? c->ld_y : s->N;
+    s->ldres = c->ld_res ? c->ld_res : s->N;
+    if (s->ldy < s->N || s->ldy > kMaxDim || s->ldres < s->N || s->ldres > kMaxDim) return false;
+    s->elem = c->elem_x;
+    s->es = c->dtype == DLC_F32 ? 4 : 2;
+    return div_up(s->M, 256) * div_up(s->N, 256) < (int64_t(1) << 24);
+}
+
+}  // namespace
+
+extern "C" size_t dlc_mx_data_bytes(const dlc_mx_config* c) { return good_mx(c) ? (size_t)c->rows * (size_t)mx_row_bytes(c->cols, c->elem) : 0; }
+extern "C" size_t dlc_mx_scale_bytes(const dlc_mx_config* c) { return good_mx(c) ? (size_t)c->rows * (size_t)mx_groups(c->cols) * 16 : 0; }
+
+extern "C" int dlc_mx_quantize(const dlc_mx_config* cfg, const void* x, void* q, void* scale, void* stream) {
+    return convert_any(cfg, x, q, scale, false, stream);
+}
+
+extern "C" int dlc_mx_dequantize(const dlc_mx_config* cfg, const void* q, const void* scale, void* y, void* stream) {
+    return convert_any(cfg, y, q, scale, true, stream);
+}
+
+extern "C" size_t dlc_mx_linear_workspace_bytes(const dlc_mx_linear_config* c) {
+    Shape s;
+    return make_shape(c, &s) ? 0 : 0;
+}
+
+extern "C" int dlc_mx_linear_forward(const dlc_mx_linear_config* c, const void* xq, const void* xs, const void* wq, const void* ws,
+                                     const void* bias, const void* res, void* y, void* work, size_t bytes, void* stream) {
+    Shape s;
+    if (!make_shape(c, &s)) return DLC_EINVAL;
+    const bool need = s.M > 0;
+    if (!good(xq, 16, need) || !good(xs, 16, need) || !good(wq, 16, need) || !good(ws, 16, need) || !good(bias, s.es, false) ||
+        !good(res, s.es, false) || !good(y, s.es, need) || !on(work, 16)) return DLC_EINVAL;
+    if (!need) return DLC_OK;
+    if (res == y && s.ldres != s.ldy && s.M > 1) return DLC_EINVAL;
+    MxGemmArgs g{};
+    g.xs = static_cast<const uint8_t*>(xs); g.ws = static_cast<const uint8_t*>(ws);
+    g.c.a = xq; g.c.b = wq;
+    g.c.lda = mx_row_bytes(s.K, s.elem); g.c.ldb = mx_row_bytes(s.K, DLC_MX_E2M1);
+    g.c.M = (int)s.M; g.c.N = (int)s.N; g.c.K = (int)mx_filled(s.K);
+    g.c.split = 1; g.c.kper = g.c.K;
+    Epi& e = g.c.e;
+    e.y = y; e.res = res; e.bias = bias;
+    e.ld_y = s.ldy; e.ld_res = s.ldres; e.act = c->act; e.n = (int)s.N;
+    hipStream_t st = (hipStream_t)stream;
+    hipError_t rc;
+    switch (c->dtype) {
+        case DLC_F32: rc = MxOps<float>::gemm(g, s.elem, st); break;
+        case DLC_F16: rc = MxOps<f16_t>::gemm(g, s.elem, st); break;
+        default: rc = MxOps<bf16_t>::gemm(g, s.elem, st); break;
+    }
+    return rc == hipSuccess ? DLC_OK : DLC_EHIP;
+}

@@ -1,0 +1,376 @@
+// Root-mean-square norm with the residual's addition, forward (results in the type, in microscaled form, or both) and backward.
+//
+// Bound by memory: every row is read once into registers, its sums are made there, and the results go out.  A team of P lanes
+// has a row, U times eight columns a lane; rows longer than 32768 columns are read twice instead.
+#include "dlc_mx.h"
+
+using namespace dlc;
+
+namespace {
+
+struct NormArgs {
+    const void* x;       // backward: s
+    const void* res;     // backward: the gradient along s
+    const void* weight;
+    const void* dy;
+    void* sum;
+    void* y;             // backward: dx
+    uint8_t* q;
+    uint8_t* scale;
+    float* part;         // backward: [work-groups][part_ld] partial sums of the weight's gradient
+    int64_t part_ld;
+    int64_t rows, ld_x, ld_res, ld_sum, ld_y, ld_dy;
+    int32_t cols, per;   // per: rows that a team takes one after the other
+    float eps, inv_cols;
+};
+
+// The sum over a team of P lanes, the same in all of them.  More than a wavefront: over `red`, which is not written again
+// before the barrier of the next sum but one.
+template <int P, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], float (*red)[N]) {
+#pragma unroll
+    for (int d = 1; d < (P < 64 ? P : 64); d <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d, 64);
+    if constexpr (P > 64) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[wave][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = red[0][i];
+#pragma unroll
+            for (int w = 1; w < P / 64; ++w) v[i] += red[w][i];
+        }
+    }
+}
+
+template <int P>
+constexpr int kTeams = P < 256 ? 256 / P : 1;
+
+template <typename T>
+__device__ __forceinline__ void load_weight(const void* weight, int col, int cnt, float w[8]) {
+    if (weight) {
+        load8(static_cast<const T*>(weight) + col, cnt, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+    }
+}
+
+// s of eight columns, 0 behind the last
+template <typename T>
+__device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, int col, int cnt, float s[8]) {
+    load8(static_cast<const T*>(a.x) + row * a.ld_x + col, cnt, s);
+    if (a.res) {
+        float r[8];
+        load8(static_cast<const T*>(a.res) + row * a.ld_res + col, cnt, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += r[i];
+    }
+}
+
+template <typename T, bool MX>
+__device__ __forceinline__ void put_row(const NormArgs& a, int64_t row, int col, float r, float s[8]) {
+    const int cnt = a.cols - col;
+    if (a.sum) store8(static_cast<T*>(a.sum) + row * a.ld_sum + col, cnt, s);
+    float w[8];
+    load_weight<T>(a.weight, col, cnt, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = i < cnt ? s[i] * r * w[i] : 0.0f;
+    if (a.y) store8(static_cast<T*>(a.y) + row * a.ld_y + col, cnt, s);
+    if constexpr (MX) mx_store8<8>(s, row, col, a.cols, a.rows, a.q, a.scale);
+}
+
+template <typename T, int P, int U, bool MX>
+__global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
+    __shared__ float red[2][P > 64 ? P / 64 : 1][1];
+    const int t = threadIdx.x % P, team = threadIdx.x / P;
+    const int64_t first = ((int64_t)blockIdx.x * kTeams<P> + team) * a.per, last = min(a.rows, first + a.per);
+    const int end = MX ? (int)mx_groups(a.cols) * kMxGroup : a.cols;
+    int odd = 0;
+    for (int64_t row = first; row < last; ++row, odd ^= 1) {
+        float s[U][8], sq[1] = {0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (u * P + t) * 8;
+            load_sum<T>(a, row, col, a.cols - col, s[u]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sq[0] += s[u][i] * s[u][i];
+        }
+        team_sum<P>(sq, red[odd]);
+        const float r = __builtin_amdgcn_rsqf(sq[0] * a.inv_cols + a.eps);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (u * P + t) * 8;
+            if (col < end) put_row<T, MX>(a, row, col, r, s[u]);
+        }
+    }
+}
+
+// ... rows of any length, read twice
+template <typename T, bool MX>
+__global__ __launch_bounds__(1024) void k_norm_long(const NormArgs a) {
+    __shared__ float red[2][16][1];
+    const int end = MX ? (int)mx_groups(a.cols) * kMxGroup : a.cols;
+    int odd = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, odd ^= 1) {
+        float sq[1] = {0.0f}, s[8];
+        for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            load_sum<T>(a, row, col, a.cols - col, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sq[0] += s[i] * s[i];
+        }
+        team_sum<1024>(sq, red[odd]);
+        const float r = __builtin_amdgcn_rsqf(sq[0] * a.inv_cols + a.eps);
+        for (int col = threadIdx.x * 8; col < end; col += 8192) {
+            load_sum<T>(a, row, col, a.cols - col, s);
+            put_row<T, MX>(a, row, col, r, s);
+        }
+    }
+}
+
+// dx of eight columns (into g), and dy s r (into s)
+template <typename T>
+__device__ __forceinline__ void back8(const NormArgs& a, int64_t row, int col, float r, float c, float s[8], float dy[8], const float w[8]) {
+    const int cnt = a.cols - col;
+    float ds[8] = {};
+    if (a.y && a.res) load8(static_cast<const T*>(a.res) + row * a.ld_res + col, cnt, ds);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float n = dy[i] * (s[i] * r);
+        dy[i] = r * (dy[i] * w[i] - s[i] * c) + ds[i];
+        s[i] = n;
+    }
+    if (a.y) store8(static_cast<T*>(a.y) + row * a.ld_y + col, cnt, dy);
+}
+
+template <typename T, int P, int U>
+__global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs a) {
+    constexpr int TEAMS = kTeams<P>;
+    __shared__ float red[2][P > 64 ? P / 64 : 1][2];
+    __shared__ float sums[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? P * U * 8 : 1];
+    const int t = threadIdx.x % P, team = threadIdx.x / P;
+    float dw[U][8] = {}, w[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_weight<T>(a.weight, (u * P + t) * 8, a.cols - (u * P + t) * 8, w[u]);
+    int odd = 0;
+    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS, odd ^= 1) {
+        float s[U][8], dy[U][8], v[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (u * P + t) * 8, cnt = a.cols - col;
+            load8(static_cast<const T*>(a.x) + row * a.ld_x + col, cnt, s[u]);
+            load8(static_cast<const T*>(a.dy) + row * a.ld_dy + col, cnt, dy[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[0] += s[u][i] * s[u][i];
+                v[1] += dy[u][i] * w[u][i] * s[u][i];
+            }
+        team_sum<P>(v, red[odd]);
+        const float r = __builtin_amdgcn_rsqf(v[0] * a.inv_cols + a.eps), c = r * r * (v[1] * a.inv_cols);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            back8<T>(a, row, (u * P + t) * 8, r, c, s[u], dy[u], w[u]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dw[u][i] += s[u][i];
+        }
+    }
+    if (!a.part) return;
+    float* const part = a.part + (int64_t)blockIdx.x * a.part_ld;
+    if constexpr (TEAMS > 1) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sums[team][(u * P + t) * 8 + i] = dw[u][i];
+        __syncthreads();
+        for (int col = threadIdx.x; col < a.cols; col += 256) {
+            float d = sums[0][col];
+#pragma unroll
+            for (int m = 1; m < TEAMS; ++m) d += sums[m][col];
+            part[col] = d;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (u * P + t) * 8;
+            if (col < a.cols) store8(part + col, 8, dw[u]);  // (the pitch has room for whole chunks)
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_back_long(const NormArgs a) {
+    __shared__ float red[2][16][2];
+    float* const part = a.part ? a.part + (int64_t)blockIdx.x * a.part_ld : nullptr;
+    int odd = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, odd ^= 1) {
+        float s[8], dy[8], w[8], v[2] = {0.0f, 0.0f};
+        const auto load = [&](int col) {
+            const int cnt = a.cols - col;
+            load8(static_cast<const T*>(a.x) + row * a.ld_x + col, cnt, s);
+            load8(static_cast<const T*>(a.dy) + row * a.ld_dy + col, cnt, dy);
+            load_weight<T>(a.weight, col, cnt, w);
+        };
+        for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            load(col);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[0] += s[i] * s[i];
+                v[1] += dy[i] * w[i] * s[i];
+            }
+        }
+        team_sum<1024>(v, red[odd]);
+        const float r = __builtin_amdgcn_rsqf(v[0] * a.inv_cols + a.eps), c = r * r * (v[1] * a.inv_cols);
+        for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            load(col);
+            back8<T>(a, row, col, r, c, s, dy, w);
+            if (part) {
+                float d[8] = {};
+                if (row != blockIdx.x) load8(part + col, 8, d);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] += s[i];
+                store8(part + col, 8, d);
+            }
+        }
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxCols = int64_t(1) << 20;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+
+// Work-groups of a backward call, each with partial sums of its own for the weight's gradient: two for every place of 1024
+// threads, and no more than there are rows for
+int64_t back_groups(int64_t rows, int64_t cols) {
+    const int teams = cols <= 128 ? 16 : cols <= 1024 ? 4 : 1;
+    const int64_t most = cols <= 4096 ? 1024 : 512, want = div_up(rows, teams);
+    return want < most ? want : most;
+}
+
+template <typename T, int P, int U>
+void go(const NormArgs& a, bool back, bool mx, int64_t groups, hipStream_t st) {
+    const dim3 block(P < 256 ? 256 : P);
+    if (back) return k_norm_back<T, P, U><<<dim3((unsigned)groups), block, 0, st>>>(a);
+    const dim3 grid((unsigned)div_up(a.rows, (int64_t)kTeams<P> * a.per));
+    if (mx) {
+        if constexpr (P >= 64) k_norm<T, P, U, true><<<grid, block, 0, st>>>(a);
+    } else {
+        k_norm<T, P, U, false><<<grid, block, 0, st>>>(a);
+    }
+}
+
+template <typename T>
+int launch(NormArgs a, bool back, bool mx, int64_t groups, hipStream_t st) {
+    const int64_t wide = mx ? mx_groups(a.cols) * kMxGroup : a.cols;
+    // (a launch has fewer than 2^32 threads: more rows than 2^20 are taken several by a team)
+    a.per = (int)div_up(a.rows, int64_t(1) << 20);
+    if (wide <= 128) go<T, 16, 1>(a, back, mx, groups, st);
+    else if (wide <= 512) go<T, 64, 1>(a, back, mx, groups, st);
+    else if (wide <= 1024) go<T, 64, 2>(a, back, mx, groups, st);
+    else if (wide <= 2048) go<T, 256, 1>(a, back, mx, groups, st);
+    else if (wide <= 4096) go<T, 256, 2>(a, back, mx, groups, st);
+    else if (wide <= 8192) go<T, 512, 2>(a, back, mx, groups, st);
+    else if (wide <= 16384) go<T, 1024, 2>(a, back, mx, groups, st);
+    else if (wide <= 32768) go<T, 1024, 4>(a, back, mx, groups, st);
+    else if (back) k_norm_back_long<T><<<dim3((unsigned)groups), dim3(1024), 0, st>>>(a);
+    else {
+        const dim3 grid((unsigned)(a.rows < (int64_t(1) << 20) ? a.rows : int64_t(1) << 20));
+        if (mx) k_norm_long<T, true><<<grid, dim3(1024), 0, st>>>(a);
+        else k_norm_long<T, false><<<grid, dim3(1024), 0, st>>>(a);
+    }
+    return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
+}
+
+// Checks the configuration and fills in what it says
+bool make_args(const dlc_norm_config* c, NormArgs* a) {
+    if (!c || (c->dtype != DLC_F32 && c->dtype != DLC_F16 && c->dtype != DLC_BF16) || c->reserved != 0) return false;
+    if (c->rows < 0 || c->rows > kMaxRows || c->cols < 1 || c->cols > kMaxCols) return false;
+    if (!(c->eps >= 0x1p-126 && c->eps <= 0x1p126)) return false;
+    const int64_t lim = c->rows > 0 ? (int64_t(1) << 60) / c->rows : int64_t(1) << 60;  // (a buffer's last byte has a 64-bit address)
+    for (const int64_t ld : {c->ld_x, c->ld_res, c->ld_sum, c->ld_y, c->ld_dy, c->ld_ds, c->ld_dx})
+        if (ld != 0 && (ld < c->cols || ld > lim)) return false;
+    a->rows = c->rows;
+    a->cols = (int)c->cols;
+    a->eps = (float)c->eps;
+    a->inv_cols = 1.0f / (float)c->cols;
+    return true;
+}
+
+int64_t ld_of(int64_t ld, int64_t cols) { return ld ? ld : cols; }
+bool good(const void* p, int es, bool need) { return p ? on(p, es) : !need; }
+// `out` may take the place of `in` element for element, not with other distances from row to row
+bool good_place(const void* in, int64_t ld_in, const void* out, int64_t ld_out, int64_t rows) { return !in || in != out || ld_in == ld_out || rows <= 1; }
+
+size_t back_bytes(int64_t rows, int64_t cols) { return (size_t)back_groups(rows, cols) * (size_t)round8(cols) * 4; }
+
+}  // namespace
+
+extern "C" size_t dlc_norm_workspace_bytes(const dlc_norm_config* c) {
+    NormArgs a{};
+    return make_args(c, &a) ? back_bytes(a.rows, a.cols) : 0;
+}
+
+extern "C" int dlc_norm_forward(const dlc_norm_config* c, const void* x, const void* res, const void* weight, void* sum, void* y, void* q,
+                                void* scale, void* stream) {
+    NormArgs a{};
+    if (!make_args(c, &a)) return DLC_EINVAL;
+    const int es = c->dtype == DLC_F32 ? 4 : 2;
+    const bool need = a.rows > 0;
+    if (!good(x, es, need) || !good(res, es, false) || !good(weight, es, false) || !good(sum, es, false) || !good(y, es, false) ||
+        !on(q, 16) || !on(scale, 16) || (q == nullptr) != (scale == nullptr) || (need && !sum && !y && !q)) return DLC_EINVAL;
+    if (!need) return DLC_OK;
+    a.ld_x = ld_of(c->ld_x, a.cols); a.ld_res = ld_of(c->ld_res, a.cols); a.ld_sum = ld_of(c->ld_sum, a.cols); a.ld_y = ld_of(c->ld_y, a.cols);
+    if (!good_place(x, a.ld_x, sum, a.ld_sum, a.rows) || !good_place(res, a.ld_res, sum, a.ld_sum, a.rows) ||
+        !good_place(x, a.ld_x, y, a.ld_y, a.rows) || (y && (y == sum || y == res))) return DLC_EINVAL;
+    a.x = x; a.res = res; a.weight = weight; a.sum = sum; a.y = y;
+    a.q = static_cast<uint8_t*>(q); a.scale = static_cast<uint8_t*>(scale);
+    hipStream_t st = (hipStream_t)stream;
+    switch (c->dtype) {
+        case DLC_F32: return launch<float>(a, false, q != nullptr, 0, st);
+        case DLC_F16: return launch<f16_t>(a, false, q != nullptr, 0, st);
+        default: return launch<bf16_t>(a, false, q != nullptr, 0, st);
+    }
+}
+
+extern "C" int dlc_norm_backward(const dlc_norm_config* c, const void* s, const void* weight, const void* dy, const void* ds, void* dx,
+                                 void* dweight, void* work, size_t work_bytes, void* stream) {
+    NormArgs a{};
+    if (!make_args(c, &a)) return DLC_EINVAL;
+    const int es = c->dtype == DLC_F32 ? 4 : 2;
+    const bool need = a.rows > 0 && (dx || dweight);
+    if (!good(s, es, need) || !good(weight, es, false) || !good(dy, es, need) || !good(ds, es, false) || !good(dx, es, false) ||
+        !good(dweight, es, false) || !on(work, 16)) return DLC_EINVAL;
+    if ((!dx || a.rows == 0) && !dweight) return DLC_OK;
+    a.ld_x = ld_of(c->ld_sum, a.cols); a.ld_res = ld_of(c->ld_ds, a.cols); a.ld_dy = ld_of(c->ld_dy, a.cols); a.ld_y = ld_of(c->ld_dx, a.cols);
+    if (!good_place(dy, a.ld_dy, dx, a.ld_y, a.rows) || !good_place(ds, a.ld_res, dx, a.ld_y, a.rows) || (dx && dx == s && a.rows > 0)) return DLC_EINVAL;
+    const int64_t groups = back_groups(a.rows, a.cols);
+    if (dweight && a.rows > 0) {
+        if (!work) return DLC_EINVAL;
+        if (work_bytes < back_bytes(a.rows, a.cols)) return DLC_ECAPACITY;
+        a.part = static_cast<float*>(work);
+        a.part_ld = round8(a.cols);
+    }
+    a.x = s; a.res = ds; a.weight = weight; a.dy = dy; a.y = dx;
+    hipStream_t st = (hipStream_t)stream;
+    const SumArgs sum{a.part, a.part_ld, (int)groups, a.cols, dweight};
+    const auto all = [&](auto one) {
+        using T = decltype(one);
+        if (a.rows > 0)
+            if (const int rc = launch<T>(a, true, false, groups, st); rc != DLC_OK) return rc;
+        if (!dweight) return (int)DLC_OK;
+        return DenseOps<T>::join(JoinArgs{}, JoinArgs{}, sum, st) == hipSuccess ? (int)DLC_OK : (int)DLC_EHIP;
+    };
+    switch (c->dtype) {
+        case DLC_F32: return all(float{});
+        case DLC_F16: return all(f16_t{});
+        default: return all(bf16_t{});
+    }
+}

@@ -1,0 +1,247 @@
+"""Microscaled form: quantisation and back bit for bit against the oracle, the product against 64 bits."""
+import numpy as np
+import pytest
+
+from dense_util import ACTS, F32, FN, ROUND, Guarded, act, assert_close, code, product, rounded, torch_type
+from mx_util import GuardedBytes, quantise, values
+
+pytestmark = pytest.mark.gpu
+TYPES = ["f32", "f16", "bf16"]
+
+
+def _matrix(rows, cols, dtype, seed, kind="normal"):
+    """values of the type, as a float64 array and a tensor"""
+    import torch
+    g = torch.Generator()
+    g.manual_seed(seed)
+    x = torch.randn((rows, cols), generator=g, dtype=torch.float64)
+    if kind == "wide":      # magnitudes from far below to far above one
+        x = x * 2.0 ** torch.randint(-14, 14, (rows, cols), generator=g).double()
+    t = x.to(torch_type(dtype))
+    return t.double().numpy(), t.cuda()
+
+
+def _quantised(x, bits, dtype, ld=None):
+    from paper_2407_04272_amd import binding as b
+    rows, cols = x.shape
+    cfg = b.make_mx_config(code(dtype), bits, rows, cols, ld_x=ld or 0)
+    q, s = GuardedBytes(b.dlc_mx_data_shape(cfg)), GuardedBytes(b.dlc_mx_scale_shape(cfg))
+    b.dlc_mx_quantize(cfg, x, q.view, s.view)
+    assert q.intact() and s.intact()
+    return q.view, s.view
+
+
+def _same(q, s, want_q, want_s, what):
+    assert np.array_equal(s.cpu().numpy(), want_s), f"{what}: scales"
+    assert np.array_equal(q.cpu().numpy(), want_q), f"{what}: elements"
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 31), (3, 32), (17, 33), (5, 128), (16, 129), (15, 511), (33, 512), (2, 513), (70, 1664), (1, 4097)])
+def test_quantise(rows, cols, dtype, bits):
+    for kind in ("normal", "wide"):
+        x, t = _matrix(rows, cols, dtype, rows * 7 + cols, kind)
+        _same(*_quantised(t, bits, dtype), *quantise(x, bits), f"{kind} {rows}x{cols}")
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantise_rows_apart(dtype, bits):
+    for shift in (0, 1, 3):
+        x, t = _matrix(9, 300, dtype, 5 + shift)
+        v = Guarded(9, 300, dtype, ld=317, shift=shift).set(t)
+        _same(*_quantised(v.view, bits, dtype, 317), *quantise(x, bits), f"shift {shift}")
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantise_borders(dtype, bits):
+    """Blocks whose largest magnitude is at, just below and just above the largest value times a power of two, ties between
+    elements, zeros of both signs, the type's smallest and largest values, NaN and infinities."""
+    import torch
+    ty = torch_type(dtype)
+    fin = torch.finfo(ty)
+    top = 448.0 if bits == 8 else 6.0
+    ulp = float(fin.eps)
+    rows = []
+    for e in (-10, -1, 0, 3, 6):
+        for m in (top, top * (1 - ulp), top * (1 + ulp), top / 2, top * 0.75, top * 0.7500001, 1.0):
+            rows.append([m * 2.0 ** e] + [m * 2.0 ** e * f for f in (0.5, -0.25, 1 / 3, -1 / 28, 0.01, 0.001, -1e-4)])
+    ties = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0] if bits == 4 else [17.0, 19.0, 1.0625, 1.1875, 2.0 ** -10, 3 * 2.0 ** -10, 432.0, 208.0]
+    rows.append([top] + [t for t in ties[:7]])
+    rows.append([-top] + [-t for t in ties[-7:]])
+    rows.append([0.0, -0.0, 0.0, -0.0, 0.0, 0.0, 0.0, -0.0])
+    rows.append([fin.tiny, fin.smallest_normal / 2, -fin.tiny, fin.tiny * 3, 0.0, -0.0, fin.tiny, fin.tiny])
+    rows.append([float(fin.smallest_normal) * ulp, 0, 0, 0, 0, 0, -float(fin.smallest_normal) * ulp, 0])
+    rows.append([fin.max, -fin.max, fin.max / 2, 1.0, fin.tiny, 0, 0, 0])
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        rows.append([1.0, 2.0, bad, 3.0, 0, 0, -1.0, 0])
+    x = torch.zeros((len(rows), 96), dtype=torch.float64)
+    for i, r in enumerate(rows):
+        x[i, 40:48] = torch.tensor(r, dtype=torch.float64)    # (the second of three blocks)
+        x[i, 3] = 1.0
+    t = x.to(ty)
+    q, s = _quantised(t.cuda(), bits, dtype)
+    _same(q, s, *quantise(t.double().numpy(), bits), "borders")
+    assert s[0, -1].cpu().tolist().count(255) == 1
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,ld", [(1, 1, 0), (19, 333, 0), (7, 1030, 1039)])
+def test_back(rows, cols, ld, dtype, bits):
+    """Any codes and scales: every element's value is exact in 64 bits and rounded once."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    rng = np.random.default_rng(rows + cols)
+    cfg = b.make_mx_config(code(dtype), bits, rows, cols, ld_y=ld)
+    q = rng.integers(0, 256, b.dlc_mx_data_shape(cfg), dtype=np.uint8)
+    s = rng.integers(127 - 20, 127 + 20, b.dlc_mx_scale_shape(cfg), dtype=np.uint8)
+    if rows > 1:
+        s[:, 1] = rng.integers(0, 256, s[:, 1].shape, dtype=np.uint8)      # far scales: subnormal, infinite, NaN
+    y = Guarded(rows, cols, dtype, ld=ld or None)
+    b.dlc_mx_dequantize(cfg, torch.from_numpy(q).cuda(), torch.from_numpy(s).cuda(), y.view)
+    with np.errstate(all="ignore"):
+        want = torch.from_numpy(values(q, s, cols, bits))
+    # (a value past fp32's range is an infinity on the way, as it is in the type)
+    assert torch.equal(y.view.cpu().nan_to_num(nan=-7.0), want.to(torch_type(dtype)).nan_to_num(nan=-7.0))
+    assert y.intact() or bool(torch.isnan(y.view).any())
+
+
+def test_no_rows():
+    import torch
+    from paper_2407_04272_amd import binding as b
+    cfg = b.make_mx_config(b.F32, b.MX_E2M1, 0, 40)
+    q, s = (torch.empty(shape, dtype=torch.uint8, device="cuda") for shape in (b.dlc_mx_data_shape(cfg), b.dlc_mx_scale_shape(cfg)))
+    x = torch.empty((0, 40), device="cuda")
+    b.dlc_mx_quantize(cfg, x, q, s)
+    b.dlc_mx_dequantize(cfg, q, s, x)
+    w = torch.zeros((24, 64), dtype=torch.uint8, device="cuda")
+    b.dlc_mx_linear_forward(b.make_mx_linear_config(b.F32, b.MX_E2M1, 0, 40, 24), q, s, w, torch.zeros((1, 24, 16), dtype=torch.uint8, device="cuda"),
+                            None, None, torch.empty((0, 24), device="cuda"))
+
+
+# ---- the product --------------------------------------------------------------------------------
+# E4M3 times E2M1 with results of half precision: of eight products each loses less than 2^-13 of the largest one, which itself
+# loses nothing
+CUT = 7 * 2.0 ** -13
+
+
+def _operand(rows, cols, bits, seed, spread=2.0):
+    """a matrix in microscaled form (on the GPU) and what it stands for (float64, on the GPU)"""
+    import torch
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((rows, cols)) * np.exp2(rng.integers(-spread, spread + 1, (rows, cols)))
+    q, s = quantise(x.astype(np.float32).astype(np.float64), bits)
+    return torch.from_numpy(q).cuda(), torch.from_numpy(s).cuda(), torch.from_numpy(values(q, s, cols, bits)).cuda()
+
+
+def _linear(rows, n_in, n_out, bits, dtype, act_name="none", bias=False, residual=False, ld=0, seed=1, inplace=False):
+    import torch
+    from paper_2407_04272_amd import binding as b
+    xq, xs, x = _operand(rows, n_in, bits, seed)
+    wq, ws, w = _operand(n_out, n_in, 4, seed + 1)
+    ty = torch_type(dtype)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    cfg = b.make_mx_linear_config(code(dtype), bits, rows, n_in, n_out, act=ACTS.index(act_name), ld_y=ld, ld_res=ld if inplace else 0)
+    vb = torch.randn((n_out,), generator=g, device="cuda").to(ty) if bias else None
+    vr = torch.randn((rows, n_out), generator=g, device="cuda").to(ty) if residual else None
+    y = Guarded(rows, n_out, dtype, ld=ld or None, shift=1 if ld else 0)
+    res = vr
+    if inplace:
+        y.set(vr)
+        res = y.view
+    work = torch.empty(b.dlc_mx_linear_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    b.dlc_mx_linear_forward(cfg, xq, xs, wq, ws, vb, res, y.view, work)
+    assert y.intact()
+    z, ez = product(x, w)
+    if bits == 8 and dtype != "f32":
+        ez = ez + CUT * (x.abs() @ w.abs().t())
+    if bias:
+        z = z + vb.double()
+        ez = ez + z.abs() * F32
+    v, _ = act(act_name, z)
+    # slopes of these functions stay below 1.13
+    err = ez if act_name == "none" else 1.13 * ez + FN * (1 + v.abs())
+    if residual:
+        v = v + vr.double()
+        err = err + v.abs() * F32
+    what = f"{rows}x{n_in}->{n_out} {bits} {dtype} {act_name}"
+    assert_close(y.view, v, rounded(v, err, dtype), what)
+    # in the norm the cut products of random signs are far below a rounding
+    if rows * n_out >= 1000:
+        assert float((y.view.double() - v).norm()) <= (ROUND[dtype] + 2.0 ** -12 * (bits == 8 and dtype != "f32") + (n_in + 2) * F32) * float(v.norm()), what
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 1, 1), (1, 1664, 1024), (2, 33, 17), (7, 128, 16), (16, 8192, 96), (17, 129, 65), (31, 513, 40),
+                                             (33, 640, 130), (64, 1024, 64), (65, 2049, 127), (130, 259, 513), (300, 512, 260), (777, 515, 1023)])
+def test_product(rows, n_in, n_out, dtype, bits):
+    _linear(rows, n_in, n_out, bits, dtype, seed=rows + n_in)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("rows,n_in,n_out", [(512, 4096, 512), (1024, 1664, 1280), (257, 8192, 2048), (2048, 768, 2304)])
+def test_large_product(rows, n_in, n_out, bits):
+    _linear(rows, n_in, n_out, bits, "f32", seed=3)
+    _linear(rows, n_in, n_out, bits, "bf16", "relu", bias=True, residual=True, seed=4)
+
+
+@pytest.mark.parametrize("act_name", ACTS)
+@pytest.mark.parametrize("rows", [1, 20, 100, 600])
+def test_epilogue(rows, act_name):
+    for dtype in TYPES:
+        _linear(rows, 96, 200, 8, dtype, act_name, bias=True, residual=True, seed=9)
+        _linear(rows, 96, 201, 4, dtype, act_name, bias=True, ld=219, seed=10)
+
+
+@pytest.mark.parametrize("rows", [1, 40, 513])
+def test_residual_in_place(rows):
+    for dtype in TYPES:
+        _linear(rows, 200, 72, 4, dtype, "relu", residual=True, ld=88, inplace=True)
+
+
+def test_exact_sums():
+    """Small whole numbers: every product and sum is exact in fp32, and so is the result, whatever the order."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    rng = np.random.default_rng(2)
+    for rows, n_in, n_out in ((5, 700, 90), (40, 3000, 70), (600, 1100, 600)):
+        for bits in (4, 8):
+            x = rng.choice([-2.0, -1.0, 0.0, 1.0, 2.0, 4.0], (rows, n_in))
+            w = rng.choice([-1.0, 0.0, 1.0, 3.0], (n_out, n_in))
+            (xq, xs), (wq, ws) = quantise(x, bits), quantise(w, 4)
+            y = torch.empty((rows, n_out), device="cuda")
+            cfg = b.make_mx_linear_config(b.F32, bits, rows, n_in, n_out)
+            work = torch.empty(b.dlc_mx_linear_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+            b.dlc_mx_linear_forward(cfg, *(torch.from_numpy(v).cuda() for v in (xq, xs, wq, ws)), None, None, y, work)
+            assert np.array_equal(y.cpu().numpy(), (x @ w.T).astype(np.float32))
+
+
+@pytest.mark.parametrize("rows", [1, 24, 200, 600])
+def test_scales_far_apart_and_nan(rows):
+    """Blocks of one row whose scales are far apart; a NaN block makes its row (of x) or column (of w) NaN and no other."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    n_in, n_out = 1200, 48
+    for bits in (4, 8):
+        xq, xs, x = _operand(rows, n_in, bits, 21, spread=12)
+        wq, ws, w = _operand(n_out, n_in, 4, 22, spread=12)
+        if rows > 1:
+            xs[1, 1, 5] = 255
+        ws[0, 7, 9] = 255
+        y = torch.empty((rows, n_out), device="cuda")
+        cfg = b.make_mx_linear_config(b.F32, bits, rows, n_in, n_out)
+        work = torch.empty(b.dlc_mx_linear_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        b.dlc_mx_linear_forward(cfg, xq, xs, wq, ws, None, None, y, work)
+        nan = torch.zeros_like(y, dtype=torch.bool)
+        nan[:, 7] = True
+        if rows > 1:
+            nan[1] = True
+        assert torch.equal(torch.isnan(y), nan)
+        v, e = product(x, w)
+        keep = ~nan
+        assert_close(y[keep], v[keep], rounded(v, e, "f32")[keep], f"{rows} {bits}")
