@@ -164,6 +164,10 @@ extern "C" int dlc_mx_linear_forward(const dlc_mx_linear_config* c, const void* 
     g.c.lda = mx_row_bytes(s.K, s.elem); g.c.ldb = mx_row_bytes(s.K, DLC_MX_E2M1);
     g.c.M = (int)s.M; g.c.N = (int)s.N; g.c.K = (int)mx_filled(s.K);
     g.c.split = 1; g.c.kper = g.c.K;
+    if (s.M > 128 && s.N > 128 && !(s.elem == DLC_MX_E4M3 && s.es == 4)) {
+        g.c.tiles_m = (int)div_up(s.M, 256);
+        g.c.tiles_n = (int)div_up(s.N, 256);
+    }
     Epi& e = g.c.e;
     e.y = y; e.res = res; e.bias = bias;
     e.ld_y = s.ldy; e.ld_res = s.ldres; e.act = c->act; e.n = (int)s.N;

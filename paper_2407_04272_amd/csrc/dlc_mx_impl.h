@@ -111,8 +111,285 @@ __global__ __launch_bounds__(64) void k_mx_direct(const MxGemmArgs ga) {
     write_block<T, false, 64>(c, acc, 0, lds, m0, n0, 0, lane);
 }
 
+// ---- 256 x 256 tiles ----
+// The pipeline of the half-precision products' widest tile (gemm_wide): four wavefronts, each with 128 x 128 of C in the second
+// half of the register file; while a step (128 k values) is multiplied, the next one's fragments are read from LDS, and tiles
+// of 128 bytes of a row are on their way there.  16 products of 16 x 16 x 128 are one block of assembly, with the reads
+// between them: a wavefront has its SIMD to itself.  Loads, scales' among them, stand between the blocks; their waits are the
+// compiler's and wait_loads'.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+#define DLC_MX(OP, BL, ACC, B, A, SB, SA) "v_mfma_scale_f32_16x16x128_f8f6f4 %" #ACC ", %" #B ", %" #A ", %" #ACC ", %" #SB ", %" #SA " " OP " cbsz:4 blgp:" BL "\n\t"
+#define DLC_MX_CHUNK4(OP, BL) \
+    asm volatile("s_nop 1\n\t" \
+    DLC_MX(OP, BL, 4, 22, 20, 32, 30) "ds_read_b128 %0, %40 offset:%41\n\t" DLC_MX(OP, BL, 5, 23, 20, 33, 30) "ds_read_b128 %1, %40 offset:%42\n\t" \
+    DLC_MX(OP, BL, 6, 24, 20, 34, 30) "ds_read_b128 %2, %40 offset:%43\n\t" DLC_MX(OP, BL, 7, 25, 20, 35, 30) "ds_read_b128 %3, %40 offset:%44\n\t" \
+    DLC_MX(OP, BL, 8, 26, 20, 36, 30) DLC_MX(OP, BL, 9, 27, 20, 37, 30) DLC_MX(OP, BL, 10, 28, 20, 38, 30) DLC_MX(OP, BL, 11, 29, 20, 39, 30) \
+    DLC_MX(OP, BL, 12, 22, 21, 32, 31) DLC_MX(OP, BL, 13, 23, 21, 33, 31) DLC_MX(OP, BL, 14, 24, 21, 34, 31) DLC_MX(OP, BL, 15, 25, 21, 35, 31) \
+    DLC_MX(OP, BL, 16, 26, 21, 36, 31) DLC_MX(OP, BL, 17, 27, 21, 37, 31) DLC_MX(OP, BL, 18, 28, 21, 38, 31) DLC_MX(OP, BL, 19, 29, 21, 39, 31) \
+    "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(next[0]), "=&v"(next[1]), "=&v"(next[2]), "=&v"(next[3]), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc0[4]), "+a"(acc0[5]), "+a"(acc0[6]), "+a"(acc0[7]), \
+      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]), "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "v"(sa0), "v"(sa1), \
+      "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), "v"(sb[4]), "v"(sb[5]), "v"(sb[6]), "v"(sb[7]), "v"(from), "i"(OFF), "i"(OFF + STEP), "i"(OFF + 2 * STEP), "i"(OFF + 3 * STEP) \
+    : "memory")
+#define DLC_MX_CHUNK8(OP, BL) \
+    asm volatile("s_nop 1\n\t" \
+    DLC_MX(OP, BL, 6, 24, 22, 34, 32) "ds_read_b128 %0, %42 offset:%45\n\t" DLC_MX(OP, BL, 7, 25, 22, 35, 32) "ds_read_b128 %1, %43 offset:%45\n\t" \
+    DLC_MX(OP, BL, 8, 26, 22, 36, 32) "ds_read_b128 %2, %42 offset:%46\n\t" DLC_MX(OP, BL, 9, 27, 22, 37, 32) "ds_read_b128 %3, %43 offset:%46\n\t" \
+    DLC_MX(OP, BL, 10, 28, 22, 38, 32) "ds_read_b128 %4, %44 offset:%47\n\t" DLC_MX(OP, BL, 11, 29, 22, 39, 32) "ds_read_b128 %5, %44 offset:%48\n\t" \
+    DLC_MX(OP, BL, 12, 30, 22, 40, 32) DLC_MX(OP, BL, 13, 31, 22, 41, 32) DLC_MX(OP, BL, 14, 24, 23, 34, 33) DLC_MX(OP, BL, 15, 25, 23, 35, 33) \
+    DLC_MX(OP, BL, 16, 26, 23, 36, 33) DLC_MX(OP, BL, 17, 27, 23, 37, 33) DLC_MX(OP, BL, 18, 28, 23, 38, 33) DLC_MX(OP, BL, 19, 29, 23, 39, 33) \
+    DLC_MX(OP, BL, 20, 30, 23, 40, 33) DLC_MX(OP, BL, 21, 31, 23, 41, 33) \
+    "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(na[0]), "=&v"(na[1]), "=&v"(na[2]), "=&v"(na[3]), "=&v"(nb[0]), "=&v"(nb[1]), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc0[4]), "+a"(acc0[5]), "+a"(acc0[6]), "+a"(acc0[7]), \
+      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]), "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "v"(sa0), "v"(sa1), \
+      "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), "v"(sb[4]), "v"(sb[5]), "v"(sb[6]), "v"(sb[7]), "v"(from0), "v"(from1), "v"(from_b), "i"(OFF_A), "i"(OFF_A + STEP), "i"(OFF_B), "i"(OFF_B + STEP) \
+    : "memory")
+#define DLC_MX_BYTE0 "op_sel_hi:[0,0,0]"
+#define DLC_MX_BYTE1 "op_sel:[1,1,0] op_sel_hi:[0,0,0]"
+#define DLC_MX_BYTE2 "op_sel_hi:[1,1,0]"
+#define DLC_MX_BYTE3 "op_sel:[1,1,0] op_sel_hi:[1,1,0]"
+
+// Rows of blocks acc0 and acc1 += a0 and a1 times b, with byte S of the scales; four fragments, STEP bytes apart, are read
+template <int S, int OFF, int STEP>
+__device__ __forceinline__ void mx_chunk4(f32x4* acc0, f32x4* acc1, const u32x4_t& a0, const u32x4_t& a1, const u32x4_t* b, uint32_t sa0,
+                                          uint32_t sa1, const uint32_t* sb, u32x4_t* next, uint32_t from) {
+    if constexpr (S == 0) DLC_MX_CHUNK4(DLC_MX_BYTE0, "4");
+    else if constexpr (S == 1) DLC_MX_CHUNK4(DLC_MX_BYTE1, "4");
+    else if constexpr (S == 2) DLC_MX_CHUNK4(DLC_MX_BYTE2, "4");
+    else DLC_MX_CHUNK4(DLC_MX_BYTE3, "4");
+}
+
+// ... a0 and a1 of 8 bits an element; two rows' fragments of two chunks each (at from0 and from1) and two of b are read
+template <int S, int OFF_A, int OFF_B, int STEP>
+__device__ __forceinline__ void mx_chunk8(f32x4* acc0, f32x4* acc1, const i32x8& a0, const i32x8& a1, const u32x4_t* b, uint32_t sa0,
+                                          uint32_t sa1, const uint32_t* sb, u32x4_t* na, u32x4_t* nb, uint32_t from0, uint32_t from1, uint32_t from_b) {
+    if constexpr (S == 0) DLC_MX_CHUNK8(DLC_MX_BYTE0, "0");
+    else if constexpr (S == 1) DLC_MX_CHUNK8(DLC_MX_BYTE1, "0");
+    else if constexpr (S == 2) DLC_MX_CHUNK8(DLC_MX_BYTE2, "0");
+    else DLC_MX_CHUNK8(DLC_MX_BYTE3, "0");
+}
+#undef DLC_MX
+#undef DLC_MX_CHUNK4
+#undef DLC_MX_CHUNK8
+#undef DLC_MX_BYTE0
+#undef DLC_MX_BYTE1
+#undef DLC_MX_BYTE2
+#undef DLC_MX_BYTE3
+#pragma clang diagnostic pop
+
+// One operand's scales: a lane's words for N blocks of 16 rows, four steps each
+template <int N>
+struct Scales {
+    const uint8_t* base;  // of the tile's first row in the next group
+    int64_t left;         // bytes from there to the end
+    int64_t step;
+    uint32_t voff;
+    uint32_t now[N], next[N];
+    // row: the tile's first; mine: the wavefront's first row in it
+    __device__ __forceinline__ void init(const uint8_t* p, int row, int mine, int rows, int group, int groups, int lane) {
+        step = (int64_t)rows * 16;
+        base = p + (int64_t)group * step + (int64_t)row * 16;
+        left = (int64_t)(groups - group) * step - (int64_t)row * 16;
+        voff = (uint32_t)((mine + (lane & 15)) * 16 + (lane >> 4) * 4);
+    }
+    // The next group's (past the last: zeros; rows past the last get others' scales, and their sums are not stored)
+    __device__ __forceinline__ void load() {
+        const uint32_t range = left <= 0 ? 0u : left < 8192 ? (uint32_t)left : 8192u;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, range, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < N; ++i) next[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rs, voff + i * 256, 0, 0);
+        base += step;
+        left -= step;
+    }
+    __device__ __forceinline__ void turn() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) now[i] = next[i];
+    }
+};
+
+template <typename T, int ELEM>
+__global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int THREADS = 256, W = 256, P = W / 2, MI = P / 16, NJ = MI, TB = 128;
+    using OpA = Operand<uint8_t, false, W, TB, THREADS, false>;
+    using OpB = OpA;
+    constexpr int B0 = 3 * OpA::BYTES, STEP = 16 * TB;
+    __shared__ __attribute__((aligned(16))) char lds[5 * OpA::BYTES];
+    const GemmArgs& ga = mx.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tm, tn, sp;
+    tile_of(blockIdx.x, gridDim.x, ga.tiles_m, ga.tiles_n, tm, tn, sp);
+    const int m0 = tm * W, n0 = tn * W;
+    const int k0 = sp * ga.kper, k1 = min(ga.K, k0 + ga.kper), groups = (ga.K + kMxGroup - 1) / kMxGroup;
+    const int wm = (wave >> 1) * P, wn = (wave & 1) * P;
+    OpA oa;
+    OpB ob;
+    oa.init(ga.a, ga.lda, m0, ga.M, k0 * ELEM / 8, k1 * ELEM / 8, tid);
+    ob.init(ga.b, ga.ldb, n0, ga.N, k0 / 2, k1 / 2, tid);
+    Scales<MI> sa;
+    Scales<NJ> sb;
+    sa.init(mx.xs, m0, wm, ga.M, k0 / kMxGroup, groups, lane);
+    sb.init(mx.ws, n0, wn, ga.N, k0 / kMxGroup, groups, lane);
+
+    f32x4 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds;
+    typename OpA::template Place<MI> pa;
+    typename OpB::template Place<NJ> pb;
+    OpA::template place<MI>(pa, at, wm, lane);
+    OpB::template place<NJ>(pb, at + B0, wn, lane);
+    keep(pa);
+    keep(pb);
+    uint32_t slot_a = 0, slot_b = 0;  // slots of the current tiles, in bytes
+    const auto after = [](uint32_t s) { return s == 2 * OpA::BYTES ? 0u : s + (uint32_t)OpA::BYTES; };
+    const auto before = [](uint32_t s) { return s == 0 ? 2u * OpA::BYTES : s - (uint32_t)OpA::BYTES; };
+    sa.load();
+    sb.load();
+    sa.turn();
+    sb.turn();
+
+    if constexpr (ELEM == 4) {
+        const int tiles = (k1 - k0 + 255) / 256;
+        struct { u32x4_t a[MI], b[NJ]; } f[2];
+        oa.fetch(lds, tid);
+        ob.fetch(lds + B0, tid);
+        oa.fetch(lds + OpA::BYTES, tid);
+        ob.fetch(lds + B0 + OpB::BYTES, tid);
+        wait_loads<2 * OpA::PASSES>();
+        bare_barrier();
+        read_rows<NJ, STEP, 0>(f[0].b, pb.a[0]);
+        read_rows<MI, STEP, 0>(f[0].a, pa.a[0]);
+        settle(acc);
+        // A step's products with c's fragments while n's are read; behind each of the four blocks two loads
+        const auto multiply = [&](auto step, auto& c, auto& n, uint32_t ra, uint32_t rb, const auto& o, char* to) {
+            constexpr int S = decltype(step)::value;
+            mx_chunk4<S, 0, STEP>(acc[0], acc[1], c.a[0], c.a[1], c.b, sa.now[0], sa.now[1], sb.now, n.b, rb);
+            o.template load<0, 2>(to, tid);
+            mx_chunk4<S, 4 * STEP, STEP>(acc[2], acc[3], c.a[2], c.a[3], c.b, sa.now[2], sa.now[3], sb.now, n.b + 4, rb);
+            o.template load<2, 2>(to, tid);
+            mx_chunk4<S, 0, STEP>(acc[4], acc[5], c.a[4], c.a[5], c.b, sa.now[4], sa.now[5], sb.now, n.a, ra);
+            o.template load<4, 2>(to, tid);
+            mx_chunk4<S, 4 * STEP, STEP>(acc[6], acc[7], c.a[6], c.a[7], c.b, sa.now[6], sa.now[7], sb.now, n.a + 4, ra);
+            o.template load<6, 2>(to, tid);
+        };
+        const auto tile = [&](auto first, auto second) {
+            // the tile's first half; A's tile after the next goes where the one before was
+            oa.mask();
+            multiply(first, f[0], f[1], pa.a[1] + slot_a, pb.a[1] + slot_b, oa, lds + before(slot_a));
+            oa.advance();
+            // the next tiles have come, and all have read this one: B's after the next takes its place
+            wait_loads<OpA::PASSES>();
+            bare_barrier();
+            slot_a = after(slot_a);
+            const uint32_t free_b = slot_b;
+            slot_b = OpB::BYTES - slot_b;
+            ob.mask();
+            multiply(second, f[1], f[0], pa.a[0] + slot_a, pb.a[0] + slot_b, ob, lds + B0 + free_b);
+            ob.advance();
+        };
+        for (int s = 0; s < tiles; s += 2) {
+            sa.load();
+            sb.load();
+            tile(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+            if (s + 1 < tiles) tile(std::integral_constant<int, 2>{}, std::integral_constant<int, 3>{});
+            sa.turn();
+            sb.turn();
+        }
+    } else {
+        const int steps = (k1 - k0 + 127) / 128;
+        u32x4_t a[2][4], b[2][NJ];  // two rows' fragments of A, two chunks each, and the next two's
+        oa.fetch(lds, tid);
+        ob.fetch(lds + B0, tid);
+        oa.fetch(lds + OpA::BYTES, tid);
+        ob.fetch(lds + B0 + OpB::BYTES, tid);
+        wait_loads<2 * OpA::PASSES>();
+        bare_barrier();
+        read_rows<NJ, STEP, 0>(b[0], pb.a[0]);
+        read_halves<2, STEP>(a[0], pa.a[0], pa.a[1]);
+        settle(acc);
+        const auto wide = [](const u32x4_t& x, const u32x4_t& y) {
+            return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+        };
+        // Step n, S of its group: multiplies A's tile n and half H of a tile of B, reads what comes next.  Behind the barrier
+        // before its last block all have read tile n, and n + 1 has come: tile n + 3 takes n's place, in eight loads until the
+        // middle of the next step.  Behind an odd step's barrier B's tile after the next goes before them.
+        const auto step = [&](auto which) {
+            constexpr int S = decltype(which)::value, H = S & 1;
+            const uint32_t ra = slot_a, nx = after(slot_a), free_b = slot_b;
+            const uint32_t rb = H == 0 ? pb.a[1] + slot_b : pb.a[0] + (OpB::BYTES - slot_b);
+            char* const early = lds + before(slot_a);
+            char* const late = lds + slot_a;
+            u32x4_t* const nb = b[1 - H];
+            const u32x4_t* const cb = b[H];
+            mx_chunk8<S, 2 * STEP, 0, STEP>(acc[0], acc[1], wide(a[0][0], a[0][1]), wide(a[0][2], a[0][3]), cb, sa.now[0], sa.now[1], sb.now, a[1], nb,
+                                            pa.a[0] + ra, pa.a[1] + ra, rb);
+            if constexpr (H == 0) oa.template load<0, 4>(early, tid);
+            else oa.template load<4, 2>(early, tid);
+            mx_chunk8<S, 4 * STEP, 2 * STEP, STEP>(acc[2], acc[3], wide(a[1][0], a[1][1]), wide(a[1][2], a[1][3]), cb, sa.now[2], sa.now[3], sb.now, a[0],
+                                                   nb + 2, pa.a[0] + ra, pa.a[1] + ra, rb);
+            if constexpr (H == 0) oa.template load<4, 4>(early, tid);
+            else oa.template load<6, 2>(early, tid);
+            oa.advance();
+            oa.mask();
+            mx_chunk8<S, 6 * STEP, 4 * STEP, STEP>(acc[4], acc[5], wide(a[0][0], a[0][1]), wide(a[0][2], a[0][3]), cb, sa.now[4], sa.now[5], sb.now, a[1],
+                                                   nb + 4, pa.a[0] + ra, pa.a[1] + ra, rb);
+            wait_loads<OpA::PASSES>();
+            bare_barrier();
+            if constexpr (H == 0) {
+                oa.template load<0, 2>(late, tid);
+            } else {
+                if constexpr (S == 1) {
+                    sa.load();
+                    sb.load();
+                }
+                ob.mask();
+                ob.template load<0, 4>(lds + B0 + free_b, tid);
+            }
+            mx_chunk8<S, 0, 6 * STEP, STEP>(acc[6], acc[7], wide(a[1][0], a[1][1]), wide(a[1][2], a[1][3]), cb, sa.now[6], sa.now[7], sb.now, a[0],
+                                            nb + 6, pa.a[0] + nx, pa.a[1] + nx, rb);
+            if constexpr (H == 0) {
+                oa.template load<2, 2>(late, tid);
+            } else {
+                ob.template load<4, 4>(lds + B0 + free_b, tid);
+                ob.advance();
+                slot_b = OpB::BYTES - slot_b;
+            }
+            slot_a = nx;
+        };
+        oa.mask();
+        for (int n = 0; n < steps; n += 4) {
+            step(std::integral_constant<int, 0>{});
+            if (n + 1 < steps) step(std::integral_constant<int, 1>{});
+            if (n + 2 < steps) step(std::integral_constant<int, 2>{});
+            if (n + 3 < steps) step(std::integral_constant<int, 3>{});
+            sa.turn();
+            sb.turn();
+        }
+    }
+    wait_loads<0>();  // (tiles past the last may still be on their way)
+    settle(acc);
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < P / 64; ++h) write_block<T, false, P>(ga, acc, h * 4, lds + wave * P * 256, m0 + wm, n0 + wn + h * 64, sp, lane);
+#endif
+}
+
 template <typename T>
 hipError_t MxOps<T>::gemm(const MxGemmArgs& g, int elem_x, hipStream_t s) {
+    if (g.c.tiles_m > 0) {
+        const dim3 grid((unsigned)(g.c.tiles_m * g.c.tiles_n * g.c.split));
+        if (elem_x == DLC_MX_E2M1) k_mx_wide<T, 4><<<grid, dim3(256), 0, s>>>(g);
+        else if constexpr (!kMxExact<T, 8>) k_mx_wide<T, 8><<<grid, dim3(256), 0, s>>>(g);
+        return hipGetLastError();
+    }
     const dim3 grid((unsigned)(((g.c.M + 63) / 64) * ((g.c.N + 63) / 64))), block(64);
     if (elem_x == DLC_MX_E4M3) k_mx_direct<T, 8><<<grid, block, 0, s>>>(g);
     else k_mx_direct<T, 4><<<grid, block, 0, s>>>(g);
