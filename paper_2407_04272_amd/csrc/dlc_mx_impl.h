@@ -120,62 +120,79 @@ __global__ __launch_bounds__(64) void k_mx_direct(const MxGemmArgs ga) {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 #define DLC_MX(OP, BL, ACC, B, A, SB, SA) "v_mfma_scale_f32_16x16x128_f8f6f4 %" #ACC ", %" #B ", %" #A ", %" #ACC ", %" #SB ", %" #SA " " OP " cbsz:4 blgp:" BL "\n\t"
-#define DLC_MX_CHUNK4(OP, BL) \
+#define DLC_MX_MOST4(OP, BL) \
     asm volatile("s_nop 1\n\t" \
-    DLC_MX(OP, BL, 4, 22, 20, 32, 30) "ds_read_b128 %0, %40 offset:%41\n\t" DLC_MX(OP, BL, 5, 23, 20, 33, 30) "ds_read_b128 %1, %40 offset:%42\n\t" \
-    DLC_MX(OP, BL, 6, 24, 20, 34, 30) "ds_read_b128 %2, %40 offset:%43\n\t" DLC_MX(OP, BL, 7, 25, 20, 35, 30) "ds_read_b128 %3, %40 offset:%44\n\t" \
-    DLC_MX(OP, BL, 8, 26, 20, 36, 30) DLC_MX(OP, BL, 9, 27, 20, 37, 30) DLC_MX(OP, BL, 10, 28, 20, 38, 30) DLC_MX(OP, BL, 11, 29, 20, 39, 30) \
-    DLC_MX(OP, BL, 12, 22, 21, 32, 31) DLC_MX(OP, BL, 13, 23, 21, 33, 31) DLC_MX(OP, BL, 14, 24, 21, 34, 31) DLC_MX(OP, BL, 15, 25, 21, 35, 31) \
-    DLC_MX(OP, BL, 16, 26, 21, 36, 31) DLC_MX(OP, BL, 17, 27, 21, 37, 31) DLC_MX(OP, BL, 18, 28, 21, 38, 31) DLC_MX(OP, BL, 19, 29, 21, 39, 31) \
+    DLC_MX(OP, BL, 4, 18, 16, 28, 26) "ds_read_b128 %0, %36 offset:%37\n\t" DLC_MX(OP, BL, 5, 19, 16, 29, 26) "ds_read_b128 %1, %36 offset:%38\n\t" \
+    DLC_MX(OP, BL, 6, 20, 16, 30, 26) "ds_read_b128 %2, %36 offset:%39\n\t" DLC_MX(OP, BL, 7, 21, 16, 31, 26) "ds_read_b128 %3, %36 offset:%40\n\t" \
+    DLC_MX(OP, BL, 8, 22, 16, 32, 26) DLC_MX(OP, BL, 9, 23, 16, 33, 26) DLC_MX(OP, BL, 10, 24, 16, 34, 26) DLC_MX(OP, BL, 11, 25, 16, 35, 26) \
+    DLC_MX(OP, BL, 12, 18, 17, 28, 27) DLC_MX(OP, BL, 13, 19, 17, 29, 27) DLC_MX(OP, BL, 14, 20, 17, 30, 27) DLC_MX(OP, BL, 15, 21, 17, 31, 27) \
     "s_waitcnt lgkmcnt(0)" \
     : "=&v"(next[0]), "=&v"(next[1]), "=&v"(next[2]), "=&v"(next[3]), \
       "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc0[4]), "+a"(acc0[5]), "+a"(acc0[6]), "+a"(acc0[7]), \
-      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]), "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]) \
     : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "v"(sa0), "v"(sa1), \
       "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), "v"(sb[4]), "v"(sb[5]), "v"(sb[6]), "v"(sb[7]), "v"(from), "i"(OFF), "i"(OFF + STEP), "i"(OFF + 2 * STEP), "i"(OFF + 3 * STEP) \
     : "memory")
-#define DLC_MX_CHUNK8(OP, BL) \
+#define DLC_MX_MOST8(OP, BL) \
     asm volatile("s_nop 1\n\t" \
-    DLC_MX(OP, BL, 6, 24, 22, 34, 32) "ds_read_b128 %0, %42 offset:%45\n\t" DLC_MX(OP, BL, 7, 25, 22, 35, 32) "ds_read_b128 %1, %43 offset:%45\n\t" \
-    DLC_MX(OP, BL, 8, 26, 22, 36, 32) "ds_read_b128 %2, %42 offset:%46\n\t" DLC_MX(OP, BL, 9, 27, 22, 37, 32) "ds_read_b128 %3, %43 offset:%46\n\t" \
-    DLC_MX(OP, BL, 10, 28, 22, 38, 32) "ds_read_b128 %4, %44 offset:%47\n\t" DLC_MX(OP, BL, 11, 29, 22, 39, 32) "ds_read_b128 %5, %44 offset:%48\n\t" \
-    DLC_MX(OP, BL, 12, 30, 22, 40, 32) DLC_MX(OP, BL, 13, 31, 22, 41, 32) DLC_MX(OP, BL, 14, 24, 23, 34, 33) DLC_MX(OP, BL, 15, 25, 23, 35, 33) \
-    DLC_MX(OP, BL, 16, 26, 23, 36, 33) DLC_MX(OP, BL, 17, 27, 23, 37, 33) DLC_MX(OP, BL, 18, 28, 23, 38, 33) DLC_MX(OP, BL, 19, 29, 23, 39, 33) \
-    DLC_MX(OP, BL, 20, 30, 23, 40, 33) DLC_MX(OP, BL, 21, 31, 23, 41, 33) \
+    DLC_MX(OP, BL, 6, 20, 18, 30, 28) "ds_read_b128 %0, %38 offset:%41\n\t" DLC_MX(OP, BL, 7, 21, 18, 31, 28) "ds_read_b128 %1, %39 offset:%41\n\t" \
+    DLC_MX(OP, BL, 8, 22, 18, 32, 28) "ds_read_b128 %2, %38 offset:%42\n\t" DLC_MX(OP, BL, 9, 23, 18, 33, 28) "ds_read_b128 %3, %39 offset:%42\n\t" \
+    DLC_MX(OP, BL, 10, 24, 18, 34, 28) "ds_read_b128 %4, %40 offset:%43\n\t" DLC_MX(OP, BL, 11, 25, 18, 35, 28) "ds_read_b128 %5, %40 offset:%44\n\t" \
+    DLC_MX(OP, BL, 12, 26, 18, 36, 28) DLC_MX(OP, BL, 13, 27, 18, 37, 28) DLC_MX(OP, BL, 14, 20, 19, 30, 29) DLC_MX(OP, BL, 15, 21, 19, 31, 29) \
+    DLC_MX(OP, BL, 16, 22, 19, 32, 29) DLC_MX(OP, BL, 17, 23, 19, 33, 29) \
     "s_waitcnt lgkmcnt(0)" \
     : "=&v"(na[0]), "=&v"(na[1]), "=&v"(na[2]), "=&v"(na[3]), "=&v"(nb[0]), "=&v"(nb[1]), \
       "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc0[4]), "+a"(acc0[5]), "+a"(acc0[6]), "+a"(acc0[7]), \
-      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]), "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+      "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]) \
     : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "v"(sa0), "v"(sa1), \
       "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), "v"(sb[4]), "v"(sb[5]), "v"(sb[6]), "v"(sb[7]), "v"(from0), "v"(from1), "v"(from_b), "i"(OFF_A), "i"(OFF_A + STEP), "i"(OFF_B), "i"(OFF_B + STEP) \
+    : "memory")
+#define DLC_MX_REST(OP, BL) \
+    asm volatile( \
+    DLC_MX(OP, BL, 0, 5, 4, 10, 9) DLC_MX(OP, BL, 1, 6, 4, 11, 9) DLC_MX(OP, BL, 2, 7, 4, 12, 9) DLC_MX(OP, BL, 3, 8, 4, 13, 9) \
+    : "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
+    : "v"(a1), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "v"(sa1), "v"(sb[4]), "v"(sb[5]), "v"(sb[6]), "v"(sb[7]) \
     : "memory")
 #define DLC_MX_BYTE0 "op_sel_hi:[0,0,0]"
 #define DLC_MX_BYTE1 "op_sel:[1,1,0] op_sel_hi:[0,0,0]"
 #define DLC_MX_BYTE2 "op_sel_hi:[1,1,0]"
 #define DLC_MX_BYTE3 "op_sel:[1,1,0] op_sel_hi:[1,1,0]"
 
-// Rows of blocks acc0 and acc1 += a0 and a1 times b, with byte S of the scales; four fragments, STEP bytes apart, are read
-template <int S, int OFF, int STEP>
+// Rows of blocks acc0 and acc1 += a0 and a1 times b, with byte S of the scales: twelve products and four reads, STEP bytes
+// apart, `then` (one load), the other four products
+template <int S, int OFF, int STEP, typename F>
 __device__ __forceinline__ void mx_chunk4(f32x4* acc0, f32x4* acc1, const u32x4_t& a0, const u32x4_t& a1, const u32x4_t* b, uint32_t sa0,
-                                          uint32_t sa1, const uint32_t* sb, u32x4_t* next, uint32_t from) {
-    if constexpr (S == 0) DLC_MX_CHUNK4(DLC_MX_BYTE0, "4");
-    else if constexpr (S == 1) DLC_MX_CHUNK4(DLC_MX_BYTE1, "4");
-    else if constexpr (S == 2) DLC_MX_CHUNK4(DLC_MX_BYTE2, "4");
-    else DLC_MX_CHUNK4(DLC_MX_BYTE3, "4");
+                                          uint32_t sa1, const uint32_t* sb, u32x4_t* next, uint32_t from, F then) {
+    if constexpr (S == 0) DLC_MX_MOST4(DLC_MX_BYTE0, "4");
+    else if constexpr (S == 1) DLC_MX_MOST4(DLC_MX_BYTE1, "4");
+    else if constexpr (S == 2) DLC_MX_MOST4(DLC_MX_BYTE2, "4");
+    else DLC_MX_MOST4(DLC_MX_BYTE3, "4");
+    then();
+    if constexpr (S == 0) DLC_MX_REST(DLC_MX_BYTE0, "4");
+    else if constexpr (S == 1) DLC_MX_REST(DLC_MX_BYTE1, "4");
+    else if constexpr (S == 2) DLC_MX_REST(DLC_MX_BYTE2, "4");
+    else DLC_MX_REST(DLC_MX_BYTE3, "4");
 }
 
 // ... a0 and a1 of 8 bits an element; two rows' fragments of two chunks each (at from0 and from1) and two of b are read
-template <int S, int OFF_A, int OFF_B, int STEP>
+template <int S, int OFF_A, int OFF_B, int STEP, typename F>
 __device__ __forceinline__ void mx_chunk8(f32x4* acc0, f32x4* acc1, const i32x8& a0, const i32x8& a1, const u32x4_t* b, uint32_t sa0,
-                                          uint32_t sa1, const uint32_t* sb, u32x4_t* na, u32x4_t* nb, uint32_t from0, uint32_t from1, uint32_t from_b) {
-    if constexpr (S == 0) DLC_MX_CHUNK8(DLC_MX_BYTE0, "0");
-    else if constexpr (S == 1) DLC_MX_CHUNK8(DLC_MX_BYTE1, "0");
-    else if constexpr (S == 2) DLC_MX_CHUNK8(DLC_MX_BYTE2, "0");
-    else DLC_MX_CHUNK8(DLC_MX_BYTE3, "0");
+                                          uint32_t sa1, const uint32_t* sb, u32x4_t* na, u32x4_t* nb, uint32_t from0, uint32_t from1,
+                                          uint32_t from_b, F then) {
+    if constexpr (S == 0) DLC_MX_MOST8(DLC_MX_BYTE0, "0");
+    else if constexpr (S == 1) DLC_MX_MOST8(DLC_MX_BYTE1, "0");
+    else if constexpr (S == 2) DLC_MX_MOST8(DLC_MX_BYTE2, "0");
+    else DLC_MX_MOST8(DLC_MX_BYTE3, "0");
+    then();
+    if constexpr (S == 0) DLC_MX_REST(DLC_MX_BYTE0, "0");
+    else if constexpr (S == 1) DLC_MX_REST(DLC_MX_BYTE1, "0");
+    else if constexpr (S == 2) DLC_MX_REST(DLC_MX_BYTE2, "0");
+    else DLC_MX_REST(DLC_MX_BYTE3, "0");
 }
 #undef DLC_MX
-#undef DLC_MX_CHUNK4
-#undef DLC_MX_CHUNK8
+#undef DLC_MX_MOST4
+#undef DLC_MX_MOST8
+#undef DLC_MX_REST
 #undef DLC_MX_BYTE0
 #undef DLC_MX_BYTE1
 #undef DLC_MX_BYTE2
@@ -248,7 +265,8 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
     OpB::template place<NJ>(pb, at + B0, wn, lane);
     keep(pa);
     keep(pb);
-    uint32_t slot_a = 0, slot_b = 0;  // slots of the current tiles, in bytes
+    char* const mine = lds + wave * 1024;  // where the wavefront's first load of a tile in the first slot goes
+    uint32_t slot_a = 0, slot_b = 0;       // slots of the current tiles, in bytes
     const auto after = [](uint32_t s) { return s == 2 * OpA::BYTES ? 0u : s + (uint32_t)OpA::BYTES; };
     const auto before = [](uint32_t s) { return s == 0 ? 2u * OpA::BYTES : s - (uint32_t)OpA::BYTES; };
     sa.load();
@@ -271,19 +289,19 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
         // A step's products with c's fragments while n's are read; behind each of the four blocks two loads
         const auto multiply = [&](auto step, auto& c, auto& n, uint32_t ra, uint32_t rb, const auto& o, char* to) {
             constexpr int S = decltype(step)::value;
-            mx_chunk4<S, 0, STEP>(acc[0], acc[1], c.a[0], c.a[1], c.b, sa.now[0], sa.now[1], sb.now, n.b, rb);
-            o.template load<0, 2>(to, tid);
-            mx_chunk4<S, 4 * STEP, STEP>(acc[2], acc[3], c.a[2], c.a[3], c.b, sa.now[2], sa.now[3], sb.now, n.b + 4, rb);
-            o.template load<2, 2>(to, tid);
-            mx_chunk4<S, 0, STEP>(acc[4], acc[5], c.a[4], c.a[5], c.b, sa.now[4], sa.now[5], sb.now, n.a, ra);
-            o.template load<4, 2>(to, tid);
-            mx_chunk4<S, 4 * STEP, STEP>(acc[6], acc[7], c.a[6], c.a[7], c.b, sa.now[6], sa.now[7], sb.now, n.a + 4, ra);
-            o.template load<6, 2>(to, tid);
+            mx_chunk4<S, 0, STEP>(acc[0], acc[1], c.a[0], c.a[1], c.b, sa.now[0], sa.now[1], sb.now, n.b, rb, [&] { o.template load<0, 1>(to, 0); });
+            o.template load<1, 1>(to, 0);
+            mx_chunk4<S, 4 * STEP, STEP>(acc[2], acc[3], c.a[2], c.a[3], c.b, sa.now[2], sa.now[3], sb.now, n.b + 4, rb, [&] { o.template load<2, 1>(to, 0); });
+            o.template load<3, 1>(to, 0);
+            mx_chunk4<S, 0, STEP>(acc[4], acc[5], c.a[4], c.a[5], c.b, sa.now[4], sa.now[5], sb.now, n.a, ra, [&] { o.template load<4, 1>(to, 0); });
+            o.template load<5, 1>(to, 0);
+            mx_chunk4<S, 4 * STEP, STEP>(acc[6], acc[7], c.a[6], c.a[7], c.b, sa.now[6], sa.now[7], sb.now, n.a + 4, ra, [&] { o.template load<6, 1>(to, 0); });
+            o.template load<7, 1>(to, 0);
         };
         const auto tile = [&](auto first, auto second) {
             // the tile's first half; A's tile after the next goes where the one before was
             oa.mask();
-            multiply(first, f[0], f[1], pa.a[1] + slot_a, pb.a[1] + slot_b, oa, lds + before(slot_a));
+            multiply(first, f[0], f[1], pa.a[1] + slot_a, pb.a[1] + slot_b, oa, mine + before(slot_a));
             oa.advance();
             // the next tiles have come, and all have read this one: B's after the next takes its place
             wait_loads<OpA::PASSES>();
@@ -292,7 +310,7 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
             const uint32_t free_b = slot_b;
             slot_b = OpB::BYTES - slot_b;
             ob.mask();
-            multiply(second, f[1], f[0], pa.a[0] + slot_a, pb.a[0] + slot_b, ob, lds + B0 + free_b);
+            multiply(second, f[1], f[0], pa.a[0] + slot_a, pb.a[0] + slot_b, ob, mine + B0 + free_b);
             ob.advance();
         };
         for (int s = 0; s < tiles; s += 2) {
@@ -325,40 +343,42 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
             constexpr int S = decltype(which)::value, H = S & 1;
             const uint32_t ra = slot_a, nx = after(slot_a), free_b = slot_b;
             const uint32_t rb = H == 0 ? pb.a[1] + slot_b : pb.a[0] + (OpB::BYTES - slot_b);
-            char* const early = lds + before(slot_a);
-            char* const late = lds + slot_a;
+            char* const early = mine + before(slot_a);
+            char* const late = mine + slot_a;
+            char* const late_b = mine + B0 + free_b;
             u32x4_t* const nb = b[1 - H];
             const u32x4_t* const cb = b[H];
             mx_chunk8<S, 2 * STEP, 0, STEP>(acc[0], acc[1], wide(a[0][0], a[0][1]), wide(a[0][2], a[0][3]), cb, sa.now[0], sa.now[1], sb.now, a[1], nb,
-                                            pa.a[0] + ra, pa.a[1] + ra, rb);
-            if constexpr (H == 0) oa.template load<0, 4>(early, tid);
-            else oa.template load<4, 2>(early, tid);
+                                            pa.a[0] + ra, pa.a[1] + ra, rb, [&] { oa.template load<H == 0 ? 0 : 4, H == 0 ? 2 : 1>(early, 0); });
+            oa.template load<H == 0 ? 2 : 5, H == 0 ? 2 : 1>(early, 0);
             mx_chunk8<S, 4 * STEP, 2 * STEP, STEP>(acc[2], acc[3], wide(a[1][0], a[1][1]), wide(a[1][2], a[1][3]), cb, sa.now[2], sa.now[3], sb.now, a[0],
-                                                   nb + 2, pa.a[0] + ra, pa.a[1] + ra, rb);
-            if constexpr (H == 0) oa.template load<4, 4>(early, tid);
-            else oa.template load<6, 2>(early, tid);
+                                                   nb + 2, pa.a[0] + ra, pa.a[1] + ra, rb, [&] { oa.template load<H == 0 ? 4 : 6, H == 0 ? 2 : 1>(early, 0); });
+            oa.template load<H == 0 ? 6 : 7, H == 0 ? 2 : 1>(early, 0);
             oa.advance();
             oa.mask();
             mx_chunk8<S, 6 * STEP, 4 * STEP, STEP>(acc[4], acc[5], wide(a[0][0], a[0][1]), wide(a[0][2], a[0][3]), cb, sa.now[4], sa.now[5], sb.now, a[1],
-                                                   nb + 4, pa.a[0] + ra, pa.a[1] + ra, rb);
+                                                   nb + 4, pa.a[0] + ra, pa.a[1] + ra, rb, [] {});
             wait_loads<OpA::PASSES>();
             bare_barrier();
-            if constexpr (H == 0) {
-                oa.template load<0, 2>(late, tid);
-            } else {
+            if constexpr (H == 1) {
                 if constexpr (S == 1) {
                     sa.load();
                     sb.load();
                 }
                 ob.mask();
-                ob.template load<0, 4>(lds + B0 + free_b, tid);
+                ob.template load<0, 2>(late_b, 0);
+            } else {
+                oa.template load<0, 1>(late, 0);
             }
             mx_chunk8<S, 0, 6 * STEP, STEP>(acc[6], acc[7], wide(a[1][0], a[1][1]), wide(a[1][2], a[1][3]), cb, sa.now[6], sa.now[7], sb.now, a[0],
-                                            nb + 6, pa.a[0] + nx, pa.a[1] + nx, rb);
+                                            nb + 6, pa.a[0] + nx, pa.a[1] + nx, rb, [&] {
+                                                if constexpr (H == 0) oa.template load<1, 2>(late, 0);
+                                                else ob.template load<2, 3>(late_b, 0);
+                                            });
             if constexpr (H == 0) {
-                oa.template load<2, 2>(late, tid);
+                oa.template load<3, 1>(late, 0);
             } else {
-                ob.template load<4, 4>(lds + B0 + free_b, tid);
+                ob.template load<5, 3>(late_b, 0);
                 ob.advance();
                 slot_b = OpB::BYTES - slot_b;
             }
