@@ -1,5 +1,7 @@
 // Matrices to microscaled form and back, and the host side of the product of microscaled operands.
 #include "dlc_mx_gemm.h"
+#include <stdio.h>
+#include <stdlib.h>
 
 using namespace dlc;
 
@@ -131,6 +133,45 @@ bool make_shape(const dlc_mx_linear_config* c, Shape* s) {
     return div_up(s->M, 256) * div_up(s->N, 256) < (int64_t(1) << 24);
 }
 
+struct Plan {
+    int tile, split, kper, tiles_m, tiles_n;
+    int64_t part_ld;
+    size_t bytes;  // of the partial sums
+};
+
+int force_tile = -1, force_split = 1;
+
+Plan plan_linear(const Shape& s) {
+    Plan p{};
+    p.split = 1;
+    if (s.M <= kMxSkinnyRows) {
+        p.tile = kMxSkinny;
+        return p;
+    }
+    const int64_t K = mx_filled(s.K);
+    if (const char* e = getenv("MXT")) sscanf(e, "%d,%d", &force_tile, &force_split);
+    p.tile = force_tile >= 0 ? force_tile : s.M > 128 && s.N > 128 && !(s.elem == DLC_MX_E4M3 && s.es == 4) ? 0 : 2;
+    const int64_t groups = div_up(K, kMxGroup), per = div_up(groups, force_split);
+    p.kper = (int)(per * kMxGroup);
+    p.split = (int)div_up(groups, per);
+    p.tiles_m = (int)div_up(s.M, kMxTileM[p.tile]);
+    p.tiles_n = (int)div_up(s.N, kMxTileN[p.tile]);
+    p.part_ld = round8(s.N);
+    p.bytes = p.split > 1 ? (size_t)p.split * (size_t)s.M * (size_t)p.part_ld * 4 : 0;
+    return p;
+}
+
+template <typename T>
+int product(MxGemmArgs g, const Plan& p, int elem, void* work, hipStream_t st) {
+    g.c.split = p.split; g.c.kper = p.kper; g.c.tiles_m = p.tiles_m; g.c.tiles_n = p.tiles_n;
+    g.c.part = static_cast<float*>(work);
+    g.c.part_ld = p.part_ld;
+    if (MxOps<T>::gemm(g, elem, p.tile, st) != hipSuccess) return DLC_EHIP;
+    if (p.split == 1) return DLC_OK;
+    const JoinArgs j{g.c.part, g.c.part_ld, g.c.M, g.c.split, 0, g.c.e};
+    return DenseOps<T>::join(j, JoinArgs{}, SumArgs{}, st) == hipSuccess ? DLC_OK : DLC_EHIP;
+}
+
 }  // namespace
 
 extern "C" size_t dlc_mx_data_bytes(const dlc_mx_config* c) { return good_mx(c) ? (size_t)c->rows * (size_t)mx_row_bytes(c->cols, c->elem) : 0; }
@@ -146,7 +187,7 @@ extern "C" int dlc_mx_dequantize(const dlc_mx_config* cfg, const void* q, const 
 
 extern "C" size_t dlc_mx_linear_workspace_bytes(const dlc_mx_linear_config* c) {
     Shape s;
-    return make_shape(c, &s) ? 0 : 0;
+    return make_shape(c, &s) && s.M > 0 ? plan_linear(s).bytes : 0;
 }
 
 extern "C" int dlc_mx_linear_forward(const dlc_mx_linear_config* c, const void* xq, const void* xs, const void* wq, const void* ws,
@@ -163,20 +204,16 @@ extern "C" int dlc_mx_linear_forward(const dlc_mx_linear_config* c, const void* 
     g.c.a = xq; g.c.b = wq;
     g.c.lda = mx_row_bytes(s.K, s.elem); g.c.ldb = mx_row_bytes(s.K, DLC_MX_E2M1);
     g.c.M = (int)s.M; g.c.N = (int)s.N; g.c.K = (int)mx_filled(s.K);
-    g.c.split = 1; g.c.kper = g.c.K;
-    if (s.M > 128 && s.N > 128 && !(s.elem == DLC_MX_E4M3 && s.es == 4)) {
-        g.c.tiles_m = (int)div_up(s.M, 256);
-        g.c.tiles_n = (int)div_up(s.N, 256);
-    }
     Epi& e = g.c.e;
     e.y = y; e.res = res; e.bias = bias;
     e.ld_y = s.ldy; e.ld_res = s.ldres; e.act = c->act; e.n = (int)s.N;
+    const Plan p = plan_linear(s);
+    if (p.bytes > 0 && !work) return DLC_EINVAL;
+    if (bytes < p.bytes) return DLC_ECAPACITY;
     hipStream_t st = (hipStream_t)stream;
-    hipError_t rc;
     switch (c->dtype) {
-        case DLC_F32: rc = MxOps<float>::gemm(g, s.elem, st); break;
-        case DLC_F16: rc = MxOps<f16_t>::gemm(g, s.elem, st); break;
-        default: rc = MxOps<bf16_t>::gemm(g, s.elem, st); break;
+        case DLC_F32: return product<float>(g, p, s.elem, work, st);
+        case DLC_F16: return product<f16_t>(g, p, s.elem, work, st);
+        default: return product<bf16_t>(g, p, s.elem, work, st);
     }
-    return rc == hipSuccess ? DLC_OK : DLC_EHIP;
 }

@@ -10,9 +10,12 @@ struct MxGemmArgs {
     const uint8_t* ws;
 };
 
+constexpr int kMxTileM[] = {256, 128, 64}, kMxTileN[] = {256, 128, 128}, kMxSkinny = 3, kMxSkinnyRows = 32;
+
 template <typename T>
 struct MxOps {
-    static hipError_t gemm(const MxGemmArgs& g, int elem_x, hipStream_t s);
+    // tile: of kMxTileM (0: not with E4M3 and results in fp32) or kMxSkinny, for at most kMxSkinnyRows rows
+    static hipError_t gemm(const MxGemmArgs& g, int elem_x, int tile, hipStream_t s);
 };
 
 }  // namespace dlc

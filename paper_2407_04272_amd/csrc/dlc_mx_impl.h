@@ -52,63 +52,217 @@ __device__ __forceinline__ f32x4 mx_mma(const u32x4_t& w, const u32x4_t& x0, con
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc, 4, ELEM == 8 ? 0 : 4, S, (int)sw, S, (int)sx);
 }
 
-// 64 x 64 of C a wavefront, fragments straight from memory
-template <typename T, int ELEM>
-__global__ __launch_bounds__(64) void k_mx_direct(const MxGemmArgs ga) {
-    __shared__ __attribute__((aligned(16))) char lds[64 * 256];
+// Both chunks of N blocks' rows, STEP bytes apart
+template <int N, int STEP = 2048>
+__device__ __forceinline__ void read_frags(u32x4_t* o, uint32_t a, uint32_t b) {
+    if constexpr (N == 1) {
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(o[0]), "=&v"(o[1]) : "v"(a), "v"(b) : "memory");
+    } else {
+        read_halves<N, STEP>(o, a, b);
+    }
+}
+
+// ---- few rows ----
+// At most 32 rows: the product is a pass over w.  A work-group takes 16 columns of C; its wavefronts take groups of 512 k
+// values in turn, each on its own, and their sums meet in LDS.  A wavefront loads 8 rows of 128 bytes at a time, whole cache
+// lines, to its two slots in LDS and reads its fragments from there.  MT: blocks of 16 rows of x
+template <typename T, int ELEM, int MT>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArgs mx) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    using Rows = SkinnyRows<uint8_t>;
     constexpr bool EXACT = kMxExact<T, ELEM>;
-    const GemmArgs& c = ga.c;
-    const int lane = threadIdx.x, g = lane >> 4, j = lane & 15;
-    const int tiles_n = (c.N + 63) / 64, m0 = (int)(blockIdx.x / tiles_n) * 64, n0 = (int)(blockIdx.x % tiles_n) * 64;
-    const char *px[4], *pw[4];
-    const uint8_t *qx[4], *qw[4];
+    constexpr int XT = ELEM / 4, OPS = 1 + XT * MT;  // 128-byte tiles of x for one of w; 256 k values of both
+    constexpr int SLOT = OPS * Rows::BYTES, SLOTS = 2, LOADS = OPS * Rows::LOADS;
+    constexpr int WSTEP = kSkinnyWaves * 256, XSTEP = WSTEP * XT;  // bytes to the wavefront's next group
+    __shared__ __attribute__((aligned(16))) char lds[kSkinnyWaves * SLOTS * SLOT];
+    const GemmArgs& ga = mx.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, j = lane & 15;
+    const int n0 = blockIdx.x * 16, k0 = wave * kMxGroup;
+    char* const mine = lds + wave * (SLOTS * SLOT);
+    Rows w, x[XT * MT];  // (x: [block][tile])
+    w.init(ga.b, ga.ldb, n0, ga.N, k0 / 2, lane);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = min(m0 + i * 16 + j, c.M - 1), n = min(n0 + i * 16 + j, c.N - 1);
-        px[i] = static_cast<const char*>(c.a) + m * c.lda + g * (EXACT ? 32 : 16);
-        pw[i] = static_cast<const char*>(c.b) + n * c.ldb + g * 16;
-        qx[i] = ga.xs + m * 16 + g * 4;
-        qw[i] = ga.ws + n * 16 + g * 4;
-    }
-    f32x4 acc[4][4];
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int t = 0; t < XT; ++t) x[m * XT + t].init(ga.a, ga.lda, m * 16, ga.M, k0 * ELEM / 8 + t * 128, lane);
+    int left = ga.K - k0;  // k values from the next tile to fetch on
+    const auto fetch = [&](char* slot, bool second) {  // a group's first 256 values, its second
+        w.fetch(slot, left / 2, second ? WSTEP - 128 : 128);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int XB = 128 * ELEM / 8;
-    for (int k = 0; k < c.K; k += kMxGroup) {
-        uint32_t sx[4], sw[4];
+        for (int i = 0; i < XT * MT; ++i) x[i].fetch(slot + (1 + i) * Rows::BYTES, left * ELEM / 8 - (i % XT) * 128, second ? XSTEP - 128 * XT : 128 * XT);
+        left -= second ? kSkinnyWaves * kMxGroup - 256 : 256;
+    };
+    // a lane's scales of a group, whose rows past the last are the last's
+    const uint8_t* qw = mx.ws + (int64_t)min(n0 + j, ga.N - 1) * 16 + g * 4 + (int64_t)wave * ga.N * 16;
+    const uint8_t* qx[MT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            sx[i] = *reinterpret_cast<const uint32_t*>(qx[i]);
-            sw[i] = *reinterpret_cast<const uint32_t*>(qw[i]);
-            qx[i] += (int64_t)c.M * 16;
-            qw[i] += (int64_t)c.N * 16;
+    for (int m = 0; m < MT; ++m) qx[m] = mx.xs + (int64_t)min(m * 16 + j, ga.M - 1) * 16 + g * 4 + (int64_t)wave * ga.M * 16;
+    uint32_t sw = 0, sx[MT] = {};
+    const auto scales = [&](int k) {
+        if (k >= ga.K) return;
+        sw = *reinterpret_cast<const uint32_t*>(qw);
+        qw += (int64_t)kSkinnyWaves * ga.N * 16;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            sx[m] = *reinterpret_cast<const uint32_t*>(qx[m]);
+            qx[m] += (int64_t)kSkinnyWaves * ga.M * 16;
         }
-        const auto step = [&](auto s) {
-            constexpr int S = decltype(s)::value;
-            if (k + S * 128 >= c.K) return;
-            u32x4_t x[4][2], w[4];
+    };
+    f32x4 acc[MT];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i][0] = *reinterpret_cast<const u32x4_t*>(px[i]);
-                if constexpr (ELEM == 8) x[i][1] = *reinterpret_cast<const u32x4_t*>(px[i] + (EXACT ? 16 : 64));
-                else x[i][1] = x[i][0];
-                w[i] = *reinterpret_cast<const u32x4_t*>(pw[i]);
-                px[i] += XB;
-                pw[i] += 64;
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    scales(k0);
+    fetch(mine, false);
+    fetch(mine + SLOT, true);
+    const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)mine + (uint32_t)(j * 128);
+    const int key = (j >> 1) & 7;
+    const uint32_t c0 = (uint32_t)((g ^ key) << 4), c1 = c0 ^ 64u;  // the lane's chunk in each half of 128 bytes
+    // ... of x: where products are exact two that stand side by side
+    const uint32_t d0 = EXACT ? (uint32_t)(((2 * g) ^ key) << 4) : c0, d1 = EXACT ? (uint32_t)(((2 * g + 1) ^ key) << 4) : c1;
+    for (int k = k0; k < ga.K; k += kSkinnyWaves * kMxGroup) {
+        const uint32_t tw = sw;
+        uint32_t tx[MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) tx[m] = sx[m];
+        const auto half = [&](auto which) {
+            constexpr int H = decltype(which)::value;
+            wait_loads<(SLOTS - 1) * LOADS>();
+            u32x4_t fw[2], fx[2 * XT * MT];
+            const uint32_t s = at + (uint32_t)(H * SLOT);
+            read_frags<1>(fw, s + c0, s + c1);
+            read_frags<XT * MT>(fx, s + Rows::BYTES + d0, s + Rows::BYTES + d1);
+            fetch(mine + H * SLOT, H == 1);
+            if constexpr (H == 0) scales(k + kSkinnyWaves * kMxGroup);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if constexpr (ELEM == 4) {
+                    acc[m] = mx_mma<4, false, 2 * H>(fw[0], fx[2 * m], fx[2 * m], tw, tx[m], acc[m]);
+                    acc[m] = mx_mma<4, false, 2 * H + 1>(fw[1], fx[2 * m + 1], fx[2 * m + 1], tw, tx[m], acc[m]);
+                } else {
+                    acc[m] = mx_mma<8, EXACT, 2 * H>(fw[0], fx[4 * m], fx[4 * m + 1], tw, tx[m], acc[m]);
+                    acc[m] = mx_mma<8, EXACT, 2 * H + 1>(fw[1], fx[4 * m + 2], fx[4 * m + 3], tw, tx[m], acc[m]);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int n = 0; n < 4; ++n) acc[i][n] = mx_mma<ELEM, EXACT, S>(w[n], x[i][0], x[i][1], sw[n], sx[i], acc[i][n]);
         };
-        step(std::integral_constant<int, 0>{});
-        step(std::integral_constant<int, 1>{});
-        step(std::integral_constant<int, 2>{});
-        step(std::integral_constant<int, 3>{});
+        half(std::integral_constant<int, 0>{});
+        half(std::integral_constant<int, 1>{});
     }
-    write_block<T, false, 64>(c, acc, 0, lds, m0, n0, 0, lane);
+    wait_loads<0>();
+    __syncthreads();
+    typedef float Sums[1][16][20];
+    Sums* const sums = reinterpret_cast<Sums*>(lds);  // [MT][wavefronts]
+    static_assert(sizeof(Sums) * MT * kSkinnyWaves <= sizeof(lds), "room for the sums");
+#pragma unroll
+    for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4*>(&sums[m * kSkinnyWaves + wave][0][j][g * 4]) = acc[m];
+    __syncthreads();
+    if (wave < MT) skinny_end<T, false>(ga, wave * 16, n0, sums + wave * kSkinnyWaves, lane);
+#endif
+}
+
+// ---- tiles of 128 x 128 and 64 x 128 ----
+// Four wavefronts, each with a quarter; tiles of 256 k values in three slots, two on their way while one is multiplied, one
+// barrier a tile.
+template <int ELEM, int BM>
+constexpr int mx_tile_lds() {
+    const int ring = 3 * (BM * 32 * ELEM + 128 * 128), out = BM / 2 * 256 * 4;
+    return ring > out ? ring : out;
+}
+
+template <typename T, int ELEM, int BM>
+__global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr bool EXACT = kMxExact<T, ELEM>;
+    constexpr int BN = 128, WM = BM / 2, WN = 64, MI = WM / 16, NJ = WN / 16, XT = ELEM / 4, STEP = 16 * 128;
+    using OpA = Operand<uint8_t, false, BM, 128, 256, false>;
+    using OpB = Operand<uint8_t, false, BN, 128, 256, false>;
+    constexpr int SLOT = XT * OpA::BYTES + OpB::BYTES, LOADS = XT * OpA::PASSES + OpB::PASSES;
+    __shared__ __attribute__((aligned(16))) char lds[mx_tile_lds<ELEM, BM>()];
+    const GemmArgs& ga = mx.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, j = lane & 15;
+    int tm, tn, sp;
+    tile_of(blockIdx.x, gridDim.x, ga.tiles_m, ga.tiles_n, tm, tn, sp);
+    const int m0 = tm * BM, n0 = tn * BN, k0 = sp * ga.kper, k1 = min(ga.K, k0 + ga.kper);
+    const int wm = (wave >> 1) * WM, wn = (wave & 1) * WN;
+    OpA oa;
+    OpB ob;
+    oa.init(ga.a, ga.lda, m0, ga.M, k0 * ELEM / 8, k1 * ELEM / 8, tid);
+    ob.init(ga.b, ga.ldb, n0, ga.N, k0 / 2, k1 / 2, tid);
+    const auto fetch = [&](int slot) {
+        char* const to = lds + slot * SLOT;
+#pragma unroll
+        for (int t = 0; t < XT; ++t) oa.fetch(to + t * OpA::BYTES, tid);
+        ob.fetch(to + XT * OpA::BYTES, tid);
+    };
+    // a lane's scales of a group, whose rows past the last are the last's
+    uint32_t px[MI], pw[NJ], sx[MI], sw[NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) px[i] = (uint32_t)(min(m0 + wm + i * 16 + j, ga.M - 1) - m0) * 16 + g * 4;
+#pragma unroll
+    for (int n = 0; n < NJ; ++n) pw[n] = (uint32_t)(min(n0 + wn + n * 16 + j, ga.N - 1) - n0) * 16 + g * 4;
+    const uint8_t* bx = mx.xs + ((int64_t)(k0 / kMxGroup) * ga.M + m0) * 16;
+    const uint8_t* bw = mx.ws + ((int64_t)(k0 / kMxGroup) * ga.N + n0) * 16;
+    const auto scales = [&](int k) {
+        if (k >= k1) return;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sx[i] = *reinterpret_cast<const uint32_t*>(bx + px[i]);
+#pragma unroll
+        for (int n = 0; n < NJ; ++n) sw[n] = *reinterpret_cast<const uint32_t*>(bw + pw[n]);
+        bx += (int64_t)ga.M * 16;
+        bw += (int64_t)ga.N * 16;
+    };
+    f32x4 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int n = 0; n < NJ; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    scales(k0);
+    fetch(0);
+    fetch(1);
+    const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds;
+    const int key = (j >> 1) & 7;
+    const uint32_t c0 = (uint32_t)((g ^ key) << 4), c1 = c0 ^ 64u;
+    const uint32_t d0 = EXACT ? (uint32_t)(((2 * g) ^ key) << 4) : c0, d1 = EXACT ? (uint32_t)(((2 * g + 1) ^ key) << 4) : c1;
+    const uint32_t ra = at + (uint32_t)((wm + j) * 128), rb = at + (uint32_t)(XT * OpA::BYTES + (wn + j) * 128);
+    int slot = 0;
+    for (int k = k0; k < k1; k += kMxGroup) {
+        uint32_t tx[MI], tw[NJ];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) tx[i] = sx[i];
+#pragma unroll
+        for (int n = 0; n < NJ; ++n) tw[n] = sw[n];
+        const auto half = [&](auto which) {
+            constexpr int H = decltype(which)::value;
+            // this tile has come; all have read the one before, whose place the tile after the next takes
+            wait_loads<LOADS>();
+            bare_barrier();
+            const uint32_t s = (uint32_t)(slot * SLOT);
+            u32x4_t fw[2 * NJ], fx[XT][2 * MI];
+            read_frags<NJ, STEP>(fw, rb + s + c0, rb + s + c1);
+#pragma unroll
+            for (int t = 0; t < XT; ++t) read_frags<MI, STEP>(fx[t], ra + s + t * OpA::BYTES + d0, ra + s + t * OpA::BYTES + d1);
+            fetch(slot == 0 ? 2 : slot - 1);
+            slot = slot == 2 ? 0 : slot + 1;
+            if constexpr (H == 0) scales(k + kMxGroup);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int n = 0; n < NJ; ++n) {
+                    if constexpr (ELEM == 4) {
+                        acc[i][n] = mx_mma<4, false, 2 * H>(fw[2 * n], fx[0][2 * i], fx[0][2 * i], tw[n], tx[i], acc[i][n]);
+                        acc[i][n] = mx_mma<4, false, 2 * H + 1>(fw[2 * n + 1], fx[0][2 * i + 1], fx[0][2 * i + 1], tw[n], tx[i], acc[i][n]);
+                    } else {
+                        acc[i][n] = mx_mma<8, EXACT, 2 * H>(fw[2 * n], fx[0][2 * i], fx[0][2 * i + 1], tw[n], tx[i], acc[i][n]);
+                        acc[i][n] = mx_mma<8, EXACT, 2 * H + 1>(fw[2 * n + 1], fx[1][2 * i], fx[1][2 * i + 1], tw[n], tx[i], acc[i][n]);
+                    }
+                }
+        };
+        half(std::integral_constant<int, 0>{});
+        if (k + 256 < k1) half(std::integral_constant<int, 1>{});
+    }
+    wait_loads<0>();  // (tiles past the last may still be on their way)
+    __syncthreads();
+    write_block<T, false, WM>(ga, acc, 0, lds + wave * WM * 256, m0 + wm, n0 + wn, sp, lane);
+#endif
 }
 
 // ---- 256 x 256 tiles ----
@@ -402,17 +556,20 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
 #endif
 }
 
+template <typename T, int ELEM>
+static void mx_go(const MxGemmArgs& g, int tile, hipStream_t s) {
+    const dim3 skinny((unsigned)((g.c.N + 15) / 16)), grid((unsigned)(g.c.tiles_m * g.c.tiles_n * g.c.split));
+    if (tile == kMxSkinny && g.c.M <= 16) k_mx_skinny<T, ELEM, 1><<<skinny, dim3(64 * kSkinnyWaves), 0, s>>>(g);
+    else if (tile == kMxSkinny) k_mx_skinny<T, ELEM, 2><<<skinny, dim3(64 * kSkinnyWaves), 0, s>>>(g);
+    else if (tile == 2) k_mx_tile<T, ELEM, 64><<<grid, dim3(256), 0, s>>>(g);
+    else if (tile == 1) k_mx_tile<T, ELEM, 128><<<grid, dim3(256), 0, s>>>(g);
+    else if constexpr (!kMxExact<T, ELEM>) k_mx_wide<T, ELEM><<<grid, dim3(256), 0, s>>>(g);
+}
+
 template <typename T>
-hipError_t MxOps<T>::gemm(const MxGemmArgs& g, int elem_x, hipStream_t s) {
-    if (g.c.tiles_m > 0) {
-        const dim3 grid((unsigned)(g.c.tiles_m * g.c.tiles_n * g.c.split));
-        if (elem_x == DLC_MX_E2M1) k_mx_wide<T, 4><<<grid, dim3(256), 0, s>>>(g);
-        else if constexpr (!kMxExact<T, 8>) k_mx_wide<T, 8><<<grid, dim3(256), 0, s>>>(g);
-        return hipGetLastError();
-    }
-    const dim3 grid((unsigned)(((g.c.M + 63) / 64) * ((g.c.N + 63) / 64))), block(64);
-    if (elem_x == DLC_MX_E4M3) k_mx_direct<T, 8><<<grid, block, 0, s>>>(g);
-    else k_mx_direct<T, 4><<<grid, block, 0, s>>>(g);
+hipError_t MxOps<T>::gemm(const MxGemmArgs& g, int elem_x, int tile, hipStream_t s) {
+    if (elem_x == DLC_MX_E4M3) mx_go<T, 8>(g, tile, s);
+    else mx_go<T, 4>(g, tile, s);
     return hipGetLastError();
 }
 
