@@ -474,6 +474,7 @@ int dlc_mx_dequantize(const dlc_mx_config* cfg /*HOST*/, const void* d_q, const 
  *   dimensions (else DLC_EINVAL)
  * Products are exact, sums and the epilogue fp32, the result is rounded once.
  *   sizes        rows 0 .. 2^30, features 1 .. 2^20, leading dimensions up to 2^20; results of fewer than 2^24 tiles of 256 x 256
+ *                (E4M3 with results in fp32: 128 x 128)
  *   d_work       as above, dlc_mx_linear_workspace_bytes
  */
 typedef struct {

@@ -1,7 +1,5 @@
 // Matrices to microscaled form and back, and the host side of the product of microscaled operands.
 #include "dlc_mx_gemm.h"
-#include <stdio.h>
-#include <stdlib.h>
 
 using namespace dlc;
 
@@ -64,6 +62,7 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(const MxArgs a) {
 
 // ---- host ---------------------------------------------------------------------------------------
 constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 20;
+constexpr int64_t kMaxGroups = int64_t(1) << 24;  // a launch's threads, work-groups of 256, are counted in 32 bits
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
@@ -130,7 +129,9 @@ bool make_shape(const dlc_mx_linear_config* c, Shape* s) {
     if (s->ldy < s->N || s->ldy > kMaxDim || s->ldres < s->N || s->ldres > kMaxDim) return false;
     s->elem = c->elem_x;
     s->es = c->dtype == DLC_F32 ? 4 : 2;
-    return div_up(s->M, 256) * div_up(s->N, 256) < (int64_t(1) << 24);
+    // (some tile's launch covers the result: the largest, which fp32 results of E4M3 have not)
+    const int64_t side = s->elem == DLC_MX_E4M3 && s->es == 4 ? 128 : 256;
+    return div_up(s->M, side) * div_up(s->N, side) < kMaxGroups;
 }
 
 struct Plan {
@@ -139,26 +140,55 @@ struct Plan {
     size_t bytes;  // of the partial sums
 };
 
-int force_tile = -1, force_split = 1;
+// What 256 k values cost with 1 and 2 work-groups on a compute unit, in us, what a work-group costs besides, and every
+// further one, measured on full and on half empty cards (0: no second work-group fits): E2M1, E4M3, E4M3 with results in fp32.
+// 64 x 128 is the best until its tiles no longer fit the card at once (256 x 2048 x 2048 of 4 bits 8.4 us for 11.4 and 21.5 of
+// the other two; 2048 x 2048 x 2048 of 8 bits 18.4, 15.7 and 29.2), 256 x 256 where there are many (2048 x 8192 x 8192 of 4
+// bits 125, 137 and 70 us).
+struct TileCost { double tile[2], first, further; };
+constexpr TileCost kCost[3][3] = {{{{1.75, 0}, 12.0, 6.0}, {{0.88, 0}, 5.0, 3.5}, {{0.62, 0.93}, 4.0, 2.8}},
+                                  {{{2.5, 0}, 13.0, 6.0}, {{1.22, 0}, 5.5, 3.5}, {{0.8, 0}, 4.2, 2.4}},
+                                  {{}, {{2.2, 0}, 5.5, 3.5}, {{1.45, 0}, 4.2, 2.4}}};
+constexpr int kUnits = 256;  // compute units
+constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
+// The tile and the cut of k with the smallest estimate
 Plan plan_linear(const Shape& s) {
-    Plan p{};
-    p.split = 1;
+    Plan best{};
+    best.split = 1;
     if (s.M <= kMxSkinnyRows) {
-        p.tile = kMxSkinny;
-        return p;
+        best.tile = kMxSkinny;
+        return best;
     }
-    const int64_t K = mx_filled(s.K);
-    if (const char* e = getenv("MXT")) sscanf(e, "%d,%d", &force_tile, &force_split);
-    p.tile = force_tile >= 0 ? force_tile : s.M > 128 && s.N > 128 && !(s.elem == DLC_MX_E4M3 && s.es == 4) ? 0 : 2;
-    const int64_t groups = div_up(K, kMxGroup), per = div_up(groups, force_split);
-    p.kper = (int)(per * kMxGroup);
-    p.split = (int)div_up(groups, per);
-    p.tiles_m = (int)div_up(s.M, kMxTileM[p.tile]);
-    p.tiles_n = (int)div_up(s.N, kMxTileN[p.tile]);
-    p.part_ld = round8(s.N);
-    p.bytes = p.split > 1 ? (size_t)p.split * (size_t)s.M * (size_t)p.part_ld * 4 : 0;
-    return p;
+    const int64_t groups = mx_groups(s.K);
+    const bool exact = s.elem == DLC_MX_E4M3 && s.es == 4;
+    const TileCost* const cost = kCost[exact ? 2 : s.elem == DLC_MX_E4M3 ? 1 : 0];
+    double least = 1e300;
+    for (int tile = exact ? 1 : 0; tile < 3; ++tile) {
+        const TileCost& c = cost[tile];
+        const int64_t tm = div_up(s.M, kMxTileM[tile]), tn = div_up(s.N, kMxTileN[tile]), tiles = tm * tn;
+        if (tiles >= kMaxGroups) continue;
+        const int fit = c.tile[1] > 0 ? 2 : 1;
+        for (const int cut : kCuts) {
+            if (cut > 1 && (cut > groups || tiles * cut > 2 * kUnits)) break;
+            const int64_t per = div_up(groups, cut), split = div_up(groups, per), wgs = tiles * split;
+            const int64_t full = wgs / (kUnits * fit), rest = wgs % (kUnits * fit);
+            double t = (double)full * (2.0 * (double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
+            if (rest) t += 2.0 * (double)per * c.tile[(rest - 1) / kUnits] + c.further;
+            if (split > 1) t += 3.0 + (double)split * (double)s.M * (double)s.N * 8.0 / 8.0e6;
+            if (t < least) {
+                least = t;
+                best.tile = tile;
+                best.split = (int)split;
+                best.kper = (int)(per * kMxGroup);
+                best.tiles_m = (int)tm;
+                best.tiles_n = (int)tn;
+            }
+        }
+    }
+    best.part_ld = round8(s.N);
+    best.bytes = best.split > 1 ? (size_t)best.split * (size_t)s.M * (size_t)best.part_ld * 4 : 0;
+    return best;
 }
 
 template <typename T>
