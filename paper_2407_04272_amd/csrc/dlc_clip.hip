@@ -9,9 +9,11 @@ using namespace dlc;
 
 namespace {
 
-constexpr int kTensors = 64;
-constexpr int64_t kChunk = 32768;       // elements of a chunk, at least
-constexpr int64_t kMaxChunks = 16384;   // ... so many that there are no more than these (and one a tensor)
+// Descriptions that go with a launch: kTensors, or kFew where there are no more (a launch's arguments are copied twice on
+// their way: 7 tensors and their 2.5 million values 14.6 us a pass with room for 64)
+constexpr int kTensors = 64, kFew = 8;
+constexpr int64_t kChunk = 4096;       // elements of a chunk, at least: two a thread, 16 bytes each
+constexpr int64_t kMaxChunks = 8192;   // ... so many that there are no more than these (and one a tensor)
 constexpr int kThreads = 256;
 
 struct Piece {
@@ -19,11 +21,12 @@ struct Piece {
     void* out;
     int64_t n, cols, ld_in, ld_out;   // n elements in all; dense: cols = n
     int32_t dtype;
-    uint32_t first;                   // its first chunk in this launch
 };
 
+template <int N>
 struct ClipArgs {
-    Piece t[kTensors];
+    Piece t[N];
+    uint32_t first[N];                // a tensor's first chunk in this launch; ~0 where there is none
     int64_t chunk;
     int32_t count;
     uint32_t chunks;
@@ -32,33 +35,46 @@ struct ClipArgs {
     double max_norm;
     float* norm;
 };
-static_assert(sizeof(ClipArgs) <= 4096, "what a launch takes along");
+static_assert(sizeof(ClipArgs<kTensors>) <= 4096, "what a launch takes along");
 
-// which tensor a chunk is of
-__device__ __forceinline__ int piece_of(const ClipArgs& a, uint32_t chunk) {
-    int lo = 0, hi = a.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.t[mid].first <= chunk) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
+// which tensor a chunk is of (all are looked at: their places come in a few wide loads, where a search would wait for one
+// after the other)
+template <int N>
+__device__ __forceinline__ int piece_of(const ClipArgs<N>& a, uint32_t chunk) {
+    int n = -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += a.first[i] <= chunk;
+    return n;
 }
 
-// f(in, out, elements) for the eights of a chunk (fewer at a row's end); V of them at a time are a thread's
+// f(values, out, elements) for the eights of a chunk (fewer at a row's end), four a thread on their way together
 template <typename T, typename F>
 __device__ __forceinline__ void each8(const Piece& p, int64_t at, int64_t end, F f) {
     const T* const in = static_cast<const T*>(p.in);
     T* const out = static_cast<T*>(p.out);
+    float v[4][8];
     if (p.cols == p.n) {
-        for (int64_t i = at + threadIdx.x * 8; i < end; i += kThreads * 8) f(in + i, out + i, (int)min((int64_t)8, end - i));
+        for (int64_t i = at + threadIdx.x * 8; i < end; i += kThreads * 32) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t left = end - i - u * (kThreads * 8);
+                load8(in + i + u * (kThreads * 8), left < 8 ? (int)left : 8, v[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t left = end - i - u * (kThreads * 8);
+                if (left > 0) f(v[u], out + i + u * (kThreads * 8), left < 8 ? (int)left : 8);
+            }
+        }
         return;
     }
     // rows apart: eights of a row, counted through all rows (chunks are whole numbers of them)
     const int64_t per = (p.cols + 7) / 8;
     for (int64_t i = at / 8 + threadIdx.x; i < end / 8; i += kThreads) {
         const int64_t row = i / per, col = (i - row * per) * 8;
-        f(in + row * p.ld_in + col, out + row * p.ld_out + col, (int)min((int64_t)8, p.cols - col));
+        const int cnt = (int)min((int64_t)8, p.cols - col);
+        load8(in + row * p.ld_in + col, cnt, v[0]);
+        f(v[0], out + row * p.ld_out + col, cnt);
     }
 }
 
@@ -77,15 +93,15 @@ __device__ __forceinline__ double block_sum(double v) {
     return s;
 }
 
-__global__ __launch_bounds__(kThreads) void k_squares(const ClipArgs a) {
-    const Piece& p = a.t[piece_of(a, blockIdx.x)];
-    const int64_t at = (int64_t)(blockIdx.x - p.first) * a.chunk, end = min(counted(p), at + a.chunk);
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_squares(const ClipArgs<N> a) {
+    const int piece = piece_of(a, blockIdx.x);
+    const Piece& p = a.t[piece];
+    const int64_t at = (int64_t)(blockIdx.x - a.first[piece]) * a.chunk, end = min(counted(p), at + a.chunk);
     double s = 0.0;
     const auto run = [&](auto one) {
         using T = decltype(one);
-        each8<T>(p, at, end, [&](const T* in, T*, int n) {
-            float f[8];
-            load8(in, n, f);
+        each8<T>(p, at, end, [&](const float* f, T*, int) {  // (0 past the last)
 #pragma unroll
             for (int i = 0; i < 8; ++i) s += (double)f[i] * (double)f[i];
         });
@@ -97,27 +113,35 @@ __global__ __launch_bounds__(kThreads) void k_squares(const ClipArgs a) {
     if (threadIdx.x == 0) a.part[blockIdx.x] = s;
 }
 
-// The chunks' sums, always in the same order
+// The chunks' sums, always in the same order, all loads of a round on their way together
 __global__ __launch_bounds__(kThreads) void k_add(const double* part, int64_t n, double* sum) {
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) s += part[i];
+    for (int64_t i = threadIdx.x; i < n; i += kThreads * 16) {
+        double v[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) v[u] = i + u * kThreads < n ? part[i + u * kThreads] : 0.0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) s += v[u];
+    }
     s = block_sum(s);
     if (threadIdx.x == 0) *sum = s;
 }
 
-__global__ __launch_bounds__(kThreads) void k_clip(const ClipArgs a) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_clip(const ClipArgs<N> a) {
     const double n = sqrt(*a.sum);
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)n;
     if (a.count == 0) return;
     const float f = n > a.max_norm && n < __builtin_inf() ? (float)(a.max_norm / n) : 1.0f;
-    const Piece& p = a.t[piece_of(a, blockIdx.x)];
+    // from the last chunk on: what the norm read last may still be in the last cache
+    const uint32_t chunk = a.chunks - 1 - blockIdx.x;
+    const int piece = piece_of(a, chunk);
+    const Piece& p = a.t[piece];
     if (f == 1.0f && p.in == p.out) return;
-    const int64_t at = (int64_t)(blockIdx.x - p.first) * a.chunk, end = min(counted(p), at + a.chunk);
+    const int64_t at = (int64_t)(chunk - a.first[piece]) * a.chunk, end = min(counted(p), at + a.chunk);
     const auto run = [&](auto one) {
         using T = decltype(one);
-        each8<T>(p, at, end, [&](const T* in, T* out, int cnt) {
-            float v[8];
-            load8(in, cnt, v);
+        each8<T>(p, at, end, [&](float* v, T* out, int cnt) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= f;
             store8(out, cnt, v);
@@ -174,22 +198,26 @@ int look(const dlc_tensor* list, const dlc_tensor* out, int64_t count, List* l) 
     return DLC_OK;
 }
 
-// launch(args): once for up to kTensors tensors
-template <typename F>
-int each_launch(ClipArgs a, const dlc_tensor* list, const dlc_tensor* out, int64_t count, F launch) {
+// launch(args): once for up to N tensors
+template <int N, typename F>
+int each_launch(ClipArgs<N> a, const dlc_tensor* list, const dlc_tensor* out, int64_t count, F launch) {
     int64_t chunks = 0;
-    a.count = 0;
+    const auto none = [&] {
+        a.count = 0;
+        chunks = 0;
+        for (uint32_t& f : a.first) f = ~0u;
+    };
+    none();
     for (int64_t i = 0; i < count; ++i) {
         if (list[i].rows == 0 || list[i].cols == 0) continue;
-        Piece p = piece(list[i], out[i]);
-        p.first = (uint32_t)chunks;
+        const Piece p = piece(list[i], out[i]);
+        a.first[a.count] = (uint32_t)chunks;
         a.t[a.count++] = p;
         chunks += div_up(counted(p), a.chunk);
         a.chunks = (uint32_t)chunks;
-        if (a.count == kTensors) {
+        if (a.count == N) {
             if (launch(a) != hipSuccess) return DLC_EHIP;
-            a.count = 0;
-            chunks = 0;
+            none();
         }
     }
     return a.count == 0 || launch(a) == hipSuccess ? DLC_OK : DLC_EHIP;
@@ -217,14 +245,16 @@ extern "C" int dlc_gradient_norm(const dlc_tensor* list, int64_t count, double* 
     if (chunks > 0 && !work) return DLC_EINVAL;
     if (bytes < (size_t)chunks * 8) return DLC_ECAPACITY;
     hipStream_t st = (hipStream_t)stream;
-    ClipArgs a{};
-    a.chunk = l.chunk;
-    a.part = static_cast<double*>(work);
-    const int rc = each_launch(a, list, list, count, [&](ClipArgs& b) {
-        k_squares<<<dim3(b.chunks), dim3(kThreads), 0, st>>>(b);
-        b.part += b.chunks;
-        return hipGetLastError();
-    });
+    const auto squares = [&](auto a) {
+        a.chunk = l.chunk;
+        a.part = static_cast<double*>(work);
+        return each_launch(a, list, list, count, [&](auto& b) {
+            k_squares<<<dim3(b.chunks), dim3(kThreads), 0, st>>>(b);
+            b.part += b.chunks;
+            return hipGetLastError();
+        });
+    };
+    const int rc = count <= kFew ? squares(ClipArgs<kFew>{}) : squares(ClipArgs<kTensors>{});
     if (rc != DLC_OK) return rc;
     k_add<<<dim3(1), dim3(kThreads), 0, st>>>(static_cast<const double*>(work), chunks, d_sum);
     return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
@@ -236,19 +266,20 @@ extern "C" int dlc_gradient_clip(const dlc_tensor* list, int64_t count, const do
     if (const int rc = look(list, out, count, &l); rc != DLC_OK) return rc;
     if (!d_sum || ((uintptr_t)d_sum & 7) != 0 || ((uintptr_t)d_norm & 3) != 0 || !(max_norm >= 0.0)) return DLC_EINVAL;
     hipStream_t st = (hipStream_t)stream;
-    ClipArgs a{};
-    a.chunk = l.chunk;
-    a.sum = d_sum;
-    a.max_norm = max_norm;
-    a.norm = d_norm;
-    bool any = false;
-    const int rc = each_launch(a, list, out, count, [&](ClipArgs& b) {
-        k_clip<<<dim3(b.chunks), dim3(kThreads), 0, st>>>(b);
-        any = true;
-        return hipGetLastError();
-    });
-    if (rc != DLC_OK || any || !d_norm) return rc;
-    a.count = 0;
-    k_clip<<<dim3(1), dim3(kThreads), 0, st>>>(a);
-    return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
+    const auto clip = [&](auto a) {
+        a.chunk = l.chunk;
+        a.sum = d_sum;
+        a.max_norm = max_norm;
+        a.norm = d_norm;
+        bool any = false;
+        const int rc = each_launch(a, list, out, count, [&](auto& b) {
+            k_clip<<<dim3(b.chunks), dim3(kThreads), 0, st>>>(b);
+            any = true;
+            return hipGetLastError();
+        });
+        if (rc != DLC_OK || any || !d_norm) return rc;
+        k_clip<<<dim3(1), dim3(kThreads), 0, st>>>(a);  // (no tensors: the norm alone)
+        return hipGetLastError() == hipSuccess ? (int)DLC_OK : (int)DLC_EHIP;
+    };
+    return count <= kFew ? clip(ClipArgs<kFew>{}) : clip(ClipArgs<kTensors>{});
 }
