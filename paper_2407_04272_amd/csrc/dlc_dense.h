@@ -286,9 +286,16 @@ __device__ __forceinline__ void load8(const T* p, int cnt, float f[8]) {
 #pragma unroll
             for (int j = 0; j < V; ++j) f[i * V + j] = (float)q[j];
         }
+    } else if (cnt > 0) {
+        // (all on their way together: with a branch and a wait for each, 777 x 515 -> 1023 with a residual took 2.8 us longer)
+        T q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = p[i < cnt ? i : cnt - 1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = i < cnt ? (float)q[i] : 0.0f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < cnt ? (float)p[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) f[i] = 0.0f;
     }
 }
 
