@@ -52,18 +52,20 @@ template <typename T, typename F>
 __device__ __forceinline__ void each8(const Piece& p, int64_t at, int64_t end, F f) {
     const T* const in = static_cast<const T*>(p.in);
     T* const out = static_cast<T*>(p.out);
-    float v[4][8];
+    Raw8<T> x[4];
+    float v[8];
     if (p.cols == p.n) {
         for (int64_t i = at + threadIdx.x * 8; i < end; i += kThreads * 32) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t left = end - i - u * (kThreads * 8);
-                load8(in + i + u * (kThreads * 8), left < 8 ? (int)left : 8, v[u]);
+                x[u].load(in + i + u * (kThreads * 8), left < 8 ? (int)left : 8);
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t left = end - i - u * (kThreads * 8);
-                if (left > 0) f(v[u], out + i + u * (kThreads * 8), left < 8 ? (int)left : 8);
+                x[u].get(v);
+                if (left > 0) f(v, out + i + u * (kThreads * 8), left < 8 ? (int)left : 8);
             }
         }
         return;
@@ -73,8 +75,8 @@ __device__ __forceinline__ void each8(const Piece& p, int64_t at, int64_t end, F
     for (int64_t i = at / 8 + threadIdx.x; i < end / 8; i += kThreads) {
         const int64_t row = i / per, col = (i - row * per) * 8;
         const int cnt = (int)min((int64_t)8, p.cols - col);
-        load8(in + row * p.ld_in + col, cnt, v[0]);
-        f(v[0], out + row * p.ld_out + col, cnt);
+        load8(in + row * p.ld_in + col, cnt, v);
+        f(v, out + row * p.ld_out + col, cnt);
     }
 }
 

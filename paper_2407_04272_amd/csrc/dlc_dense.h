@@ -286,18 +286,49 @@ __device__ __forceinline__ void load8(const T* p, int cnt, float f[8]) {
 #pragma unroll
             for (int j = 0; j < V; ++j) f[i * V + j] = (float)q[j];
         }
-    } else if (cnt > 0) {
-        // (all on their way together: with a branch and a wait for each, 777 x 515 -> 1023 with a residual took 2.8 us longer)
-        T q[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = p[i < cnt ? i : cnt - 1];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = i < cnt ? (float)q[i] : 0.0f;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 0.0f;
+        for (int i = 0; i < 8; ++i) f[i] = i < cnt ? (float)p[i] : 0.0f;
     }
 }
+
+// The same in two steps: several are asked for before the first is waited for.  (load8's conversions may stand inside its
+// branches, with a wait each; and behind a row's last whole chunk it waits for element after element: 777 x 515 -> 1023 with
+// a residual 11.4 us that way, 9.6 this way.)
+template <typename T>
+struct Raw8 {
+    static constexpr int V = 16 / sizeof(T);
+    typename Vec8<T>::type q[8 / V];
+    __device__ __forceinline__ void load(const T* p, int cnt) {
+        if (cnt >= 8) {
+#pragma unroll
+            for (int i = 0; i < 8 / V; ++i) q[i] = *reinterpret_cast<const typename Vec8<T>::type*>(p + i * V);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i / V][i % V] = (T)0.0f;
+            if (cnt > 0) {
+                T t[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = p[i < cnt ? i : cnt - 1];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[i / V][i % V] = i < cnt ? t[i] : (T)0.0f;
+            }
+        }
+    }
+    // ... where rows end with a whole eight: all of it, or nothing
+    __device__ __forceinline__ void load_whole(const T* p, bool there) {
+#pragma unroll
+        for (int i = 0; i < 8 / V; ++i) q[i] = typename Vec8<T>::type{};
+        if (there) {
+#pragma unroll
+            for (int i = 0; i < 8 / V; ++i) q[i] = *reinterpret_cast<const typename Vec8<T>::type*>(p + i * V);
+        }
+    }
+    __device__ __forceinline__ void get(float f[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)q[i / V][i % V];
+    }
+};
 
 template <typename T>
 __device__ __forceinline__ void store8(T* p, int cnt, const float f[8]) {
@@ -330,8 +361,11 @@ __device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t
     if (e.bias) {
         const T* bias = static_cast<const T*>(e.bias);
         float b[8], c[8];
-        load8(bias + col, cnt, b);
-        if constexpr (GATED) load8(bias + e.n + col, cnt, c);
+        Raw8<T> rb, rc;
+        rb.load(bias + col, cnt);
+        if constexpr (GATED) rc.load(bias + e.n + col, cnt);
+        rb.get(b);
+        if constexpr (GATED) rc.get(c);
 #pragma unroll
         for (int r = 0; r < U; ++r)
 #pragma unroll
@@ -365,14 +399,16 @@ __device__ __forceinline__ void epilogue8(const Epi& e, uint64_t offset, int64_t
         }
     }
     if (e.res) {
-        float x[U][8];
+        Raw8<T> x[U];
 #pragma unroll
-        for (int r = 0; r < U; ++r)
-            if (r * STEP < rows) load8(static_cast<const T*>(e.res) + (m + r * STEP) * e.ld_res + col, cnt, x[r]);
+        for (int r = 0; r < U; ++r) x[r].load(static_cast<const T*>(e.res) + (m + r * STEP) * e.ld_res + col, r * STEP < rows ? cnt : 0);
 #pragma unroll
-        for (int r = 0; r < U; ++r)
+        for (int r = 0; r < U; ++r) {
+            float v[8];
+            x[r].get(v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[r][i] += x[r][i];
+            for (int i = 0; i < 8; ++i) s[r][i] += v[i];
+        }
     }
 #pragma unroll
     for (int r = 0; r < U; ++r)

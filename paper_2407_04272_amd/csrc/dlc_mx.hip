@@ -23,13 +23,15 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {
     for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
         const int64_t band = tile / a.groups, row0 = band * kTileRows + wave * R;
         const int col = (int)(tile - band * a.groups) * kMxGroup + lane * 8;
-        float f[R][8];
+        Raw8<T> x[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            load8(static_cast<const T*>(a.x) + (row0 + i) * a.ld + col, row0 + i < a.rows ? a.cols - col : 0, f[i]);
+        for (int i = 0; i < R; ++i) x[i].load(static_cast<const T*>(a.x) + (row0 + i) * a.ld + col, row0 + i < a.rows ? a.cols - col : 0);
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (row0 + i < a.rows) mx_store8<ELEM>(f[i], row0 + i, col, a.cols, a.rows, a.q, a.scale);
+        for (int i = 0; i < R; ++i) {
+            float f[8];
+            x[i].get(f);
+            if (row0 + i < a.rows) mx_store8<ELEM>(f, row0 + i, col, a.cols, a.rows, a.q, a.scale);
+        }
     }
 }
 

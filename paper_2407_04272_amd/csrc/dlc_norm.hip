@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition, forward (results in the type, in microscaled form, or both) and backward.
 //
 // Bound by memory: every row is read once into registers, its sums are made there, and the results go out.  A team of P lanes
-// has a row, U times eight columns a lane; rows longer than 32768 columns are read twice instead.
+// has a row, U times eight columns a lane; rows longer than 16384 columns (backward 8192) are read twice instead.
 #include "dlc_mx.h"
 
 using namespace dlc;
@@ -50,6 +50,22 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float (*red)[N]) {
 template <int P>
 constexpr int kTeams = P < 256 ? 256 / P : 1;
 
+// Eight columns of a row.  WHOLE: rows end with a whole eight, and there is no code for others: it costs registers, and with
+// them the wavefronts that hide the loads (16384 x 8192 bf16, 157 registers and 233 us for 68 and 178)
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void ask(Raw8<T>& q, const void* p, int64_t row, int64_t ld, int col, int cols) {
+    const T* const at = static_cast<const T*>(p) + row * ld + col;
+    if constexpr (WHOLE) q.load_whole(at, col < cols);
+    else q.load(at, cols - col);
+}
+
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void put(void* p, int64_t row, int64_t ld, int col, int cols, const float f[8]) {
+    T* const at = static_cast<T*>(p) + row * ld + col;
+    if constexpr (!WHOLE) store8(at, cols - col, f);
+    else if (col < cols) store8(at, 8, f);
+}
+
 template <typename T>
 __device__ __forceinline__ void load_weight(const void* weight, int col, int cnt, float w[8]) {
     if (weight) {
@@ -72,19 +88,17 @@ __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, int col
     }
 }
 
-template <typename T, bool MX>
-__device__ __forceinline__ void put_row(const NormArgs& a, int64_t row, int col, float r, float s[8]) {
+template <typename T, bool MX, bool WHOLE>
+__device__ __forceinline__ void put_row(const NormArgs& a, int64_t row, int col, float r, float s[8], const float w[8]) {
     const int cnt = a.cols - col;
-    if (a.sum) store8(static_cast<T*>(a.sum) + row * a.ld_sum + col, cnt, s);
-    float w[8];
-    load_weight<T>(a.weight, col, cnt, w);
+    if (a.sum) put<WHOLE, T>(a.sum, row, a.ld_sum, col, a.cols, s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = i < cnt ? s[i] * r * w[i] : 0.0f;
-    if (a.y) store8(static_cast<T*>(a.y) + row * a.ld_y + col, cnt, s);
+    if (a.y) put<WHOLE, T>(a.y, row, a.ld_y, col, a.cols, s);
     if constexpr (MX) mx_store8<8>(s, row, col, a.cols, a.rows, a.q, a.scale);
 }
 
-template <typename T, int P, int U, bool MX>
+template <typename T, int P, int U, bool MX, bool WHOLE>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
     __shared__ float red[2][P > 64 ? P / 64 : 1][1];
     const int t = threadIdx.x % P, team = threadIdx.x / P;
@@ -93,10 +107,35 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
     int odd = 0;
     for (int64_t row = first; row < last; ++row, odd ^= 1) {
         float s[U][8], sq[1] = {0.0f};
+        Raw8<T> x[U], res[U], w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (u * P + t) * 8;
-            load_sum<T>(a, row, col, a.cols - col, s[u]);
+            ask<WHOLE>(x[u], a.x, row, a.ld_x, col, a.cols);
+        }
+        if (a.res) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int col = (u * P + t) * 8;
+                ask<WHOLE>(res[u], a.res, row, a.ld_res, col, a.cols);
+            }
+        }
+        if (a.weight) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int col = (u * P + t) * 8;
+                ask<WHOLE>(w[u], a.weight, 0, 0, col, a.cols);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u].get(s[u]);
+            if (a.res) {
+                float r[8];
+                res[u].get(r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[u][i] += r[i];
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sq[0] += s[u][i] * s[u][i];
         }
@@ -105,7 +144,12 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (u * P + t) * 8;
-            if (col < end) put_row<T, MX>(a, row, col, r, s[u]);
+            float g[8];
+            w[u].get(g);
+            if (!a.weight)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] = 1.0f;
+            if (col < end) put_row<T, MX, WHOLE>(a, row, col, r, s[u], g);
         }
     }
 }
@@ -126,57 +170,78 @@ __global__ __launch_bounds__(1024) void k_norm_long(const NormArgs a) {
         team_sum<1024>(sq, red[odd]);
         const float r = __builtin_amdgcn_rsqf(sq[0] * a.inv_cols + a.eps);
         for (int col = threadIdx.x * 8; col < end; col += 8192) {
+            float w[8];
             load_sum<T>(a, row, col, a.cols - col, s);
-            put_row<T, MX>(a, row, col, r, s);
+            load_weight<T>(a.weight, col, a.cols - col, w);
+            put_row<T, MX, false>(a, row, col, r, s, w);
         }
     }
 }
 
 // dx of eight columns (into g), and dy s r (into s)
-template <typename T>
-__device__ __forceinline__ void back8(const NormArgs& a, int64_t row, int col, float r, float c, float s[8], float dy[8], const float w[8]) {
-    const int cnt = a.cols - col;
-    float ds[8] = {};
-    if (a.y && a.res) load8(static_cast<const T*>(a.res) + row * a.ld_res + col, cnt, ds);
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void back8(const NormArgs& a, int64_t row, int col, float r, float c, float s[8], float dy[8], const float w[8], const float ds[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float n = dy[i] * (s[i] * r);
         dy[i] = r * (dy[i] * w[i] - s[i] * c) + ds[i];
         s[i] = n;
     }
-    if (a.y) store8(static_cast<T*>(a.y) + row * a.ld_y + col, cnt, dy);
+    if (a.y) put<WHOLE, T>(a.y, row, a.ld_y, col, a.cols, dy);
 }
 
-template <typename T, int P, int U>
+template <typename T, int P, int U, bool WHOLE>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs a) {
     constexpr int TEAMS = kTeams<P>;
     __shared__ float red[2][P > 64 ? P / 64 : 1][2];
     __shared__ float sums[TEAMS > 1 ? TEAMS : 1][TEAMS > 1 ? P * U * 8 : 1];
     const int t = threadIdx.x % P, team = threadIdx.x / P;
-    float dw[U][8] = {}, w[U][8];
+    const bool along = a.y && a.res;
+    float dw[U][8] = {};
+    Raw8<T> rw[U];
+    if (a.weight) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_weight<T>(a.weight, (u * P + t) * 8, a.cols - (u * P + t) * 8, w[u]);
-    int odd = 0;
-    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS, odd ^= 1) {
-        float s[U][8], dy[U][8], v[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int col = (u * P + t) * 8, cnt = a.cols - col;
-            load8(static_cast<const T*>(a.x) + row * a.ld_x + col, cnt, s[u]);
-            load8(static_cast<const T*>(a.dy) + row * a.ld_dy + col, cnt, dy[u]);
-        }
+        for (int u = 0; u < U; ++u) ask<WHOLE>(rw[u], a.weight, 0, 0, (u * P + t) * 8, a.cols);
+    } else {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
+            for (int i = 0; i < 8; ++i) rw[u].q[i / Raw8<T>::V][i % Raw8<T>::V] = (T)1.0f;
+    }
+    int odd = 0;
+    for (int64_t row = (int64_t)blockIdx.x * TEAMS + team; row < a.rows; row += (int64_t)gridDim.x * TEAMS, odd ^= 1) {
+        float s[U][8], dy[U][8], v[2] = {0.0f, 0.0f};
+        Raw8<T> rs[U], ry[U], rd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int col = (u * P + t) * 8;
+            ask<WHOLE>(rs[u], a.x, row, a.ld_x, col, a.cols);
+            ask<WHOLE>(ry[u], a.dy, row, a.ld_dy, col, a.cols);
+        }
+        if (along) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) ask<WHOLE>(rd[u], a.res, row, a.ld_res, (u * P + t) * 8, a.cols);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float w[8];
+            rs[u].get(s[u]);
+            ry[u].get(dy[u]);
+            rw[u].get(w);
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v[0] += s[u][i] * s[u][i];
-                v[1] += dy[u][i] * w[u][i] * s[u][i];
+                v[1] += dy[u][i] * w[i] * s[u][i];
             }
+        }
         team_sum<P>(v, red[odd]);
         const float r = __builtin_amdgcn_rsqf(v[0] * a.inv_cols + a.eps), c = r * r * (v[1] * a.inv_cols);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            back8<T>(a, row, (u * P + t) * 8, r, c, s[u], dy[u], w[u]);
+            float w[8], ds[8] = {};
+            rw[u].get(w);
+            if (along) rd[u].get(ds);
+            back8<T, WHOLE>(a, row, (u * P + t) * 8, r, c, s[u], dy[u], w, ds);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dw[u][i] += s[u][i];
         }
@@ -228,8 +293,10 @@ __global__ __launch_bounds__(1024) void k_norm_back_long(const NormArgs a) {
         team_sum<1024>(v, red[odd]);
         const float r = __builtin_amdgcn_rsqf(v[0] * a.inv_cols + a.eps), c = r * r * (v[1] * a.inv_cols);
         for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            float ds[8] = {};
             load(col);
-            back8<T>(a, row, col, r, c, s, dy, w);
+            if (a.y && a.res) load8(static_cast<const T*>(a.res) + row * a.ld_res + col, a.cols - col, ds);
+            back8<T, false>(a, row, col, r, c, s, dy, w, ds);
             if (part) {
                 float d[8] = {};
                 if (row != blockIdx.x) load8(part + col, 8, d);
@@ -247,45 +314,66 @@ constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxCols = int64_t(1) << 20;
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
-// Work-groups of a backward call, each with partial sums of its own for the weight's gradient: two for every place of 1024
-// threads, and no more than there are rows for
+// Work-groups of a backward call, each with partial sums of its own for the weight's gradient: what the compute units hold at
+// once (16384 x 8192 bf16: 256 work-groups of 1024 lanes 196 us, 512 199, 1024 207), no more than there are rows for
 int64_t back_groups(int64_t rows, int64_t cols) {
     const int teams = cols <= 128 ? 16 : cols <= 1024 ? 4 : 1;
-    const int64_t most = cols <= 4096 ? 1024 : 512, want = div_up(rows, teams);
+    const int64_t most = cols <= 2048 ? 1024 : cols <= 4096 ? 512 : 256, want = div_up(rows, teams);
     return want < most ? want : most;
 }
 
 template <typename T, int P, int U>
-void go(const NormArgs& a, bool back, bool mx, int64_t groups, hipStream_t st) {
-    const dim3 block(P < 256 ? 256 : P);
-    if (back) return k_norm_back<T, P, U><<<dim3((unsigned)groups), block, 0, st>>>(a);
-    const dim3 grid((unsigned)div_up(a.rows, (int64_t)kTeams<P> * a.per));
-    if (mx) {
-        if constexpr (P >= 64) k_norm<T, P, U, true><<<grid, block, 0, st>>>(a);
-    } else {
-        k_norm<T, P, U, false><<<grid, block, 0, st>>>(a);
+void forward(const NormArgs& a, bool mx, hipStream_t st) {
+    const dim3 block(P < 256 ? 256 : P), grid((unsigned)div_up(a.rows, (int64_t)kTeams<P> * a.per));
+    const bool whole = a.cols % 8 == 0;
+    if constexpr (P >= 64) {
+        if (mx && whole) return k_norm<T, P, U, true, true><<<grid, block, 0, st>>>(a);
+        if (mx) return k_norm<T, P, U, true, false><<<grid, block, 0, st>>>(a);
     }
+    if (whole) k_norm<T, P, U, false, true><<<grid, block, 0, st>>>(a);
+    else k_norm<T, P, U, false, false><<<grid, block, 0, st>>>(a);
 }
 
+template <typename T, int P, int U>
+void backward(const NormArgs& a, int64_t groups, hipStream_t st) {
+    const dim3 block(P < 256 ? 256 : P), grid((unsigned)groups);
+    if (a.cols % 8 == 0) k_norm_back<T, P, U, true><<<grid, block, 0, st>>>(a);
+    else k_norm_back<T, P, U, false><<<grid, block, 0, st>>>(a);
+}
+
+// Teams for a row's length.  Forward, 16384 x 8192 bf16 into 8 bits: 512 lanes of two eights 164 us, 256 of four the same,
+// 1024 of one 209; several rows a team one after the other 179 (4) and 191 (8).
 template <typename T>
-int launch(NormArgs a, bool back, bool mx, int64_t groups, hipStream_t st) {
+int launch_forward(NormArgs a, bool mx, hipStream_t st) {
     const int64_t wide = mx ? mx_groups(a.cols) * kMxGroup : a.cols;
-    // (a launch has fewer than 2^32 threads: more rows than 2^20 are taken several by a team)
-    a.per = (int)div_up(a.rows, int64_t(1) << 20);
-    if (wide <= 128) go<T, 16, 1>(a, back, mx, groups, st);
-    else if (wide <= 512) go<T, 64, 1>(a, back, mx, groups, st);
-    else if (wide <= 1024) go<T, 64, 2>(a, back, mx, groups, st);
-    else if (wide <= 2048) go<T, 256, 1>(a, back, mx, groups, st);
-    else if (wide <= 4096) go<T, 256, 2>(a, back, mx, groups, st);
-    else if (wide <= 8192) go<T, 512, 2>(a, back, mx, groups, st);
-    else if (wide <= 16384) go<T, 1024, 2>(a, back, mx, groups, st);
-    else if (wide <= 32768) go<T, 1024, 4>(a, back, mx, groups, st);
-    else if (back) k_norm_back_long<T><<<dim3((unsigned)groups), dim3(1024), 0, st>>>(a);
+    a.per = (int)div_up(a.rows, int64_t(1) << 20);  // (a launch has fewer than 2^32 threads)
+    if (wide <= 128) forward<T, 16, 1>(a, mx, st);
+    else if (wide <= 512) forward<T, 64, 1>(a, mx, st);
+    else if (wide <= 1024) forward<T, 64, 2>(a, mx, st);
+    else if (wide <= 2048) forward<T, 256, 1>(a, mx, st);
+    else if (wide <= 4096) forward<T, 256, 2>(a, mx, st);
+    else if (wide <= 8192) forward<T, 512, 2>(a, mx, st);
+    else if (wide <= 16384) forward<T, 1024, 2>(a, mx, st);
     else {
         const dim3 grid((unsigned)(a.rows < (int64_t(1) << 20) ? a.rows : int64_t(1) << 20));
         if (mx) k_norm_long<T, true><<<grid, dim3(1024), 0, st>>>(a);
         else k_norm_long<T, false><<<grid, dim3(1024), 0, st>>>(a);
     }
+    return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
+}
+
+// Backward a lane also keeps its columns' sums: one eight each as long as a work-group has the lanes.  16384 x 8192 bf16: 1024
+// lanes of one eight 196 us, 512 of two 199 (two work-groups' worth of registers do not fit a compute unit); asking for the
+// next row while one is summed up 199.
+template <typename T>
+int launch_backward(const NormArgs& a, int64_t groups, hipStream_t st) {
+    if (a.cols <= 128) backward<T, 16, 1>(a, groups, st);
+    else if (a.cols <= 512) backward<T, 64, 1>(a, groups, st);
+    else if (a.cols <= 1024) backward<T, 64, 2>(a, groups, st);
+    else if (a.cols <= 2048) backward<T, 256, 1>(a, groups, st);
+    else if (a.cols <= 4096) backward<T, 512, 1>(a, groups, st);
+    else if (a.cols <= 8192) backward<T, 1024, 1>(a, groups, st);
+    else k_norm_back_long<T><<<dim3((unsigned)groups), dim3(1024), 0, st>>>(a);
     return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
 }
 
@@ -334,9 +422,9 @@ extern "C" int dlc_norm_forward(const dlc_norm_config* c, const void* x, const v
     a.q = static_cast<uint8_t*>(q); a.scale = static_cast<uint8_t*>(scale);
     hipStream_t st = (hipStream_t)stream;
     switch (c->dtype) {
-        case DLC_F32: return launch<float>(a, false, q != nullptr, 0, st);
-        case DLC_F16: return launch<f16_t>(a, false, q != nullptr, 0, st);
-        default: return launch<bf16_t>(a, false, q != nullptr, 0, st);
+        case DLC_F32: return launch_forward<float>(a, q != nullptr, st);
+        case DLC_F16: return launch_forward<f16_t>(a, q != nullptr, st);
+        default: return launch_forward<bf16_t>(a, q != nullptr, st);
     }
 }
 
@@ -364,7 +452,7 @@ extern "C" int dlc_norm_backward(const dlc_norm_config* c, const void* s, const 
     const auto all = [&](auto one) {
         using T = decltype(one);
         if (a.rows > 0)
-            if (const int rc = launch<T>(a, true, false, groups, st); rc != DLC_OK) return rc;
+            if (const int rc = launch_backward<T>(a, groups, st); rc != DLC_OK) return rc;
         if (!dweight) return (int)DLC_OK;
         return DenseOps<T>::join(JoinArgs{}, JoinArgs{}, sum, st) == hipSuccess ? (int)DLC_OK : (int)DLC_EHIP;
     };
