@@ -12,7 +12,7 @@ namespace {
 // Descriptions that go with a launch: kTensors, or kFew where there are no more (a launch's arguments are copied twice on
 // their way: 7 tensors and their 2.5 million values 14.6 us a pass with room for 64)
 constexpr int kTensors = 64, kFew = 8;
-constexpr int64_t kChunk = 4096;       // elements of a chunk, at least: two a thread, 16 bytes each
+constexpr int64_t kChunk = 8192;       // elements of a chunk, at least: four eights a thread
 constexpr int64_t kMaxChunks = 8192;   // ... so many that there are no more than these (and one a tensor)
 constexpr int kThreads = 256;
 
@@ -52,21 +52,23 @@ template <typename T, typename F>
 __device__ __forceinline__ void each8(const Piece& p, int64_t at, int64_t end, F f) {
     const T* const in = static_cast<const T*>(p.in);
     T* const out = static_cast<T*>(p.out);
-    Raw8<T> x[4];
     float v[8];
     if (p.cols == p.n) {
-        for (int64_t i = at + threadIdx.x * 8; i < end; i += kThreads * 32) {
+        int64_t i = at + threadIdx.x * 8;
+        for (int64_t whole = (end - at) / (kThreads * 32); whole > 0; --whole, i += kThreads * 32) {
+            Raw8<T> x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u].load_whole(in + i + u * (kThreads * 8), true);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t left = end - i - u * (kThreads * 8);
-                x[u].load(in + i + u * (kThreads * 8), left < 8 ? (int)left : 8);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int64_t left = end - i - u * (kThreads * 8);
                 x[u].get(v);
-                if (left > 0) f(v, out + i + u * (kThreads * 8), left < 8 ? (int)left : 8);
+                f(v, out + i + u * (kThreads * 8), 8);
             }
+        }
+        for (; i < end; i += kThreads * 8) {
+            const int cnt = (int)min((int64_t)8, end - i);
+            load8(in + i, cnt, v);
+            f(v, out + i, cnt);
         }
         return;
     }

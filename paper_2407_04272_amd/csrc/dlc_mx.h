@@ -54,7 +54,7 @@ __device__ __forceinline__ uint32_t max_of_quad(uint32_t m) {
 template <int ELEM>
 struct MxWords;
 template <>
-struct MxWords<8> { uint32_t w[2]; };
+struct alignas(8) MxWords<8> { uint32_t w[2]; };
 template <>
 struct MxWords<4> { uint32_t w[1]; };
 

@@ -16,7 +16,8 @@ struct MxArgs {
 constexpr int kTileRows = 16;  // rows of a work-group's tile: four a wavefront, whose loads are on their way together
 
 // A tile is a group of 512 columns, eight a lane, of 16 rows: their scales are 256 bytes side by side.  Bound by memory.
-template <typename T, int ELEM>
+// WHOLE: rows end with a whole eight
+template <typename T, int ELEM, bool WHOLE>
 __global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {
     constexpr int R = kTileRows / 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -25,7 +26,11 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {
         const int col = (int)(tile - band * a.groups) * kMxGroup + lane * 8;
         Raw8<T> x[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) x[i].load(static_cast<const T*>(a.x) + (row0 + i) * a.ld + col, row0 + i < a.rows ? a.cols - col : 0);
+        for (int i = 0; i < R; ++i) {
+            const T* const p = static_cast<const T*>(a.x) + (row0 + i) * a.ld + col;
+            if constexpr (WHOLE) x[i].load_whole(p, row0 + i < a.rows && col < a.cols);
+            else x[i].load(p, row0 + i < a.rows ? a.cols - col : 0);
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             float f[8];
@@ -35,7 +40,7 @@ __global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {
     }
 }
 
-template <typename T, int ELEM>
+template <typename T, int ELEM, bool WHOLE>
 __global__ __launch_bounds__(256) void k_mx_dequantize(const MxArgs a) {
     constexpr int R = kTileRows / 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -57,7 +62,7 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(const MxArgs a) {
             if (row0 + i >= a.rows) continue;
             float f[8];
             mx_decode8<ELEM>(w[i], byte[i], f);
-            store8(static_cast<T*>(const_cast<void*>(a.x)) + (row0 + i) * a.ld + col, cnt, f);
+            store8(static_cast<T*>(const_cast<void*>(a.x)) + (row0 + i) * a.ld + col, WHOLE ? 8 : cnt, f);
         }
     }
 }
@@ -81,16 +86,18 @@ bool good_mx(const dlc_mx_config* c) {
     return true;
 }
 
+template <typename T, int ELEM, bool WHOLE>
+void convert(const MxArgs& a, bool back, hipStream_t st) {
+    const dim3 grid((unsigned)(a.tiles < (int64_t(1) << 20) ? a.tiles : int64_t(1) << 20)), block(256);
+    if (back) k_mx_dequantize<T, ELEM, WHOLE><<<grid, block, 0, st>>>(a);
+    else k_mx_quantize<T, ELEM, WHOLE><<<grid, block, 0, st>>>(a);
+}
+
 template <typename T>
 void convert(const MxArgs& a, int elem, bool back, hipStream_t st) {
-    const dim3 grid((unsigned)(a.tiles < (int64_t(1) << 20) ? a.tiles : int64_t(1) << 20)), block(256);
-    if (back) {
-        if (elem == DLC_MX_E4M3) k_mx_dequantize<T, 8><<<grid, block, 0, st>>>(a);
-        else k_mx_dequantize<T, 4><<<grid, block, 0, st>>>(a);
-    } else {
-        if (elem == DLC_MX_E4M3) k_mx_quantize<T, 8><<<grid, block, 0, st>>>(a);
-        else k_mx_quantize<T, 4><<<grid, block, 0, st>>>(a);
-    }
+    const bool whole = a.cols % 8 == 0;
+    if (elem == DLC_MX_E4M3) whole ? convert<T, 8, true>(a, back, st) : convert<T, 8, false>(a, back, st);
+    else whole ? convert<T, 4, true>(a, back, st) : convert<T, 4, false>(a, back, st);
 }
 
 int convert_any(const dlc_mx_config* c, const void* x, const void* q, const void* scale, bool back, void* stream) {

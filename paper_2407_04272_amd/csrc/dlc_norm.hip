@@ -51,7 +51,7 @@ template <int P>
 constexpr int kTeams = P < 256 ? 256 / P : 1;
 
 // Eight columns of a row.  WHOLE: rows end with a whole eight, and there is no code for others: it costs registers, and with
-// them the wavefronts that hide the loads (16384 x 8192 bf16, 157 registers and 233 us for 68 and 178)
+// them the wavefronts that hide the loads (16384 x 8192 bf16 into 8 bits: 157 registers and 233 us for 80 and 164)
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void ask(Raw8<T>& q, const void* p, int64_t row, int64_t ld, int col, int cols) {
     const T* const at = static_cast<const T*>(p) + row * ld + col;
