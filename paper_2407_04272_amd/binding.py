@@ -499,8 +499,9 @@ def dlc_mx_linear_forward(cfg: MxLinearConfig, xq, xs, wq, ws, bias, residual, y
 
 class GradientList:
     """Tensors of dlc_gradient_norm and dlc_gradient_clip, checked and described once: of one or two dimensions, columns one
-    element apart, or contiguous; all on one GPU, none twice.  Holds the tensors; make another when a program's gradients move
-    (a tensor's memory is read again in every call, its address is not)."""
+    element apart, or contiguous; all on one GPU, none twice (a parameter that two layers share has one gradient), and none
+    inside another (checked where both are contiguous).  Holds the tensors; make another when a program's gradients move (a
+    tensor's memory is read again in every call, its address is not)."""
 
     def __init__(self, tensors):
         import torch
@@ -509,7 +510,8 @@ class GradientList:
         self.device = None
         self.shapes = [(t.dtype, tuple(t.shape)) for t in self.tensors]
         self.entries = (Tensor * len(self.tensors))()
-        seen = set()
+        self.places = {}  # address -> the tensor's place in the list
+        self.extents = []  # (first byte, behind the last, place) of contiguous tensors
         for i, t in enumerate(self.tensors):
             if t.dtype not in codes or not t.is_cuda:
                 raise DlcError(EINVAL, f"tensor {i}: {t.dtype} on {t.device}")
@@ -527,13 +529,33 @@ class GradientList:
             else:
                 raise DlcError(EINVAL, f"tensor {i}: strides {t.stride()} of {tuple(shape)}")
             if n > 0:
-                if t.data_ptr() in seen:
+                p = t.data_ptr()
+                if p in self.places:
                     raise DlcError(EINVAL, f"tensor {i}: in the list twice")
-                seen.add(t.data_ptr())
+                self.places[p] = i
+                if t.is_contiguous():
+                    self.extents.append((p, p + n * t.element_size(), i))
             self.entries[i] = Tensor(t.data_ptr(), rows, cols, ld, codes[t.dtype], 0)
+        _check_extents(self.extents)
 
     def __len__(self):
         return len(self.tensors)
+
+
+def _check_extents(extents):
+    last = (0, 0, -1)
+    for e in sorted(extents):
+        if e[0] < last[1] and e != last:
+            raise DlcError(EINVAL, f"tensors {last[2]} and {e[2]} overlap")
+        last = e
+
+
+def _check_apart(lst, out):
+    """Outputs may be the gradients, each its own, and nothing else of them."""
+    for p, i in out.places.items():
+        if lst.places.get(p, i) != i:
+            raise DlcError(EINVAL, f"out {i}: gradient {lst.places[p]}")
+    _check_extents(lst.extents + out.extents)
 
 
 def _word(name, t, dtype, device):
@@ -572,6 +594,7 @@ def dlc_gradient_clip(lst: GradientList, sum, max_norm, norm=None, out: Gradient
         _gradients(out, stream)
         if out.shapes != lst.shapes:
             raise DlcError(EINVAL, "out: other types or shapes than the gradients")
+        _check_apart(lst, out)
     _check(lib().dlc_gradient_clip(lst.entries, len(lst), _word("sum", sum, _float64, device), float(max_norm),
                                    _word("norm", norm, _float32, device), out.entries, st), "dlc_gradient_clip")
 

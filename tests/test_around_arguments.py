@@ -233,3 +233,26 @@ def test_gradient_lists_of_the_binding():
     _refused(b.dlc_gradient_clip, one, total, 1.0, None, b.GradientList([At(f, 0), At(f, 0)]), stream=Stream())
     _refused(b.dlc_gradient_clip, one, total, 1.0, None, b.GradientList([At(torch.float16, 0)]), stream=Stream())
     _refused(b.dlc_gradient_norm, one, total, Stub(torch.uint8, 64, device=1), stream=Stream())
+
+
+def test_gradients_that_overlap():
+    """Memory that two entries share would be counted twice, and clipped by two work-groups at once."""
+    import torch
+    b = _b()
+    f, total = torch.float32, Stub(torch.float64, 1)
+    _refused(b.GradientList, [At(f, 10, ptr=4096), At(f, 10, ptr=4096 + 36)])
+    _refused(b.GradientList, [At(f, 10, ptr=4096 + 36), At(f, 2, 5, ptr=4096)])
+    _refused(b.GradientList, [At(f, 100, ptr=4096), At(f, 1, ptr=8192), At(f, 3, ptr=4096 + 40)])
+    _refused(b.GradientList, [At(f, 100, ptr=4096), At(torch.float16, 2, ptr=4096 + 4), At(f, 1, ptr=4096 + 200)])
+
+    def rows(ptr):
+        return At(f, 4, 2, ptr=ptr, strides=(4, 1), contiguous=False)
+
+    # side by side, and rows between rows
+    lst = b.GradientList([At(f, 10, ptr=4096), At(f, 10, ptr=4096 + 40), rows(8192), rows(8200)])
+    for p, q in ((4096 + 40, 4096), (4096 + 4, 65536), (65536, 4096 + 36), (65536, 4096)):
+        _refused(b.dlc_gradient_clip, lst, total, 1.0, None, b.GradientList([At(f, 10, ptr=p), At(f, 10, ptr=q), rows(1 << 20), rows((1 << 20) + 8)]), stream=Stream())
+    _refused(b.dlc_gradient_clip, lst, total, 1.0, None, b.GradientList([At(f, 10, ptr=65536), At(f, 10, ptr=65536 + 40), rows(8200), rows(1 << 20)]), stream=Stream())
+    # some of the outputs may be the gradients themselves
+    for p, q in ((4096, 65536), (65536, 4096 + 40), (4096, 4096 + 40), (65536, 65536 + 40)):
+        b._check_apart(lst, b.GradientList([At(f, 10, ptr=p), At(f, 10, ptr=q), rows(8192), rows(1 << 20)]))
