@@ -37,14 +37,7 @@ __device__ __forceinline__ float mx_scale(uint32_t byte) {
 
 __device__ __forceinline__ uint32_t magnitude_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu; }
 
-__device__ __forceinline__ uint32_t max_bits8(const float f[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, magnitude_bits(f[i]));
-    return m;
-}
-
-// ... of the four lanes that hold a block
+// The largest of the four lanes that hold a block
 __device__ __forceinline__ uint32_t max_of_quad(uint32_t m) {
     m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xB1, 0xF, 0xF, true));         // quad_perm 1 0 3 2
     return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4E, 0xF, 0xF, true));      // quad_perm 2 3 0 1
@@ -104,15 +97,24 @@ __device__ __forceinline__ void mx_decode8(const MxWords<ELEM>& q, uint32_t byte
 }
 
 // Stores a lane's eight columns col .. col + 7 of a row (0 behind the last) and, with three lanes beside it, their block's
-// scale.  All four lanes of a block come here; col runs to the end of the last group.
+// scale.  All four lanes of a block come here; col runs to the end of the last group.  `shared` of f stand before col, and so
+// many columns are missing behind the last of f: the elements are moved as one word.
 template <int ELEM>
-__device__ __forceinline__ void mx_store8(const float f[8], int64_t row, int col, int cols, int64_t rows, uint8_t* q, uint8_t* scale) {
-    const uint32_t byte = mx_scale_byte<ELEM>(max_of_quad(max_bits8(f)));
+__device__ __forceinline__ void mx_store8(const float f[8], int shared, int64_t row, int col, int cols, int64_t rows, uint8_t* q, uint8_t* scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, i < shared ? 0u : magnitude_bits(f[i]));
+    const uint32_t byte = mx_scale_byte<ELEM>(max_of_quad(top));
     if (col < (int)mx_filled(cols)) {
         const MxWords<ELEM> w = mx_encode8<ELEM>(f, byte);
         uint8_t* const p = q + row * mx_row_bytes(cols, ELEM) + col * ELEM / 8;
-        if constexpr (ELEM == 8) *reinterpret_cast<uint2*>(p) = uint2{w.w[0], w.w[1]};
-        else *reinterpret_cast<uint32_t*>(p) = w.w[0];
+        const int by = byte == 255u ? 0 : (shared & 7) * ELEM;  // (a NaN block's are all alike)
+        if constexpr (ELEM == 8) {
+            const uint64_t v = ((uint64_t)w.w[1] << 32 | w.w[0]) >> by;
+            *reinterpret_cast<uint2*>(p) = uint2{(uint32_t)v, (uint32_t)(v >> 32)};
+        } else {
+            *reinterpret_cast<uint32_t*>(p) = w.w[0] >> by;
+        }
     }
     if ((col & (kMxBlock - 1)) == 0) {
         const int block = col / kMxBlock;

@@ -1,7 +1,7 @@
 // Root-mean-square norm with the residual's addition, forward (results in the type, in microscaled form, or both) and backward.
 //
 // Bound by memory: every row is read once into registers, its sums are made there, and the results go out.  A team of P lanes
-// has a row, U times eight columns a lane; rows longer than 16384 columns (backward 8192) are read twice instead.
+// has a row, U times eight columns a lane; rows longer than 16384 columns are read twice instead.
 #include "dlc_mx.h"
 
 using namespace dlc;
@@ -50,19 +50,35 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float (*red)[N]) {
 template <int P>
 constexpr int kTeams = P < 256 ? 256 / P : 1;
 
-// Eight columns of a row.  WHOLE: rows end with a whole eight, and there is no code for others: it costs registers, and with
-// them the wavefronts that hide the loads (16384 x 8192 bf16 into 8 bits: 157 registers and 233 us for 80 and 164)
-template <bool WHOLE, typename T>
-__device__ __forceinline__ void ask(Raw8<T>& q, const void* p, int64_t row, int64_t ld, int col, int cols) {
-    const T* const at = static_cast<const T*>(p) + row * ld + col;
-    if constexpr (WHOLE) q.load_whole(at, col < cols);
-    else q.load(at, cols - col);
+// How rows end.  Whole: with a whole eight.  Back: not, but they have eight columns: the lane with the last ones takes the last
+// eight instead, those that the lane before it has as well among them: they count once, and are stored twice alike.  Short rows
+// alone are loaded and stored element by element: as code for all others it took registers and a wait for every element (8192 x
+// 4099 bf16: forward 90 us for 47, into 8 bits 92 for 52, backward 93 for 60; with 4096 columns 39, 35 and 46).
+enum Ends { kShort, kWhole, kBack };
+
+// ... the first of a lane's columns
+template <int E>
+__device__ __forceinline__ int first_of(int col, int cols) {
+    return E == kBack && col < cols ? min(col, cols - 8) : col;
 }
 
-template <bool WHOLE, typename T>
+// ... how many of them the lane before has as well
+template <int E>
+__device__ __forceinline__ int shared_of(int col, int cols) {
+    return E == kBack ? max(col + 8 - cols, 0) : 0;
+}
+
+template <int E, typename T>
+__device__ __forceinline__ void ask(Raw8<T>& q, const void* p, int64_t row, int64_t ld, int col, int cols) {
+    const T* const at = static_cast<const T*>(p) + row * ld + first_of<E>(col, cols);
+    if constexpr (E == kShort) q.load(at, cols - col);
+    else q.load_whole(at, col < cols);
+}
+
+template <int E, typename T>
 __device__ __forceinline__ void put(void* p, int64_t row, int64_t ld, int col, int cols, const float f[8]) {
-    T* const at = static_cast<T*>(p) + row * ld + col;
-    if constexpr (!WHOLE) store8(at, cols - col, f);
+    T* const at = static_cast<T*>(p) + row * ld + first_of<E>(col, cols);
+    if constexpr (E == kShort) store8(at, cols - col, f);
     else if (col < cols) store8(at, 8, f);
 }
 
@@ -88,17 +104,17 @@ __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, int col
     }
 }
 
-template <typename T, bool MX, bool WHOLE>
+template <typename T, bool MX, int E>
 __device__ __forceinline__ void put_row(const NormArgs& a, int64_t row, int col, float r, float s[8], const float w[8]) {
-    const int cnt = a.cols - col;
-    if (a.sum) put<WHOLE, T>(a.sum, row, a.ld_sum, col, a.cols, s);
+    if (a.sum) put<E, T>(a.sum, row, a.ld_sum, col, a.cols, s);
+    if (MX && col >= a.cols) r = 0.0f;  // (a row's NaN stays in its columns)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] = i < cnt ? s[i] * r * w[i] : 0.0f;
-    if (a.y) put<WHOLE, T>(a.y, row, a.ld_y, col, a.cols, s);
-    if constexpr (MX) mx_store8<8>(s, row, col, a.cols, a.rows, a.q, a.scale);
+    for (int i = 0; i < 8; ++i) s[i] = s[i] * r * w[i];
+    if (a.y) put<E, T>(a.y, row, a.ld_y, col, a.cols, s);
+    if constexpr (MX) mx_store8<8>(s, shared_of<E>(col, a.cols), row, col, a.cols, a.rows, a.q, a.scale);
 }
 
-template <typename T, int P, int U, bool MX, bool WHOLE>
+template <typename T, int P, int U, bool MX, int E>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
     __shared__ float red[2][P > 64 ? P / 64 : 1][1];
     const int t = threadIdx.x % P, team = threadIdx.x / P;
@@ -111,20 +127,20 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (u * P + t) * 8;
-            ask<WHOLE>(x[u], a.x, row, a.ld_x, col, a.cols);
+            ask<E>(x[u], a.x, row, a.ld_x, col, a.cols);
         }
         if (a.res) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int col = (u * P + t) * 8;
-                ask<WHOLE>(res[u], a.res, row, a.ld_res, col, a.cols);
+                ask<E>(res[u], a.res, row, a.ld_res, col, a.cols);
             }
         }
         if (a.weight) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int col = (u * P + t) * 8;
-                ask<WHOLE>(w[u], a.weight, 0, 0, col, a.cols);
+                ask<E>(w[u], a.weight, 0, 0, col, a.cols);
             }
         }
 #pragma unroll
@@ -137,7 +153,8 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
                 for (int i = 0; i < 8; ++i) s[u][i] += r[i];
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sq[0] += s[u][i] * s[u][i];
+            for (int i = 0; i < 8; ++i)
+                if (E != kBack || i >= shared_of<E>((u * P + t) * 8, a.cols)) sq[0] += s[u][i] * s[u][i];
         }
         team_sum<P>(sq, red[odd]);
         const float r = __builtin_amdgcn_rsqf(sq[0] * a.inv_cols + a.eps);
@@ -149,7 +166,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
             if (!a.weight)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] = 1.0f;
-            if (col < end) put_row<T, MX, WHOLE>(a, row, col, r, s[u], g);
+            if (col < end) put_row<T, MX, E>(a, row, col, r, s[u], g);
         }
     }
 }
@@ -173,13 +190,13 @@ __global__ __launch_bounds__(1024) void k_norm_long(const NormArgs a) {
             float w[8];
             load_sum<T>(a, row, col, a.cols - col, s);
             load_weight<T>(a.weight, col, a.cols - col, w);
-            put_row<T, MX, false>(a, row, col, r, s, w);
+            put_row<T, MX, kShort>(a, row, col, r, s, w);
         }
     }
 }
 
 // dx of eight columns (into g), and dy s r (into s)
-template <typename T, bool WHOLE>
+template <typename T, int E>
 __device__ __forceinline__ void back8(const NormArgs& a, int64_t row, int col, float r, float c, float s[8], float dy[8], const float w[8], const float ds[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -187,10 +204,10 @@ __device__ __forceinline__ void back8(const NormArgs& a, int64_t row, int col, f
         dy[i] = r * (dy[i] * w[i] - s[i] * c) + ds[i];
         s[i] = n;
     }
-    if (a.y) put<WHOLE, T>(a.y, row, a.ld_y, col, a.cols, dy);
+    if (a.y) put<E, T>(a.y, row, a.ld_y, col, a.cols, dy);
 }
 
-template <typename T, int P, int U, bool WHOLE>
+template <typename T, int P, int U, int E>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs a) {
     constexpr int TEAMS = kTeams<P>;
     __shared__ float red[2][P > 64 ? P / 64 : 1][2];
@@ -201,7 +218,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs 
     Raw8<T> rw[U];
     if (a.weight) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) ask<WHOLE>(rw[u], a.weight, 0, 0, (u * P + t) * 8, a.cols);
+        for (int u = 0; u < U; ++u) ask<E>(rw[u], a.weight, 0, 0, (u * P + t) * 8, a.cols);
     } else {
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -215,12 +232,12 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (u * P + t) * 8;
-            ask<WHOLE>(rs[u], a.x, row, a.ld_x, col, a.cols);
-            ask<WHOLE>(ry[u], a.dy, row, a.ld_dy, col, a.cols);
+            ask<E>(rs[u], a.x, row, a.ld_x, col, a.cols);
+            ask<E>(ry[u], a.dy, row, a.ld_dy, col, a.cols);
         }
         if (along) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) ask<WHOLE>(rd[u], a.res, row, a.ld_res, (u * P + t) * 8, a.cols);
+            for (int u = 0; u < U; ++u) ask<E>(rd[u], a.res, row, a.ld_res, (u * P + t) * 8, a.cols);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -230,6 +247,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs 
             rw[u].get(w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                if (E == kBack && i < shared_of<E>((u * P + t) * 8, a.cols)) continue;
                 v[0] += s[u][i] * s[u][i];
                 v[1] += dy[u][i] * w[i] * s[u][i];
             }
@@ -241,7 +259,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs 
             float w[8], ds[8] = {};
             rw[u].get(w);
             if (along) rd[u].get(ds);
-            back8<T, WHOLE>(a, row, (u * P + t) * 8, r, c, s[u], dy[u], w, ds);
+            back8<T, E>(a, row, (u * P + t) * 8, r, c, s[u], dy[u], w, ds);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dw[u][i] += s[u][i];
         }
@@ -252,7 +270,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs 
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sums[team][(u * P + t) * 8 + i] = dw[u][i];
+            for (int i = 0; i < 8; ++i) sums[team][first_of<E>((u * P + t) * 8, a.cols) + i] = dw[u][i];
         __syncthreads();
         for (int col = threadIdx.x; col < a.cols; col += 256) {
             float d = sums[0][col];
@@ -264,7 +282,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm_back(const NormArgs 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int col = (u * P + t) * 8;
-            if (col < a.cols) store8(part + col, 8, dw[u]);  // (the pitch has room for whole chunks)
+            if (col < a.cols) store8(part + first_of<E>(col, a.cols), 8, dw[u]);  // (the pitch has room for whole chunks)
         }
     }
 }
@@ -296,7 +314,7 @@ __global__ __launch_bounds__(1024) void k_norm_back_long(const NormArgs a) {
             float ds[8] = {};
             load(col);
             if (a.y && a.res) load8(static_cast<const T*>(a.res) + row * a.ld_res + col, a.cols - col, ds);
-            back8<T, false>(a, row, col, r, c, s, dy, w, ds);
+            back8<T, kShort>(a, row, col, r, c, s, dy, w, ds);
             if (part) {
                 float d[8] = {};
                 if (row != blockIdx.x) load8(part + col, 8, d);
@@ -318,7 +336,7 @@ bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes
 // once (16384 x 8192 bf16: 256 work-groups of 1024 lanes 196 us, 512 199, 1024 207), no more than there are rows for
 int64_t back_groups(int64_t rows, int64_t cols) {
     const int teams = cols <= 128 ? 16 : cols <= 1024 ? 4 : 1;
-    const int64_t most = cols <= 2048 ? 1024 : cols <= 4096 ? 512 : 256, want = div_up(rows, teams);
+    const int64_t most = cols <= 2048 ? 1024 : cols <= 6144 ? 512 : 256, want = div_up(rows, teams);
     return want < most ? want : most;
 }
 
@@ -327,22 +345,28 @@ void forward(const NormArgs& a, bool mx, hipStream_t st) {
     const dim3 block(P < 256 ? 256 : P), grid((unsigned)div_up(a.rows, (int64_t)kTeams<P> * a.per));
     const bool whole = a.cols % 8 == 0;
     if constexpr (P >= 64) {
-        if (mx && whole) return k_norm<T, P, U, true, true><<<grid, block, 0, st>>>(a);
-        if (mx) return k_norm<T, P, U, true, false><<<grid, block, 0, st>>>(a);
+        if constexpr (P == 64 && U == 1)
+            if (mx && a.cols < 8) return k_norm<T, P, U, true, kShort><<<grid, block, 0, st>>>(a);
+        if (mx && whole) return k_norm<T, P, U, true, kWhole><<<grid, block, 0, st>>>(a);
+        if (mx) return k_norm<T, P, U, true, kBack><<<grid, block, 0, st>>>(a);
+    } else {
+        if (a.cols < 8) return k_norm<T, P, U, false, kShort><<<grid, block, 0, st>>>(a);
     }
-    if (whole) k_norm<T, P, U, false, true><<<grid, block, 0, st>>>(a);
-    else k_norm<T, P, U, false, false><<<grid, block, 0, st>>>(a);
+    if (whole) k_norm<T, P, U, false, kWhole><<<grid, block, 0, st>>>(a);
+    else k_norm<T, P, U, false, kBack><<<grid, block, 0, st>>>(a);
 }
 
 template <typename T, int P, int U>
 void backward(const NormArgs& a, int64_t groups, hipStream_t st) {
     const dim3 block(P < 256 ? 256 : P), grid((unsigned)groups);
-    if (a.cols % 8 == 0) k_norm_back<T, P, U, true><<<grid, block, 0, st>>>(a);
-    else k_norm_back<T, P, U, false><<<grid, block, 0, st>>>(a);
+    if constexpr (P < 64)
+        if (a.cols < 8) return k_norm_back<T, P, U, kShort><<<grid, block, 0, st>>>(a);
+    if (a.cols % 8 == 0) k_norm_back<T, P, U, kWhole><<<grid, block, 0, st>>>(a);
+    else k_norm_back<T, P, U, kBack><<<grid, block, 0, st>>>(a);
 }
 
 // Teams for a row's length.  Forward, 16384 x 8192 bf16 into 8 bits: 512 lanes of two eights 164 us, 256 of four the same,
-// 1024 of one 209; several rows a team one after the other 179 (4) and 191 (8).
+// 1024 of one 209; several rows a team one after the other 179 (4) and 191 (8).  8192 x 8195 bf16: 1024 lanes 146 us, 768 120.
 template <typename T>
 int launch_forward(NormArgs a, bool mx, hipStream_t st) {
     const int64_t wide = mx ? mx_groups(a.cols) * kMxGroup : a.cols;
@@ -353,6 +377,7 @@ int launch_forward(NormArgs a, bool mx, hipStream_t st) {
     else if (wide <= 2048) forward<T, 256, 1>(a, mx, st);
     else if (wide <= 4096) forward<T, 256, 2>(a, mx, st);
     else if (wide <= 8192) forward<T, 512, 2>(a, mx, st);
+    else if (wide <= 12288) forward<T, 768, 2>(a, mx, st);
     else if (wide <= 16384) forward<T, 1024, 2>(a, mx, st);
     else {
         const dim3 grid((unsigned)(a.rows < (int64_t(1) << 20) ? a.rows : int64_t(1) << 20));
@@ -364,7 +389,8 @@ int launch_forward(NormArgs a, bool mx, hipStream_t st) {
 
 // Backward a lane also keeps its columns' sums: one eight each as long as a work-group has the lanes.  16384 x 8192 bf16: 1024
 // lanes of one eight 196 us, 512 of two 199 (two work-groups' worth of registers do not fit a compute unit); asking for the
-// next row while one is summed up 199.
+// next row while one is summed up 199.  8192 x 4099: 1024 lanes 81 us, 768 (two work-groups a compute unit) 60.  4096 x 12288: read
+// twice 176 us, 1024 lanes of two eights 110 (registers do not hold them all), 768 82; 16384 columns, 1024 lanes, 138 for 213.
 template <typename T>
 int launch_backward(const NormArgs& a, int64_t groups, hipStream_t st) {
     if (a.cols <= 128) backward<T, 16, 1>(a, groups, st);
@@ -372,7 +398,10 @@ int launch_backward(const NormArgs& a, int64_t groups, hipStream_t st) {
     else if (a.cols <= 1024) backward<T, 64, 2>(a, groups, st);
     else if (a.cols <= 2048) backward<T, 256, 1>(a, groups, st);
     else if (a.cols <= 4096) backward<T, 512, 1>(a, groups, st);
+    else if (a.cols <= 6144) backward<T, 768, 1>(a, groups, st);
     else if (a.cols <= 8192) backward<T, 1024, 1>(a, groups, st);
+    else if (a.cols <= 12288) backward<T, 768, 2>(a, groups, st);
+    else if (a.cols <= 16384) backward<T, 1024, 2>(a, groups, st);
     else k_norm_back_long<T><<<dim3((unsigned)groups), dim3(1024), 0, st>>>(a);
     return hipGetLastError() == hipSuccess ? DLC_OK : DLC_EHIP;
 }

@@ -245,3 +245,63 @@ def test_scales_far_apart_and_nan(rows):
         v, e = product(x, w)
         keep = ~nan
         assert_close(y[keep], v[keep], rounded(v, e, "f32")[keep], f"{rows} {bits}")
+
+
+@pytest.mark.parametrize("rows", [3, 50, 300])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_values_below_the_normal_range(rows, bits):
+    """Scales down to 2^-127, whose elements are below fp32's normal numbers, times weights large enough that the results are
+    not.  E4M3 with results in fp32 may take each value below 2^-126 for 0; nothing else is lost anywhere."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    n_in, n_out = 600, 40
+    rng = np.random.default_rng(31)
+    x = rng.standard_normal((rows, n_in)) * np.exp2(rng.integers(-133, -118, (rows, n_in // 50)).repeat(50, axis=1).astype(float))
+    w = rng.standard_normal((n_out, n_in)) * np.exp2(rng.integers(70, 90, (n_out, n_in)).astype(float))
+    (xq, xs), (wq, ws) = quantise(x, bits), quantise(w, 4)
+    assert (xs == 0).any()
+    vx, vw = (torch.from_numpy(v).cuda() for v in (values(xq, xs, n_in, bits), values(wq, ws, n_in, 4)))
+    for dtype in ("f32", "bf16"):
+        y = torch.empty((rows, n_out), dtype=torch_type(dtype), device="cuda")
+        cfg = b.make_mx_linear_config(code(dtype), bits, rows, n_in, n_out)
+        work = torch.empty(b.dlc_mx_linear_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        b.dlc_mx_linear_forward(cfg, *(torch.from_numpy(v).cuda() for v in (xq, xs, wq, ws)), None, None, y, work)
+        v, e = product(vx, vw)
+        if bits == 8 and dtype == "f32":
+            e = e + torch.where(vx.abs() < 2.0 ** -126, vx.abs(), 0.0) @ vw.abs().t()
+        elif bits == 8:
+            e = e + CUT * (vx.abs() @ vw.abs().t())
+        assert_close(y, v, rounded(v, e, dtype), f"{rows} {bits} {dtype}")
+
+
+def test_scales_from_end_to_end():
+    """Hand-made scales, 2^-127 against 2^127: the results are whole numbers of products of elements."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    rows, n_in, n_out = 70, 256, 48
+    rng = np.random.default_rng(32)
+    for bits, lo in ((4, 0), (8, 15)):      # (E4M3: from 2^-112 on every element is a normal number)
+        xq, xs = quantise(rng.choice([-2.0, -1.0, 0.0, 1.0, 2.0], (rows, n_in)), bits)
+        wq, ws = quantise(rng.choice([-1.0, 0.0, 1.0, 3.0], (n_out, n_in)), 4)
+        one = values(xq, np.full_like(xs, 127), n_in, bits) @ values(wq, np.full_like(ws, 127), n_in, 4).T
+        for a, c in ((lo, 254 - lo), (254 - 8, 8), (100, 150)):
+            y = torch.empty((rows, n_out), device="cuda")
+            cfg = b.make_mx_linear_config(b.F32, bits, rows, n_in, n_out)
+            work = torch.empty(b.dlc_mx_linear_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+            if bits == 8 and a > 246:
+                continue
+            b.dlc_mx_linear_forward(cfg, torch.from_numpy(xq).cuda(), torch.full(xs.shape, a, dtype=torch.uint8, device="cuda"), torch.from_numpy(wq).cuda(),
+                                    torch.full(ws.shape, c, dtype=torch.uint8, device="cuda"), None, None, y, work)
+            assert np.array_equal(y.cpu().numpy().astype(np.float64), one * 2.0 ** (a + c - 254)), (bits, a, c)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(9, 7), (20, 9), (18, 23), (5, 35), (3, 95), (17, 121), (33, 519), (2, 1021)])
+def test_quantise_rows_that_end_inside_an_eight(rows, cols, dtype, bits):
+    """... a value that two lanes have must not count for the block of the second, a NaN neither"""
+    x, t = _matrix(rows, cols, dtype, 51, "wide")
+    for at in range(max(cols - 9, 0), cols):
+        t = t.clone()
+        t[at % rows, at] = float("nan") if at % 2 else 1000.0
+        _same(*_quantised(t, bits, dtype), *quantise(t.double().cpu().numpy(), bits), f"{rows}x{cols} {bits} {dtype} {at}")

@@ -218,3 +218,40 @@ def test_no_rows():
         dw = torch.full_like(w, 7.0)
         b.dlc_norm_backward(cfg, e, w, e, None, e, dw)
         assert bool((dw == 0).all())
+
+
+# the last eight of a row starts in the lane before: behind every border between the teams' sizes, short rows of less than eight
+ENDS = [(40, 5), (50, 9), (70, 15), (3, 127), (20, 131), (9, 519), (7, 1023), (5, 1025), (40, 2049), (4, 4097), (3, 8191), (3, 8193), (2, 12291), (2, 16383)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", ENDS)
+def test_rows_that_end_inside_an_eight(rows, cols, dtype):
+    test_forward(rows, cols, dtype)
+    test_eight_bits(rows, cols, dtype)
+    test_backward(rows, cols, dtype)
+    test_rows_apart_and_in_place(cols, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [24, 600, 2000, 4099, 12288, 12289])
+def test_many_rows_backward(cols, dtype):
+    """More rows than work-groups: a team's sums for the weight's gradient go on from row to row."""
+    test_backward(1100 if cols < 4000 else 600, cols, dtype)
+
+
+@pytest.mark.parametrize("cols", [33, 1023, 12289])
+def test_a_nan_stays_in_its_row(cols):
+    """... of the columns that two lanes have, too, and of rows in 8 bits"""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    for at in (0, cols - 9, cols - 8, cols - 1):
+        x, w = _normal(5, cols, "f32", 41), _normal(cols, 0, "f32", 42)
+        x[2, at] = float("nan")
+        cfg, mx = b.make_norm_config(b.F32, 5, cols, EPS), b.make_mx_config(b.F32, b.MX_E4M3, 5, cols)
+        y, q, sc = torch.empty_like(x), GuardedBytes(b.dlc_mx_data_shape(mx)), GuardedBytes(b.dlc_mx_scale_shape(mx))
+        b.dlc_norm_forward(cfg, x, None, w, None, y, q.view, sc.view)
+        rows = [0, 1, 3, 4]
+        assert bool(torch.isnan(y[2]).all()) and not bool(torch.isnan(y[rows]).any())
+        want_q, want_s = quantise(y.double().cpu().numpy(), 8)
+        assert np.array_equal(sc.view.cpu().numpy(), want_s) and np.array_equal(q.view.cpu().numpy(), want_q) and q.intact() and sc.intact()
