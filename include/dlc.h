@@ -472,7 +472,12 @@ int dlc_mx_dequantize(const dlc_mx_config* cfg /*HOST*/, const void* d_q, const 
  *   d_xq, d_xs   x [M][K], elements elem_x     d_wq, d_ws   w [N][K], elements E2M1
  *   d_bias [N] or NULL   d_residual [M][N] or NULL   d_y [M][N], all of type dtype.  d_residual may be d_y, with equal leading
  *   dimensions (else DLC_EINVAL)
- * Products are exact, sums and the epilogue fp32, the result is rounded once.
+ * Sums and the epilogue are fp32, the result is rounded once.  Products are exact, but for two cases of E4M3 rows:
+ *   results in half precision   of eight products in a row each loses what lies more than 13 binary places below the leading
+ *                bit of the largest (less than 2^-13 of that one's magnitude; nothing of the largest itself): the matrix cores' way, and in
+ *                the norm some 2^-14 of a result
+ *   results in fp32             an element that stands for less than 2^-126 may count as 0, one past fp32's range (a scale made by hand)
+ *                as infinite
  *   sizes        rows 0 .. 2^30, features 1 .. 2^20, leading dimensions up to 2^20; results of fewer than 2^24 tiles of 256 x 256
  *                (E4M3 with results in fp32: 128 x 128)
  *   d_work       as above, dlc_mx_linear_workspace_bytes
@@ -507,7 +512,7 @@ size_t dlc_mx_linear_workspace_bytes(const dlc_mx_linear_config* cfg /*HOST*/);
  *   d_s as the forward call stored it (r is made again from it)   d_dx: the gradient of x and of the residual; may be d_dy or
  *   d_ds, with equal leading dimensions   d_dweight [cols]; d_dx and d_dweight may be NULL and are then not computed.
  *   No rows: dweight is zeros.
- *   d_work  as above, dlc_norm_workspace_bytes (only the backward call takes one; 0 without d_dweight's sums to put together)
+ *   d_work  as above, dlc_norm_workspace_bytes; only the backward call takes one, and only with d_dweight
  * rows 0 .. 2^30, cols 1 .. 2^20, leading dimensions any that hold the row.
  */
 typedef struct {
@@ -532,7 +537,8 @@ size_t dlc_norm_workspace_bytes(const dlc_norm_config* cfg /*HOST*/);
  *                     reads it
  *   d_norm    DEVICE  float[1] or NULL: gets n = sqrt(*d_sum)
  *   out       HOST    as `list`, the same types and sizes: gets every element times f = min(1, max_norm / n), rounded once; the
- *                     same tensors (with the same ld) for clipping in place, which writes nothing where f is 1
+ *                     same tensors (with the same ld) for clipping in place, which writes nothing where f is 1.  Each may be
+ *                     its own gradient, none may overlap another's
  *   max_norm          >= 0.  If n is not finite f is 1: the gradients stay as they are, and *d_norm tells
  *   d_work            as above, dlc_gradient_workspace_bytes
  * Returns DLC_ELIMIT for more than 2^40 elements in a tensor or 2^44 in all.

