@@ -98,8 +98,9 @@ __device__ __forceinline__ void mx_decode8(const MxWords<ELEM>& q, uint32_t byte
 
 // Stores a lane's eight columns col .. col + 7 of a row (0 behind the last) and, with three lanes beside it, their block's
 // scale.  All four lanes of a block come here; col runs to the end of the last group.  `shared` of f stand before col, and so
-// many columns are missing behind the last of f: the elements are moved as one word.
-template <int ELEM>
+// many columns are missing behind the last of f: the elements are moved as one word.  NARROW: rows of at most 128 columns,
+// whose 16 lanes write the whole group of scales, a word each block, as blocks 0 .. 3 are four bytes apart.
+template <int ELEM, bool NARROW>
 __device__ __forceinline__ void mx_store8(const float f[8], int shared, int64_t row, int col, int cols, int64_t rows, uint8_t* q, uint8_t* scale) {
     uint32_t top = 0;
 #pragma unroll
@@ -118,7 +119,8 @@ __device__ __forceinline__ void mx_store8(const float f[8], int shared, int64_t 
     }
     if ((col & (kMxBlock - 1)) == 0) {
         const int block = col / kMxBlock;
-        scale[((int64_t)(col / kMxGroup) * rows + row) * 16 + mx_scale_place(block)] = (uint8_t)byte;
+        if constexpr (NARROW) *reinterpret_cast<uint32_t*>(scale + row * 16 + mx_scale_place(block)) = byte;
+        else scale[((int64_t)(col / kMxGroup) * rows + row) * 16 + mx_scale_place(block)] = (uint8_t)byte;
     }
 }
 

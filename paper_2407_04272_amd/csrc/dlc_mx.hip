@@ -13,58 +13,73 @@ struct MxArgs {
     int32_t cols, groups;
 };
 
-constexpr int kTileRows = 16;  // rows of a work-group's tile: four a wavefront, whose loads are on their way together
+constexpr int kAhead = 4;  // rows of a lane, whose loads are on their way together
 
-// A tile is a group of 512 columns, eight a lane, of 16 rows: their scales are 256 bytes side by side.  Bound by memory: 16384 x
-// 4096 bf16 into 4 bits 31 us and back 26 (170 MB, 5.5 and 6.6 TB/s), 8192 x 8192 into 8 bits 32 and 30 (6.3 and 6.7 TB/s).
-// Rows that end inside an eight may be loaded element by element here: the row's last eight instead, as in the norm, took as
-// long (8192 x 4099 bf16 20.5 us; with 4096 columns 18.5).  WHOLE: rows end with a whole eight
-template <typename T, int ELEM, bool WHOLE>
+// A work-group's tile and a lane's part of it: L lanes have a row, or 512 columns of it; 64 / L rows side by side
+template <int L>
+struct Part {
+    static constexpr int ROWS = 4 * kAhead * 64 / L;  // of a tile
+    static constexpr int STEP = 64 / L;               // from a lane's row to its next
+    int64_t row;
+    int group, col;
+    __device__ __forceinline__ Part(int64_t tile, int groups) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int64_t band = L < 64 ? tile : tile / groups;
+        row = band * ROWS + wave * (kAhead * STEP) + lane / L;
+        group = L < 64 ? 0 : (int)(tile - band * groups);
+        col = group * kMxGroup + lane % L * 8;
+    }
+};
+
+// A tile is a group of 512 columns, eight a lane, of 16 rows: their scales are 256 bytes side by side.  Rows of at most 128
+// columns: 64 of them, on 16 lanes each (65536 x 128 bf16 into 8 bits 5.6 us, back 6.1; on 64 lanes 10.4 and 8.4).  Bound by
+// memory: 16384 x 4096 bf16 into 4 bits 31 us and back 26 (170 MB, 5.5 and 6.6 TB/s), 8192 x 8192 into 8 bits 32 and 30 (6.3 and
+// 6.7 TB/s).  Rows that end inside an eight may be loaded element by element here: the row's last eight instead, as in the norm,
+// took as long (8192 x 4099 bf16 20.5 us; with 4096 columns 18.5).  WHOLE: rows end with a whole eight
+template <typename T, int ELEM, bool WHOLE, int L>
 __global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {
-    constexpr int R = kTileRows / 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int64_t band = tile / a.groups, row0 = band * kTileRows + wave * R;
-        const int col = (int)(tile - band * a.groups) * kMxGroup + lane * 8;
-        Raw8<T> x[R];
+        const Part<L> at(tile, a.groups);
+        Raw8<T> x[kAhead];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const T* const p = static_cast<const T*>(a.x) + (row0 + i) * a.ld + col;
-            if constexpr (WHOLE) x[i].load_whole(p, row0 + i < a.rows && col < a.cols);
-            else x[i].load(p, row0 + i < a.rows ? a.cols - col : 0);
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = at.row + i * at.STEP;
+            const T* const p = static_cast<const T*>(a.x) + row * a.ld + at.col;
+            if constexpr (WHOLE) x[i].load_whole(p, row < a.rows && at.col < a.cols);
+            else x[i].load(p, row < a.rows ? a.cols - at.col : 0);
         }
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = at.row + i * at.STEP;
             float f[8];
             x[i].get(f);
-            if (row0 + i < a.rows) mx_store8<ELEM>(f, 0, row0 + i, col, a.cols, a.rows, a.q, a.scale);
+            if (row < a.rows) mx_store8<ELEM, (L < 64)>(f, 0, row, at.col, a.cols, a.rows, a.q, a.scale);
         }
     }
 }
 
-template <typename T, int ELEM, bool WHOLE>
+template <typename T, int ELEM, bool WHOLE, int L>
 __global__ __launch_bounds__(256) void k_mx_dequantize(const MxArgs a) {
-    constexpr int R = kTileRows / 4;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t row_bytes = mx_row_bytes(a.cols, ELEM);
     for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int64_t band = tile / a.groups, row0 = band * kTileRows + wave * R;
-        const int group = (int)(tile - band * a.groups), col = group * kMxGroup + lane * 8, cnt = a.cols - col;
+        const Part<L> at(tile, a.groups);
+        const int cnt = a.cols - at.col;
         if (cnt <= 0) continue;
-        MxWords<ELEM> w[R];
-        uint32_t byte[R];
+        MxWords<ELEM> w[kAhead];
+        uint32_t byte[kAhead];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t row = row0 + i < a.rows ? row0 + i : a.rows - 1;
-            w[i] = *reinterpret_cast<const MxWords<ELEM>*>(a.q + row * row_bytes + col * ELEM / 8);
-            byte[i] = a.scale[((int64_t)group * a.rows + row) * 16 + mx_scale_place(lane >> 2)];
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = min(at.row + i * at.STEP, a.rows - 1);
+            w[i] = *reinterpret_cast<const MxWords<ELEM>*>(a.q + row * row_bytes + at.col * ELEM / 8);
+            byte[i] = a.scale[((int64_t)at.group * a.rows + row) * 16 + mx_scale_place(at.col / kMxBlock)];
         }
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if (row0 + i >= a.rows) continue;
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t row = at.row + i * at.STEP;
+            if (row >= a.rows) continue;
             float f[8];
             mx_decode8<ELEM>(w[i], byte[i], f);
-            store8(static_cast<T*>(const_cast<void*>(a.x)) + (row0 + i) * a.ld + col, WHOLE ? 8 : cnt, f);
+            store8(static_cast<T*>(const_cast<void*>(a.x)) + row * a.ld + at.col, WHOLE ? 8 : cnt, f);
         }
     }
 }
@@ -88,18 +103,24 @@ bool good_mx(const dlc_mx_config* c) {
     return true;
 }
 
-template <typename T, int ELEM, bool WHOLE>
-void convert(const MxArgs& a, bool back, hipStream_t st) {
+template <typename T, int ELEM, bool WHOLE, int L>
+void convert(MxArgs a, bool back, hipStream_t st) {
+    a.tiles = div_up(a.rows, Part<L>::ROWS) * a.groups;
     const dim3 grid((unsigned)(a.tiles < (int64_t(1) << 20) ? a.tiles : int64_t(1) << 20)), block(256);
-    if (back) k_mx_dequantize<T, ELEM, WHOLE><<<grid, block, 0, st>>>(a);
-    else k_mx_quantize<T, ELEM, WHOLE><<<grid, block, 0, st>>>(a);
+    if (back) k_mx_dequantize<T, ELEM, WHOLE, L><<<grid, block, 0, st>>>(a);
+    else k_mx_quantize<T, ELEM, WHOLE, L><<<grid, block, 0, st>>>(a);
+}
+
+template <typename T, int ELEM>
+void convert(const MxArgs& a, bool back, hipStream_t st) {
+    const bool whole = a.cols % 8 == 0;
+    if (a.cols <= kMxFill) whole ? convert<T, ELEM, true, 16>(a, back, st) : convert<T, ELEM, false, 16>(a, back, st);
+    else whole ? convert<T, ELEM, true, 64>(a, back, st) : convert<T, ELEM, false, 64>(a, back, st);
 }
 
 template <typename T>
 void convert(const MxArgs& a, int elem, bool back, hipStream_t st) {
-    const bool whole = a.cols % 8 == 0;
-    if (elem == DLC_MX_E4M3) whole ? convert<T, 8, true>(a, back, st) : convert<T, 8, false>(a, back, st);
-    else whole ? convert<T, 4, true>(a, back, st) : convert<T, 4, false>(a, back, st);
+    elem == DLC_MX_E4M3 ? convert<T, 8>(a, back, st) : convert<T, 4>(a, back, st);
 }
 
 int convert_any(const dlc_mx_config* c, const void* x, const void* q, const void* scale, bool back, void* stream) {
@@ -114,7 +135,6 @@ int convert_any(const dlc_mx_config* c, const void* x, const void* q, const void
     a.ld = back ? c->ld_y : c->ld_x;
     if (a.ld == 0) a.ld = c->cols;
     a.groups = (int)mx_groups(c->cols);
-    a.tiles = div_up(c->rows, kTileRows) * a.groups;
     hipStream_t st = (hipStream_t)stream;
     switch (c->dtype) {
         case DLC_F32: convert<float>(a, c->elem, back, st); break;

@@ -105,14 +105,14 @@ __device__ __forceinline__ void load_sum(const NormArgs& a, int64_t row, int col
     }
 }
 
-template <typename T, bool MX, int E>
+template <typename T, bool MX, int E, bool NARROW = false>
 __device__ __forceinline__ void put_row(const NormArgs& a, int64_t row, int col, float r, float s[8], const float w[8]) {
     if (a.sum) put<E, T>(a.sum, row, a.ld_sum, col, a.cols, s);
     if (MX && col >= a.cols) r = 0.0f;  // (a row's NaN stays in its columns)
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = s[i] * r * w[i];
     if (a.y) put<E, T>(a.y, row, a.ld_y, col, a.cols, s);
-    if constexpr (MX) mx_store8<8>(s, shared_of<E>(col, a.cols), row, col, a.cols, a.rows, a.q, a.scale);
+    if constexpr (MX) mx_store8<8, NARROW>(s, shared_of<E>(col, a.cols), row, col, a.cols, a.rows, a.q, a.scale);
 }
 
 template <typename T, int P, int U, bool MX, int E>
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
     __shared__ float red[2][P > 64 ? P / 64 : 1][1];
     const int t = threadIdx.x % P, team = threadIdx.x / P;
     const int64_t first = ((int64_t)blockIdx.x * kTeams<P> + team) * a.per, last = min(a.rows, first + a.per);
-    const int end = MX ? (int)mx_groups(a.cols) * kMxGroup : a.cols;
+    const int end = !MX ? a.cols : P == 16 ? kMxFill : (int)mx_groups(a.cols) * kMxGroup;
     int odd = 0;
     for (int64_t row = first; row < last; ++row, odd ^= 1) {
         float s[U][8], sq[1] = {0.0f};
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void k_norm(const NormArgs a) {
             if (!a.weight)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] = 1.0f;
-            if (col < end) put_row<T, MX, E>(a, row, col, r, s[u], g);
+            if (col < end) put_row<T, MX, E, P == 16>(a, row, col, r, s[u], g);
         }
     }
 }
@@ -345,15 +345,13 @@ template <typename T, int P, int U>
 void forward(const NormArgs& a, bool mx, hipStream_t st) {
     const dim3 block(P < 256 ? 256 : P), grid((unsigned)div_up(a.rows, (int64_t)kTeams<P> * a.per));
     const bool whole = a.cols % 8 == 0;
-    if constexpr (P >= 64) {
-        if constexpr (P == 64 && U == 1)
-            if (mx && a.cols < 8) return k_norm<T, P, U, true, kShort><<<grid, block, 0, st>>>(a);
-        if (mx && whole) return k_norm<T, P, U, true, kWhole><<<grid, block, 0, st>>>(a);
-        if (mx) return k_norm<T, P, U, true, kBack><<<grid, block, 0, st>>>(a);
-    } else {
+    if constexpr (P < 64) {
+        if (a.cols < 8 && mx) return k_norm<T, P, U, true, kShort><<<grid, block, 0, st>>>(a);
         if (a.cols < 8) return k_norm<T, P, U, false, kShort><<<grid, block, 0, st>>>(a);
     }
-    if (whole) k_norm<T, P, U, false, kWhole><<<grid, block, 0, st>>>(a);
+    if (mx && whole) k_norm<T, P, U, true, kWhole><<<grid, block, 0, st>>>(a);
+    else if (mx) k_norm<T, P, U, true, kBack><<<grid, block, 0, st>>>(a);
+    else if (whole) k_norm<T, P, U, false, kWhole><<<grid, block, 0, st>>>(a);
     else k_norm<T, P, U, false, kBack><<<grid, block, 0, st>>>(a);
 }
 
@@ -368,9 +366,10 @@ void backward(const NormArgs& a, int64_t groups, hipStream_t st) {
 
 // Teams for a row's length.  Forward, 16384 x 8192 bf16 into 8 bits: 512 lanes of two eights 164 us, 256 of four the same,
 // 1024 of one 209; several rows a team one after the other 179 (4) and 191 (8).  8192 x 8195 bf16: 1024 lanes 146 us, 768 120.
+// 65536 x 128 bf16 into 8 bits: 16 lanes 11 us, 64 (the group of scales has 512 columns) 27.
 template <typename T>
 int launch_forward(NormArgs a, bool mx, hipStream_t st) {
-    const int64_t wide = mx ? mx_groups(a.cols) * kMxGroup : a.cols;
+    const int64_t wide = mx && a.cols > kMxFill ? mx_groups(a.cols) * kMxGroup : a.cols;
     a.per = (int)div_up(a.rows, int64_t(1) << 20);  // (a launch has fewer than 2^32 threads)
     if (wide <= 128) forward<T, 16, 1>(a, mx, st);
     else if (wide <= 512) forward<T, 64, 1>(a, mx, st);

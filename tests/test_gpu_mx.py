@@ -305,3 +305,15 @@ def test_quantise_rows_that_end_inside_an_eight(rows, cols, dtype, bits):
         t = t.clone()
         t[at % rows, at] = float("nan") if at % 2 else 1000.0
         _same(*_quantised(t, bits, dtype), *quantise(t.double().cpu().numpy(), bits), f"{rows}x{cols} {bits} {dtype} {at}")
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,ld", [(63, 8, 0), (64, 127, 0), (65, 128, 0), (130, 100, 0), (200, 5, 0), (300, 64, 71), (129, 33, 40), (4100, 128, 0)])
+def test_narrow_rows(rows, cols, ld, dtype, bits):
+    """At most 128 columns: several rows a wavefront, and all 16 bytes of a row's scales from a quarter of it."""
+    x, t = _matrix(rows, cols, dtype, 61, "wide")
+    if ld:
+        t = Guarded(rows, cols, dtype, ld, 1).set(t).view
+    _same(*_quantised(t, bits, dtype, ld), *quantise(x, bits), f"{rows}x{cols} {bits} {dtype}")
+    test_back(rows, cols, ld, dtype, bits)
