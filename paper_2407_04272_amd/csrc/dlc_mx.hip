@@ -172,14 +172,15 @@ struct Plan {
 };
 
 // What 256 k values cost with 1 and 2 work-groups on a compute unit, in us, what a work-group costs besides, and every
-// further one, measured on full and on half empty cards (0: no second work-group fits): E2M1, E4M3, E4M3 with results in fp32.
-// 64 x 128 is the best until its tiles no longer fit the card at once (256 x 2048 x 2048 of 4 bits 8.4 us for 11.4 and 21.5 of
-// the other two; 2048 x 2048 x 2048 of 8 bits 18.4, 15.7 and 29.2), 256 x 256 where there are many (2048 x 8192 x 8192 of 4
-// bits 125, 137 and 70 us).
+// further one, measured on full cards (0: no second work-group fits; up to half of a card, whose work-groups have more of the
+// caches and the power, kHalf of it): E2M1, E4M3, E4M3 with results in fp32.  64 x 128 is the best until its tiles no longer fit
+// the card at once (1024 x 2048 x 2048 of 4 bits 8.1 us for 10.3 and 22; 2048 x 2048 x 2048 12.3, 11.1 and 22.7, of 8 bits 17.3,
+// 13.9 and 29.4), 256 x 256 where there are many (2048 x 8192 x 8192 of 4 bits 120, 98 and 66 us).
 struct TileCost { double tile[2], first, further; };
-constexpr TileCost kCost[3][3] = {{{{1.75, 0}, 12.0, 6.0}, {{0.88, 0}, 5.0, 3.5}, {{0.62, 0.93}, 4.0, 2.8}},
-                                  {{{2.5, 0}, 13.0, 6.0}, {{1.22, 0}, 5.5, 3.5}, {{0.8, 0}, 4.2, 2.4}},
+constexpr TileCost kCost[3][3] = {{{{1.66, 0}, 12.8, 11.0}, {{0.64, 0}, 5.8, 3.7}, {{0.46, 0.86}, 4.4, 2.0}},
+                                  {{{2.42, 0}, 13.6, 8.3}, {{0.89, 0}, 6.6, 4.2}, {{0.6, 0}, 4.6, 2.6}},
                                   {{}, {{2.2, 0}, 5.5, 3.5}, {{1.45, 0}, 4.2, 2.4}}};
+constexpr double kHalf = 0.85;
 constexpr int kUnits = 256;  // compute units
 constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
@@ -205,8 +206,8 @@ Plan plan_linear(const Shape& s) {
             const int64_t per = div_up(groups, cut), split = div_up(groups, per), wgs = tiles * split;
             const int64_t full = wgs / (kUnits * fit), rest = wgs % (kUnits * fit);
             double t = (double)full * (2.0 * (double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
-            if (rest) t += 2.0 * (double)per * c.tile[(rest - 1) / kUnits] + c.further;
-            if (split > 1) t += 3.0 + (double)split * (double)s.M * (double)s.N * 8.0 / 8.0e6;
+            if (rest) t += 2.0 * (double)per * c.tile[(rest - 1) / kUnits] * (wgs <= kUnits / 2 ? kHalf : 1.0) + c.further;
+            if (split > 1) t += 3.8 + (double)split * (double)s.M * (double)s.N * 8.0 / 6.2e6;  // (the second launch, the sums out and in)
             if (t < least) {
                 least = t;
                 best.tile = tile;

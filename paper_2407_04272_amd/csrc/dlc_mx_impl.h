@@ -163,10 +163,90 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArg
 }
 
 // ---- tiles of 128 x 128 and 64 x 128 ----
-// Four wavefronts, each with a quarter; tiles of 256 k values in three slots, two on their way while one is multiplied, one
-// barrier a tile.  For results that 256 x 256 tiles would leave most of the card without: 777 x 515 -> 1023, E4M3 rows, 64 x 128:
-// 8.5 us of the kernel, two groups of k values whose operands come cold from memory, and an epilogue with bias, gelu and
-// residual.  Two work-groups of 64 x 128 and 4 bits fit a compute unit (72 KB of LDS each).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+#define DLC_MX(OP, BL, ACC, B, A, SB, SA) "v_mfma_scale_f32_16x16x128_f8f6f4 %" #ACC ", %" #B ", %" #A ", %" #ACC ", %" #SB ", %" #SA " " OP " cbsz:4 blgp:" BL "\n\t"
+#define DLC_MX_BYTE0 "op_sel_hi:[0,0,0]"
+#define DLC_MX_BYTE1 "op_sel:[1,1,0] op_sel_hi:[0,0,0]"
+#define DLC_MX_BYTE2 "op_sel_hi:[1,1,0]"
+#define DLC_MX_BYTE3 "op_sel:[1,1,0] op_sel_hi:[1,1,0]"
+#define DLC_MX_PAIR4(OP, BL) \
+    asm volatile("s_nop 1\n\t" \
+    DLC_MX(OP, BL, 4, 14, 12, 20, 18) "ds_read_b128 %0, %24 offset:%28\n\t" DLC_MX(OP, BL, 5, 15, 12, 21, 18) "ds_read_b128 %1, %25 offset:%29\n\t" \
+    DLC_MX(OP, BL, 6, 16, 12, 22, 18) "ds_read_b128 %2, %26 offset:%30\n\t" DLC_MX(OP, BL, 7, 17, 12, 23, 18) "ds_read_b128 %3, %27 offset:%31\n\t" \
+    DLC_MX(OP, BL, 8, 14, 13, 20, 19) DLC_MX(OP, BL, 9, 15, 13, 21, 19) \
+    DLC_MX(OP, BL, 10, 16, 13, 22, 19) DLC_MX(OP, BL, 11, 17, 13, 23, 19) \
+    "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(next[0]), "=&v"(next[1]), "=&v"(next[2]), "=&v"(next[3]), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(sa0), "v"(sa1), "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), \
+      "v"(from[Next::source(0)]), "v"(from[Next::source(1)]), "v"(from[Next::source(2)]), "v"(from[Next::source(3)]), \
+      "i"(Next::offset(0)), "i"(Next::offset(1)), "i"(Next::offset(2)), "i"(Next::offset(3)) \
+    : "memory")
+#define DLC_MX_PAIR6(OP, BL) \
+    asm volatile("s_nop 1\n\t" \
+    DLC_MX(OP, BL, 6, 16, 14, 22, 20) "ds_read_b128 %0, %26 offset:%32\n\t" DLC_MX(OP, BL, 7, 17, 14, 23, 20) "ds_read_b128 %1, %27 offset:%33\n\t" \
+    DLC_MX(OP, BL, 8, 18, 14, 24, 20) "ds_read_b128 %2, %28 offset:%34\n\t" DLC_MX(OP, BL, 9, 19, 14, 25, 20) "ds_read_b128 %3, %29 offset:%35\n\t" \
+    DLC_MX(OP, BL, 10, 16, 15, 22, 21) "ds_read_b128 %4, %30 offset:%36\n\t" DLC_MX(OP, BL, 11, 17, 15, 23, 21) "ds_read_b128 %5, %31 offset:%37\n\t" \
+    DLC_MX(OP, BL, 12, 18, 15, 24, 21) DLC_MX(OP, BL, 13, 19, 15, 25, 21) \
+    "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(next[0]), "=&v"(next[1]), "=&v"(next[2]), "=&v"(next[3]), "=&v"(next[4]), "=&v"(next[5]), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(sa0), "v"(sa1), "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), \
+      "v"(from[Next::source(0)]), "v"(from[Next::source(1)]), "v"(from[Next::source(2)]), "v"(from[Next::source(3)]), "v"(from[Next::source(4)]), "v"(from[Next::source(5)]), \
+      "i"(Next::offset(0)), "i"(Next::offset(1)), "i"(Next::offset(2)), "i"(Next::offset(3)), "i"(Next::offset(4)), "i"(Next::offset(5)) \
+    : "memory")
+#define DLC_MX_PAIR8(OP, BL) \
+    asm volatile("s_nop 1\n\t" \
+    DLC_MX(OP, BL, 8, 18, 16, 24, 22) "ds_read_b128 %0, %28 offset:%36\n\t" DLC_MX(OP, BL, 9, 19, 16, 25, 22) "ds_read_b128 %1, %29 offset:%37\n\t" \
+    DLC_MX(OP, BL, 10, 20, 16, 26, 22) "ds_read_b128 %2, %30 offset:%38\n\t" DLC_MX(OP, BL, 11, 21, 16, 27, 22) "ds_read_b128 %3, %31 offset:%39\n\t" \
+    DLC_MX(OP, BL, 12, 18, 17, 24, 23) "ds_read_b128 %4, %32 offset:%40\n\t" DLC_MX(OP, BL, 13, 19, 17, 25, 23) "ds_read_b128 %5, %33 offset:%41\n\t" \
+    DLC_MX(OP, BL, 14, 20, 17, 26, 23) "ds_read_b128 %6, %34 offset:%42\n\t" DLC_MX(OP, BL, 15, 21, 17, 27, 23) "ds_read_b128 %7, %35 offset:%43\n\t" \
+    "s_waitcnt lgkmcnt(0)" \
+    : "=&v"(next[0]), "=&v"(next[1]), "=&v"(next[2]), "=&v"(next[3]), "=&v"(next[4]), "=&v"(next[5]), "=&v"(next[6]), "=&v"(next[7]), \
+      "+a"(acc0[0]), "+a"(acc0[1]), "+a"(acc0[2]), "+a"(acc0[3]), "+a"(acc1[0]), "+a"(acc1[1]), "+a"(acc1[2]), "+a"(acc1[3]) \
+    : "v"(a0), "v"(a1), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "v"(sa0), "v"(sa1), "v"(sb[0]), "v"(sb[1]), "v"(sb[2]), "v"(sb[3]), \
+      "v"(from[Next::source(0)]), "v"(from[Next::source(1)]), "v"(from[Next::source(2)]), "v"(from[Next::source(3)]), "v"(from[Next::source(4)]), "v"(from[Next::source(5)]), "v"(from[Next::source(6)]), "v"(from[Next::source(7)]), \
+      "i"(Next::offset(0)), "i"(Next::offset(1)), "i"(Next::offset(2)), "i"(Next::offset(3)), "i"(Next::offset(4)), "i"(Next::offset(5)), "i"(Next::offset(6)), "i"(Next::offset(7)) \
+    : "memory")
+
+// A step's fragments, in the order of their reads: four of w, those of x (E4M3: two of each block).  FIRST: of some of them
+template <int ELEM, int FIRST, int STEP>
+struct MxNext {
+    static constexpr int place(int i) { return FIRST + i - 4; }                                                    // among x's
+    static constexpr int source(int i) { return place(i) < 0 ? 0 : ELEM == 4 ? 1 : 1 + place(i) % 2; }             // of {w, x, x's second chunk}
+    static constexpr int offset(int i) { return place(i) < 0 ? (FIRST + i) * STEP : place(i) * 4 / ELEM * STEP; }  // blocks STEP bytes apart
+};
+
+// Rows of blocks acc0 and acc1 += a0 and a1 times b, with byte S of the scales, while R fragments are read
+template <int ELEM, int S, int R, typename Next, typename A>
+__device__ __forceinline__ void mx_pair(f32x4* acc0, f32x4* acc1, const A& a0, const A& a1, const u32x4_t* b, uint32_t sa0, uint32_t sa1,
+                                        const uint32_t* sb, u32x4_t* next, const uint32_t (&from)[3]) {
+#define DLC_MX_PAIR(OP) \
+    if constexpr (R == 4) DLC_MX_PAIR4(OP, "4"); \
+    else if constexpr (R == 6 && ELEM == 4) DLC_MX_PAIR6(OP, "4"); \
+    else if constexpr (R == 6) DLC_MX_PAIR6(OP, "0"); \
+    else DLC_MX_PAIR8(OP, "0")
+    static_assert(R == 4 ? ELEM == 4 : R == 6 || (R == 8 && ELEM == 8), "reads of a pair");
+    if constexpr (S == 0) { DLC_MX_PAIR(DLC_MX_BYTE0); }
+    else if constexpr (S == 1) { DLC_MX_PAIR(DLC_MX_BYTE1); }
+    else if constexpr (S == 2) { DLC_MX_PAIR(DLC_MX_BYTE2); }
+    else { DLC_MX_PAIR(DLC_MX_BYTE3); }
+#undef DLC_MX_PAIR
+}
+#undef DLC_MX_PAIR4
+#undef DLC_MX_PAIR6
+#undef DLC_MX_PAIR8
+
+// Four wavefronts, each with a quarter; tiles of 256 k values in three slots.  While a step (half a tile) is multiplied, the
+// next one's fragments are read from LDS, between the products of one block of assembly; between a tile's two steps stands
+// the only barrier, behind which the third tile from there is on its way to this one's place.  Where products are exact the
+// compiler has the inner loop, and reading and multiplying take turns.
+// For results that 256 x 256 tiles would leave most of the card without: 512 x 8192 -> 2048 of 4 bits 17 us (23 with reads and
+// products in turn), 1024 x 8192 18 (27), 2048 x 8192 25 (36); 777 x 515 -> 1023, E4M3 rows, bias, gelu and residual 8.5 us.
+// Bound by the way from L2 to LDS (128 x 128: 32 KB a tile on every unit in 0.64 us, 13 TB/s) and at small sizes by the start and
+// the epilogue, 4.4 us; more slots were no faster.  Two work-groups of 64 x 128 and 4 bits fit a compute unit.  A group's scales are asked for two tiles ahead, for one tile ahead cost a
+// fifth (33 us for 28), and what is left of their cost is a tenth.
 template <int ELEM, int BM>
 constexpr int mx_tile_lds() {
     const int ring = 3 * (BM * 32 * ELEM + 128 * 128), out = BM / 2 * 256 * 4;
@@ -199,70 +279,140 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
         ob.fetch(to + XT * OpA::BYTES, tid);
     };
     // a lane's scales of a group, whose rows past the last are the last's
-    uint32_t px[MI], pw[NJ], sx[MI], sw[NJ];
+    uint32_t px[MI], pw[NJ];
+    struct { uint32_t x[MI], w[NJ]; } sc[2];
 #pragma unroll
     for (int i = 0; i < MI; ++i) px[i] = (uint32_t)(min(m0 + wm + i * 16 + j, ga.M - 1) - m0) * 16 + g * 4;
 #pragma unroll
     for (int n = 0; n < NJ; ++n) pw[n] = (uint32_t)(min(n0 + wn + n * 16 + j, ga.N - 1) - n0) * 16 + g * 4;
     const uint8_t* bx = mx.xs + ((int64_t)(k0 / kMxGroup) * ga.M + m0) * 16;
     const uint8_t* bw = mx.ws + ((int64_t)(k0 / kMxGroup) * ga.N + n0) * 16;
-    const auto scales = [&](int k) {
-        if (k >= k1) return;
+    const auto scales = [&](auto& to, int k) {  // of the group at k, or the last once more: always as many loads
+        if (k > k0 && k < k1) {
+            bx += (int64_t)ga.M * 16;
+            bw += (int64_t)ga.N * 16;
+        }
 #pragma unroll
-        for (int i = 0; i < MI; ++i) sx[i] = *reinterpret_cast<const uint32_t*>(bx + px[i]);
+        for (int i = 0; i < MI; ++i) to.x[i] = *reinterpret_cast<const uint32_t*>(bx + px[i]);
 #pragma unroll
-        for (int n = 0; n < NJ; ++n) sw[n] = *reinterpret_cast<const uint32_t*>(bw + pw[n]);
-        bx += (int64_t)ga.M * 16;
-        bw += (int64_t)ga.N * 16;
+        for (int n = 0; n < NJ; ++n) to.w[n] = *reinterpret_cast<const uint32_t*>(bw + pw[n]);
     };
     f32x4 acc[MI][NJ];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int n = 0; n < NJ; ++n) acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    scales(k0);
-    fetch(0);
-    fetch(1);
     const uint32_t at = (uint32_t)(uintptr_t)(const lds_char*)lds;
     const int key = (j >> 1) & 7;
     const uint32_t c0 = (uint32_t)((g ^ key) << 4), c1 = c0 ^ 64u;
     const uint32_t d0 = EXACT ? (uint32_t)(((2 * g) ^ key) << 4) : c0, d1 = EXACT ? (uint32_t)(((2 * g + 1) ^ key) << 4) : c1;
     const uint32_t ra = at + (uint32_t)((wm + j) * 128), rb = at + (uint32_t)(XT * OpA::BYTES + (wn + j) * 128);
-    int slot = 0;
-    for (int k = k0; k < k1; k += kMxGroup) {
-        uint32_t tx[MI], tw[NJ];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) tx[i] = sx[i];
-#pragma unroll
-        for (int n = 0; n < NJ; ++n) tw[n] = sw[n];
-        const auto half = [&](auto which) {
-            constexpr int H = decltype(which)::value;
-            // this tile has come; all have read the one before, whose place the tile after the next takes
-            wait_loads<LOADS>();
-            bare_barrier();
-            const uint32_t s = (uint32_t)(slot * SLOT);
-            u32x4_t fw[2 * NJ], fx[XT][2 * MI];
-            read_frags<NJ, STEP>(fw, rb + s + c0, rb + s + c1);
-#pragma unroll
-            for (int t = 0; t < XT; ++t) read_frags<MI, STEP>(fx[t], ra + s + t * OpA::BYTES + d0, ra + s + t * OpA::BYTES + d1);
-            fetch(slot == 0 ? 2 : slot - 1);
-            slot = slot == 2 ? 0 : slot + 1;
-            if constexpr (H == 0) scales(k + kMxGroup);
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int n = 0; n < NJ; ++n) {
-                    if constexpr (ELEM == 4) {
-                        acc[i][n] = mx_mma<4, false, 2 * H>(fw[2 * n], fx[0][2 * i], fx[0][2 * i], tw[n], tx[i], acc[i][n]);
-                        acc[i][n] = mx_mma<4, false, 2 * H + 1>(fw[2 * n + 1], fx[0][2 * i + 1], fx[0][2 * i + 1], tw[n], tx[i], acc[i][n]);
-                    } else {
-                        acc[i][n] = mx_mma<8, EXACT, 2 * H>(fw[2 * n], fx[0][2 * i], fx[0][2 * i + 1], tw[n], tx[i], acc[i][n]);
-                        acc[i][n] = mx_mma<8, EXACT, 2 * H + 1>(fw[2 * n + 1], fx[1][2 * i], fx[1][2 * i + 1], tw[n], tx[i], acc[i][n]);
-                    }
+    if constexpr (!EXACT) {
+        struct { u32x4_t f[NJ + XT * MI]; } f[2];
+        constexpr int WORDS = MI + NJ;  // loads of scales
+        const int tiles = (k1 - k0 + 255) / 256;
+        scales(sc[0], k0);
+        fetch(0);
+        fetch(1);
+        fetch(2);
+        scales(sc[1], k0 + kMxGroup);
+        wait_loads<2 * LOADS + WORDS>();
+        bare_barrier();
+        read_rows<NJ, STEP, 0>(f[0].f, rb + c0);
+        if constexpr (ELEM == 4) read_rows<MI, STEP, 0>(f[0].f + NJ, ra + c0);
+        else read_halves<MI, STEP>(f[0].f + NJ, ra + d0, ra + d1);
+        settle(acc);
+        // a step's products with c while n is read; `first` and `second` behind their halves
+        const auto multiply = [&](auto step, const auto& sc, const auto& c, auto& n, const uint32_t (&from)[3], auto first, auto second) {
+            constexpr int S = decltype(step)::value;
+            const auto a = [&](int i) {
+                if constexpr (ELEM == 4) return c.f[NJ + i];
+                else {
+                    const u32x4_t &x = c.f[NJ + 2 * i], &y = c.f[NJ + 2 * i + 1];
+                    return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
                 }
+            };
+            constexpr int R = (NJ + XT * MI) * 2 / MI;
+            mx_pair<ELEM, S, R, MxNext<ELEM, 0, STEP>>(acc[0], acc[1], a(0), a(1), c.f, sc.x[0], sc.x[1], sc.w, n.f, from);
+            first();
+            if constexpr (MI == 4) mx_pair<ELEM, S, R, MxNext<ELEM, R, STEP>>(acc[2], acc[3], a(2), a(3), c.f, sc.x[2], sc.x[3], sc.w, n.f + R, from);
+            second();
         };
-        half(std::integral_constant<int, 0>{});
-        if (k + 256 < k1) half(std::integral_constant<int, 1>{});
+        uint32_t s = 0;  // the current tile's slot, in bytes
+        const auto tile = [&](auto s0, auto s1, const auto& sc, auto last) {
+            const uint32_t now = s;
+            s = s == 2 * SLOT ? 0 : s + SLOT;
+            const uint32_t mid[3] = {rb + now + c1, ra + now + (ELEM == 8 ? OpA::BYTES + d0 : c1), ra + now + OpA::BYTES + d1};
+            const uint32_t end[3] = {rb + s + c0, ra + s + (ELEM == 8 ? d0 : c0), ra + s + d1};
+            multiply(s0, sc, f[0], f[1], mid, [] {}, [] {});
+            // the next tile has come, the one after it and the next scales but one need not have; all have read this one, whose
+            // place the third from here takes
+            wait_loads<LOADS + WORDS>();
+            bare_barrier();
+            char* const to = lds + now;
+            multiply(s1, sc, f[1], f[0], end,
+                     [&] {
+#pragma unroll
+                         for (int t = 0; t < XT; ++t) oa.fetch(to + t * OpA::BYTES, tid);
+                     },
+                     [&] {
+                         ob.fetch(to + XT * OpA::BYTES, tid);
+                         last();
+                     });
+        };
+        // Two groups in turn, each with its scales in registers of its own, which are asked for two tiles before their first use.
+        // (One path through the loop: the compiler waits for what any path to a use may have left on its way.)
+        constexpr std::integral_constant<int, 0> s0{};
+        constexpr std::integral_constant<int, 1> s1{};
+        constexpr std::integral_constant<int, 2> s2{};
+        constexpr std::integral_constant<int, 3> s3{};
+        int t = 0;
+        for (; t + 4 <= tiles; t += 4) {
+            const int k = k0 + t * 256 + 2 * kMxGroup;
+            tile(s0, s1, sc[0], [] {});
+            tile(s2, s3, sc[0], [&] { scales(sc[0], k); });
+            tile(s0, s1, sc[1], [] {});
+            tile(s2, s3, sc[1], [&] { scales(sc[1], k + kMxGroup); });
+        }
+        if (t < tiles) tile(s0, s1, sc[0], [] {});
+        if (t + 1 < tiles) tile(s2, s3, sc[0], [] {});
+        if (t + 2 < tiles) tile(s0, s1, sc[1], [] {});
+        settle(acc);
+    } else {
+        int slot = 0;
+        scales(sc[0], k0);
+        fetch(0);
+        fetch(1);
+        for (int k = k0; k < k1; k += kMxGroup) {
+            uint32_t tx[MI], tw[NJ];
+#pragma unroll
+            for (int i = 0; i < MI; ++i) tx[i] = sc[0].x[i];
+#pragma unroll
+            for (int n = 0; n < NJ; ++n) tw[n] = sc[0].w[n];
+            const auto half = [&](auto which) {
+                constexpr int H = decltype(which)::value;
+                // this tile has come; all have read the one before, whose place the tile after the next takes
+                wait_loads<LOADS>();
+                bare_barrier();
+                const uint32_t s = (uint32_t)(slot * SLOT);
+                u32x4_t fw[2 * NJ], fx[XT][2 * MI];
+                read_frags<NJ, STEP>(fw, rb + s + c0, rb + s + c1);
+#pragma unroll
+                for (int t = 0; t < XT; ++t) read_frags<MI, STEP>(fx[t], ra + s + t * OpA::BYTES + d0, ra + s + t * OpA::BYTES + d1);
+                fetch(slot == 0 ? 2 : slot - 1);
+                slot = slot == 2 ? 0 : slot + 1;
+                if constexpr (H == 0) scales(sc[0], k + kMxGroup);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int n = 0; n < NJ; ++n) {
+                        acc[i][n] = mx_mma<8, true, 2 * H>(fw[2 * n], fx[0][2 * i], fx[0][2 * i + 1], tw[n], tx[i], acc[i][n]);
+                        acc[i][n] = mx_mma<8, true, 2 * H + 1>(fw[2 * n + 1], fx[1][2 * i], fx[1][2 * i + 1], tw[n], tx[i], acc[i][n]);
+                    }
+            };
+            half(std::integral_constant<int, 0>{});
+            if (k + 256 < k1) half(std::integral_constant<int, 1>{});
+        }
     }
     wait_loads<0>();  // (tiles past the last may still be on their way)
     __syncthreads();
@@ -278,13 +428,10 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
 // compiler's and wait_loads'.
 // Bound by the matrix cores and the card's power: with its scales the instruction takes 24 cycles (without, 16; one of 32 x 32 x
 // 64, which does twice as much, 33; with an E4M3 operand 32), and 16384 x 8192 -> 4096 with random elements 282 us, 3900
-// TFLOP/s, at 1.9-2.1 GHz; the bare instruction on the same elements reaches 5640 on the whole card.  E4M3 rows 370 us, 2970
+// TFLOP/s (265-282), at 1.9-2.1 GHz; the bare instruction on the same elements reaches 5640 on the whole card.  E4M3 rows 370 us, 2970
 // TFLOP/s.  Measured and left: blocks of 32 x 32 (280 us where this took 254), work-groups that stay and ask for the next
 // tile's operands during the epilogue (the same), results stored from the registers without LDS (265-286 for 254), no masks
 // on the loads (268 for 270).
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-#define DLC_MX(OP, BL, ACC, B, A, SB, SA) "v_mfma_scale_f32_16x16x128_f8f6f4 %" #ACC ", %" #B ", %" #A ", %" #ACC ", %" #SB ", %" #SA " " OP " cbsz:4 blgp:" BL "\n\t"
 #define DLC_MX_MOST4(OP, BL) \
     asm volatile("s_nop 1\n\t" \
     DLC_MX(OP, BL, 4, 18, 16, 28, 26) "ds_read_b128 %0, %36 offset:%37\n\t" DLC_MX(OP, BL, 5, 19, 16, 29, 26) "ds_read_b128 %1, %36 offset:%38\n\t" \
@@ -318,11 +465,6 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
     : "+a"(acc1[4]), "+a"(acc1[5]), "+a"(acc1[6]), "+a"(acc1[7]) \
     : "v"(a1), "v"(b[4]), "v"(b[5]), "v"(b[6]), "v"(b[7]), "v"(sa1), "v"(sb[4]), "v"(sb[5]), "v"(sb[6]), "v"(sb[7]) \
     : "memory")
-#define DLC_MX_BYTE0 "op_sel_hi:[0,0,0]"
-#define DLC_MX_BYTE1 "op_sel:[1,1,0] op_sel_hi:[0,0,0]"
-#define DLC_MX_BYTE2 "op_sel_hi:[1,1,0]"
-#define DLC_MX_BYTE3 "op_sel:[1,1,0] op_sel_hi:[1,1,0]"
-
 // Rows of blocks acc0 and acc1 += a0 and a1 times b, with byte S of the scales: twelve products and four reads, STEP bytes
 // apart, `then` (one load), the other four products
 template <int S, int OFF, int STEP, typename F>
@@ -388,9 +530,13 @@ struct Scales {
         base += step;
         left -= step;
     }
+    // (to the compiler all of them are used, and none of the loads that waits count can go)
     __device__ __forceinline__ void turn() {
 #pragma unroll
-        for (int i = 0; i < N; ++i) now[i] = next[i];
+        for (int i = 0; i < N; ++i) {
+            now[i] = next[i];
+            asm volatile("" : "+v"(now[i]));
+        }
     }
 };
 
@@ -468,8 +614,9 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
             oa.mask();
             multiply(first, f[0], f[1], pa.a[1] + slot_a, pb.a[1] + slot_b, oa, mine + before(slot_a));
             oa.advance();
-            // the next tiles have come, and all have read this one: B's after the next takes its place
-            wait_loads<OpA::PASSES>();
+            // the next tiles have come (scales need not have, behind which are A's loads), and all have read this one: B's after
+            // the next takes its place
+            wait_loads<OpA::PASSES + (decltype(first)::value == 0 ? MI + NJ : 0)>();
             bare_barrier();
             slot_a = after(slot_a);
             const uint32_t free_b = slot_b;
