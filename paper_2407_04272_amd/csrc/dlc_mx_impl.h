@@ -17,8 +17,9 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 //     bit (towards zero); their sums are fp32.  That is below 7 2^-13 of a group's magnitudes, in the norm some 2^-14 of a
 //     result, against its own rounding of 2^-11 or 2^-8.
 //   ELEM 8, results in fp32 (EXACT): elements times scales as bf16, which holds all from 2^-126 on exactly, and the bf16
-//     instruction, whose sums are fp32 throughout.  2048 x 8192 -> 8192 303 us, 907 TFLOP/s, bound by the conversions, which
-//     every wavefront makes for itself (the scaled instruction: some 2950 TFLOP/s).
+//     instruction, whose sums are fp32 throughout.  2048 x 8192 -> 8192 292-305 us, 940 TFLOP/s, bound by the conversions,
+//     which every wavefront makes for itself (the scaled instruction 91 us).  Their order does not matter: all of a quarter
+//     in front of its products 310, between those of the quarter before 330.
 template <typename T, int ELEM>
 constexpr bool kMxExact = ELEM == 8 && std::is_same<T, float>::value;
 
@@ -245,8 +246,8 @@ __device__ __forceinline__ void mx_pair(f32x4* acc0, f32x4* acc1, const A& a0, c
 // For results that 256 x 256 tiles would leave most of the card without: 512 x 8192 -> 2048 of 4 bits 17 us (23 with reads and
 // products in turn), 1024 x 8192 18 (27), 2048 x 8192 25 (36); 777 x 515 -> 1023, E4M3 rows, bias, gelu and residual 8.5 us.
 // Bound by the way from L2 to LDS (128 x 128: 32 KB a tile on every unit in 0.64 us, 13 TB/s) and at small sizes by the start and
-// the epilogue, 4.4 us; more slots were no faster.  Two work-groups of 64 x 128 and 4 bits fit a compute unit.  A group's scales are asked for two tiles ahead, for one tile ahead cost a
-// fifth (33 us for 28), and what is left of their cost is a tenth.
+// the epilogue, 4.4 us; more slots were no faster.  Two work-groups of 64 x 128 and 4 bits fit a compute unit.  A group's
+// scales are asked for two tiles ahead: one tile ahead they cost a fifth (2048 x 8192 33 us for 28), now a tenth.
 template <int ELEM, int BM>
 constexpr int mx_tile_lds() {
     const int ring = 3 * (BM * 32 * ELEM + 128 * 128), out = BM / 2 * 256 * 4;
@@ -427,8 +428,8 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
 // between them: a wavefront has its SIMD to itself.  Loads, scales' among them, stand between the blocks; their waits are the
 // compiler's and wait_loads'.
 // Bound by the matrix cores and the card's power: with its scales the instruction takes 24 cycles (without, 16; one of 32 x 32 x
-// 64, which does twice as much, 33; with an E4M3 operand 32), and 16384 x 8192 -> 4096 with random elements 282 us, 3900
-// TFLOP/s (265-282), at 1.9-2.1 GHz; the bare instruction on the same elements reaches 5640 on the whole card.  E4M3 rows 370 us, 2970
+// 64, which does twice as much, 33; with an E4M3 operand 32), and 16384 x 8192 -> 4096 with random elements 274 us, 4020
+// TFLOP/s, at 1.9-2.1 GHz; the bare instruction on random elements reaches 5640 on the whole card.  E4M3 rows 358 us, 3070
 // TFLOP/s.  Measured and left: blocks of 32 x 32 (280 us where this took 254), work-groups that stay and ask for the next
 // tile's operands during the epilogue (the same), results stored from the registers without LDS (265-286 for 254), no masks
 // on the loads (268 for 270).
