@@ -173,7 +173,7 @@ struct Plan {
 
 // What 256 k values cost with 1 and 2 work-groups on a compute unit, in us, what a work-group costs besides, and every
 // further one, measured on full cards (0: no second work-group fits; up to half of a card, whose work-groups have more of the
-// caches and the power, kHalf of it): E2M1, E4M3, E4M3 with results in fp32.  64 x 128 is the best until its tiles no longer fit
+// caches and the power, kHalf of it): E2M1, E4M3, E4M3 with results in fp32.  64 x 128 is the best of the tiles until its tiles no longer fit
 // the card at once (1024 x 2048 x 2048 of 4 bits 8.1 us for 10.3 and 22; 2048 x 2048 x 2048 12.3, 11.1 and 22.7, of 8 bits 17.3,
 // 13.9 and 29.4), 256 x 256 where there are many (2048 x 8192 x 8192 of 4 bits 120, 98 and 66 us).
 struct TileCost { double tile[2], first, further; };
@@ -181,6 +181,13 @@ constexpr TileCost kCost[3][3] = {{{{1.66, 0}, 12.8, 11.0}, {{0.64, 0}, 5.8, 3.7
                                   {{{2.42, 0}, 13.6, 8.3}, {{0.89, 0}, 6.6, 4.2}, {{0.6, 0}, 4.6, 2.6}},
                                   {{}, {{2.2, 0}, 5.5, 3.5}, {{1.45, 0}, 4.2, 2.4}}};
 constexpr double kHalf = 0.85;
+
+// Few rows: a round of work-groups (a band of 32 rows and 16 columns each, one on a compute unit) with 1024 k values, what the
+// first round costs besides and every further one; the kinds as above.  64 x 2048 -> 2048 of 4 bits 4.0 us, 7.4 the best of the
+// tiles; 64 x 8192 -> 2048 5.8 and 10.4; 128 x 8192 -> 2048 in two rounds 9.7 and 12.0; 64 x 65536 -> 2048 22.9 and 19.8.
+struct SkinnyCost { double k, first, further; };
+constexpr SkinnyCost kSkinnyCost[3] = {{0.30, 3.4, 1.5}, {0.44, 4.1, 1.9}, {0.50, 4.2, 2.2}};
+constexpr int kSkinnyRounds = 4;
 constexpr int kUnits = 256;  // compute units
 constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
@@ -188,14 +195,18 @@ constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
 Plan plan_linear(const Shape& s) {
     Plan best{};
     best.split = 1;
-    if (s.M <= kMxSkinnyRows) {
-        best.tile = kMxSkinny;
-        return best;
-    }
+    best.tile = kMxSkinny;
+    if (s.M <= kMxSkinnyRows / 2) return best;
     const int64_t groups = mx_groups(s.K);
     const bool exact = s.elem == DLC_MX_E4M3 && s.es == 4;
-    const TileCost* const cost = kCost[exact ? 2 : s.elem == DLC_MX_E4M3 ? 1 : 0];
+    const int kind = exact ? 2 : s.elem == DLC_MX_E4M3 ? 1 : 0;
+    const TileCost* const cost = kCost[kind];
     double least = 1e300;
+    const int64_t rounds = div_up(div_up(s.M, kMxSkinnyRows) * div_up(s.N, 16), kUnits);
+    if (rounds <= kSkinnyRounds) {
+        const SkinnyCost& c = kSkinnyCost[kind];
+        least = c.first + (double)rounds * (double)s.K / 1024.0 * c.k + (double)(rounds - 1) * c.further;
+    }
     for (int tile = exact ? 1 : 0; tile < 3; ++tile) {
         const TileCost& c = cost[tile];
         const int64_t tm = div_up(s.M, kMxTileM[tile]), tn = div_up(s.N, kMxTileN[tile]), tiles = tm * tn;

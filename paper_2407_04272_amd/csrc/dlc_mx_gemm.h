@@ -14,7 +14,7 @@ constexpr int kMxTileM[] = {256, 128, 64}, kMxTileN[] = {256, 128, 128}, kMxSkin
 
 template <typename T>
 struct MxOps {
-    // tile: of kMxTileM (0: not with E4M3 and results in fp32) or kMxSkinny, for at most kMxSkinnyRows rows
+    // tile: of kMxTileM (0: not with E4M3 and results in fp32) or kMxSkinny (bands of kMxSkinnyRows rows)
     static hipError_t gemm(const MxGemmArgs& g, int elem_x, int tile, hipStream_t s);
 };
 

@@ -65,8 +65,8 @@ __device__ __forceinline__ void read_frags(u32x4_t* o, uint32_t a, uint32_t b) {
 }
 
 // ---- few rows ----
-// At most 32 rows: the product is a pass over w.  A work-group takes 16 columns of C; its wavefronts take groups of 512 k
-// values in turn, each on its own, and their sums meet in LDS.  A wavefront loads 8 rows of 128 bytes at a time, whole cache
+// The product is a pass over w for a band of 32 rows (16, if there are no more).  A work-group takes 16 columns of C; its
+// wavefronts take groups of 512 k values in turn, each on its own, and their sums meet in LDS.  A wavefront loads 8 rows of 128 bytes at a time, whole cache
 // lines, to its two slots in LDS and reads its fragments from there.  Bound by the latency of memory: 1 x 1664 -> 1024 4.0 us
 // (0.9 MB, fp16), 16 x 8192 -> 2048 5.3 us (8.9 MB: 1.7 TB/s with 128 work-groups), of which an empty launch is 2.  MT: blocks
 // of 16 rows of x
@@ -81,14 +81,14 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArg
     __shared__ __attribute__((aligned(16))) char lds[kSkinnyWaves * SLOTS * SLOT];
     const GemmArgs& ga = mx.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, j = lane & 15;
-    const int n0 = blockIdx.x * 16, k0 = wave * kMxGroup;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * kMxSkinnyRows, k0 = wave * kMxGroup;
     char* const mine = lds + wave * (SLOTS * SLOT);
     Rows w, x[XT * MT];  // (x: [block][tile])
     w.init(ga.b, ga.ldb, n0, ga.N, k0 / 2, lane);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int t = 0; t < XT; ++t) x[m * XT + t].init(ga.a, ga.lda, m * 16, ga.M, k0 * ELEM / 8 + t * 128, lane);
+        for (int t = 0; t < XT; ++t) x[m * XT + t].init(ga.a, ga.lda, m0 + m * 16, ga.M, k0 * ELEM / 8 + t * 128, lane);
     int left = ga.K - k0;  // k values from the next tile to fetch on
     const auto fetch = [&](char* slot, bool second) {  // a group's first 256 values, its second
         w.fetch(slot, left / 2, second ? WSTEP - 128 : 128);
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArg
     const uint8_t* qw = mx.ws + (int64_t)min(n0 + j, ga.N - 1) * 16 + g * 4 + (int64_t)wave * ga.N * 16;
     const uint8_t* qx[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) qx[m] = mx.xs + (int64_t)min(m * 16 + j, ga.M - 1) * 16 + g * 4 + (int64_t)wave * ga.M * 16;
+    for (int m = 0; m < MT; ++m) qx[m] = mx.xs + (int64_t)min(m0 + m * 16 + j, ga.M - 1) * 16 + g * 4 + (int64_t)wave * ga.M * 16;
     uint32_t sw = 0, sx[MT] = {};
     const auto scales = [&](int k) {
         if (k >= ga.K) return;
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArg
 #pragma unroll
     for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4*>(&sums[m * kSkinnyWaves + wave][0][j][g * 4]) = acc[m];
     __syncthreads();
-    if (wave < MT) skinny_end<T, false>(ga, wave * 16, n0, sums + wave * kSkinnyWaves, lane);
+    if (wave < MT) skinny_end<T, false>(ga, m0 + wave * 16, n0, sums + wave * kSkinnyWaves, lane);
 #endif
 }
 
@@ -717,7 +717,7 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
 
 template <typename T, int ELEM>
 static void mx_go(const MxGemmArgs& g, int tile, hipStream_t s) {
-    const dim3 skinny((unsigned)((g.c.N + 15) / 16)), grid((unsigned)(g.c.tiles_m * g.c.tiles_n * g.c.split));
+    const dim3 skinny((unsigned)((g.c.N + 15) / 16), (unsigned)((g.c.M + kMxSkinnyRows - 1) / kMxSkinnyRows)), grid((unsigned)(g.c.tiles_m * g.c.tiles_n * g.c.split));
     if (tile == kMxSkinny && g.c.M <= 16) k_mx_skinny<T, ELEM, 1><<<skinny, dim3(64 * kSkinnyWaves), 0, s>>>(g);
     else if (tile == kMxSkinny) k_mx_skinny<T, ELEM, 2><<<skinny, dim3(64 * kSkinnyWaves), 0, s>>>(g);
     else if (tile == 2) k_mx_tile<T, ELEM, 64><<<grid, dim3(256), 0, s>>>(g);

@@ -317,3 +317,20 @@ def test_narrow_rows(rows, cols, ld, dtype, bits):
         t = Guarded(rows, cols, dtype, ld, 1).set(t).view
     _same(*_quantised(t, bits, dtype, ld), *quantise(x, bits), f"{rows}x{cols} {bits} {dtype}")
     test_back(rows, cols, ld, dtype, bits)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(33, 512, 16), (64, 2048, 300), (65, 129, 17), (96, 4100, 33), (127, 33, 1), (250, 700, 64), (1000, 640, 40), (5000, 300, 7)])
+def test_bands_of_rows(rows, n_in, n_out, dtype, bits):
+    """More than one band of 32 rows in a pass over the weights each, the last one not full."""
+    _linear(rows, n_in, n_out, bits, dtype)
+    _linear(rows, n_in, n_out, bits, dtype, "gelu", bias=True, residual=True, ld=n_out + 3)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 2048, 2048), (300, 2000, 2040), (400, 1290, 1500), (200, 4000, 1100), (700, 768, 1030), (260, 513, 3000), (1100, 256, 1100)])
+def test_tiles_of_every_length(rows, n_in, n_out, bits):
+    """Numbers of tiles of k values from one to eight in middle tiles: whole turns through the loop, and every rest."""
+    for dtype in ("bf16", "f32"):
+        _linear(rows, n_in, n_out, bits, dtype, bias=True)
