@@ -158,3 +158,12 @@ def test_parts_on_several_gpus_add_up():
     b.dlc_gradient_clip(lc, both, 0.7)
     for v, t in zip(before, a + c):
         assert_close(t, v.double() * (0.7 / math.sqrt(want)), v.double().abs() * (0.7 / math.sqrt(want)) * 4 * F32, "part")
+
+
+@pytest.mark.parametrize("sizes", [[(32768,)], [(32767,), (1,)], [(32768,), (1,)], [(512, 1)] * 64, [(512, 1)] * 65, [(8, 3), (0,), (100, 7), (20000,)], [(17,)] * 9])
+def test_lists_that_one_work_group_adds_up(sizes):
+    """... and the next larger ones"""
+    for dtype in TYPES:
+        _check(_tensors(sizes, [dtype], 71), 0.25)
+        t = _tensors(sizes, [dtype], 72)
+        assert len({float(_norm(t)[1]) for _ in range(3)}) == 1
