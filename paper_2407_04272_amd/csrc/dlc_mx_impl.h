@@ -54,6 +54,9 @@ __device__ __forceinline__ f32x4 mx_mma(const u32x4_t& w, const u32x4_t& x0, con
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc, 4, ELEM == 8 ? 0 : 4, S, (int)sw, S, (int)sx);
 }
 
+// The loads before it are asked for before those behind it: waits that leave some on their way count on the order
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
 // Both chunks of N blocks' rows, STEP bytes apart
 template <int N, int STEP = 2048>
 __device__ __forceinline__ void read_frags(u32x4_t* o, uint32_t a, uint32_t b) {
@@ -316,6 +319,7 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
         fetch(0);
         fetch(1);
         fetch(2);
+        in_order();
         scales(sc[1], k0 + kMxGroup);
         wait_loads<2 * LOADS + WORDS>();
         bare_barrier();
@@ -358,6 +362,7 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
                      },
                      [&] {
                          ob.fetch(to + XT * OpA::BYTES, tid);
+                         in_order();
                          last();
                      });
         };
@@ -627,6 +632,7 @@ __global__ __launch_bounds__(256, 1) void k_mx_wide(const MxGemmArgs mx) {
             ob.advance();
         };
         for (int s = 0; s < tiles; s += 2) {
+            in_order();
             sa.load();
             sb.load();
             tile(std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
