@@ -69,7 +69,7 @@ class MxLinearConfig(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("act", C.c_int32), ("elem_x", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64),
                 ("in_features", C.c_int64), ("out_features", C.c_int64), ("ld_y", C.c_int64), ("ld_res", C.c_int64)]
     counter = None
-    sizes = shapes = None  # of the operands' buffers, and the sizes that they were worked out for
+    shapes = None, None  # the sizes that the operands' buffers were worked out for, and those: one tuple, for all threads
 
 
 class NormConfig(C.Structure):
@@ -485,11 +485,11 @@ def dlc_mx_linear_workspace_bytes(cfg: MxLinearConfig) -> int:
 def dlc_mx_linear_forward(cfg: MxLinearConfig, xq, xs, wq, ws, bias, residual, y, work=None, stream=None):
     """y = act(x w' + bias) + residual; x (elements cfg.elem_x) and w (E2M1) in microscaled form.  Raises DlcError."""
     ty, st = _where(cfg, stream)
-    M, K, N = sizes = cfg.rows, cfg.in_features, cfg.out_features
-    if (sizes, cfg.elem_x) != cfg.sizes:
-        cfg.sizes = sizes, cfg.elem_x
-        cfg.shapes = _mx_data_shape(cfg.elem_x, M, K), _mx_scale_shape(M, K), _mx_data_shape(MX_E2M1, N, K), _mx_scale_shape(N, K)
-    shapes = cfg.shapes
+    M, K, N, elem = sizes = cfg.rows, cfg.in_features, cfg.out_features, cfg.elem_x
+    known, shapes = cfg.shapes
+    if sizes != known:
+        shapes = _mx_data_shape(elem, M, K), _mx_scale_shape(M, K), _mx_data_shape(MX_E2M1, N, K), _mx_scale_shape(N, K)
+        cfg.shapes = sizes, shapes
     wk, nb = _work(work, ty)
     _check(lib().dlc_mx_linear_forward(
         C.byref(cfg), _bytes("xq", xq, ty, shapes[0]), _bytes("xs", xs, ty, shapes[1]),

@@ -256,3 +256,62 @@ def test_gradients_that_overlap():
     # some of the outputs may be the gradients themselves
     for p, q in ((4096, 65536), (65536, 4096 + 40), (4096, 4096 + 40), (65536, 65536 + 40)):
         b._check_apart(lst, b.GradientList([At(f, 10, ptr=p), At(f, 10, ptr=q), rows(8192), rows(1 << 20)]))
+
+
+# ---- one configuration, several threads -----------------------------------------------------------
+def _linear_tensors(M, K, N):
+    import torch
+    u = torch.uint8
+    return [Stub(u, M, -(-K // 128) * 128), Stub(u, -(-K // 512), M, 16), Stub(u, N, -(-K // 128) * 64), Stub(u, -(-K // 512), N, 16), None, None,
+            Stub(torch.float32, M, N)]
+
+
+def test_a_call_in_the_middle_of_another():
+    """What a call keeps on its configuration is complete whenever another thread may read it: here the other's whole call stands
+    behind every single attribute that the first one sets."""
+    b = _b()
+    inner = []
+
+    class Watched(b.MxLinearConfig):
+        def __setattr__(self, name, value):
+            super().__setattr__(name, value)
+            if name not in fields and not inner:
+                inner.append(name)
+                b.dlc_mx_linear_forward(self, *_linear_tensors(0, self.in_features, self.out_features), stream=Stream())
+
+    fields = {f for f, _ in b.MxLinearConfig._fields_}
+    cfg = Watched(b.F32, b.ACT_NONE, b.MX_E4M3, 0, 0, 40, 24, 0, 0)
+    for K, N in ((40, 24), (700, 24), (700, 30)):
+        cfg.in_features, cfg.out_features = K, N
+        del inner[:]
+        b.dlc_mx_linear_forward(cfg, *_linear_tensors(0, K, N), stream=Stream())
+        _refused(b.dlc_mx_linear_forward, cfg, *_linear_tensors(0, K + 512, N), stream=Stream())
+        _refused(b.dlc_mx_linear_forward, cfg, *_linear_tensors(0, K, N + 1), stream=Stream())
+
+
+def test_threads_that_share_a_configuration():
+    import sys
+    import threading
+    b = _b()
+    b.lib()
+    wrong, was = [], sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        for _ in range(300):
+            cfg, start = b.make_mx_linear_config(b.F32, b.MX_E4M3, 0, 40, 24), threading.Barrier(6)
+
+            def call():
+                start.wait()
+                try:
+                    b.dlc_mx_linear_forward(cfg, *_linear_tensors(0, 40, 24), stream=Stream())
+                except Exception as e:
+                    wrong.append(e)
+
+            threads = [threading.Thread(target=call) for _ in range(6)]
+            for t in threads:
+                t.start()
+            for t in threads:
+                t.join()
+    finally:
+        sys.setswitchinterval(was)
+    assert not wrong, wrong[0]
