@@ -473,9 +473,10 @@ int dlc_mx_dequantize(const dlc_mx_config* cfg /*HOST*/, const void* d_q, const 
  *   d_bias [N] or NULL   d_residual [M][N] or NULL   d_y [M][N], all of type dtype.  d_residual may be d_y, with equal leading
  *   dimensions (else DLC_EINVAL)
  * Sums and the epilogue are fp32, the result is rounded once.  Products are exact, but for two cases of E4M3 rows:
- *   results in half precision   of eight products in a row each loses what lies more than 13 binary places below the leading
- *                bit of the largest (less than 2^-13 of that one's magnitude; nothing of the largest itself): the matrix cores' way, and in
- *                the norm some 2^-14 of a result
+ *   results in half precision, more than 16 rows   of eight products in a row each loses what lies more than 13 binary places below
+ *                2^E, E the largest sum of two factors' exponents among them (0.5 has that of 1): less than 2^-13 of the largest
+ *                product's magnitude, 2^-12 if its weight is 0.5; nothing of the largest itself.  The matrix cores' way, and in the norm
+ *                some 2^-14 of a result
  *   results in fp32             an element that stands for less than 2^-126 may count as 0, one past fp32's range (a scale made by hand)
  *                as infinite
  *   sizes        rows 0 .. 2^30, features 1 .. 2^20, leading dimensions up to 2^20; results of fewer than 2^24 tiles of 256 x 256

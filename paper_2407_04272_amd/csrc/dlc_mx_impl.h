@@ -13,9 +13,10 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // How the products are made:
 //   ELEM 4, E2M1 times E2M1: the scaled instruction, exact products (whole numbers of quarters up to 36), fp32 sums.
 //   ELEM 8, E4M3 times E2M1, results of half precision: the scaled instruction.  It lines up the eight products of a lane's
-//     consecutive elements at the largest of them and drops what lies more than 13 binary places below that one's leading
-//     bit (towards zero); their sums are fp32.  That is below 7 2^-13 of a group's magnitudes, in the norm some 2^-14 of a
-//     result, against its own rounding of 2^-11 or 2^-8.
+//     consecutive elements at 2^E, E the largest sum of two factors' exponents (0.5 has that of 1; products of 0 do not count), and
+//     drops what lies more than 13 binary places below (towards zero); their sums are fp32.  That is below 7 2^-13 of the
+//     largest's magnitude (2^-12 if its weight is 0.5), in the norm some 2^-14 of a result, against its own rounding of 2^-11 or
+//     2^-8, and taken where the matrix cores set the time.  Up to 16 rows, where memory does, mx_mma_split keeps all.
 //   ELEM 8, results in fp32 (EXACT): elements times scales as bf16, which holds all from 2^-126 on exactly, and the bf16
 //     instruction, whose sums are fp32 throughout.  2048 x 8192 -> 8192 292-305 us, 940 TFLOP/s, bound by the conversions,
 //     which every wavefront makes for itself (the scaled instruction 91 us).  Their order does not matter: all of a quarter
@@ -54,6 +55,22 @@ __device__ __forceinline__ f32x4 mx_mma(const u32x4_t& w, const u32x4_t& x0, con
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc, 4, ELEM == 8 ? 0 : 4, S, (int)sw, S, (int)sx);
 }
 
+// ... E4M3 times E2M1 by the scaled instruction with nothing cut off: x's elements from 2 on, whose codes have bit 6, then the
+// others.  From 2 on the largest sum of exponents is 8 + 2 and a product's last place 2^-3; below 2, 0 + 2 and 2^-10.
+template <int S>
+__device__ __forceinline__ f32x4 mx_mma_split(const u32x4_t& w, const u32x4_t& x0, const u32x4_t& x1, uint32_t sw, uint32_t sx, f32x4 acc) {
+    u32x4_t big[2], rest[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t x = i < 4 ? x0[i] : x1[i - 4];
+        const uint32_t mask = __builtin_amdgcn_perm(x << 9, x << 1, 0x090B080Au);  // bit 6 in all of its byte
+        big[i >> 2][i & 3] = x & mask;
+        rest[i >> 2][i & 3] = x & ~mask;
+    }
+    acc = mx_mma<8, false, S>(w, big[0], big[1], sw, sx, acc);
+    return mx_mma<8, false, S>(w, rest[0], rest[1], sw, sx, acc);
+}
+
 // The loads before it are asked for before those behind it: waits that leave some on their way count on the order
 __device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
 
@@ -70,9 +87,9 @@ __device__ __forceinline__ void read_frags(u32x4_t* o, uint32_t a, uint32_t b) {
 // ---- few rows ----
 // The product is a pass over w for a band of 32 rows (16, if there are no more).  A work-group takes 16 columns of C; its
 // wavefronts take groups of 512 k values in turn, each on its own, and their sums meet in LDS.  A wavefront loads 8 rows of 128 bytes at a time, whole cache
-// lines, to its two slots in LDS and reads its fragments from there.  Bound by the latency of memory: 1 x 1664 -> 1024 4.0 us
-// (0.9 MB, fp16), 16 x 8192 -> 2048 5.3 us (8.9 MB: 1.7 TB/s with 128 work-groups), of which an empty launch is 2.  MT: blocks
-// of 16 rows of x
+// lines, to its two slots in LDS and reads its fragments from there.  Bound by the latency of memory, one call after the other in
+// a graph: 1 x 1664 -> 1024 3.5 us (0.9 MB, fp16), 16 x 8192 -> 2048 5.9 us (8.9 MB: 1.5 TB/s with 128 work-groups), of which an
+// empty launch is 2; with E4M3 products that are cut 3.2 and 5.4.  MT: blocks of 16 rows of x
 template <typename T, int ELEM, int MT>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArgs mx) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -145,6 +162,9 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void k_mx_skinny(const MxGemmArg
                 if constexpr (ELEM == 4) {
                     acc[m] = mx_mma<4, false, 2 * H>(fw[0], fx[2 * m], fx[2 * m], tw, tx[m], acc[m]);
                     acc[m] = mx_mma<4, false, 2 * H + 1>(fw[1], fx[2 * m + 1], fx[2 * m + 1], tw, tx[m], acc[m]);
+                } else if constexpr (MT == 1 && !EXACT) {
+                    acc[m] = mx_mma_split<2 * H>(fw[0], fx[0], fx[1], tw, tx[m], acc[m]);
+                    acc[m] = mx_mma_split<2 * H + 1>(fw[1], fx[2], fx[3], tw, tx[m], acc[m]);
                 } else {
                     acc[m] = mx_mma<8, EXACT, 2 * H>(fw[0], fx[4 * m], fx[4 * m + 1], tw, tx[m], acc[m]);
                     acc[m] = mx_mma<8, EXACT, 2 * H + 1>(fw[1], fx[4 * m + 2], fx[4 * m + 3], tw, tx[m], acc[m]);

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from dense_util import ACTS, F32, FN, ROUND, Guarded, act, assert_close, code, product, rounded, torch_type
-from mx_util import GuardedBytes, quantise, values
+from mx_util import GuardedBytes, TABLE, quantise, values
 
 pytestmark = pytest.mark.gpu
 TYPES = ["f32", "f16", "bf16"]
@@ -334,3 +334,28 @@ def test_tiles_of_every_length(rows, n_in, n_out, bits):
     """Numbers of tiles of k values from one to eight in middle tiles: whole turns through the loop, and every rest."""
     for dtype in ("bf16", "f32"):
         _linear(rows, n_in, n_out, bits, dtype, bias=True)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 40, 17), (1, 1100, 64), (2, 513, 5), (9, 130, 16), (16, 1000, 40)])
+def test_few_rows_lose_nothing(rows, n_in, n_out, dtype):
+    """Every block of 32 has +448 and -448 in different groups of eight, whose products (w 0.5 there) add up to nothing, and elements
+    of at most 2^-4.  Products are whole numbers of 2^-10 and stay below 2^14 together (35 blocks of two 224 and 1100 of 0.375): fp32
+    sums are exact in any order, and the result is rounded once."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    rng = np.random.default_rng(rows + n_in)
+    x = rng.choice(np.arange(25), (rows, n_in))                     # codes of 0 .. 2^-4
+    x = TABLE[8][x] * rng.choice([-1.0, 1.0], (rows, n_in))
+    w = rng.choice(TABLE[4], (n_out, n_in)) * rng.choice([-1.0, 1.0], (n_out, n_in))
+    w[:, 31::32] = 6.0                                              # (its scale is 1 too)
+    at = np.arange(3, n_in - 17, 32)
+    x[:, at] = 448.0 * rng.choice([-1.0, 1.0], (rows, len(at)))
+    x[:, at + 17] = -x[:, at]
+    w[:, at] = w[:, at + 17] = 0.5
+    (xq, xs), (wq, ws) = quantise(x, 8), quantise(w, 4)
+    assert np.array_equal(values(xq, xs, n_in, 8), x) and np.array_equal(values(wq, ws, n_in, 4), w) and (np.abs(x) @ np.abs(w).T).max() < 2 ** 14
+    cfg = b.make_mx_linear_config(code(dtype), b.MX_E4M3, rows, n_in, n_out)
+    y = torch.empty((rows, n_out), dtype=torch_type(dtype), device="cuda")
+    b.dlc_mx_linear_forward(cfg, *(torch.from_numpy(v).cuda() for v in (xq, xs, wq, ws)), None, None, y)
+    assert torch.equal(y.cpu(), torch.from_numpy(x @ w.T).to(torch_type(dtype)))
