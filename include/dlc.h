@@ -536,8 +536,8 @@ size_t dlc_norm_workspace_bytes(const dlc_norm_config* cfg /*HOST*/);
  *   list      HOST    `count` tensors, 0 .. 2^20 of them; types may differ; none overlaps another.  Read during the call only
  *   d_sum     DEVICE  double[1]: dlc_gradient_norm writes the sum of all squares (in 64 bits throughout), dlc_gradient_clip
  *                     reads it
- *   d_norm    DEVICE  float[1] or NULL: gets n = sqrt(*d_sum)
- *   out       HOST    as `list`, the same types and sizes: gets every element times f = min(1, max_norm / n), rounded once; the
+ *   d_norm    DEVICE  float[1] or NULL: gets n = sqrt(*d_sum); a finite n past fp32's range as its largest value
+ *   out       HOST    as `list`, the same types and sizes: gets every element times f = min(1, max_norm / n) (in 64 bits), rounded once; the
  *                     same tensors (with the same ld) for clipping in place, which writes nothing where f is 1.  Each may be
  *                     its own gradient, none may overlap another's
  *   max_norm          >= 0.  If n is not finite f is 1: the gradients stay as they are, and *d_norm tells

@@ -4,6 +4,8 @@
 // writes them.  The tensors' descriptions go with the launch, kTensors of them at a time; a work-group takes a chunk of one
 // tensor.  Sums are 64-bit: no gradient's square is lost or too large, whatever the type.  400 million bf16 elements: the norm
 // 160 us (5.0 TB/s), clipping 277 (5.8 TB/s); 2.5 million of fp32 4 + 2 + 2.5 us and the gaps between three launches.
+#include <cfloat>
+
 #include "dlc_dense.h"
 
 using namespace dlc;
@@ -139,20 +141,22 @@ __global__ __launch_bounds__(kThreads) void k_add(const double* part, int64_t n,
 template <int N>
 __global__ __launch_bounds__(kThreads) void k_clip(const ClipArgs<N> a) {
     const double n = sqrt(*a.sum);
-    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)n;
+    // (finite means that f is what it should be: a finite n past fp32's range is its largest value)
+    if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = n < __builtin_inf() ? (float)fmin(n, (double)FLT_MAX) : (float)n;
     if (a.count == 0) return;
-    const float f = n > a.max_norm && n < __builtin_inf() ? (float)(a.max_norm / n) : 1.0f;
+    // (64-bit too: with far gradients and a small limit it lies below fp32's normal range where the results do not)
+    const double f = n > a.max_norm && n < __builtin_inf() ? a.max_norm / n : 1.0;
     // from the last chunk on: what the norm read last may still be in the last cache
     const uint32_t chunk = a.chunks - 1 - blockIdx.x;
     const int piece = piece_of(a, chunk);
     const Piece& p = a.t[piece];
-    if (f == 1.0f && p.in == p.out) return;
+    if (f == 1.0 && p.in == p.out) return;
     const int64_t at = (int64_t)(chunk - a.first[piece]) * a.chunk, end = min(counted(p), at + a.chunk);
     const auto run = [&](auto one) {
         using T = decltype(one);
         each8<T>(p, at, end, [&](float* v, T* out, int cnt) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= f;
+            for (int i = 0; i < 8; ++i) v[i] = (float)((double)v[i] * f);
             store8(out, cnt, v);
         });
     };

@@ -167,3 +167,47 @@ def test_lists_that_one_work_group_adds_up(sizes):
         _check(_tensors(sizes, [dtype], 71), 0.25)
         t = _tensors(sizes, [dtype], 72)
         assert len({float(_norm(t)[1]) for _ in range(3)}) == 1
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length,limit", [(3e31, 1e-9), (1e35, 1e-7), (1e20, 1e-25), (5e-20, 1e-44), (2.0, 1.5)])
+def test_factors_far_below_one(length, limit, dtype):
+    """Factors below fp32's normal range, with results that are not: off by the rounding of the result alone (what f loses in 64
+    bits is far below; bf16 rounds a second time, from fp32)."""
+    import torch
+    t = _tensors([(1000,), (37, 5)], [dtype])
+    t = [(v.double() * (length / 40.0)).to(v.dtype) for v in t]
+    before = [v.clone() for v in t]
+    from paper_2407_04272_amd import binding as b
+    lst, total = _norm(t)
+    b.dlc_gradient_clip(lst, total, limit)
+    f = min(1.0, limit / math.sqrt(_exact(before)))
+    for old, new in zip(before, t):
+        v = old.double() * f
+        assert_close(new, v, rounded(v, v.abs() * F32 + 2.0 ** -149 if dtype != "f32" else v.abs() * 2.0 ** -50, dtype), f"{length} {limit} {dtype}")
+
+
+@pytest.mark.parametrize("where", ["in place", "elsewhere", "nothing to clip"])
+def test_a_finite_norm_past_the_range_of_floats(where):
+    """The gradients are clipped, and the norm that is stored says so: it is finite.  An infinite one says that they were not."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    big = float(torch.finfo(torch.float32).max)
+    t = [torch.full((100,), big, device="cuda"), torch.full((7, 9), -big / 2, dtype=torch.bfloat16, device="cuda")]
+    before = [v.clone() for v in t]
+    lst, total = _norm(t)
+    n, exact = torch.zeros(1, device="cuda"), math.sqrt(_exact(before))
+    assert exact > big
+    if where == "nothing to clip":
+        b.dlc_gradient_clip(b.GradientList([]), total, 1.0, n)
+        assert float(n) == big
+        return
+    out = [torch.zeros_like(v) for v in t] if where == "elsewhere" else t
+    b.dlc_gradient_clip(lst, total, 1.0, n, b.GradientList(out) if where == "elsewhere" else None)
+    assert float(n) == big
+    for old, new, name in zip(before, out, ("f32", "bf16")):
+        v = old.double() / exact
+        assert_close(new, v, rounded(v, v.abs() * F32, name), name)
+    total.fill_(float("inf"))
+    b.dlc_gradient_clip(lst, total, 1.0, n)
+    assert float(n) == float("inf")
