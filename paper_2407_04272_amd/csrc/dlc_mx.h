@@ -2,10 +2,11 @@
 // read it share.
 #pragma once
 #include "dlc_dense.h"
+#include "dlc_mx_plan.h"
 
 namespace dlc {
 
-constexpr int kMxBlock = 32, kMxFill = 128, kMxGroup = 512;  // columns of a scale, that a row is filled up to, of a group of scales
+constexpr int kMxBlock = 32, kMxFill = 128;  // columns of a scale, that a row is filled up to
 
 inline __host__ __device__ int64_t mx_groups(int64_t cols) { return (cols + kMxGroup - 1) / kMxGroup; }
 inline __host__ __device__ int64_t mx_filled(int64_t cols) { return (cols + kMxFill - 1) / kMxFill * kMxFill; }

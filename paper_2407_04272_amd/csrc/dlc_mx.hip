@@ -86,7 +86,6 @@ __global__ __launch_bounds__(256) void k_mx_dequantize(const MxArgs a) {
 
 // ---- host ---------------------------------------------------------------------------------------
 constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 20;
-constexpr int64_t kMaxGroups = int64_t(1) << 24;  // a launch's threads, work-groups of 256, are counted in 32 bits
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool on(const void* p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
@@ -148,6 +147,7 @@ int convert_any(const dlc_mx_config* c, const void* x, const void* q, const void
 struct Shape {
     int64_t M, K, N, ldy, ldres;
     int elem, es;
+    MxPlan plan() const { return mx_plan(M, K, N, elem == DLC_MX_E4M3, es == 4); }
 };
 
 bool make_shape(const dlc_mx_linear_config* c, Shape* s) {
@@ -162,80 +162,11 @@ bool make_shape(const dlc_mx_linear_config* c, Shape* s) {
     s->es = c->dtype == DLC_F32 ? 4 : 2;
     // (some tile's launch covers the result: the largest, which fp32 results of E4M3 have not)
     const int64_t side = s->elem == DLC_MX_E4M3 && s->es == 4 ? 128 : 256;
-    return div_up(s->M, side) * div_up(s->N, side) < kMaxGroups;
-}
-
-struct Plan {
-    int tile, split, kper, tiles_m, tiles_n;
-    int64_t part_ld;
-    size_t bytes;  // of the partial sums
-};
-
-// What 256 k values cost with 1 and 2 work-groups on a compute unit, in us, what a work-group costs besides, and every
-// further one, measured on full cards (0: no second work-group fits; up to half of a card, whose work-groups have more of the
-// caches and the power, kHalf of it): E2M1, E4M3, E4M3 with results in fp32.  64 x 128 is the best of the tiles until its tiles no longer fit
-// the card at once (1024 x 2048 x 2048 of 4 bits 8.1 us for 10.3 and 22; 2048 x 2048 x 2048 12.3, 11.1 and 22.7, of 8 bits 17.3,
-// 13.9 and 29.4), 256 x 256 where there are many (2048 x 8192 x 8192 of 4 bits 120, 98 and 66 us).
-struct TileCost { double tile[2], first, further; };
-constexpr TileCost kCost[3][3] = {{{{1.66, 0}, 12.8, 11.0}, {{0.64, 0}, 5.8, 3.7}, {{0.46, 0.86}, 4.4, 2.0}},
-                                  {{{2.42, 0}, 13.6, 8.3}, {{0.89, 0}, 6.6, 4.2}, {{0.6, 0}, 4.6, 2.6}},
-                                  {{}, {{2.2, 0}, 5.5, 3.5}, {{1.45, 0}, 4.2, 2.4}}};
-constexpr double kHalf = 0.85;
-
-// Few rows: a round of work-groups (a band of 32 rows and 16 columns each, one on a compute unit) with 1024 k values, what the
-// first round costs besides and every further one; the kinds as above.  64 x 2048 -> 2048 of 4 bits 4.0 us, 7.4 the best of the
-// tiles; 64 x 8192 -> 2048 5.8 and 10.4; 128 x 8192 -> 2048 in two rounds 9.7 and 12.0; 64 x 65536 -> 2048 22.9 and 19.8.
-struct SkinnyCost { double k, first, further; };
-constexpr SkinnyCost kSkinnyCost[3] = {{0.30, 3.4, 1.5}, {0.44, 4.1, 1.9}, {0.50, 4.2, 2.2}};
-constexpr int kSkinnyRounds = 4;
-constexpr int kUnits = 256;  // compute units
-constexpr int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16};
-
-// The tile and the cut of k with the smallest estimate
-Plan plan_linear(const Shape& s) {
-    Plan best{};
-    best.split = 1;
-    best.tile = kMxSkinny;
-    if (s.M <= kMxSkinnyRows / 2) return best;
-    const int64_t groups = mx_groups(s.K);
-    const bool exact = s.elem == DLC_MX_E4M3 && s.es == 4;
-    const int kind = exact ? 2 : s.elem == DLC_MX_E4M3 ? 1 : 0;
-    const TileCost* const cost = kCost[kind];
-    double least = 1e300;
-    const int64_t rounds = div_up(div_up(s.M, kMxSkinnyRows) * div_up(s.N, 16), kUnits);
-    if (rounds <= kSkinnyRounds) {
-        const SkinnyCost& c = kSkinnyCost[kind];
-        least = c.first + (double)rounds * (double)s.K / 1024.0 * c.k + (double)(rounds - 1) * c.further;
-    }
-    for (int tile = exact ? 1 : 0; tile < 3; ++tile) {
-        const TileCost& c = cost[tile];
-        const int64_t tm = div_up(s.M, kMxTileM[tile]), tn = div_up(s.N, kMxTileN[tile]), tiles = tm * tn;
-        if (tiles >= kMaxGroups) continue;
-        const int fit = c.tile[1] > 0 ? 2 : 1;
-        for (const int cut : kCuts) {
-            if (cut > 1 && (cut > groups || tiles * cut > 2 * kUnits)) break;
-            const int64_t per = div_up(groups, cut), split = div_up(groups, per), wgs = tiles * split;
-            const int64_t full = wgs / (kUnits * fit), rest = wgs % (kUnits * fit);
-            double t = (double)full * (2.0 * (double)per * c.tile[fit - 1] + c.further) + c.first - c.further;
-            if (rest) t += 2.0 * (double)per * c.tile[(rest - 1) / kUnits] * (wgs <= kUnits / 2 ? kHalf : 1.0) + c.further;
-            if (split > 1) t += 3.8 + (double)split * (double)s.M * (double)s.N * 8.0 / 6.2e6;  // (the second launch, the sums out and in)
-            if (t < least) {
-                least = t;
-                best.tile = tile;
-                best.split = (int)split;
-                best.kper = (int)(per * kMxGroup);
-                best.tiles_m = (int)tm;
-                best.tiles_n = (int)tn;
-            }
-        }
-    }
-    best.part_ld = round8(s.N);
-    best.bytes = best.split > 1 ? (size_t)best.split * (size_t)s.M * (size_t)best.part_ld * 4 : 0;
-    return best;
+    return div_up(s->M, side) * div_up(s->N, side) < kMxMaxTiles;
 }
 
 template <typename T>
-int product(MxGemmArgs g, const Plan& p, int elem, void* work, hipStream_t st) {
+int product(MxGemmArgs g, const MxPlan& p, int elem, void* work, hipStream_t st) {
     g.c.split = p.split; g.c.kper = p.kper; g.c.tiles_m = p.tiles_m; g.c.tiles_n = p.tiles_n;
     g.c.part = static_cast<float*>(work);
     g.c.part_ld = p.part_ld;
@@ -260,7 +191,7 @@ extern "C" int dlc_mx_dequantize(const dlc_mx_config* cfg, const void* q, const 
 
 extern "C" size_t dlc_mx_linear_workspace_bytes(const dlc_mx_linear_config* c) {
     Shape s;
-    return make_shape(c, &s) && s.M > 0 ? plan_linear(s).bytes : 0;
+    return make_shape(c, &s) && s.M > 0 ? s.plan().bytes : 0;
 }
 
 extern "C" int dlc_mx_linear_forward(const dlc_mx_linear_config* c, const void* xq, const void* xs, const void* wq, const void* ws,
@@ -280,7 +211,7 @@ extern "C" int dlc_mx_linear_forward(const dlc_mx_linear_config* c, const void* 
     Epi& e = g.c.e;
     e.y = y; e.res = res; e.bias = bias;
     e.ld_y = s.ldy; e.ld_res = s.ldres; e.act = c->act; e.n = (int)s.N;
-    const Plan p = plan_linear(s);
+    const MxPlan p = s.plan();
     if (p.bytes > 0 && !work) return DLC_EINVAL;
     if (bytes < p.bytes) return DLC_ECAPACITY;
     hipStream_t st = (hipStream_t)stream;

@@ -10,8 +10,6 @@ struct MxGemmArgs {
     const uint8_t* ws;
 };
 
-constexpr int kMxTileM[] = {256, 128, 64}, kMxTileN[] = {256, 128, 128}, kMxSkinny = 3, kMxSkinnyRows = 32;
-
 template <typename T>
 struct MxOps {
     // tile: of kMxTileM (0: not with E4M3 and results in fp32) or kMxSkinny (bands of kMxSkinnyRows rows)

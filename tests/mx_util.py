@@ -90,3 +90,38 @@ class GuardedBytes:
 
     def intact(self):
         return bool((self.buf[:256] == self.fill).all()) and bool((self.buf[256 + self.n:] == self.fill).all())
+
+
+# ---- the product's kernels ------------------------------------------------------------------------
+# Sizes that the plan sends to a tile (0: 256 x 256, 1: 128 x 128, 2: 64 x 128; 3: a pass over the weights for bands of 32 rows), for
+# (element bits of x, results in fp32): "E2M1" any type, "E4M3" half precision, "E4M3 f32".  A name, its tile, in how many parts k
+# is cut, rows, out_features, and in_features: numbers of tiles of 256 k values (or steps of 128) from one to nine, k that ends in
+# each half of a tile and inside a step, edges in rows and columns.  test_mx_plan.py asks the plan itself.
+LENGTHS = (1, 100, 129, 256, 300, 512, 600, 700, 800, 1000, 1100, 1300, 1536, 1700, 2000, 2300)
+TILES = [
+    ("E2M1", 0, 1, 3338, 3606, LENGTHS),
+    ("E2M1", 1, 1, 4173, 402, (1700, 1800, 2100, 2400, 2600, 3000)),
+    ("E2M1", 2, 1, 65, 2745, LENGTHS),
+    ("E2M1", 2, 1, 498, 585, (100, 640, 900)),
+    ("E4M3", 0, 1, 4724, 1668, LENGTHS),
+    ("E4M3", 1, 1, 4173, 402, LENGTHS),
+    ("E4M3", 2, 1, 65, 2745, LENGTHS),
+    ("E4M3", 2, 1, 498, 585, (100, 640, 900)),
+    ("E4M3 f32", 1, 1, 4173, 402, LENGTHS),
+    ("E4M3 f32", 2, 1, 132, 3606, LENGTHS),
+]
+CUTS = [
+    ("E2M1", 0, 3, 1929, 2263, (12930,)),
+    ("E2M1", 1, 5, 1929, 295, (9231,)),
+    ("E2M1", 2, 4, 1000, 257, (8192,)),
+    ("E2M1", 2, 6, 1300, 200, (8000,)),
+    ("E4M3", 0, 3, 1929, 2263, (9231,)),
+    ("E4M3", 1, 3, 4097, 130, (8192,)),
+    ("E4M3", 1, 5, 983, 734, (9231,)),
+    ("E4M3", 2, 4, 33, 4097, (4096,)),
+    ("E4M3", 2, 8, 65, 1537, (8100,)),
+    ("E4M3 f32", 1, 5, 784, 734, (4702,)),
+    ("E4M3 f32", 1, 4, 2047, 257, (4096,)),
+    ("E4M3 f32", 2, 4, 300, 1300, (1700,)),
+]
+KINDS = {"E2M1": (4, ("f32", "f16", "bf16")), "E4M3": (8, ("f16", "bf16")), "E4M3 f32": (8, ("f32",))}
