@@ -255,3 +255,42 @@ def test_a_nan_stays_in_its_row(cols):
         assert bool(torch.isnan(y[2]).all()) and not bool(torch.isnan(y[rows]).any())
         want_q, want_s = quantise(y.double().cpu().numpy(), 8)
         assert np.array_equal(sc.view.cpu().numpy(), want_s) and np.array_equal(q.view.cpu().numpy(), want_q) and q.intact() and sc.intact()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(256, 16392), (257, 20000), (600, 16385), (700, 24583)])
+def test_many_long_rows_backward(rows, cols, dtype):
+    """Rows past 16384 columns, as many as there are work-groups and more: the weight's sums go on in memory from row to row."""
+    test_backward(rows, cols, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(5, 5), (3000, 40), (1100, 131), (2999, 259), (1100, 1023), (1100, 2047), (700, 4099), (600, 6100), (600, 8191), (300, 12283),
+                                       (300, 16383), (300, 16391)])
+def test_backward_in_place(rows, cols, dtype):
+    """dx in place of the gradient along s, of y's, and of both where they are one tensor; rows that end inside an eight, whose last
+    columns two lanes load and store, and more rows than teams."""
+    import torch
+    from paper_2407_04272_amd import binding as b
+    s, w, dy, ds = _normal(rows, cols, dtype, 81), _normal(cols, 0, dtype, 82), _normal(rows, cols, dtype, 83), _normal(rows, cols, dtype, 84)
+    cfg = b.make_norm_config(code(dtype), rows, cols, EPS)
+    work = torch.empty(b.dlc_norm_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+
+    def call(dy, ds, dx, cfg=cfg):
+        dw = torch.empty_like(w)
+        b.dlc_norm_backward(cfg, s, w, dy, ds, dx, dw, work)
+        return dw
+
+    dx, same = torch.empty_like(s), torch.empty_like(s)
+    dw = call(dy, ds, dx)
+    dw_same = call(dy, dy, same)
+    for _ in range(3):
+        a = ds.clone()
+        assert torch.equal(call(dy, a, a), dw) and torch.equal(a, dx)
+        a = dy.clone()
+        assert torch.equal(call(a, ds, a), dw) and torch.equal(a, dx)
+        a = dy.clone()
+        assert torch.equal(call(a, a, a), dw_same) and torch.equal(a, same)
+    far = Guarded(rows, cols, dtype, cols + 7, 1).set(ds)
+    apart = b.make_norm_config(code(dtype), rows, cols, EPS, ld_ds=cols + 7, ld_dx=cols + 7)
+    assert torch.equal(call(dy, far.view, far.view, apart), dw) and torch.equal(far.view, dx) and far.intact()
