@@ -506,8 +506,10 @@ size_t dlc_mx_linear_workspace_bytes(const dlc_mx_linear_config* cfg /*HOST*/);
  *         that is x itself).  May be d_x or d_residual, with equal leading dimensions (else DLC_EINVAL)
  *   d_y [rows][cols], or d_q and d_scale (y in microscaled form with E4M3 elements, as a product takes it; both or neither),
  *         or all three.  d_y may be d_x, with equal leading dimensions, unless d_sum is.  No other overlap
- * s, sums and y are fp32 up to the one rounding of each output; r is made of the unrounded s.  A row whose squares' sum passes
- * fp32's range (values from about 1.8e19 / sqrt(cols) on) has r = 0.
+ * s, sums and y are fp32 up to the one rounding of each output; r is made of the unrounded s.  y is off by a few of fp32's
+ * roundings before its own: an element of the microscaled form whose y lies that near the middle of two is one of the two (a
+ * scale likewise), and another order of the row's sum may give the other.  A row whose squares' sum passes fp32's range (values
+ * from about 1.8e19 / sqrt(cols) on) has r = 0.
  * Backward, of y's gradient and (d_ds, or NULL) the gradient that comes back along s:
  *   g = dy weight;   dx = r (g - s r^2 mean of g s over the row) + ds;   dweight = sum over rows of dy s r
  *   d_s as the forward call stored it (r is made again from it)   d_dx: the gradient of x and of the residual; may be d_dy or
