@@ -33,8 +33,10 @@ struct Part {
 
 // A tile is a group of 512 columns, eight a lane, of 16 rows: their scales are 256 bytes side by side.  Rows of at most 128
 // columns: 64 of them, on 16 lanes each (65536 x 128 bf16 into 8 bits 5.6 us, back 6.1; on 64 lanes 10.4 and 8.4).  Bound by
-// memory: 16384 x 4096 bf16 into 4 bits 31 us and back 26 (170 MB, 5.5 and 6.6 TB/s), 8192 x 8192 into 8 bits 32 and 30 (6.3 and
-// 6.7 TB/s).  Rows that end inside an eight may be loaded element by element here: the row's last eight instead, as in the norm,
+// memory: 16384 x 4096 bf16 into 4 bits 34 us and back 35 (170 MB, 5.0 and 4.9 TB/s, as a copy), 8192 x 8192 into 8 bits 39 and 37
+// (5.2 and 5.5 TB/s), eight inputs in turn; 29 and 26, 33 and 30 with one that the last cache still holds in part.  Right behind
+// a call whose results are still on their way out of that cache it is slower: 16384 x 4096 there and back 40 + 26.
+// Rows that end inside an eight may be loaded element by element here: the row's last eight instead, as in the norm,
 // took as long (8192 x 4099 bf16 20.5 us; with 4096 columns 18.5).  WHOLE: rows end with a whole eight
 template <typename T, int ELEM, bool WHOLE, int L>
 __global__ __launch_bounds__(256) void k_mx_quantize(const MxArgs a) {

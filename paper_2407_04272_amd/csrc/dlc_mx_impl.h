@@ -268,8 +268,10 @@ __device__ __forceinline__ void mx_pair(f32x4* acc0, f32x4* acc1, const A& a0, c
 // compiler has the inner loop, and reading and multiplying take turns.
 // For results that 256 x 256 tiles would leave most of the card without: 512 x 8192 -> 2048 of 4 bits 17 us (23 with reads and
 // products in turn), 1024 x 8192 18 (27), 2048 x 8192 25 (36); 777 x 515 -> 1023, E4M3 rows, bias, gelu and residual 8.5 us.
-// Bound by the way from L2 to LDS (128 x 128: 32 KB a tile on every unit in 0.64 us, 13 TB/s) and at small sizes by the start and
-// the epilogue, 4.4 us; more slots were no faster.  Two work-groups of 64 x 128 and 4 bits fit a compute unit.  A group's
+// Where the tiles fill the card, bound by the way from L2 to LDS (128 x 128: 32 KB a tile on every unit in 0.64 us, 13 TB/s); where
+// they do not, by what one unit gets (512 x 8192 -> 2048: 128 work-groups, 24 KB a tile in 0.39-0.44 us, 7-8 TB/s together; a cut
+// of k that gives the others work costs a second launch and the sums' way, 4 us and more); at small sizes by the start and
+// the epilogue, 4.4 us.  More slots were no faster.  Two work-groups of 64 x 128 and 4 bits fit a compute unit.  A group's
 // scales are asked for two tiles ahead: one tile ahead they cost a fifth (2048 x 8192 33 us for 28), now a tenth.
 template <int ELEM, int BM>
 constexpr int mx_tile_lds() {
@@ -452,10 +454,11 @@ __global__ __launch_bounds__(256) void k_mx_tile(const MxGemmArgs mx) {
 // of 128 bytes of a row are on their way there.  16 products of 16 x 16 x 128 are one block of assembly, with the reads
 // between them: a wavefront has its SIMD to itself.  Loads, scales' among them, stand between the blocks; their waits are the
 // compiler's and wait_loads'.
-// Bound by the matrix cores and the card's power: with its scales the instruction takes 24 cycles (without, 16; one of 32 x 32 x
-// 64, which does twice as much, 33; with an E4M3 operand 32), and 16384 x 8192 -> 4096 with random elements 274 us, 4020
-// TFLOP/s, at 1.9-2.1 GHz; the bare instruction on random elements reaches 5640 on the whole card.  E4M3 rows 358 us, 3070
-// TFLOP/s.  Measured and left: blocks of 32 x 32 (280 us where this took 254), work-groups that stay and ask for the next
+// The main loop is bound by the matrix cores and the card's power: with its scales the instruction takes 24 cycles (without, 16; one
+// of 32 x 32 x 64, which does twice as much, 33; with an E4M3 operand 32), and on random elements it reaches 5640 TFLOP/s on the
+// whole card.  16384 x 8192 -> 4096 274 us, 4020 TFLOP/s: with 2048, 4096 and 8192 k values 105, 157 and 262 us in one session, so
+// that 208 are the main loop, 5290 TFLOP/s, and 53 the starts and ends of four rounds of tiles, which all units reach at the same
+// time.  E4M3 rows 358 us, 3070 TFLOP/s.  Measured and left: blocks of 32 x 32 (280 us where this took 254), work-groups that stay and ask for the next
 // tile's operands during the epilogue (the same), results stored from the registers without LDS (265-286 for 254), no masks
 // on the loads (268 for 270).
 #define DLC_MX_MOST4(OP, BL) \
